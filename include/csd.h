@@ -43,6 +43,7 @@ extern "C" {
 
 #define CSD_DTYPE_FP32 0
 #define CSD_DTYPE_BF16 1
+#define CSD_DTYPE_FP8  2   /* e4m3 with a scale per row; paged caches only */
 #define CSD_MODE_SAMPLE 0
 #define CSD_MODE_GREEDY 1
 
@@ -319,6 +320,77 @@ int32_t csd_tree_accept(const float *p, const int32_t *tokens, const int32_t *pa
  */
 int32_t csd_tree_commit(const csd_model *model, void *kv, const int32_t *cache_len, const int32_t *path,
                         const int32_t *n_accepted, int32_t B, int32_t m, void *stream);
+
+/*
+ * Paged KV cache.  The cache of a model is dense: max_seq rows for each of max_batch sequences.  The calls below keep
+ * rows in pages instead, so that memory follows the rows that exist, sequences share the pages of a common prompt
+ * (Section 2's reviews of several sequences read them in place), and a cached row may be held in 8 bits.
+ *
+ * A pool holds the rows of n_layers layers in n_pages pages of page_rows rows each (a power of two, 16 to 1024):
+ *   k, v              [n_layers][n_pages][n_kv_heads][page_rows][head_dim] in dtype (head_dim a multiple of 8, 8 to 256)
+ *   k_scale, v_scale  CSD_DTYPE_FP8: [n_layers][n_pages][n_kv_heads][page_rows]; NULL for the other types
+ * Both pools are 16-byte aligned.  table[B][table_stride] names the pages of every sequence in order, the same in every
+ * layer: position pos of sequence b is row pos % page_rows of page table[b][pos / page_rows].  An entry outside [0, n_pages), and every
+ * position from table_stride * page_rows on, is a place without a row: what would be written there is dropped, it reads as zeros,
+ * and the attention leaves it out (so pages that are no longer wanted may be given back and their entries set to -1).
+ *
+ * A row of an e4m3 pool is one token of one head.  With a the largest finite |x| of the row and e the smallest integer >= -126 with
+ * a <= 448 * 2^e, its codes are x / 2^e rounded to the nearest e4m3 value (ties to even; at e = 120 to 240 at most, so that all values
+ * are fp32 values) and its scale byte is e + 127:
+ * entries are off by at most 2^-4 of themselves or, near zero, 2^(e-10); a row that was read back and is written again keeps its values.
+ * NaN and infinities become the NaN code.
+ *
+ * The rows of a batch are ragged: row r of a call, 0 <= r < rows, belongs to the sequence b with
+ * row_start[b] <= r < row_start[b + 1] (row_start[B + 1], non-decreasing) and has position
+ * pos[b] + r - row_start[b].  Rows of no sequence (before row_start[0], from row_start[B] on) are left alone, in outputs too.
+ * row_start, pos and table are device arrays and are clamped to the call's buffers by the kernels.
+ * Pages that two sequences share may be read by both; two rows of one call, or of calls that overlap, must not be
+ * written to the same place.
+ */
+typedef struct csd_paged_kv {
+    int32_t n_layers, n_pages, page_rows, n_kv_heads, head_dim, dtype;
+    void *k, *v;
+    uint8_t *k_scale, *v_scale;
+    const int32_t *table;
+    int32_t table_stride;          /* entries per sequence, >= 1; table_stride * page_rows < 2^31 */
+} csd_paged_kv;
+
+/* Write rows k_rows, v_rows (dtype CSD_DTYPE_FP32 or CSD_DTYPE_BF16; [rows][n_kv_heads][head_dim] with k_stride / v_stride elements from one
+ * row to the next, multiples of 8; 16-byte aligned) of one layer.  Values are rounded to the pool's type (to nearest, ties to even). */
+int32_t csd_paged_write(const csd_paged_kv *kv, int32_t layer, const int32_t *row_start, const int32_t *pos, int32_t B, int32_t rows,
+                        const void *k_rows, int64_t k_stride, const void *v_rows, int64_t v_stride, int32_t dtype, void *stream);
+
+/* Read rows back, to [rows][n_kv_heads][head_dim] of dtype CSD_DTYPE_FP32 or CSD_DTYPE_BF16 (one rounding at most: the values of a bf16 or
+ * e4m3 pool are exact in either, down to the type's smallest normal value), strides as above. */
+int32_t csd_paged_read(const csd_paged_kv *kv, int32_t layer, const int32_t *row_start, const int32_t *pos, int32_t B, int32_t rows,
+                       void *k_rows, int64_t k_stride, void *v_rows, int64_t v_stride, int32_t dtype, void *stream);
+
+/*
+ * Attention of new rows (a token, a drafted block, a chunk of a prompt) over the paged rows of their sequences, their own
+ * among them: the rows' keys and values have been written (csd_paged_write with the same row_start and pos = cache_len).
+ * Row i of sequence b sits at position cache_len[b] + i and attends positions 0 .. cache_len[b] + i;
+ * with parent (tree blocks of at most 64 rows; parent[r] in [0, i) names the row of its block that row i continues, row 0's is not read,
+ * a value outside that range is read as 0) it attends the cached positions [0, cache_len[b]), the rows above it in the tree and itself.
+ * q, out: [rows][n_heads][head_dim] of dtype (q_stride elements from one row to the next, a multiple of 8; out is contiguous;
+ * 16-byte aligned, not overlapping); n_heads a multiple of n_kv_heads, query head h reads key-value head h / (n_heads / n_kv_heads).
+ * out = softmax(scale * q k^T) v, scores, maxima and sums in fp32; a row that has nothing to attend gives zeros, and what
+ * a row does not attend never reaches it (not even infinities and NaN).  max_rows: at least the rows of the longest sequence of the batch
+ * (a longer one is cut to it), 1 <= max_rows; CSD_ESHAPE for trees with max_rows > 64.
+ * workspace: device, 256-byte aligned, CSD_PAGED_WORKSPACE_BYTES; zeroed before its first use; every call leaves what the next one
+ * needs zeroed.  Calls that share it must not overlap.
+ */
+#define CSD_PAGED_WORKSPACE_BYTES (96u << 20)
+int32_t csd_paged_attention(const csd_paged_kv *kv, int32_t layer, const int32_t *row_start, const int32_t *cache_len,
+                            const int32_t *parent, int32_t B, int32_t rows, int32_t max_rows, const void *q, int64_t q_stride,
+                            int32_t n_heads, int32_t dtype, float scale, void *out, void *workspace, void *stream);
+
+/*
+ * csd_tree_commit over pages, in all layers: after a tree block of m <= 64 rows per sequence was written, attended and
+ * reviewed, the rows path[b][0 .. n_accepted[b]) of the block move to positions cache_len[b] + 1 ...  path as csd_tree_accept
+ * writes it (increasing, path[b][j] >= j + 1); an entry that is not cuts the move there.  Codes and scales move as they are.
+ */
+int32_t csd_paged_commit(const csd_paged_kv *kv, const int32_t *cache_len, const int32_t *path, const int32_t *n_accepted,
+                         int32_t B, int32_t m, void *stream);
 
 /* Test hook: when trace != NULL the next verify calls also copy the residual stream of all
  * B*m rows after the embedding and after every layer to trace[(n_layers+1)][B*m][d] (fp32). */

@@ -16,7 +16,8 @@ _LIB_PATH = os.path.join(_HERE, "libcsd.so")
 
 EXPORTS = ["csd_version", "csd_last_hip_error", "csd_model_create", "csd_model_destroy", "csd_kv_bytes",
            "csd_kv_write", "csd_kv_read", "csd_cross_kv_init", "csd_bigram_fit", "csd_bigram_draft", "csd_maxgram_draft", "csd_verify_block",
-           "csd_accept", "csd_verify_accept", "csd_verify_accept_static", "csd_review_ctx", "csd_bigram_draft_append", "csd_cascade_gate", "csd_verify_tree", "csd_tree_accept", "csd_tree_commit", "csd_debug_set_trace", "csd_debug_path", "csd_debug_gemm_plan", "csd_debug_tall_plan", "csd_debug_copy", "csd_debug_read", "csd_debug_mfma",
+           "csd_accept", "csd_verify_accept", "csd_verify_accept_static", "csd_review_ctx", "csd_bigram_draft_append", "csd_cascade_gate", "csd_verify_tree", "csd_tree_accept", "csd_tree_commit",
+           "csd_paged_write", "csd_paged_read", "csd_paged_attention", "csd_paged_commit", "csd_debug_set_trace", "csd_debug_path", "csd_debug_gemm_plan", "csd_debug_tall_plan", "csd_debug_copy", "csd_debug_read", "csd_debug_mfma",
            "csd_prof_enable", "csd_prof_read"]
 
 _STATUS = {-1: "CSD_EINVAL", -2: "CSD_ESHAPE", -3: "CSD_ENULL", -4: "CSD_EHIP", -5: "CSD_EUNSUPPORTED"}
@@ -45,6 +46,20 @@ class Review(C.Structure):
                 ("next_token", C.c_void_p), ("status", C.c_void_p), ("ext_rows", C.c_void_p)]
 
 
+class PagedPool(C.Structure):
+    """csd_paged_kv: a paged cache and the page table of a call."""
+    _fields_ = [(n, C.c_int32) for n in ("n_layers", "n_pages", "page_rows", "n_kv_heads", "head_dim", "dtype")] + \
+               [(n, C.c_void_p) for n in ("k", "v", "k_scale", "v_scale", "table")] + [("table_stride", C.c_int32)]
+
+
+_P, _I, _L = C.c_void_p, C.c_int32, C.c_int64
+# the paged calls are short: ctypes converts plain integers by these, without an object per argument
+_ARGTYPES = {"csd_paged_write": [_P, _I, _P, _P, _I, _I, _P, _L, _P, _L, _I, _P],
+             "csd_paged_read": [_P, _I, _P, _P, _I, _I, _P, _L, _P, _L, _I, _P],
+             "csd_paged_attention": [_P, _I, _P, _P, _P, _I, _I, _I, _P, _L, _I, _I, C.c_float, _P, _P, _P],
+             "csd_paged_commit": [_P, _P, _P, _P, _I, _I, _P]}
+PAGED_WORKSPACE_BYTES = 96 << 20
+
 _lib = None
 
 
@@ -65,6 +80,8 @@ def lib():
         for n in EXPORTS:
             if n not in ("csd_version", "csd_kv_bytes"):
                 getattr(L, n).restype = C.c_int32
+        for n, types in _ARGTYPES.items():
+            getattr(L, n).argtypes = types
         _lib = L
     return _lib
 
@@ -226,6 +243,136 @@ class Model:
         ms, n = C.c_double(), C.c_int64()
         _chk(lib().csd_prof_read(self._h, kernel_class, C.byref(ms), C.byref(n), 1 if reset else 0), "csd_prof_read")
         return ms.value, n.value
+
+
+class PagedKv:
+    """A paged KV cache: the pools k and v [layers][pages][kv heads][rows of a page][head dim] (torch.float32, bfloat16 or float8_e4m3fn;
+    the latter with scale bytes k_scale, v_scale, uint8 of the same shape without the last dimension), which the caller made and owns.
+
+    Every call takes the page table [B][n] int32 (entries outside [0, pages): no rows there) and the ragged rows of a batch: row_start
+    [B + 1] int32, and a position [B] int32 for each sequence's first row.  Rows are [rows][heads][head dim], float32 or bfloat16,
+    with any distance between rows that is a multiple of 8 elements.  All tensors are on the pools' device, which has to be the current one,
+    and the work is enqueued on its current stream.  The attention's workspace belongs to this object: calls of attention() that
+    may overlap (other streams or threads, captured graphs that are replayed side by side) need an object of their own."""
+
+    def __init__(self, k, v, k_scale=None, v_scale=None, workspace=None):
+        types = {torch.float32: 0, torch.bfloat16: 1, torch.float8_e4m3fn: 2}
+        if k.ndim != 5 or k.shape != v.shape or k.dtype != v.dtype or k.dtype not in types:
+            raise ValueError("k and v: [layers][pages][kv heads][rows of a page][head dim], both float32, bfloat16 or float8_e4m3fn")
+        if (k.dtype == torch.float8_e4m3fn) != (k_scale is not None) or (k_scale is None) != (v_scale is None):
+            raise ValueError("k_scale and v_scale belong to float8_e4m3fn pools")
+        self._dev = k.get_device()
+        for t in (v, k_scale, v_scale, workspace):
+            if t is not None and t.get_device() != self._dev:
+                raise ValueError("all tensors of a cache belong on one device")
+        if k_scale is not None and (k_scale.shape != k.shape[:-1] or v_scale.shape != k.shape[:-1]):
+            raise ValueError("k_scale and v_scale: the pools' shape without the last dimension")
+        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        self.n_layers, self.n_pages, self.n_kv_heads, self.page_rows, self.head_dim = k.shape
+        self._pool = PagedPool(self.n_layers, self.n_pages, self.page_rows, self.n_kv_heads, self.head_dim, types[k.dtype],
+                               _ptr(k).value, _ptr(v).value, _ptr(k_scale, torch.uint8).value, _ptr(v_scale, torch.uint8).value, None, 0)
+        self._ref = C.addressof(self._pool)
+        if workspace is None:
+            self._check_device()
+            workspace = torch.zeros(PAGED_WORKSPACE_BYTES, dtype=torch.uint8, device=k.device)
+            torch.cuda.current_stream().synchronize()     # zeroed for whatever stream the first call runs on
+        elif workspace.numel() * workspace.element_size() < PAGED_WORKSPACE_BYTES:
+            raise ValueError(f"workspace: {PAGED_WORKSPACE_BYTES} bytes, zeroed")
+        self.workspace = workspace
+        self._ws = _ptr(workspace).value
+
+    def _check_device(self):
+        if torch.cuda.current_device() != self._dev:
+            raise ValueError("the cache is on another device than the current one")
+
+    def _ints(self, t, n, what):
+        """Address of a contiguous int32 tensor with n elements on the cache's device."""
+        if t.get_device() != self._dev:
+            raise ValueError(f"{what}: a tensor on the cache's device is required")
+        if t.dtype is not torch.int32:
+            raise TypeError(f"{what}: expected torch.int32, got {t.dtype}")
+        if t.numel() != n or not t.is_contiguous():
+            raise ValueError(f"{what}: {n} contiguous elements are required")
+        return t.data_ptr()
+
+    def _rows(self, t, rows, heads, what, dtype=None):
+        """(address, elements from row to row, type) of a [rows][heads][head dim] tensor."""
+        if t.get_device() != self._dev:
+            raise ValueError(f"{what}: a tensor on the cache's device is required")
+        code = 1 if t.dtype is torch.bfloat16 else 0 if t.dtype is torch.float32 else -1
+        if code < 0 or (dtype is not None and code != dtype):
+            raise TypeError(f"{what}: rows are float32 or bfloat16, all of a call alike, got {t.dtype}")
+        d = self.head_dim
+        if t.ndim != 3 or t.shape[0] != rows or t.shape[1] != heads or t.shape[2] != d:
+            raise ValueError(f"{what}: [{rows}][{heads}][{d}] is required, got {list(t.shape)}")
+        if t.stride(2) != 1 or (heads > 1 and t.stride(1) != d):
+            raise ValueError(f"{what}: the elements of a row must be contiguous")
+        return t.data_ptr(), t.stride(0) if rows > 1 else heads * d, code
+
+    def _call(self, table, row_start, pos):
+        """Puts the table into the pool's description; (B, row_start, pos) of the call."""
+        if table.ndim != 2:
+            raise ValueError("table: [B][pages of a sequence]")
+        B, n = table.shape
+        self._check_device()
+        pool = self._pool
+        pool.table, pool.table_stride = self._ints(table, B * n, "table"), n
+        return B, self._ints(row_start, B + 1, "row_start") if row_start is not None else None, self._ints(pos, B, "cache_len")
+
+    def write(self, layer, table, row_start, cache_len, k_rows, v_rows):
+        """csd_paged_write: row r of sequence b becomes position cache_len[b] + r - row_start[b]."""
+        B, start, pos = self._call(table, row_start, cache_len)
+        rows = k_rows.shape[0]
+        kp, ks, code = self._rows(k_rows, rows, self.n_kv_heads, "k_rows")
+        vp, vs, _ = self._rows(v_rows, rows, self.n_kv_heads, "v_rows", code)
+        rc = lib().csd_paged_write(self._ref, layer, start, pos, B, rows, kp, ks, vp, vs, code, _raw_stream(self._dev))
+        if rc:
+            _chk(rc, "csd_paged_write")
+
+    def read(self, layer, table, row_start, cache_len, rows, dtype=torch.float32, out=None):
+        """csd_paged_read: (k, v) [rows][kv heads][head dim], row r of sequence b from position cache_len[b] + r - row_start[b].
+        out: the two tensors to fill; rows of no sequence are left as they are (undefined in new tensors)."""
+        B, start, pos = self._call(table, row_start, cache_len)
+        if out is None:
+            shape = (rows, self.n_kv_heads, self.head_dim)
+            out = torch.empty((2,) + shape, dtype=dtype, device=self.k.device).unbind(0)
+        kp, ks, code = self._rows(out[0], rows, self.n_kv_heads, "out")
+        vp, vs, _ = self._rows(out[1], rows, self.n_kv_heads, "out", code)
+        rc = lib().csd_paged_read(self._ref, layer, start, pos, B, rows, kp, ks, vp, vs, code, _raw_stream(self._dev))
+        if rc:
+            _chk(rc, "csd_paged_read")
+        return out[0], out[1]
+
+    def attention(self, layer, table, row_start, cache_len, q, scale, max_rows=None, parent=None, out=None):
+        """csd_paged_attention: q [rows][heads][head dim] -> out, contiguous and of q's type; rows of no sequence are left as they are
+        (undefined in a new tensor).
+        max_rows: at least the rows of the longest sequence of the batch (default: all rows of the call); parent: tree blocks."""
+        B, start, pos = self._call(table, row_start, cache_len)
+        rows, heads = q.shape[0], q.shape[1]
+        qp, qs, code = self._rows(q, rows, heads, "q")
+        if out is None:
+            out = torch.empty((rows, heads, self.head_dim), dtype=q.dtype, device=q.device)
+        else:
+            self._rows(out, rows, heads, "out", code)
+            if not out.is_contiguous():
+                raise ValueError("out: a contiguous tensor is required")
+        up = self._ints(parent, rows, "parent") if parent is not None else None
+        rc = lib().csd_paged_attention(self._ref, layer, start, pos, up, B, rows, rows or 1 if max_rows is None else max_rows, qp, qs, heads,
+                                       code, scale, out.data_ptr(), self._ws, _raw_stream(self._dev))
+        if rc:
+            _chk(rc, "csd_paged_attention")
+        return out
+
+    def commit(self, table, cache_len, path, n_accepted):
+        """csd_paged_commit: the kept rows of a tree block, path[b][: n_accepted[b]], to positions cache_len[b] + 1 .., in all layers."""
+        B, _, pos = self._call(table, None, cache_len)
+        if path.ndim != 2:
+            raise ValueError("path: [B][rows of the tree]")
+        m = path.shape[1]
+        rc = lib().csd_paged_commit(self._ref, pos, self._ints(path, B * m, "path"), self._ints(n_accepted, B, "n_accepted"), B, m,
+                                    _raw_stream(self._dev))
+        if rc:
+            _chk(rc, "csd_paged_commit")
 
 
 def debug_copy(dst, src):

@@ -1,0 +1,110 @@
+// Shared by the kernels of the paged KV cache (csd_paged.hip: rows in and out, commit; csd_paged_attn.hip: attention).
+#pragma once
+
+#include <type_traits>
+
+#include "csd_internal.h"
+
+// The pool of one layer and the page table, by value in the kernels' arguments.
+struct PagedPool {
+    void *k, *v;                  // this layer's [n_pages][Hkv][page_rows][D]
+    uint8_t *ks, *vs;             // e4m3: this layer's scale bytes [n_pages][Hkv][page_rows]
+    const int32_t *table;
+    int32_t table_stride, n_pages, page_shift, Hkv, D;
+};
+
+// The ragged batch of a call.
+struct PagedRows {
+    const int32_t *row_start, *pos;
+    int32_t B, rows;
+};
+
+// rows [start, start + m) of the call are sequence b's, from position t on
+struct PagedSeq {
+    int start, m, t;
+};
+__device__ __forceinline__ PagedSeq paged_seq(const PagedRows &r, int b) {
+    const int s = min(max(r.row_start[b], 0), r.rows);
+    const int e = min(max(r.row_start[b + 1], s), r.rows);
+    return PagedSeq{s, e - s, min(max(r.pos[b], 0), 0x3FFFFFFF)};
+}
+
+// The sequence of a row (uniform in the wave): how many sequences end at or before it.  64 ends are looked at at once; B if there is none.
+__device__ __forceinline__ int paged_find(const PagedRows &r, int row) {
+    const int lane = threadIdx.x & 63;
+    int b = 0;
+    for (int b0 = 0; b0 < r.B; b0 += 64) {
+        const bool ends = b0 + lane < r.B && r.row_start[b0 + lane + 1] <= row;
+        const int n = __popcll(__ballot(ends));
+        b += n;
+        if (n < 64) break;
+    }
+    return b;
+}
+
+// page of a position, -1: there is none
+__device__ __forceinline__ int paged_page(const PagedPool &p, int b, int pos) {
+    const int i = pos >> p.page_shift;
+    if (pos < 0 || i >= p.table_stride) return -1;
+    const int page = p.table[(size_t)b * p.table_stride + i];
+    return (unsigned)page < (unsigned)p.n_pages ? page : -1;
+}
+// row index of (page, head, position) in a layer's pool
+__device__ __forceinline__ size_t paged_row(const PagedPool &p, int page, int head, int pos) {
+    return (((size_t)page * p.Hkv + head) << p.page_shift) + (pos & ((1 << p.page_shift) - 1));
+}
+
+__device__ __forceinline__ float pow2_of_byte(unsigned s) { return __uint_as_float(s << 23); }   // 2^(s - 127), s in 1 .. 254
+
+// Eight consecutive elements as floats, from fp32, bf16 or (unscaled) e4m3 memory.
+template <typename T> __device__ __forceinline__ void load8(const T *p, float (&x)[8]);
+template <> __device__ __forceinline__ void load8<float>(const float *p, float (&x)[8]) {
+    const f32x4 a = *reinterpret_cast<const f32x4 *>(p), b = *reinterpret_cast<const f32x4 *>(p + 4);
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+        x[i] = a[i];
+        x[4 + i] = b[i];
+    }
+}
+template <> __device__ __forceinline__ void load8<bf16_t>(const bf16_t *p, float (&x)[8]) {
+    const u32x4 a = *reinterpret_cast<const u32x4 *>(p);
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+        x[2 * i] = __uint_as_float(a[i] << 16);
+        x[2 * i + 1] = __uint_as_float(a[i] & 0xFFFF0000u);
+    }
+}
+template <> __device__ __forceinline__ void load8<uint8_t>(const uint8_t *p, float (&x)[8]) {
+    const u32x2 a = *reinterpret_cast<const u32x2 *>(p);
+#pragma unroll
+    for (int i = 0; i < 2; i++) {
+        const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)a[i], false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)a[i], true);
+        x[4 * i] = lo[0];
+        x[4 * i + 1] = lo[1];
+        x[4 * i + 2] = hi[0];
+        x[4 * i + 3] = hi[1];
+    }
+}
+template <typename T> __device__ __forceinline__ void store8(T *p, const float (&x)[8]);
+template <> __device__ __forceinline__ void store8<float>(float *p, const float (&x)[8]) {
+    *reinterpret_cast<f32x4 *>(p) = f32x4{x[0], x[1], x[2], x[3]};
+    *reinterpret_cast<f32x4 *>(p + 4) = f32x4{x[4], x[5], x[6], x[7]};
+}
+template <> __device__ __forceinline__ void store8<bf16_t>(bf16_t *p, const float (&x)[8]) {
+    *reinterpret_cast<u32x4 *>(p) =
+        u32x4{pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7])};
+}
+
+// One attention call.
+struct PagedAttn {
+    PagedPool p;
+    PagedRows r;
+    const int32_t *parent;        // tree blocks, or null
+    int max_rows, group;          // rows of a sequence at most; query heads per key-value head
+    const void *q;
+    long long q_stride;
+    void *out;
+    float scale;
+    void *ws;
+};
+int32_t csd_paged_attention_enqueue(const PagedAttn &a, int32_t pool_dtype, int32_t q_dtype, hipStream_t st);

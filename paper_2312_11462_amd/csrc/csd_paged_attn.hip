@@ -1,0 +1,124 @@
+// Attention of new rows over a paged KV cache.
+#include "csd_paged.h"
+
+// Any types and head sizes: one workgroup per (row, query head).  The four waves take 64 keys in turn, a key per lane for the scores
+// and an element (or D / 64 of them) per lane for the products with the values, and keep a running maximum, sum and output each;
+// they are joined at the end.  Only keys that the row attends are looked at in the second half, so that nothing else reaches it.
+// All arithmetic is in fp32.
+template <typename TQ, typename TP>
+__global__ __launch_bounds__(256) void k_paged_attn_any(PagedAttn a) {
+    __shared__ float s_q[256], s_o[4][256], s_m[4], s_l[4];
+    const int row = blockIdx.x, head = blockIdx.y, tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
+    const PagedPool &p = a.p;
+    const int D = p.D, kvh = head / a.group;
+    const int b = paged_find(a.r, row);
+    if (b >= a.r.B) return;
+    const PagedSeq s = paged_seq(a.r, b);
+    const int i = row - s.start;
+    if (i < 0 || i >= min(s.m, a.max_rows)) return;
+    // the row's ancestors in its block, one bit each
+    unsigned long long above = ~0ull;
+    if (a.parent) {
+        above = 1ull << i;
+        for (int x = i; x > 0;) {
+            const int up = a.parent[s.start + x];
+            x = up >= 0 && up < x ? up : 0;
+            above |= 1ull << x;
+        }
+    }
+    const TQ *q = reinterpret_cast<const TQ *>(a.q) + (size_t)row * a.q_stride + (size_t)head * D;
+    if (tid < D) s_q[tid] = to_f32<TQ>(q[tid]);
+    __syncthreads();
+    constexpr float kLog2e = 1.44269504088896f;
+    float m_run = -INFINITY, l_run = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
+    const int keys = min(s.t + i + 1, p.table_stride << p.page_shift);
+    for (int key0 = wave * 64; key0 < keys; key0 += 256) {
+        const int key = key0 + lane;
+        int page = key < keys ? paged_page(p, b, key) : -1;
+        if (a.parent && key >= s.t && !((above >> (key - s.t)) & 1ull)) page = -1;
+        const size_t at = page >= 0 ? paged_row(p, page, kvh, key) : 0;
+        float score = -INFINITY;
+        if (page >= 0) {
+            const TP *kp = reinterpret_cast<const TP *>(p.k) + at * D;
+            float dot = 0.f;
+            for (int c = 0; c < D; c += 8) {
+                float x[8];
+                load8<TP>(kp + c, x);
+#pragma unroll
+                for (int e = 0; e < 8; e++) dot = fmaf(x[e], s_q[c + e], dot);
+            }
+            if constexpr (sizeof(TP) == 1) dot *= pow2_of_byte(p.ks[at]);
+            score = dot * a.scale;
+        }
+        unsigned long long seen = __ballot(page >= 0);
+        if (!seen) continue;
+        const float m_new = fmaxf(m_run, wave_max(score)), m_ref = m_new == -INFINITY ? 0.f : m_new;
+        const float w = page >= 0 ? exp2f((score - m_ref) * kLog2e) : 0.f, fade = exp2f((m_run - m_ref) * kLog2e);
+        l_run = l_run * fade + wave_sum(w);
+        m_run = m_new;
+#pragma unroll
+        for (int e = 0; e < 4; e++) o[e] *= fade;
+        float vw = w;
+        if constexpr (sizeof(TP) == 1) vw = page >= 0 ? w * pow2_of_byte(p.vs[at]) : 0.f;
+        while (seen) {
+            const int j = __ffsll((long long)seen) - 1;
+            seen &= seen - 1;
+            const float wj = __shfl(vw, j, 64);
+            const unsigned lo = __shfl((unsigned)at, j, 64), hi = __shfl((unsigned)(at >> 32), j, 64);
+            const TP *vp = reinterpret_cast<const TP *>(p.v) + (((size_t)hi << 32) | lo) * D;
+#pragma unroll
+            for (int e = 0; e < 4; e++) {
+                const int c = e * 64 + lane;
+                if (c < D) {
+                    float x;
+                    if constexpr (sizeof(TP) == 1) x = __builtin_amdgcn_cvt_f32_fp8((int)vp[c], 0);
+                    else x = to_f32<TP>(vp[c]);
+                    o[e] = fmaf(wj, x, o[e]);
+                }
+            }
+        }
+    }
+#pragma unroll
+    for (int e = 0; e < 4; e++) s_o[wave][e * 64 + lane] = o[e];
+    if (lane == 0) {
+        s_m[wave] = m_run;
+        s_l[wave] = l_run;
+    }
+    __syncthreads();
+    if (tid >= D) return;
+    float m_all = s_m[0];
+    for (int w = 1; w < 4; w++) m_all = fmaxf(m_all, s_m[w]);
+    if (m_all == -INFINITY) m_all = 0.f;
+    float l = 0.f, x = 0.f;
+    for (int w = 0; w < 4; w++) {
+        const float f = exp2f((s_m[w] - m_all) * kLog2e);
+        l += f * s_l[w];
+        x += f * s_o[w][tid];
+    }
+    // nothing to attend: zeros (0 / 0 where there are keys but all scores are -inf, as the formula has it)
+    bool any = l != 0.f;
+    if (!any)
+        for (int key = 0; key < keys && !any; key++)
+            any = paged_page(p, b, key) >= 0 && (!a.parent || key < s.t || ((above >> (key - s.t)) & 1ull));
+    TQ *out = reinterpret_cast<TQ *>(a.out) + ((size_t)row * p.Hkv * a.group + head) * D;
+    out[tid] = from_f32<TQ>(any ? x / l : 0.f);
+}
+
+template <typename TQ, typename TP>
+static void any_launch(const PagedAttn &a, hipStream_t st) {
+    hipLaunchKernelGGL((k_paged_attn_any<TQ, TP>), dim3(a.r.rows, a.p.Hkv * a.group), dim3(256), 0, st, a);
+}
+
+int32_t csd_paged_attention_enqueue(const PagedAttn &a, int32_t pool_dtype, int32_t q_dtype, hipStream_t st) {
+    if (q_dtype == CSD_DTYPE_FP32) {
+        if (pool_dtype == CSD_DTYPE_FP32) any_launch<float, float>(a, st);
+        else if (pool_dtype == CSD_DTYPE_BF16) any_launch<float, bf16_t>(a, st);
+        else any_launch<float, uint8_t>(a, st);
+    } else {
+        if (pool_dtype == CSD_DTYPE_FP32) any_launch<bf16_t, float>(a, st);
+        else if (pool_dtype == CSD_DTYPE_BF16) any_launch<bf16_t, bf16_t>(a, st);
+        else any_launch<bf16_t, uint8_t>(a, st);
+    }
+    CSD_LAUNCH_CHECK();
+    return CSD_OK;
+}

@@ -1,0 +1,556 @@
+"""The paged KV cache on the GPU against the plain form in 64 bits (oracle/paged.py).
+
+Bounds.  A value rounded to a type is off by at most u = eps / 2 of itself (bf16 2^-8, fp32 2^-24).  An attention output is sum p v with
+weights off by (1 + u_p) exp(e): u_p = 2^-8 where the weights are rounded to bf16 on their way into the matrix cores, and e the error of a
+score, at most (D + 4) 2^-24 scale sum |q k| from the fp32 product, plus 2^-21 for the exponential and its argument (|x| <= 64 in steps of
+2^-24 times the bits, two roundings) and n 2^-24 for the sums over n keys.  So
+|out - exact| <= u_out |exact| + 2 (u_p + e) sum p |v|, the factor 2 for the sum of weights in the denominator.
+"""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import paged as O
+
+pytestmark = pytest.mark.gpu
+
+TORCH = {"fp32": torch.float32, "bf16": torch.bfloat16, "fp8": torch.float8_e4m3fn}
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _need_gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    import paper_2312_11462_amd as P
+    P.lib()
+
+
+class Paged:
+    """A cache on the GPU, and the values it holds as float64 on the host."""
+
+    def __init__(self, cache, rows, cached, new, kv_heads=2, group=1, d=64, page=16, layers=1, seed=0, spare=3, width=0, poison=True):
+        import paper_2312_11462_amd as P
+        self.rng = np.random.default_rng(seed)
+        self.cache, self.rows, self.cached, self.new = cache, rows, list(cached), list(new)
+        self.kv_heads, self.group, self.d, self.page, self.layers = kv_heads, group, d, page, layers
+        need = [-(-(t + m) // page) for t, m in zip(cached, new)]
+        self.n_pages = sum(need) + spare
+        order = self.rng.permutation(self.n_pages)
+        self.table = np.full((len(cached), max(max(need), 1) + width), -1, dtype=np.int32)
+        at = 0
+        for b, n in enumerate(need):
+            self.table[b, :n] = order[at:at + n]
+            at += n
+        self.start = np.concatenate([[0], np.cumsum(new)]).astype(np.int32)
+        self.total = int(self.start[-1])
+        shape = (layers, self.n_pages, kv_heads, page, d)
+        # places that nobody wrote hold NaN
+        if cache == "fp8":
+            self.k = torch.full(shape, 0x7F, dtype=torch.uint8, device="cuda").view(torch.float8_e4m3fn)
+            self.v = self.k.view(torch.uint8).clone().view(torch.float8_e4m3fn)
+            self.ks = torch.full(shape[:-1], 200, dtype=torch.uint8, device="cuda")
+            self.vs = self.ks.clone()
+        else:
+            fill = float("nan") if poison else 0.0
+            self.k = torch.full(shape, fill, dtype=TORCH[cache], device="cuda")
+            self.v = self.k.clone()
+            self.ks = self.vs = None
+        self.kv = P.PagedKv(self.k, self.v, self.ks, self.vs)
+        self.dev = [torch.tensor(x, dtype=torch.int32, device="cuda") for x in (self.table, self.start, np.array(cached, dtype=np.int32))]
+
+    def values(self, pool, scale):
+        if scale is None:
+            return pool.double().cpu().numpy()
+        x = pool.view(torch.uint8).cpu().view(torch.float8_e4m3fn).double().numpy()
+        return x * np.exp2(scale.cpu().numpy().astype(np.float64) - 127)[..., None]
+
+    def random_rows(self, n, heads=None, loud=True):
+        x = self.rng.standard_normal((n, heads or self.kv_heads, self.d))
+        if loud:
+            x[:, :, self.rng.integers(self.d)] *= 5
+        return torch.tensor(x, dtype=torch.float32).to(TORCH[self.rows]).cuda()
+
+    def fill(self, layer=0):
+        """Writes every row, cached and new, with one call; returns the dense rows."""
+        whole = [t + m for t, m in zip(self.cached, self.new)]
+        start = torch.tensor(np.concatenate([[0], np.cumsum(whole)]), dtype=torch.int32, device="cuda")
+        k, v = self.random_rows(sum(whole)), self.random_rows(sum(whole), loud=False)
+        self.kv.write(layer, self.dev[0], start, torch.zeros(len(whole), dtype=torch.int32, device="cuda"), k, v)
+        return k, v
+
+    def attend(self, q, scale, max_rows=None, parent=None, layer=0, **kw):
+        up = torch.tensor(parent, dtype=torch.int32, device="cuda") if parent is not None else None
+        return self.kv.attention(layer, *self.dev, q, scale, max_rows, parent=up, **kw)
+
+    def check(self, out, q, scale, parent=None, layer=0, start=None, cached=None):
+        start, cached = self.start if start is None else start, self.cached if cached is None else cached
+        k, v = self.values(self.k, self.ks)[layer], self.values(self.v, self.vs)[layer]
+        qq = q.double().cpu().numpy()
+        want = O.attention(k, v, self.table, start, cached, qq, scale, parent)
+        size = O.attention(k, np.abs(v), self.table, start, cached, qq, scale, parent)
+        n = max(t + m for t, m in zip(self.cached, self.new))
+        # sum |q k| of a score is at most |q| |k| (Cauchy-Schwarz)
+        live = k[np.isfinite(k).all(-1)]
+        dot = abs(scale) * np.sqrt((qq ** 2).sum(-1)).max(initial=0) * np.sqrt((live ** 2).sum(-1)).max(initial=0)
+        e = (self.d + 4) * 2.0 ** -24 * dot + 2.0 ** -21 + n * 2.0 ** -24
+        bf = self.rows == "bf16"
+        tol = (2.0 ** -8 if bf else 2.0 ** -24) * np.abs(want) + 2 * ((2.0 ** -8 if bf else 0.0) + e) * size
+        got = out.double().cpu().numpy()
+        covered = np.zeros(len(got), dtype=bool)
+        covered[start[0]:start[-1]] = True
+        assert np.array_equal(np.isfinite(got[covered]), np.isfinite(want[covered]))
+        fine = np.isfinite(want) & covered[:, None, None]
+        err = np.abs(got - want)[fine]
+        assert (err <= tol[fine]).all(), f"off by {(err / np.maximum(tol[fine], 1e-300)).max():.2f} times the bound, {err.max():.3g}"
+        return want
+
+
+TYPES = [("fp32", "fp32"), ("fp32", "bf16"), ("fp32", "fp8"), ("bf16", "bf16"), ("bf16", "fp8"), ("bf16", "fp32")]
+
+
+@pytest.mark.parametrize("d,kv_heads,page", [(8, 1, 16), (64, 3, 16), (80, 2, 32), (128, 8, 64), (256, 1, 128)])
+@pytest.mark.parametrize("rows,cache", TYPES)
+def test_rows_in_and_out(rows, cache, d, kv_heads, page):
+    """Ragged sequences, one without rows, one over a page border; what is not written keeps its bytes."""
+    c = Paged(cache, rows, [0, 5, page - 1, 3 * page, 2], [1, 0, 2, page + 3, 17], kv_heads=kv_heads, d=d, page=page, layers=2, seed=d)
+    for x, s in ((c.k, c.ks), (c.v, c.vs)):
+        x.view(torch.uint8).copy_(torch.randint(0, 100, x.view(torch.uint8).shape, dtype=torch.uint8))
+        if s is not None:
+            s.copy_(torch.randint(100, 150, s.shape, dtype=torch.uint8))
+    before = [c.values(c.k, c.ks), c.values(c.v, c.vs)]
+    k, v = c.random_rows(c.total), c.random_rows(c.total)
+    special = c.total - 1
+    k[special, 0] = 0
+    v[special, 0, :3] = torch.tensor([1e30, -1e-30, 3e4])
+    c.kv.write(1, *c.dev, k, v)
+    where = O.places(c.start, c.cached, c.table, page, c.n_pages, c.total)
+    for pool, scale, was, x in ((c.k, c.ks, before[0], k), (c.v, c.vs, before[1], v)):
+        dense = x.double().cpu().numpy()
+        if cache == "fp8":
+            dense, byte = O.quantise(dense)
+            bytes_ = scale.cpu().numpy()[1]
+            assert all(np.array_equal(bytes_[page_, :, slot], byte[r]) for r, _, _, page_, slot in where)
+        elif cache == "bf16":
+            dense = x.float().cpu().to(torch.bfloat16).double().numpy()
+        O.write(was[1], dense, where)
+        assert np.array_equal(c.values(pool, scale), was)
+    t = TORCH[rows]
+    got = c.kv.read(1, *c.dev, c.total, dtype=t)
+    for pool, scale, x in ((c.k, c.ks, got[0]), (c.v, c.vs, got[1])):
+        want = O.read(c.values(pool, scale)[1], where, c.total)
+        assert np.array_equal(x.double().cpu().numpy(), torch.tensor(want).to(t).double().numpy())
+
+
+def test_quantised_rows_at_the_borders_of_the_type():
+    """Rows whose maximum sits at a step of the scale, in fp32's subnormal range, or is zero; ties; NaN and infinities among the entries."""
+    d = 64
+    rows = []
+    for top in (448.0, 448.00003, 224.0, 1.75, 1.7500001, 3.4e38, 1e-37, 1.2e-38, 1e-40, 0.0):
+        x = np.linspace(-1, 1, d) * top
+        x[3] = top
+        rows.append(x)
+    ties = np.arange(d) * 0.5 + 1.0625 * 2.0 ** (np.arange(d) % 8)           # halfway between two codes at several exponents
+    ties[0] = 448.0
+    rows.append(ties)
+    for bad in (np.nan, np.inf, -np.inf):
+        x = np.linspace(-3, 5, d)
+        x[7] = bad
+        rows.append(x)
+    rows.append(np.full(d, np.nan))
+    x = torch.tensor(np.stack(rows), dtype=torch.float32).cuda()[:, None].contiguous()
+    n = x.shape[0]
+    c = Paged("fp8", "fp32", [0], [n], kv_heads=1, d=d)
+    c.kv.write(0, *c.dev, x, x.flip(0).contiguous())
+    want, byte = O.quantise(x.double().cpu().numpy())
+    where = O.places(c.start, c.cached, c.table, c.page, c.n_pages, n)
+    pool, scales = c.values(c.k, c.ks)[0], c.ks.cpu().numpy()[0]
+    for r, _, _, page, slot in where:
+        assert np.array_equal(scales[page, :, slot], byte[r]), r
+        assert np.array_equal(pool[page, :, slot], want[r], equal_nan=True), r
+    # a row that is read and written again keeps its values
+    k, v = c.kv.read(0, *c.dev, n)
+    c.kv.write(0, *c.dev, k, v)
+    again = c.values(c.k, c.ks)[0]
+    for r, _, _, page, slot in where:
+        assert np.array_equal(again[page, :, slot], want[r], equal_nan=True), r
+
+
+def test_rows_without_a_place_and_rows_of_no_sequence():
+    c = Paged("bf16", "bf16", [0, 10], [20, 30], kv_heads=2, d=64, page=16)
+    c.table[0, 1] = -1                                    # given back
+    c.table[1, 0] = c.n_pages                             # out of range
+    c.table[1, 2] = 2 ** 31 - 1
+    c.dev[0].copy_(torch.tensor(c.table))
+    pad = 7
+    start = torch.tensor([pad, pad + 20, pad + 50], dtype=torch.int32, device="cuda")
+    c.start = start.cpu().numpy()
+    k, v = c.random_rows(pad + 50 + pad), c.random_rows(pad + 50 + pad)
+    before = c.values(c.k, None)
+    c.kv.write(0, c.dev[0], start, c.dev[2], k, v)
+    where = O.places(c.start, c.cached, c.table, 16, c.n_pages, 10 ** 9)
+    O.write(before[0], k.double().cpu().numpy(), where)
+    assert np.array_equal(c.values(c.k, None), before, equal_nan=True)
+    out = [torch.full((pad + 50 + pad, 2, 64), 9.0, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    c.kv.read(0, c.dev[0], start, c.dev[2], pad + 50 + pad, out=out)
+    want = O.read(before[0], where, pad + 50 + pad)
+    want[:pad] = want[pad + 50:] = 9.0
+    assert np.array_equal(out[0].double().cpu().numpy(), want)
+    # rows past the end of the table
+    short = c.dev[0][:, :1].contiguous()
+    c.kv.read(0, short, start, c.dev[2], pad + 50 + pad, out=out)
+    assert (out[0][pad + 16:pad + 20] == 0).all() and (out[0][pad + 26:pad + 50] == 0).all()
+
+
+HEADS = [(1, 1), (2, 4), (8, 1), (1, 8), (4, 3)]
+
+
+@pytest.mark.parametrize("rows,cache,d", [("fp32", "fp32", 16), ("fp32", "fp32", 64), ("fp32", "bf16", 128), ("fp32", "fp8", 64), ("bf16", "bf16", 64), ("bf16", "bf16", 128),
+                                          ("bf16", "fp8", 64), ("bf16", "fp8", 128), ("bf16", "bf16", 80), ("bf16", "fp8", 256), ("bf16", "fp32", 64)])
+@pytest.mark.parametrize("kv_heads,group", HEADS)
+def test_attention_of_small_batches(rows, cache, d, kv_heads, group):
+    """Single tokens, blocks and short chunks of one batch, at lengths around tiles and pages; a sequence without rows; an empty cache."""
+    for page, new in ((16, [1, 1, 1, 1, 1, 1, 1, 1]), (32, [5, 0, 1, 5, 2, 5, 5, 4]), (16, [17, 1, 16, 0, 33, 3, 15, 8])):
+        c = Paged(cache, rows, [0, 7, 31, 32, 33, 63, 127, 200], new, kv_heads=kv_heads, group=group, d=d, page=page, seed=page + d)
+        c.fill()
+        q = c.random_rows(c.total, kv_heads * group)
+        out = c.attend(q, d ** -0.5, max(new))
+        c.check(out, q, d ** -0.5)
+        assert torch.equal(out, c.attend(q, d ** -0.5))                 # whatever bound on the rows the caller knows
+
+
+@pytest.mark.parametrize("rows,cache,d,kv_heads,group", [("bf16", "bf16", 128, 2, 4), ("bf16", "fp8", 128, 2, 2), ("bf16", "bf16", 64, 3, 1), ("bf16", "fp8", 64, 1, 8), ("fp32", "fp32", 32, 2, 2)])
+@pytest.mark.parametrize("cached,new", [([0], [129]), ([77], [200]), ([0, 300, 5], [64, 65, 1]), ([1000], [70]), ([511, 2], [1, 257]), ([3, 0, 0], [300, 1, 0])])
+def test_attention_of_chunks(rows, cache, d, kv_heads, group, cached, new):
+    c = Paged(cache, rows, cached, new, kv_heads=kv_heads, group=group, d=d, page=64, seed=d + len(new))
+    c.fill()
+    q = c.random_rows(c.total, kv_heads * group)
+    c.check(c.attend(q, d ** -0.5, max(new)), q, d ** -0.5)
+
+
+@pytest.mark.parametrize("rows,cache,d,new", [("bf16", "bf16", 128, 1), ("bf16", "fp8", 128, 5), ("bf16", "bf16", 64, 1), ("bf16", "fp8", 64, 9), ("fp32", "fp32", 64, 2), ("bf16", "bf16", 128, 40)])
+def test_attention_of_long_caches(rows, cache, d, new):
+    """The work of a sequence is split over its keys and joined."""
+    c = Paged(cache, rows, [9001, 3, 4097, 0], [new] * 4, kv_heads=2, group=2, d=d, page=16, seed=new)
+    c.fill()
+    q = c.random_rows(c.total, 4)
+    out = c.attend(q, d ** -0.5, new)
+    c.check(out, q, d ** -0.5)
+    for _ in range(3):
+        assert torch.equal(c.attend(q, d ** -0.5, new), out)           # sums in one order, and a workspace that is as it was
+
+
+def test_attention_of_many_sequences():
+    n = 150                                                             # more than a wave looks at in one go
+    rng = np.random.default_rng(1)
+    c = Paged("bf16", "bf16", rng.integers(0, 90, n), rng.integers(0, 4, n), kv_heads=1, group=2, d=64, seed=2)
+    c.fill()
+    q = c.random_rows(c.total, 2)
+    c.check(c.attend(q, 0.125, 3), q, 0.125)
+    c.check(c.attend(q, 0.125), q, 0.125)
+
+
+SPREAD = [("fp32", "fp32", 32), ("bf16", "bf16", 128), ("bf16", "fp8", 64), ("bf16", "bf16", 80)]
+
+
+@pytest.mark.parametrize("rows,cache,d", SPREAD)
+@pytest.mark.parametrize("m,group", [(2, 1), (9, 1), (41, 1), (64, 1), (9, 4), (33, 2)])
+def test_attention_over_trees(rows, cache, d, m, group):
+    rng = np.random.default_rng(m)
+    c = Paged(cache, rows, [0, 65, 130], [m] * 3, kv_heads=2, group=group, d=d, seed=m)
+    c.fill()
+    parent = np.concatenate([[int(rng.integers(max(0, i - 9), i)) if i else -1 for i in range(m)] for _ in range(3)]).astype(np.int32)
+    q = c.random_rows(c.total, 2 * group)
+    c.check(c.attend(q, d ** -0.5, m, parent), q, d ** -0.5, parent)
+    chain = np.concatenate([np.arange(m) - 1] * 3).astype(np.int32)
+    plain = c.attend(q, d ** -0.5, m)
+    c.check(c.attend(q, d ** -0.5, m, chain), q, d ** -0.5)
+    wild = parent.copy()
+    wild[m // 2] = m                                                    # outside [0, i): read as 0
+    wild[-1] = -7
+    c.check(c.attend(q, d ** -0.5, m, wild), q, d ** -0.5, wild)
+    assert torch.equal(plain, c.attend(q, d ** -0.5, m))
+
+
+@pytest.mark.parametrize("rows,cache,d", SPREAD)
+@pytest.mark.parametrize("m", [1, 3, 50])
+def test_pages_that_were_given_back_and_rows_with_nothing_to_attend(rows, cache, d, m):
+    c = Paged(cache, rows, [100, 200, 5, 0], [m, m, m, 1], kv_heads=2, group=2, d=d, seed=m)
+    c.fill()
+    c.table[0, 2:4] = -1
+    c.table[1, 0], c.table[1, 5] = c.n_pages, -5
+    c.table[2] = -1                                                     # nothing left
+    c.dev[0].copy_(torch.tensor(c.table))
+    q = c.random_rows(c.total, 4)
+    out = c.attend(q, d ** -0.5, m)
+    c.check(out, q, d ** -0.5)
+    assert (out[2 * m:3 * m] == 0).all()
+
+
+@pytest.mark.parametrize("rows,cache,d", SPREAD)
+@pytest.mark.parametrize("m,tree", [(2, False), (16, False), (40, False), (70, False), (40, True)])
+@pytest.mark.parametrize("what", [math.nan, math.inf, -math.inf])
+def test_values_that_are_not_finite_reach_only_the_rows_that_attend_them(rows, cache, d, m, tree, what):
+    """A later token of the block, or a row beside this one in the tree, has such keys or values."""
+    c = Paged(cache, rows, [37, 0], [m, m], kv_heads=2, group=2, d=d, seed=m)
+    k, v = c.fill()
+    bad = m // 2
+    one = torch.tensor([0, 1], dtype=torch.int32, device="cuda")
+    kr, vr = c.random_rows(1), c.random_rows(1)
+    vr[0, 1, d // 3] = what
+    c.kv.write(0, c.dev[0][:1].contiguous(), one, torch.tensor([37 + bad], dtype=torch.int32, device="cuda"), kr, vr)
+    kr, vr = c.random_rows(1), c.random_rows(1)
+    kr[0, 0, 1] = what
+    c.kv.write(0, c.dev[0][1:].contiguous(), one, torch.tensor([bad], dtype=torch.int32, device="cuda"), kr, vr)
+    parent = np.concatenate([[-1] + [0] * (m - 1)] * 2).astype(np.int32) if tree else None
+    q = c.random_rows(c.total, 4).abs()
+    out = c.attend(q, d ** -0.5, m, parent).float().cpu()
+    clean_rows = [i for i in range(m) if (i != bad if tree else i < bad)]
+    assert torch.isfinite(out[clean_rows]).all() and torch.isfinite(out[[m + i for i in clean_rows]]).all()
+    # the values' feature of the second key-value head, in the rows that attend the bad one: as the formula has it
+    assert not torch.isfinite(out[bad, 2:, d // 3]).any()
+    rest = torch.ones(d, dtype=torch.bool)
+    rest[d // 3] = False
+    assert torch.isfinite(out[bad, 2:, rest]).all() and torch.isfinite(out[bad, :2]).all()
+    kk, vv = c.values(c.k, c.ks)[0], c.values(c.v, c.vs)[0]
+    with np.errstate(invalid="ignore"):
+        want = O.attention(kk, vv, c.table, c.start, c.cached, q.double().cpu().numpy(), d ** -0.5, parent)
+    ok = np.isfinite(want)
+    assert np.allclose(out.double().numpy()[ok], want[ok], rtol=0.05, atol=0.05)
+
+
+@pytest.mark.parametrize("rows,cache,d,m", [("bf16", "bf16", 128, 3), ("bf16", "fp8", 64, 60), ("fp32", "fp32", 64, 3)])
+def test_large_scores(rows, cache, d, m):
+    """Scores of several hundred, one key that takes all the weight, and a later key that takes it over."""
+    c = Paged(cache, rows, [300], [m], kv_heads=1, group=2, d=d)
+    c.fill()
+    q = c.random_rows(m, 2)
+    c.check(c.attend(q, 8.0, m), q, 8.0)
+    c.check(c.attend(q, -3.0, m), q, -3.0)
+    c.check(c.attend(q, 0.0, m), q, 0.0)
+
+
+@pytest.mark.parametrize("rows,cache,d,m", [("bf16", "fp8", 128, 4), ("bf16", "bf16", 64, 100), ("fp32", "fp32", 16, 3)])
+def test_rows_inside_a_wider_buffer_and_padded_batches(rows, cache, d, m):
+    """Queries, keys and values as slices of one projection's output; rows behind the last sequence are left as they were."""
+    c = Paged(cache, rows, [40, 11], [m, m], kv_heads=2, group=2, d=d)
+    c.fill()
+    pad = 5
+    fused = torch.randn(2 * m + pad, (4 + 2 + 2) * d + 8, device="cuda").to(TORCH[rows])
+    q = fused[:, :4 * d].view(2 * m + pad, 4, d)
+    k = fused[:, 4 * d:6 * d].view(2 * m + pad, 2, d)
+    v = fused[:, 6 * d:8 * d].view(2 * m + pad, 2, d)
+    c.kv.write(0, *c.dev, k, v)
+    out = torch.full((2 * m + pad, 4, d), 7.0, dtype=TORCH[rows], device="cuda")
+    got = c.attend(q, d ** -0.5, m, out=out)
+    assert got is out and (out[2 * m:] == 7).all()
+    c.check(out[:2 * m], q[:2 * m], d ** -0.5)
+    back = c.kv.read(0, *c.dev, 2 * m + pad, out=(fused[:, 4 * d:6 * d].view(2 * m + pad, 2, d), fused[:, 6 * d:8 * d].view(2 * m + pad, 2, d)))
+    assert torch.equal(back[0][2 * m:], k[2 * m:])
+
+
+@pytest.mark.parametrize("cache", ["fp32", "bf16", "fp8"])
+def test_commit_of_a_trees_path(cache):
+    m, page = 41, 16
+    c = Paged(cache, "fp32" if cache == "fp32" else "bf16", [0, 33, 15, 7, 9], [m] * 5, kv_heads=3, d=64, page=page, layers=3, seed=4)
+    for layer in range(3):
+        c.fill(layer)
+    path = np.full((5, m), -1, dtype=np.int32)
+    kept = np.array([4, 0, 40, 3, 60], dtype=np.int32)
+    path[0, :4] = [1, 9, 17, 40]
+    path[2, :40] = np.arange(1, 41)                       # everything is where it belongs
+    path[3, :3] = [2, 5, 5]                               # not increasing: cut at the third
+    path[4, :6] = [3, 4, 5, 6, 7, 41]                     # out of the block: cut at the sixth
+    c.table[0, 1] = -1                                    # rows 16 .. 31 of the first sequence have no place
+    c.dev[0].copy_(torch.tensor(c.table))
+    pools = [c.values(c.k, c.ks), c.values(c.v, c.vs)]
+    for pool in pools:
+        O.commit(pool, c.table, c.cached, path, kept)
+    c.kv.commit(c.dev[0], c.dev[2], torch.tensor(path).cuda(), torch.tensor(kept).cuda())
+    assert np.array_equal(c.values(c.k, c.ks), pools[0], equal_nan=True) and np.array_equal(c.values(c.v, c.vs), pools[1], equal_nan=True)
+
+
+@pytest.mark.parametrize("cache", ["bf16", "fp8"])
+def test_a_review_over_pages_write_attend_commit_and_the_next_block(cache):
+    """As a decoding loop does it: the rows of a tree are written and attended, a path is kept, the next block sees it as plain rows."""
+    m, d = 9, 128
+    c = Paged(cache, "bf16", [50, 17], [m, m], kv_heads=2, group=2, d=d, layers=2, width=1, seed=8)
+    c.fill(0)
+    c.fill(1)
+    k, v = c.random_rows(2 * m), c.random_rows(2 * m)
+    parent = np.array([-1, 0, 0, 1, 1, 2, 3, 4, 7] * 2, dtype=np.int32)
+    path = np.array([[2, 5, 0, 0, 0, 0, 0, 0, 0], [1, 4, 7, 8, 0, 0, 0, 0, 0]], dtype=np.int32)
+    kept = np.array([2, 4], dtype=np.int32)
+    q = c.random_rows(2 * m, 4)
+    for layer in range(2):
+        c.kv.write(layer, *c.dev, k, v)
+        c.check(c.attend(q, 0.1, m, parent, layer=layer), q, 0.1, parent, layer=layer)
+    tree = c.attend(q, 0.1, m, parent)
+    c.kv.commit(c.dev[0], c.dev[2], torch.tensor(path).cuda(), torch.tensor(kept).cuda())
+    # the kept rows as a plain block of their own, with the same queries: the same outputs up to rounding
+    rows = np.concatenate([[0] + list(path[0, :2]), [0] + list(path[1, :4])])
+    rows[3:] += m
+    start = torch.tensor([0, 3, 8], dtype=torch.int32, device="cuda")
+    block = c.kv.attention(0, c.dev[0], start, c.dev[2], q[rows].contiguous(), 0.1, 5)
+    c.check(block, q[rows], 0.1, start=np.array([0, 3, 8]))
+    size = tree.float().abs().max()
+    assert ((block.float() - tree[torch.tensor(rows).cuda()].float()).abs() <= 2.0 ** -6 * size).all()
+
+
+@pytest.mark.parametrize("m", [1, 6, 80])
+def test_captured_calls_replay_to_the_eager_result(m):
+    c = Paged("fp8", "bf16", [600, 0, 1500], [m] * 3, kv_heads=2, group=2, d=128, width=2, seed=m)
+    c.fill()
+    q, k, v = c.random_rows(3 * m, 4), c.random_rows(3 * m), c.random_rows(3 * m)
+    out = torch.zeros_like(q)
+
+    def step():
+        c.kv.write(0, *c.dev, k, v)
+        c.kv.attention(0, *c.dev, q, 0.09, m, out=out)
+
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for rep in range(4):
+        q.copy_(c.random_rows(3 * m, 4))
+        k.copy_(c.random_rows(3 * m))
+        c.dev[2].copy_(torch.tensor([600 - rep, 2 * rep, 1500 - 300 * rep]))
+        step()
+        torch.cuda.synchronize()
+        want = out.clone()
+        out.fill_(-1)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out.view(torch.int16), want.view(torch.int16)), rep      # bits: the second sequence meets rows that nobody wrote, NaN
+
+
+def test_calls_on_another_stream_follow_that_stream():
+    c = Paged("bf16", "bf16", [700], [3], kv_heads=2, group=2, d=128)
+    c.fill()
+    q = c.random_rows(3, 4)
+    want = c.attend(q, 0.1, 3)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        late = torch.zeros_like(q)
+        for _ in range(20):
+            late.copy_(q)                                  # in order on that stream
+        got = c.attend(late, 0.1, 3)
+    side.synchronize()
+    assert torch.equal(got, want)
+
+
+def test_offsets_beyond_32_bits():
+    """A pool of more than 4 GiB, the rows at its end."""
+    import paper_2312_11462_amd as P
+    heads, page, d = 8, 128, 128
+    n = (1 << 32) // (heads * page * d) + 40               # codes of 2^32 bytes and some
+    c = Paged("fp8", "bf16", [300], [3], kv_heads=heads, d=d, page=page)
+    small = c.n_pages
+    c.n_pages = n
+    c.k = torch.empty((1, n, heads, page, d), dtype=torch.float8_e4m3fn, device="cuda")
+    c.v = torch.empty_like(c.k)
+    c.ks = torch.empty((1, n, heads, page), dtype=torch.uint8, device="cuda")
+    c.vs = torch.empty_like(c.ks)
+    for x in (c.k.view(torch.uint8), c.v.view(torch.uint8)):
+        x.fill_(0x7F)
+    c.kv = P.PagedKv(c.k, c.v, c.ks, c.vs)
+    c.table[0, :3] = [n - 1, n - 7, n - 39]
+    c.dev[0].copy_(torch.tensor(c.table))
+    k, v = c.fill()
+    back = c.kv.read(0, c.dev[0], torch.tensor([0, 303], dtype=torch.int32, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda"), 303)
+    want, _ = O.quantise(k.double().cpu().numpy())
+    assert np.array_equal(back[0].double().cpu().numpy(), want)
+    q = c.random_rows(3, heads)
+    out = c.attend(q, 0.1, 3)
+    # the same rows in a small pool give the same bits
+    s = Paged("fp8", "bf16", [300], [3], kv_heads=heads, d=d, page=page)
+    s.kv.write(0, s.dev[0], torch.tensor([0, 303], dtype=torch.int32, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda"), k, v)
+    assert torch.equal(out, s.attend(q, 0.1, 3)) and small < n
+    path = torch.full((1, 3), -1, dtype=torch.int32, device="cuda")
+    path[0, 0] = 2
+    for x in (c, s):
+        x.kv.commit(x.dev[0], x.dev[2], path, torch.ones(1, dtype=torch.int32, device="cuda"))
+    assert torch.equal(c.attend(q, 0.1, 3), s.attend(q, 0.1, 3))
+
+
+def test_a_models_sequence_is_parked_in_the_pool_and_taken_back():
+    """The rows of a model's dense cache go into pages (a bf16 pool keeps them exactly) and come back into another slot: the next review is the same
+    to the bit.  Attention over the pages is the model's own, seen through its first layer."""
+    import csd_inputs as I
+    import paper_2312_11462_amd as P
+    shape = I.ModelShape("park", 0, "bf16", 3, 256, 4, 64, 512, 1024)
+    gm = P.Model(shape, I.make_weights(shape, 5, device="cuda", std=0.05), max_batch=2, max_seq=160, max_block=8)
+    toks = I.token_ids(120, shape.vocab, 5, 1).cuda()
+    n = 96
+    for pos in range(0, n, 8):
+        both = toks[None, pos:pos + 8].expand(2, 8).contiguous()
+        gm.verify_block(both, torch.full((2,), pos, dtype=torch.int32, device="cuda"))
+    block = toks[None, n:n + 5].expand(2, 5).contiguous()
+    cl = torch.full((2,), n, dtype=torch.int32, device="cuda")
+    want = gm.verify_block(block, cl)[0].clone()
+    k = torch.zeros((3, 8, 4, 16, 64), dtype=torch.bfloat16, device="cuda")
+    kv = P.PagedKv(k, torch.zeros_like(k))
+    table = torch.tensor([[5, 0, 7, 2, 1, 6]], dtype=torch.int32, device="cuda")
+    start, zero = torch.tensor([0, n], dtype=torch.int32, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda")
+    for layer in range(3):
+        K, V = gm.kv_read(layer, 0, 0, n)
+        kv.write(layer, table, start, zero, K.view(n, 4, 64), V.view(n, 4, 64))
+    junk = torch.randn(n, 256, device="cuda")
+    for layer in range(3):
+        gm.kv_write(layer, 0, 0, junk, junk)
+    assert not torch.equal(gm.verify_block(block, cl)[0], want)
+    for layer in range(3):
+        K, V = kv.read(layer, table, start, zero, n)
+        gm.kv_write(layer, 0, 0, K.reshape(n, 256), V.reshape(n, 256))
+    assert torch.equal(gm.verify_block(block, cl)[0], want)
+
+
+def test_refusals_of_the_binding():
+    import paper_2312_11462_amd as P
+    c = Paged("bf16", "bf16", [3], [2], kv_heads=2, group=2, d=64)
+    t, s, cl = c.dev
+    q, k = c.random_rows(2, 4), c.random_rows(2)
+    c.kv.write(0, t, s, cl, k, k)
+    with pytest.raises(ValueError):
+        c.kv.attention(0, t.cpu(), s, cl, q, 0.1)
+    with pytest.raises(ValueError):
+        c.kv.attention(0, t, s[:1], cl, q, 0.1)
+    with pytest.raises(TypeError):
+        c.kv.attention(0, t.long(), s, cl, q, 0.1)
+    with pytest.raises(ValueError):
+        c.kv.attention(0, t, s, cl, q.cpu(), 0.1)
+    with pytest.raises(TypeError):
+        c.kv.attention(0, t, s, cl, q.half(), 0.1)
+    with pytest.raises(ValueError):
+        c.kv.attention(0, t, s, cl, q.transpose(0, 1), 0.1)
+    with pytest.raises(ValueError):
+        c.kv.attention(0, t, s, cl, q, 0.1, out=torch.empty(3, 4, 64, dtype=torch.bfloat16, device="cuda"))
+    with pytest.raises(TypeError):
+        c.kv.attention(0, t, s, cl, q, 0.1, out=torch.empty(2, 4, 64, device="cuda"))
+    with pytest.raises(ValueError):
+        c.kv.attention(0, t, s, cl, q, 0.1, parent=torch.zeros(1, dtype=torch.int32, device="cuda"))
+    with pytest.raises(P.CsdError) as e:
+        c.kv.attention(0, t, s, cl, q[:, :3].contiguous(), 0.1)
+    assert e.value.status == -1
+    with pytest.raises(P.CsdError) as e:
+        c.kv.write(1, t, s, cl, k, k)
+    assert e.value.status == -1
+    with pytest.raises(P.CsdError):
+        c.kv.write(0, t, s, cl, k[:1].expand(2, 2, 64), k)               # one row for all: no distance between rows
+    with pytest.raises(TypeError):
+        c.kv.write(0, t, s, cl, k, k.float())
+    with pytest.raises(ValueError):
+        c.kv.write(0, t, s, cl, k, k[:1])
+    with pytest.raises(ValueError):
+        c.kv.commit(t, cl, torch.zeros(2, 3, dtype=torch.int32, device="cuda"), cl)
+    with pytest.raises(ValueError):
+        P.PagedKv(c.k, c.v, workspace=torch.zeros(1024, dtype=torch.uint8, device="cuda"))
+    # no rows at all: nothing happens
+    none = torch.zeros(2, dtype=torch.int32, device="cuda")
+    assert c.kv.attention(0, t, none, cl, q[:0], 0.1).shape == (0, 4, 64)
+    c.kv.write(0, t, none, cl, k[:0], k[:0])
+    assert c.kv.read(0, t, none, cl, 0)[0].shape == (0, 2, 64)
