@@ -108,3 +108,14 @@ struct PagedAttn {
     void *ws;
 };
 int32_t csd_paged_attention_enqueue(const PagedAttn &a, int32_t pool_dtype, int32_t q_dtype, hipStream_t st);
+
+// csd_paged_few.hip: sequences of up to 32 rows per key-value head.  The workspace holds counters (zero between launches) and behind
+// them the partial results, two of up to 32 rows per workgroup.
+#define CSD_PAGED_COUNTER_BYTES 65536
+#define CSD_PAGED_FEW_GRID 512       /* two workgroups per compute unit */
+#define CSD_PAGED_FEW_SHARE 4        /* tiles of 32 keys per workgroup at least */
+#define CSD_PAGED_FEW_PARTS 64       /* parts of an item at most */
+#define CSD_PAGED_FEW_ROWS 32
+static_assert(CSD_PAGED_COUNTER_BYTES + 2ull * CSD_PAGED_FEW_GRID * CSD_PAGED_FEW_ROWS * 130 * 4 <= CSD_PAGED_WORKSPACE_BYTES, "");
+bool csd_paged_few_fits(const PagedAttn &a, int32_t pool_dtype, int32_t q_dtype);
+void csd_paged_few_enqueue(const PagedAttn &a, int rows, int32_t pool_dtype, hipStream_t st);

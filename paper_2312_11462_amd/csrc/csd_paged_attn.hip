@@ -110,6 +110,12 @@ static void any_launch(const PagedAttn &a, hipStream_t st) {
 }
 
 int32_t csd_paged_attention_enqueue(const PagedAttn &a, int32_t pool_dtype, int32_t q_dtype, hipStream_t st) {
+    const long long rows = (long long)a.max_rows * a.group;
+    if (rows <= CSD_PAGED_FEW_ROWS && csd_paged_few_fits(a, pool_dtype, q_dtype)) {
+        csd_paged_few_enqueue(a, (int)rows, pool_dtype, st);
+        CSD_LAUNCH_CHECK();
+        return CSD_OK;
+    }
     if (q_dtype == CSD_DTYPE_FP32) {
         if (pool_dtype == CSD_DTYPE_FP32) any_launch<float, float>(a, st);
         else if (pool_dtype == CSD_DTYPE_BF16) any_launch<float, bf16_t>(a, st);

@@ -1,0 +1,537 @@
+// Attention of few rows (a token, a drafted block, a small tree) over a paged KV cache: bf16 queries, heads of 64 or 128, bf16 or e4m3 pools,
+// up to 32 rows per key-value head (rows of a sequence times the query heads that share its keys).
+//
+// Every cached row is read once and takes part in few products, so the cache's bytes bound this: what matters is that all compute units
+// read all the time.  The tiles of 32 keys of all sequences and key-value heads are counted through, and every workgroup takes an
+// equal, contiguous share of them (sequences of very different length share the chip evenly, and nobody outside the device has to know the
+// lengths).  A share ends inside an item (sequence, key-value head) in general; the parts of such an item are joined by the workgroup
+// that finishes last.
+//
+// The four waves of a workgroup take the tiles of its share in turn.  Both
+// products are transposed so that nothing passes through LDS:
+//   S^T = K q^T    A = K (16 keys x 32 features), B = q^T.  Key of A-row r of tile half T: 8 (r / 4) + 4 T + r % 4, so that lane group g
+//                  (lane / 16) ends up with the scores of keys 8 g .. 8 g + 7 of the tile, all in one page
+//   O^T = V^T P^T  A = V^T (16 features x 32 keys), B = P^T, which those scores are already.  A lane loads DH / 16 consecutive features of
+//                  eight keys (a row of V is read by 16 neighbouring lanes) and transposes them in registers by byte permutations; A-row i of
+//                  product j is then feature DH / 16 * i + j.
+// e4m3 keys and values become bf16 without loss; the keys' scales multiply the scores, the values' scales the weights (powers of
+// two: exact).  Weights enter the second product as two bf16 planes (w = hi + lo, 16 bits): the matrix cores have time to spare here.
+#include "csd_paged.h"
+
+static constexpr int kFewPages = 1024;      // entries of the page table held in LDS at a time
+
+template <int DH, bool F8>
+struct FewTile {
+    static constexpr int F = DH / 16;                        // features per lane of a V row
+    static constexpr int VW = F8 ? F / 4 : F / 2;            // dwords that hold them
+    static constexpr int KV = F8 ? DH / 64 : DH / 32;        // 16-byte pieces of a K row per lane
+    u32x4 k[2][KV];
+    uint32_t v[8][VW];
+    u32x2 ks, vs;                                            // e4m3: scale bytes of the lane group's eight keys
+    bool here;                                               // the group's keys have a page
+};
+
+template <int VW>
+__device__ __forceinline__ void load_words(const void *p, uint32_t (&w)[VW]) {
+    if constexpr (VW == 4) {
+        const u32x4 x = *reinterpret_cast<const u32x4 *>(p);
+#pragma unroll
+        for (int i = 0; i < 4; i++) w[i] = x[i];
+    } else if constexpr (VW == 2) {
+        const u32x2 x = *reinterpret_cast<const u32x2 *>(p);
+        w[0] = x[0];
+        w[1] = x[1];
+    } else {
+        w[0] = *reinterpret_cast<const uint32_t *>(p);
+    }
+}
+
+// two e4m3 codes (the low or the high half of w) as bf16, exact
+template <bool HI>
+__device__ __forceinline__ uint32_t bf16x2_of_fp8(uint32_t w) {
+    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, HI));
+}
+
+// V^T operand of feature j from the eight keys' words: dword i holds keys 2 i, 2 i + 1
+template <int DH, bool F8>
+__device__ __forceinline__ void v_operands(const uint32_t (&v)[8][FewTile<DH, F8>::VW], u32x4 (&f)[DH / 16]) {
+    constexpr int F = DH / 16;
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+        const uint32_t *a = v[2 * i], *b = v[2 * i + 1];
+        if constexpr (F8) {
+#pragma unroll
+            for (int w = 0; w < F / 4; w++) {
+                const uint32_t lo = __builtin_amdgcn_perm(b[w], a[w], 0x05010400u), hi = __builtin_amdgcn_perm(b[w], a[w], 0x07030602u);
+                f[4 * w][i] = bf16x2_of_fp8<false>(lo);
+                f[4 * w + 1][i] = bf16x2_of_fp8<true>(lo);
+                f[4 * w + 2][i] = bf16x2_of_fp8<false>(hi);
+                f[4 * w + 3][i] = bf16x2_of_fp8<true>(hi);
+            }
+        } else {
+#pragma unroll
+            for (int w = 0; w < F / 2; w++) {
+                f[2 * w][i] = __builtin_amdgcn_perm(b[w], a[w], 0x05040100u);
+                f[2 * w + 1][i] = __builtin_amdgcn_perm(b[w], a[w], 0x07060302u);
+            }
+        }
+    }
+}
+
+// The shares: T tiles over n workgroups, the first T % n of them one tile longer.
+struct FewShares {
+    int q, r;
+    __device__ __forceinline__ FewShares(int T, int n) : q(T / n), r(T % n) {}
+    __device__ __forceinline__ int first(int w) const { return w * q + min(w, r); }
+    __device__ __forceinline__ int owner(int tile) const {
+        const int wide = r * (q + 1);
+        return tile < wide ? tile / (q + 1) : r + (tile - wide) / q;
+    }
+};
+
+__device__ __forceinline__ f32x4 mfma16(u32x4 a, u32x4 b, f32x4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+
+// Partial results live in memory that other compute dies read within the same launch: stores and loads of device scope.
+__device__ __forceinline__ void store_dev(float *p, float a, float b) {
+    const uint64_t x = ((uint64_t)__float_as_uint(b) << 32) | __float_as_uint(a);
+    __hip_atomic_store(reinterpret_cast<uint64_t *>(p), x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ float2 load_dev(const float *p) {
+    const uint64_t x = __hip_atomic_load(reinterpret_cast<const uint64_t *>(p), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    return float2{__uint_as_float((uint32_t)x), __uint_as_float((uint32_t)(x >> 32))};
+}
+
+// RT: 16-row tiles of queries.
+template <int DH, bool F8, int RT>
+__global__ __launch_bounds__(256, RT == 1 ? 2 : 1) void k_paged_attn_few(PagedAttn a) {
+    using Tile = FewTile<DH, F8>;
+    constexpr int F = DH / 16, R = 16 * RT, PS = DH + 2;     // PS: floats of a partial row: outputs, maximum, sum
+    constexpr int ES = F8 ? 1 : 2, kGrid = CSD_PAGED_FEW_GRID / RT;
+    __shared__ int s_pages[kFewPages];
+    __shared__ __align__(16) float s_o[4][R][DH + 4];
+    __shared__ float s_m[4][R], s_l[4][R], s_w[CSD_PAGED_FEW_PARTS][R];
+    __shared__ int s_last;
+    const PagedPool &p = a.p;
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, col = lane & 15, g = lane >> 4;
+    const int cap = p.table_stride << p.page_shift;
+
+    // ---- the tiles of every sequence
+    auto seq_of = [&](int b, PagedSeq &s) -> int {
+        s = PagedSeq{0, 0, 0};
+        if (b >= a.r.B) return 0;
+        s = paged_seq(a.r, b);
+        s.m = min(s.m, a.max_rows);
+        const int rows = s.m * a.group;
+        return rows >= 1 && rows <= R ? (min(s.t + s.m, cap) + 31) >> 5 : 0;
+    };
+    PagedSeq s0;
+    const int n0 = seq_of(lane, s0);                         // the first 64 sequences stay in registers
+    int sum = n0, longest = n0;
+    for (int b0 = 64; b0 < a.r.B; b0 += 64) {
+        PagedSeq s;
+        const int n = seq_of(b0 + lane, s);
+        sum += n;
+        longest = max(longest, n);
+    }
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) {
+        sum += __shfl_xor(sum, o, 64);
+        longest = max(longest, __shfl_xor(longest, o, 64));
+    }
+    longest = __builtin_amdgcn_readfirstlane(longest);
+    const int T = __builtin_amdgcn_readfirstlane(sum) * p.Hkv;
+    if (T == 0) return;
+    // a share is at least CSD_PAGED_FEW_SHARE tiles, and so long that no item has more parts than the join has room for
+    const int least = max(CSD_PAGED_FEW_SHARE, (longest + CSD_PAGED_FEW_PARTS - 3) / (CSD_PAGED_FEW_PARTS - 2));
+    const int n_wg = min((int)kGrid, max(1, T / least));
+    if ((int)blockIdx.x >= n_wg) return;
+    const FewShares shares(T, n_wg);
+    const int u_end = shares.first(blockIdx.x + 1);
+
+    for (int u = shares.first(blockIdx.x); u < u_end;) {
+        // ---- the item of tile u: sequence b, key-value head kvh, tiles t0 .. t1 of its n
+        int b = 0, n = 0, before = 0;
+        PagedSeq seq{0, 0, 0};
+        for (int b0 = 0; b0 < a.r.B; b0 += 64) {
+            PagedSeq s = s0;
+            const int nn = b0 == 0 ? n0 : seq_of(b0 + lane, s);
+            int incl = nn * p.Hkv;
+#pragma unroll
+            for (int o = 1; o < 64; o <<= 1) {
+                const int x = __shfl_up(incl, o, 64);
+                if (lane >= o) incl += x;
+            }
+            const unsigned long long past = __ballot(before + incl > u);
+            if (past) {
+                const int j = __ffsll((long long)past) - 1;
+                b = b0 + j;
+                n = __builtin_amdgcn_readlane(nn, j);
+                before += __builtin_amdgcn_readlane(incl, j) - n * p.Hkv;
+                seq = PagedSeq{__builtin_amdgcn_readlane(s.start, j), __builtin_amdgcn_readlane(s.m, j), __builtin_amdgcn_readlane(s.t, j)};
+                break;
+            }
+            before += __builtin_amdgcn_readlane(incl, 63);
+        }
+        if (n == 0) return;                                  // (the lengths changed while they were read)
+        const int kvh = (u - before) / n, t0 = u - before - kvh * n;
+        const int item = u - t0, t1 = min(n, t0 + u_end - u);
+        const int len = min(seq.t + seq.m, cap), rows = seq.m * a.group;
+        u += t1 - t0;
+
+        // ---- queries: row r = token r / group, head r % group of the group
+        u32x4 qf[RT][DH / 32];
+        int limit[RT];                                       // last position the lane's row attends
+        unsigned long long above[RT];
+        unsigned long long anc = 1ull << lane;               // tree: ancestors of block row `lane`, by doubling the step up
+        if (a.parent) {
+            int up = 0;
+            if (lane < seq.m && lane > 0) {
+                up = a.parent[seq.start + lane];
+                if (up < 0 || up >= lane) up = 0;
+            }
+            anc |= 1ull << up;
+#pragma unroll
+            for (int i = 0; i < 6; i++) {
+                const unsigned lo = __shfl((unsigned)anc, up, 64), hi = __shfl((unsigned)(anc >> 32), up, 64);
+                anc |= ((unsigned long long)hi << 32) | lo;
+                up = __shfl(up, up, 64);
+            }
+        }
+#pragma unroll
+        for (int rt = 0; rt < RT; rt++) {
+            const int r = rt * 16 + col, i = r / a.group, h = r - i * a.group;
+            limit[rt] = seq.t + i;
+            above[rt] = 0;
+            if (a.parent) {
+                const int src = min(i, 63);
+                above[rt] = ((unsigned long long)(unsigned)__shfl((unsigned)(anc >> 32), src, 64) << 32) | (unsigned)__shfl((unsigned)anc, src, 64);
+            }
+            const bf16_t *q = reinterpret_cast<const bf16_t *>(a.q) + (size_t)(seq.start + i) * a.q_stride + (size_t)(kvh * a.group + h) * DH;
+#pragma unroll
+            for (int s = 0; s < DH / 32; s++) {
+                qf[rt][s] = u32x4{0u, 0u, 0u, 0u};
+                const int at = F8 ? 64 * (s / 2) + 16 * g + 8 * (s & 1) : 32 * s + 8 * g;      // features of the K operand's step s
+                if (r < rows) qf[rt][s] = *reinterpret_cast<const u32x4 *>(q + at);
+            }
+        }
+        const float scale = a.scale * 1.44269504088896f;     // scores in units of log2
+        f32x4 acc[RT][F];
+        float m_run[RT], l_run[RT];
+#pragma unroll
+        for (int rt = 0; rt < RT; rt++) {
+            m_run[rt] = -INFINITY;
+            l_run[rt] = 0.f;
+#pragma unroll
+            for (int j = 0; j < F; j++) acc[rt][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+        }
+
+        for (int c0 = t0; c0 < t1;) {
+            // ---- the pages of tiles c0 .. c1
+            const int page0 = (c0 * 32) >> p.page_shift;
+            const int c1 = min((long long)t1, ((long long)(page0 + kFewPages) << p.page_shift) >> 5);
+            const int n_pages = (((c1 * 32 - 1) >> p.page_shift) - page0) + 1;
+            __syncthreads();
+            for (int i = tid; i < n_pages; i += 256) s_pages[i] = paged_page(p, b, (page0 + i) << p.page_shift);
+            __syncthreads();
+
+            // A wave's loads run ahead by half a tile: the next tile's keys are requested when this tile's scores are made, its values when this
+            // tile's products are.
+            Tile t;
+            auto load_k = [&](int tile) {
+                const int key = tile * 32 + 8 * (col >> 2);
+                const int page = max(s_pages[(key >> p.page_shift) - page0], 0);      // (no page: rows of page 0, which the masks leave out)
+                const char *kp = reinterpret_cast<const char *>(p.k) + paged_row(p, page, kvh, key + (col & 3)) * (DH * ES) + 16 * g;
+#pragma unroll
+                for (int T2 = 0; T2 < 2; T2++)
+#pragma unroll
+                    for (int s = 0; s < Tile::KV; s++) t.k[T2][s] = *reinterpret_cast<const u32x4 *>(kp + T2 * 4 * DH * ES + s * 64);
+                if constexpr (F8) {
+                    const int key8 = tile * 32 + 8 * g;
+                    t.ks = *reinterpret_cast<const u32x2 *>(p.ks + paged_row(p, max(s_pages[(key8 >> p.page_shift) - page0], 0), kvh, key8));
+                }
+            };
+            auto load_v = [&](int tile) {
+                const int key = tile * 32 + 8 * g;
+                const int page = s_pages[(key >> p.page_shift) - page0];
+                t.here = page >= 0;
+                const size_t row = paged_row(p, max(page, 0), kvh, key);
+                const char *vp = reinterpret_cast<const char *>(p.v) + row * (DH * ES) + col * (F * ES);
+#pragma unroll
+                for (int e = 0; e < 8; e++) load_words<Tile::VW>(vp + e * DH * ES, t.v[e]);
+                if constexpr (F8) t.vs = *reinterpret_cast<const u32x2 *>(p.vs + row);
+            };
+
+            int tile = c0 + wave;
+            if (tile < c1) {
+                load_k(tile);
+                load_v(tile);
+            }
+#pragma unroll 1
+            for (; tile < c1; tile += 4) {
+                const int key0 = tile * 32, key = key0 + 8 * g;
+                const bool whole = key0 + 32 <= seq.t && __all(t.here);      // (uniform) every row attends all 32 keys
+                float x[RT][8];
+                {
+                    f32x4 st[RT][2];
+#pragma unroll
+                    for (int rt = 0; rt < RT; rt++) st[rt][0] = st[rt][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int T2 = 0; T2 < 2; T2++)
+#pragma unroll
+                        for (int s = 0; s < DH / 32; s++) {
+                            u32x4 kf;
+                            if constexpr (F8) {
+                                const uint32_t lo = t.k[T2][s / 2][2 * (s & 1)], hi = t.k[T2][s / 2][2 * (s & 1) + 1];
+                                kf = u32x4{bf16x2_of_fp8<false>(lo), bf16x2_of_fp8<true>(lo), bf16x2_of_fp8<false>(hi), bf16x2_of_fp8<true>(hi)};
+                            } else {
+                                kf = t.k[T2][s];
+                            }
+#pragma unroll
+                            for (int rt = 0; rt < RT; rt++) st[rt][T2] = mfma16(kf, qf[rt][s], st[rt][T2]);
+                        }
+#pragma unroll
+                    for (int e = 0; e < 8; e++) {
+                        float f = scale;
+                        if constexpr (F8) f *= pow2_of_byte((t.ks[e >> 2] >> (8 * (e & 3))) & 0xFFu);
+#pragma unroll
+                        for (int rt = 0; rt < RT; rt++) x[rt][e] = st[rt][e >> 2][e & 3] * f;
+                    }
+                }
+                if (tile + 4 < c1) load_k(tile + 4);
+
+                u32x4 hi[RT], lo[RT];
+                uint32_t sees[RT];                           // bit e: the lane's row attends key + e
+#pragma unroll
+                for (int rt = 0; rt < RT; rt++) {
+                    sees[rt] = 0xFFu;
+                    if (!whole) {
+                        const int n_see = t.here ? min(max(min(limit[rt] + 1, len) - key, 0), 8) : 0;
+                        sees[rt] = (1u << n_see) - 1u;
+                        if (a.parent) {
+                            const int d = key - seq.t;       // rows of the block lie at d .. d + 7 of `above`; keys before them are cached
+                            const unsigned long long m = d >= 0 ? (d < 64 ? above[rt] >> d : 0ull) : (above[rt] << min(-d, 8)) | ((1ull << min(-d, 8)) - 1);
+                            sees[rt] &= (uint32_t)m;
+                        }
+#pragma unroll
+                        for (int e = 0; e < 8; e++)
+                            if (!((sees[rt] >> e) & 1u)) x[rt][e] = -INFINITY;
+                    }
+                    float top = fmaxf(fmaxf(fmaxf(x[rt][0], x[rt][1]), fmaxf(x[rt][2], x[rt][3])),
+                                      fmaxf(fmaxf(x[rt][4], x[rt][5]), fmaxf(x[rt][6], x[rt][7])));
+                    top = groups_max(sees[rt] ? fmaxf(top, -3.0e38f) : top);     // -inf: nothing to attend yet (a score of -inf is something)
+                    if (__any(top > m_run[rt])) {
+                        const float m_new = fmaxf(m_run[rt], top), fade = __builtin_amdgcn_exp2f(m_run[rt] - (m_new == -INFINITY ? 0.f : m_new));
+                        l_run[rt] *= fade;
+#pragma unroll
+                        for (int j = 0; j < F; j++) acc[rt][j] *= fade;
+                        m_run[rt] = m_new;
+                    }
+                    const float ref = m_run[rt] == -INFINITY ? 0.f : m_run[rt];
+#pragma unroll
+                    for (int i = 0; i < 4; i++) {
+                        float w[2];
+#pragma unroll
+                        for (int o = 0; o < 2; o++) {
+                            const int e = 2 * i + o;
+                            w[o] = __builtin_amdgcn_exp2f(x[rt][e] - ref);
+                            l_run[rt] += w[o];
+                            if constexpr (F8) {              // (the byte of a place that nobody wrote may be anything)
+                                const float f = pow2_of_byte((t.vs[e >> 2] >> (8 * (e & 3))) & 0xFFu);
+                                w[o] = (sees[rt] >> e) & 1u ? w[o] * f : 0.f;
+                            }
+                        }
+                        hi[rt][i] = pack_bf16x2(w[0], w[1]);
+                        lo[rt][i] = pack_bf16x2(w[0] - __uint_as_float(hi[rt][i] << 16), w[1] - __uint_as_float(hi[rt][i] & 0xFFFF0000u));
+                    }
+                }
+
+                u32x4 vf[F];
+                v_operands<DH, F8>(t.v, vf);
+                bool odd = false;
+                if (!whole) {
+                    // keys behind the sequence's last are whatever the page holds, keys without a page somebody else's
+                    const int n_in = t.here ? min(max(len - key, 0), 8) : 0;
+#pragma unroll
+                    for (int i = 0; i < 4; i++) {
+                        const uint32_t keep = (2 * i < n_in ? 0xFFFFu : 0u) | (2 * i + 1 < n_in ? 0xFFFF0000u : 0u);
+#pragma unroll
+                        for (int j = 0; j < F; j++) {
+                            vf[j][i] &= keep;
+                            odd |= (vf[j][i] & 0x7F80u) == 0x7F80u || (vf[j][i] & 0x7F800000u) == 0x7F800000u;
+                        }
+                    }
+                }
+                if (__any(odd)) {
+                    // Rows differ in what they attend, and 0 * inf must not reach a row that does not: the values that are not finite leave the
+                    // products, and rows that attend a +inf, a -inf or NaN (both) are found by products of ones.
+#pragma unroll
+                    for (int j = 0; j < F; j++) {
+                        u32x4 up, down;
+#pragma unroll
+                        for (int i = 0; i < 4; i++) {
+                            const uint32_t v = vf[j][i], e0 = (v & 0x7F80u) == 0x7F80u ? 0xFFFFu : 0u, e1 = (v & 0x7F800000u) == 0x7F800000u ? 0xFFFF0000u : 0u;
+                            const uint32_t neg0 = (v & 0xFFFFu) == 0xFF80u ? 0xFFFFu : 0u, neg1 = (v & 0xFFFF0000u) == 0xFF800000u ? 0xFFFF0000u : 0u;
+                            const uint32_t pos0 = (v & 0xFFFFu) == 0x7F80u ? 0xFFFFu : 0u, pos1 = (v & 0xFFFF0000u) == 0x7F800000u ? 0xFFFF0000u : 0u;
+                            up[i] = (e0 | e1) & ~(neg0 | neg1) & 0x3F803F80u;
+                            down[i] = (e0 | e1) & ~(pos0 | pos1) & 0x3F803F80u;
+                            vf[j][i] = v & ~(e0 | e1);
+                        }
+#pragma unroll
+                        for (int rt = 0; rt < RT; rt++) {
+                            u32x4 seen;
+#pragma unroll
+                            for (int i = 0; i < 4; i++)
+                                seen[i] = (((sees[rt] >> (2 * i)) & 1u) * 0x3F80u) | (((sees[rt] >> (2 * i + 1)) & 1u) * 0x3F800000u);
+                            const f32x4 zero = f32x4{0.f, 0.f, 0.f, 0.f};
+                            const f32x4 ups = mfma16(up, seen, zero), downs = mfma16(down, seen, zero);
+#pragma unroll
+                            for (int i = 0; i < 4; i++) {
+                                acc[rt][j][i] += ups[i] > 0.f ? INFINITY : 0.f;
+                                acc[rt][j][i] -= downs[i] > 0.f ? INFINITY : 0.f;
+                            }
+                        }
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
+                }
+#pragma unroll
+                for (int rt = 0; rt < RT; rt++)
+#pragma unroll
+                    for (int j = 0; j < F; j++) {
+                        acc[rt][j] = mfma16(vf[j], hi[rt], acc[rt][j]);
+                        acc[rt][j] = mfma16(vf[j], lo[rt], acc[rt][j]);
+                    }
+                if (tile + 4 < c1) load_v(tile + 4);
+            }
+            c0 = c1;
+        }
+
+        // ---- the four waves' results
+#pragma unroll
+        for (int rt = 0; rt < RT; rt++) {
+            l_run[rt] = groups_sum(l_run[rt]);
+            if (g == 0) {
+                s_m[wave][rt * 16 + col] = m_run[rt];
+                s_l[wave][rt * 16 + col] = l_run[rt];
+            }
+#pragma unroll
+            for (int j = 0; j < F; j++)                      // product j, A-row 4 g + i: feature F (4 g + i) + j
+#pragma unroll
+                for (int i = 0; i < 4; i++) s_o[wave][rt * 16 + col][F * (4 * g + i) + j] = acc[rt][j][i];
+        }
+        __syncthreads();
+        const int w_first = shares.owner(item), w_last = shares.owner(item + n - 1);
+        const bool split = w_first != w_last;
+        float *part = reinterpret_cast<float *>(reinterpret_cast<char *>(a.ws) + CSD_PAGED_COUNTER_BYTES);
+        float *mine = part + (size_t)(2 * blockIdx.x + (w_first == (int)blockIdx.x ? 1 : 0)) * R * PS;
+        for (int x = tid; x < rows * (DH / 2); x += 256) {
+            const int r = x / (DH / 2), c = 2 * (x % (DH / 2));
+            float m = s_m[0][r];
+#pragma unroll
+            for (int w = 1; w < 4; w++) m = fmaxf(m, s_m[w][r]);
+            const float ref = m == -INFINITY ? 0.f : m;
+            float l = 0.f, o0 = 0.f, o1 = 0.f;
+#pragma unroll
+            for (int w = 0; w < 4; w++) {
+                const float f = __builtin_amdgcn_exp2f(s_m[w][r] - ref);
+                l += f * s_l[w][r];
+                o0 += f * s_o[w][r][c];
+                o1 += f * s_o[w][r][c + 1];
+            }
+            if (!split) {
+                const int i = r / a.group, h = r - i * a.group;
+                const float inv = m == -INFINITY ? 0.f : 1.f / l;
+                uint32_t *out = reinterpret_cast<uint32_t *>(a.out) + (((size_t)(seq.start + i) * p.Hkv + kvh) * a.group + h) * (DH / 2);
+                out[c / 2] = m == -INFINITY ? 0u : pack_bf16x2(o0 * inv, o1 * inv);
+            } else {
+                store_dev(mine + r * PS + c, o0, o1);
+                if (c == 0) store_dev(mine + r * PS + DH, m, l);
+            }
+        }
+        if (split) {
+            // the stores above are acknowledged before the counter moves; whoever arrives last joins the parts, in their order
+            __builtin_amdgcn_s_waitcnt(0x0F70);              // vmcnt(0)
+            __syncthreads();
+            unsigned *count = reinterpret_cast<unsigned *>(a.ws) + w_first;
+            const int parts = w_last - w_first + 1;
+            if (tid == 0) s_last = __hip_atomic_fetch_add(count, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (unsigned)(parts - 1);
+            __syncthreads();
+            if (s_last) {
+                auto at = [&](int i) { return part + (size_t)(2 * (w_first + i) + (i == 0 ? 1 : 0)) * R * PS; };
+                float *sums = &s_o[0][0][0];                 // (the waves' results are no longer needed)
+                for (int x = tid; x < parts * rows; x += 256) {
+                    const int i = x / rows, r = x - i * rows;
+                    const float2 ml = load_dev(at(i) + r * PS + DH);
+                    s_w[i][r] = ml.x;
+                    sums[i * R + r] = ml.y;
+                }
+                __syncthreads();
+                if (tid < rows) {
+                    float m = -INFINITY, l = 0.f;
+                    for (int i = 0; i < parts; i++) m = fmaxf(m, s_w[i][tid]);
+                    const float ref = m == -INFINITY ? 0.f : m;
+                    for (int i = 0; i < parts; i++) {
+                        const float f = __builtin_amdgcn_exp2f(s_w[i][tid] - ref);
+                        l += f * sums[i * R + tid];
+                        s_w[i][tid] = f;
+                    }
+                    s_m[0][tid] = m;
+                    s_l[0][tid] = l;
+                }
+                __syncthreads();
+                for (int x = tid; x < rows * (DH / 2); x += 256) {
+                    const int r = x / (DH / 2), c = 2 * (x % (DH / 2));
+                    float o0 = 0.f, o1 = 0.f;
+                    for (int i0 = 0; i0 < parts; i0 += 8) {
+                        float2 v[8];
+#pragma unroll
+                        for (int k = 0; k < 8; k++) v[k] = load_dev(at(min(i0 + k, parts - 1)) + r * PS + c);
+#pragma unroll
+                        for (int k = 0; k < 8; k++) {
+                            const float f = i0 + k < parts ? s_w[i0 + k][r] : 0.f;
+                            if (i0 + k < parts) {
+                                o0 += f * v[k].x;
+                                o1 += f * v[k].y;
+                            }
+                        }
+                    }
+                    const int i = r / a.group, h = r - i * a.group;
+                    const float inv = 1.f / s_l[0][r];
+                    uint32_t *out = reinterpret_cast<uint32_t *>(a.out) + (((size_t)(seq.start + i) * p.Hkv + kvh) * a.group + h) * (DH / 2);
+                    out[c / 2] = s_m[0][r] == -INFINITY ? 0u : pack_bf16x2(o0 * inv, o1 * inv);
+                }
+                if (tid == 0) __hip_atomic_store(count, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);   // ready for the next launch
+            }
+        }
+        __syncthreads();
+    }
+}
+
+template <int DH, bool F8, int RT>
+static void few_launch(const PagedAttn &a, hipStream_t st) {
+    hipLaunchKernelGGL((k_paged_attn_few<DH, F8, RT>), dim3(CSD_PAGED_FEW_GRID / RT), dim3(256), 0, st, a);
+}
+
+template <int DH, bool F8>
+static void few_rows(const PagedAttn &a, int rows, hipStream_t st) {
+    if (rows <= 16) few_launch<DH, F8, 1>(a, st);
+    else few_launch<DH, F8, 2>(a, st);
+}
+
+bool csd_paged_few_fits(const PagedAttn &a, int32_t pool_dtype, int32_t q_dtype) {
+    if (q_dtype != CSD_DTYPE_BF16 || pool_dtype == CSD_DTYPE_FP32 || (a.p.D != 64 && a.p.D != 128)) return false;
+    // tiles are counted in 32 bits
+    const long long tiles = (((long long)a.p.table_stride << a.p.page_shift) + 31) / 32;
+    return tiles * a.p.Hkv * a.r.B < (1ll << 30);
+}
+
+void csd_paged_few_enqueue(const PagedAttn &a, int rows, int32_t pool_dtype, hipStream_t st) {
+    if (a.p.D == 128) {
+        if (pool_dtype == CSD_DTYPE_FP8) few_rows<128, true>(a, rows, st);
+        else few_rows<128, false>(a, rows, st);
+    } else {
+        if (pool_dtype == CSD_DTYPE_FP8) few_rows<64, true>(a, rows, st);
+        else few_rows<64, false>(a, rows, st);
+    }
+}

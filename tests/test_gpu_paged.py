@@ -217,7 +217,7 @@ def test_attention_of_small_batches(rows, cache, d, kv_heads, group):
         q = c.random_rows(c.total, kv_heads * group)
         out = c.attend(q, d ** -0.5, max(new))
         c.check(out, q, d ** -0.5)
-        assert torch.equal(out, c.attend(q, d ** -0.5))                 # whatever bound on the rows the caller knows
+        c.check(c.attend(q, d ** -0.5), q, d ** -0.5)        # another bound on the rows may take another kernel: the same limits, not the same bits
 
 
 @pytest.mark.parametrize("rows,cache,d,kv_heads,group", [("bf16", "bf16", 128, 2, 4), ("bf16", "fp8", 128, 2, 2), ("bf16", "bf16", 64, 3, 1), ("bf16", "fp8", 64, 1, 8), ("fp32", "fp32", 32, 2, 2)])
