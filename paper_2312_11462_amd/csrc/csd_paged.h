@@ -95,6 +95,22 @@ template <> __device__ __forceinline__ void store8<bf16_t>(bf16_t *p, const floa
         u32x4{pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7])};
 }
 
+// Values that are not finite.  Rows of a block differ in what they attend, and on the matrix cores 0 * inf = NaN would reach the rows that do
+// not attend such a value.  Where rows differ, the kernels take these values out of the products and remember that there were some;
+// in that rare case they go through the keys once more and add the values themselves to the outputs of the rows that attend them.
+// Bits of a pair of bf16 that are not finite, as masks of 16 ones.
+__device__ __forceinline__ uint32_t odd_halves(uint32_t v) {
+    return ((v & 0x7F80u) == 0x7F80u ? 0xFFFFu : 0u) | ((v & 0x7F800000u) == 0x7F800000u ? 0xFFFF0000u : 0u);
+}
+// what element c of a row adds to the output of a row that attends it: 0, or the value if it is not finite
+template <bool F8>
+__device__ __forceinline__ float odd_value(const void *row, int c) {
+    float v;
+    if constexpr (F8) v = __builtin_amdgcn_cvt_f32_fp8((int)reinterpret_cast<const uint8_t *>(row)[c], 0);
+    else v = bf16_to_f32(reinterpret_cast<const bf16_t *>(row)[c]);
+    return fabsf(v) < INFINITY ? 0.f : v;
+}
+
 // One attention call.
 struct PagedAttn {
     PagedPool p;
@@ -119,3 +135,11 @@ int32_t csd_paged_attention_enqueue(const PagedAttn &a, int32_t pool_dtype, int3
 static_assert(CSD_PAGED_COUNTER_BYTES + 2ull * CSD_PAGED_FEW_GRID * CSD_PAGED_FEW_ROWS * 130 * 4 <= CSD_PAGED_WORKSPACE_BYTES, "");
 bool csd_paged_few_fits(const PagedAttn &a, int32_t pool_dtype, int32_t q_dtype);
 void csd_paged_few_enqueue(const PagedAttn &a, int rows, int32_t pool_dtype, hipStream_t st);
+
+// csd_paged_many.hip: the others, 128 rows per workgroup, in the same types and head sizes.
+#define CSD_PAGED_MANY_ROWS 128
+#define CSD_PAGED_MANY_SHARE 4       /* tiles of 64 keys per part of an item at least */
+#define CSD_PAGED_MANY_PARTS 8       /* parts of an item at most */
+#define CSD_PAGED_MANY_SLOTS 1024    /* items times parts at most, where items are split */
+static_assert(CSD_PAGED_COUNTER_BYTES + (size_t)CSD_PAGED_MANY_SLOTS * CSD_PAGED_MANY_ROWS * 130 * 4 <= CSD_PAGED_WORKSPACE_BYTES, "");
+void csd_paged_many_enqueue(const PagedAttn &a, int min_rows, int32_t pool_dtype, hipStream_t st);

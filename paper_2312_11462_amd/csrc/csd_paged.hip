@@ -213,7 +213,7 @@ static int32_t check_rows(const csd_paged_kv *kv, int32_t layer, const int32_t *
     if (!row_start || !pos) return CSD_ENULL;
     if (B < 1 || rows < 0 || layer < 0 || layer >= kv->n_layers) return CSD_EINVAL;
     if (dtype != CSD_DTYPE_FP32 && dtype != CSD_DTYPE_BF16) return CSD_EINVAL;
-    if (rows > (1 << 24) || B > (1 << 20)) return CSD_ESHAPE;
+    if (rows > (1 << 22) || B > (1 << 20)) return CSD_ESHAPE;
     return CSD_OK;
 }
 
@@ -266,7 +266,7 @@ extern "C" int32_t csd_paged_write(const csd_paged_kv *kv, int32_t layer, const 
     const int log_w = ilog2(kv->head_dim / 8);
     const long long threads = ((long long)rows * kv->n_kv_heads) << log_w;
     const long long grid = (threads + kPagedThreads - 1) / kPagedThreads;
-    if (grid > 0x7FFFFFFF) return CSD_ESHAPE;
+    if (grid > 0xFFFFFF) return CSD_ESHAPE;                  // (work items of a launch are counted in 32 bits)
     by_types(dtype, kv->dtype, [&](auto *dense, auto *pool) {
         using TR = std::remove_pointer_t<decltype(dense)>;
         using TP = std::remove_pointer_t<decltype(pool)>;
@@ -290,7 +290,7 @@ extern "C" int32_t csd_paged_read(const csd_paged_kv *kv, int32_t layer, const i
     const int log_w = ilog2(kv->head_dim / 8);
     const long long threads = ((long long)rows * kv->n_kv_heads) << log_w;
     const long long grid = (threads + kPagedThreads - 1) / kPagedThreads;
-    if (grid > 0x7FFFFFFF) return CSD_ESHAPE;
+    if (grid > 0xFFFFFF) return CSD_ESHAPE;                  // (work items of a launch are counted in 32 bits)
     by_types(dtype, kv->dtype, [&](auto *dense, auto *pool) {
         using TR = std::remove_pointer_t<decltype(dense)>;
         using TP = std::remove_pointer_t<decltype(pool)>;

@@ -219,6 +219,7 @@ __global__ __launch_bounds__(256, RT == 1 ? 2 : 1) void k_paged_attn_few(PagedAt
         const float scale = a.scale * 1.44269504088896f;     // scores in units of log2
         f32x4 acc[RT][F];
         float m_run[RT], l_run[RT];
+        uint32_t odd = 0;                                    // the wave took values out of its products
 #pragma unroll
         for (int rt = 0; rt < RT; rt++) {
             m_run[rt] = -INFINITY;
@@ -230,7 +231,8 @@ __global__ __launch_bounds__(256, RT == 1 ? 2 : 1) void k_paged_attn_few(PagedAt
         for (int c0 = t0; c0 < t1;) {
             // ---- the pages of tiles c0 .. c1
             const int page0 = (c0 * 32) >> p.page_shift;
-            const int c1 = min((long long)t1, ((long long)(page0 + kFewPages) << p.page_shift) >> 5);
+            const long long fits = ((long long)(page0 + kFewPages) << p.page_shift) >> 5;
+            const int c1 = fits >= t1 ? t1 : t0 + (((int)fits - t0) & ~3);      // (a wave keeps its turn from piece to piece)
             const int n_pages = (((c1 * 32 - 1) >> p.page_shift) - page0) + 1;
             __syncthreads();
             for (int i = tid; i < n_pages; i += 256) s_pages[i] = paged_page(p, b, (page0 + i) << p.page_shift);
@@ -349,9 +351,8 @@ __global__ __launch_bounds__(256, RT == 1 ? 2 : 1) void k_paged_attn_few(PagedAt
 
                 u32x4 vf[F];
                 v_operands<DH, F8>(t.v, vf);
-                bool odd = false;
                 if (!whole) {
-                    // keys behind the sequence's last are whatever the page holds, keys without a page somebody else's
+                    // keys behind the sequence's last are whatever the page holds, keys without a page somebody else's; and values that are not finite
                     const int n_in = t.here ? min(max(len - key, 0), 8) : 0;
 #pragma unroll
                     for (int i = 0; i < 4; i++) {
@@ -359,40 +360,10 @@ __global__ __launch_bounds__(256, RT == 1 ? 2 : 1) void k_paged_attn_few(PagedAt
 #pragma unroll
                         for (int j = 0; j < F; j++) {
                             vf[j][i] &= keep;
-                            odd |= (vf[j][i] & 0x7F80u) == 0x7F80u || (vf[j][i] & 0x7F800000u) == 0x7F800000u;
+                            const uint32_t o = odd_halves(vf[j][i]);
+                            odd |= o;
+                            vf[j][i] &= ~o;
                         }
-                    }
-                }
-                if (__any(odd)) {
-                    // Rows differ in what they attend, and 0 * inf must not reach a row that does not: the values that are not finite leave the
-                    // products, and rows that attend a +inf, a -inf or NaN (both) are found by products of ones.
-#pragma unroll
-                    for (int j = 0; j < F; j++) {
-                        u32x4 up, down;
-#pragma unroll
-                        for (int i = 0; i < 4; i++) {
-                            const uint32_t v = vf[j][i], e0 = (v & 0x7F80u) == 0x7F80u ? 0xFFFFu : 0u, e1 = (v & 0x7F800000u) == 0x7F800000u ? 0xFFFF0000u : 0u;
-                            const uint32_t neg0 = (v & 0xFFFFu) == 0xFF80u ? 0xFFFFu : 0u, neg1 = (v & 0xFFFF0000u) == 0xFF800000u ? 0xFFFF0000u : 0u;
-                            const uint32_t pos0 = (v & 0xFFFFu) == 0x7F80u ? 0xFFFFu : 0u, pos1 = (v & 0xFFFF0000u) == 0x7F800000u ? 0xFFFF0000u : 0u;
-                            up[i] = (e0 | e1) & ~(neg0 | neg1) & 0x3F803F80u;
-                            down[i] = (e0 | e1) & ~(pos0 | pos1) & 0x3F803F80u;
-                            vf[j][i] = v & ~(e0 | e1);
-                        }
-#pragma unroll
-                        for (int rt = 0; rt < RT; rt++) {
-                            u32x4 seen;
-#pragma unroll
-                            for (int i = 0; i < 4; i++)
-                                seen[i] = (((sees[rt] >> (2 * i)) & 1u) * 0x3F80u) | (((sees[rt] >> (2 * i + 1)) & 1u) * 0x3F800000u);
-                            const f32x4 zero = f32x4{0.f, 0.f, 0.f, 0.f};
-                            const f32x4 ups = mfma16(up, seen, zero), downs = mfma16(down, seen, zero);
-#pragma unroll
-                            for (int i = 0; i < 4; i++) {
-                                acc[rt][j][i] += ups[i] > 0.f ? INFINITY : 0.f;
-                                acc[rt][j][i] -= downs[i] > 0.f ? INFINITY : 0.f;
-                            }
-                        }
-                        __builtin_amdgcn_sched_barrier(0);
                     }
                 }
 #pragma unroll
@@ -405,6 +376,26 @@ __global__ __launch_bounds__(256, RT == 1 ? 2 : 1) void k_paged_attn_few(PagedAt
                 if (tile + 4 < c1) load_v(tile + 4);
             }
             c0 = c1;
+        }
+
+        if (__any(odd != 0u)) {
+            for (int tile = t0 + wave; tile < t1; tile += 4)
+                for (int key = tile * 32; key < min(tile * 32 + 32, len); key++) {
+                    const int page = paged_page(p, b, key);
+                    if (page < 0) continue;
+                    const char *row = reinterpret_cast<const char *>(p.v) + paged_row(p, page, kvh, key) * (DH * ES);
+#pragma unroll
+                    for (int rt = 0; rt < RT; rt++) {
+                        const bool attends = key <= limit[rt] && (!a.parent || key < seq.t || ((above[rt] >> min(key - seq.t, 63)) & 1ull));
+#pragma unroll
+                        for (int j = 0; j < F; j++)
+#pragma unroll
+                            for (int i = 0; i < 4; i++) {
+                                const float v = odd_value<F8>(row, F * (4 * g + i) + j);
+                                if (attends) acc[rt][j][i] += v;
+                            }
+                    }
+                }
         }
 
         // ---- the four waves' results
@@ -523,7 +514,7 @@ bool csd_paged_few_fits(const PagedAttn &a, int32_t pool_dtype, int32_t q_dtype)
     if (q_dtype != CSD_DTYPE_BF16 || pool_dtype == CSD_DTYPE_FP32 || (a.p.D != 64 && a.p.D != 128)) return false;
     // tiles are counted in 32 bits
     const long long tiles = (((long long)a.p.table_stride << a.p.page_shift) + 31) / 32;
-    return tiles * a.p.Hkv * a.r.B < (1ll << 30);
+    return tiles * a.p.Hkv * a.r.B < (1ll << 30) && (long long)a.r.rows * a.p.Hkv * a.group < (1ll << 30);
 }
 
 void csd_paged_few_enqueue(const PagedAttn &a, int rows, int32_t pool_dtype, hipStream_t st) {
