@@ -102,13 +102,13 @@ template <> __device__ __forceinline__ void store8<bf16_t>(bf16_t *p, const floa
 __device__ __forceinline__ uint32_t odd_halves(uint32_t v) {
     return ((v & 0x7F80u) == 0x7F80u ? 0xFFFFu : 0u) | ((v & 0x7F800000u) == 0x7F800000u ? 0xFFFF0000u : 0u);
 }
-// what element c of a row adds to the output of a row that attends it: 0, or the value if it is not finite
+// what element c of a row adds to the output of a row that attends it (or does not): the value if it is not finite, else 0
 template <bool F8>
-__device__ __forceinline__ float odd_value(const void *row, int c) {
+__device__ __forceinline__ float odd_value(const void *row, int c, bool attends) {
     float v;
     if constexpr (F8) v = __builtin_amdgcn_cvt_f32_fp8((int)reinterpret_cast<const uint8_t *>(row)[c], 0);
     else v = bf16_to_f32(reinterpret_cast<const bf16_t *>(row)[c]);
-    return fabsf(v) < INFINITY ? 0.f : v;
+    return fabsf(v) < INFINITY || !attends ? 0.f : v;
 }
 
 // One attention call.

@@ -52,27 +52,24 @@ __device__ __forceinline__ uint32_t bf16x2_of_fp8(uint32_t w) {
     return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, HI));
 }
 
-// V^T operand of feature j from the eight keys' words: dword i holds keys 2 i, 2 i + 1
+// V^T operands of features y .. y + 3 (of the lane's DH / 16) from the eight keys' words: dword i holds keys 2 i, 2 i + 1
 template <int DH, bool F8>
-__device__ __forceinline__ void v_operands(const uint32_t (&v)[8][FewTile<DH, F8>::VW], u32x4 (&f)[DH / 16]) {
-    constexpr int F = DH / 16;
+__device__ __forceinline__ void v_operands(const uint32_t (&v)[8][FewTile<DH, F8>::VW], u32x4 (&f)[4], int y) {
 #pragma unroll
     for (int i = 0; i < 4; i++) {
         const uint32_t *a = v[2 * i], *b = v[2 * i + 1];
         if constexpr (F8) {
-#pragma unroll
-            for (int w = 0; w < F / 4; w++) {
-                const uint32_t lo = __builtin_amdgcn_perm(b[w], a[w], 0x05010400u), hi = __builtin_amdgcn_perm(b[w], a[w], 0x07030602u);
-                f[4 * w][i] = bf16x2_of_fp8<false>(lo);
-                f[4 * w + 1][i] = bf16x2_of_fp8<true>(lo);
-                f[4 * w + 2][i] = bf16x2_of_fp8<false>(hi);
-                f[4 * w + 3][i] = bf16x2_of_fp8<true>(hi);
-            }
+            const int w = y / 4;
+            const uint32_t lo = __builtin_amdgcn_perm(b[w], a[w], 0x05010400u), hi = __builtin_amdgcn_perm(b[w], a[w], 0x07030602u);
+            f[0][i] = bf16x2_of_fp8<false>(lo);
+            f[1][i] = bf16x2_of_fp8<true>(lo);
+            f[2][i] = bf16x2_of_fp8<false>(hi);
+            f[3][i] = bf16x2_of_fp8<true>(hi);
         } else {
 #pragma unroll
-            for (int w = 0; w < F / 2; w++) {
-                f[2 * w][i] = __builtin_amdgcn_perm(b[w], a[w], 0x05040100u);
-                f[2 * w + 1][i] = __builtin_amdgcn_perm(b[w], a[w], 0x07060302u);
+            for (int w = 0; w < 2; w++) {
+                f[2 * w][i] = __builtin_amdgcn_perm(b[y / 2 + w], a[y / 2 + w], 0x05040100u);
+                f[2 * w + 1][i] = __builtin_amdgcn_perm(b[y / 2 + w], a[y / 2 + w], 0x07060302u);
             }
         }
     }
@@ -105,13 +102,16 @@ __device__ __forceinline__ float2 load_dev(const float *p) {
 
 // RT: 16-row tiles of queries.
 template <int DH, bool F8, int RT>
-__global__ __launch_bounds__(256, RT == 1 ? 2 : 1) void k_paged_attn_few(PagedAttn a) {
+__global__ __launch_bounds__(256, 2) void k_paged_attn_few(PagedAttn a) {
     using Tile = FewTile<DH, F8>;
     constexpr int F = DH / 16, R = 16 * RT, PS = DH + 2;     // PS: floats of a partial row: outputs, maximum, sum
-    constexpr int ES = F8 ? 1 : 2, kGrid = CSD_PAGED_FEW_GRID / RT;
+    constexpr bool LO = RT == 1;
+    constexpr int NB = F8 && (RT == 1 || DH == 64) ? 2 : 1;
+    constexpr int ES = F8 ? 1 : 2, kGrid = CSD_PAGED_FEW_GRID;
     __shared__ int s_pages[kFewPages];
     __shared__ __align__(16) float s_o[4][R][DH + 4];
-    __shared__ float s_m[4][R], s_l[4][R], s_w[CSD_PAGED_FEW_PARTS][R];
+    __shared__ float s_m[4][R], s_l[4][R];
+    static_assert(2 * CSD_PAGED_FEW_PARTS * R <= 4 * R * (DH + 4) && RT * (DH / 32) * 64 * 16 <= 4 * R * (DH + 4) * 4, "");
     __shared__ int s_last;
     const PagedPool &p = a.p;
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, col = lane & 15, g = lane >> 4;
@@ -181,7 +181,8 @@ __global__ __launch_bounds__(256, RT == 1 ? 2 : 1) void k_paged_attn_few(PagedAt
         u += t1 - t0;
 
         // ---- queries: row r = token r / group, head r % group of the group
-        u32x4 qf[RT][DH / 32];
+        u32x4 qf[RT == 1 ? DH / 32 : 1];                      // (two row tiles: in LDS, where the waves' results will be; the registers are needed)
+        u32x4 *s_q = reinterpret_cast<u32x4 *>(&s_o[0][0][0]) + lane;
         int limit[RT];                                       // last position the lane's row attends
         unsigned long long above[RT];
         unsigned long long anc = 1ull << lane;               // tree: ancestors of block row `lane`, by doubling the step up
@@ -211,11 +212,14 @@ __global__ __launch_bounds__(256, RT == 1 ? 2 : 1) void k_paged_attn_few(PagedAt
             const bf16_t *q = reinterpret_cast<const bf16_t *>(a.q) + (size_t)(seq.start + i) * a.q_stride + (size_t)(kvh * a.group + h) * DH;
 #pragma unroll
             for (int s = 0; s < DH / 32; s++) {
-                qf[rt][s] = u32x4{0u, 0u, 0u, 0u};
+                u32x4 x = u32x4{0u, 0u, 0u, 0u};
                 const int at = F8 ? 64 * (s / 2) + 16 * g + 8 * (s & 1) : 32 * s + 8 * g;      // features of the K operand's step s
-                if (r < rows) qf[rt][s] = *reinterpret_cast<const u32x4 *>(q + at);
+                if (r < rows) x = *reinterpret_cast<const u32x4 *>(q + at);
+                if constexpr (RT == 1) qf[s] = x;
+                else if (wave == 0) s_q[(rt * (DH / 32) + s) * 64] = x;
             }
         }
+        const bool second = RT > 1 && rows > 16;             // the second row tile holds rows
         const float scale = a.scale * 1.44269504088896f;     // scores in units of log2
         f32x4 acc[RT][F];
         float m_run[RT], l_run[RT];
@@ -237,11 +241,14 @@ __global__ __launch_bounds__(256, RT == 1 ? 2 : 1) void k_paged_attn_few(PagedAt
             __syncthreads();
             for (int i = tid; i < n_pages; i += 256) s_pages[i] = paged_page(p, b, (page0 + i) << p.page_shift);
             __syncthreads();
+            // The queries have come too (before the table's entries, in order); said here, as otherwise the first product below waits for them, and
+            // with them for every load in flight, at every turn.
+            __builtin_amdgcn_s_waitcnt(0x0F70);              // vmcnt(0)
 
-            // A wave's loads run ahead by half a tile: the next tile's keys are requested when this tile's scores are made, its values when this
-            // tile's products are.
-            Tile t;
-            auto load_k = [&](int tile) {
+            // A wave has NB tiles' loads in flight, and the next one's as parts of a tile become free: its keys when the scores are made, its values
+            // when the products are.
+            Tile ring[NB];
+            auto load_k = [&](Tile &t, int tile) {
                 const int key = tile * 32 + 8 * (col >> 2);
                 const int page = max(s_pages[(key >> p.page_shift) - page0], 0);      // (no page: rows of page 0, which the masks leave out)
                 const char *kp = reinterpret_cast<const char *>(p.k) + paged_row(p, page, kvh, key + (col & 3)) * (DH * ES) + 16 * g;
@@ -254,7 +261,7 @@ __global__ __launch_bounds__(256, RT == 1 ? 2 : 1) void k_paged_attn_few(PagedAt
                     t.ks = *reinterpret_cast<const u32x2 *>(p.ks + paged_row(p, max(s_pages[(key8 >> p.page_shift) - page0], 0), kvh, key8));
                 }
             };
-            auto load_v = [&](int tile) {
+            auto load_v = [&](Tile &t, int tile) {
                 const int key = tile * 32 + 8 * g;
                 const int page = s_pages[(key >> p.page_shift) - page0];
                 t.here = page >= 0;
@@ -265,48 +272,62 @@ __global__ __launch_bounds__(256, RT == 1 ? 2 : 1) void k_paged_attn_few(PagedAt
                 if constexpr (F8) t.vs = *reinterpret_cast<const u32x2 *>(p.vs + row);
             };
 
-            int tile = c0 + wave;
-            if (tile < c1) {
-                load_k(tile);
-                load_v(tile);
-            }
-#pragma unroll 1
-            for (; tile < c1; tile += 4) {
+            auto step = [&](Tile &t, int tile, auto always) {
                 const int key0 = tile * 32, key = key0 + 8 * g;
                 const bool whole = key0 + 32 <= seq.t && __all(t.here);      // (uniform) every row attends all 32 keys
                 float x[RT][8];
+                int q_off = 0;
+                if constexpr (RT > 1) asm volatile("" : "+v"(q_off));   // (read here, at every tile)
                 {
-                    f32x4 st[RT][2];
+                    // (a half of the keys at a time, and below half of the features: the operands of a whole tile at once would not leave room for
+                    // two waves per SIMD)
 #pragma unroll
-                    for (int rt = 0; rt < RT; rt++) st[rt][0] = st[rt][1] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                    for (int T2 = 0; T2 < 2; T2++)
+                    for (int T2 = 0; T2 < 2; T2++) {
+                        u32x4 kf[DH / 32];
 #pragma unroll
                         for (int s = 0; s < DH / 32; s++) {
-                            u32x4 kf;
                             if constexpr (F8) {
                                 const uint32_t lo = t.k[T2][s / 2][2 * (s & 1)], hi = t.k[T2][s / 2][2 * (s & 1) + 1];
-                                kf = u32x4{bf16x2_of_fp8<false>(lo), bf16x2_of_fp8<true>(lo), bf16x2_of_fp8<false>(hi), bf16x2_of_fp8<true>(hi)};
+                                kf[s] = u32x4{bf16x2_of_fp8<false>(lo), bf16x2_of_fp8<true>(lo), bf16x2_of_fp8<false>(hi), bf16x2_of_fp8<true>(hi)};
                             } else {
-                                kf = t.k[T2][s];
+                                kf[s] = t.k[T2][s];
                             }
+                        }
+                        float f[4];
 #pragma unroll
-                            for (int rt = 0; rt < RT; rt++) st[rt][T2] = mfma16(kf, qf[rt][s], st[rt][T2]);
+                        for (int e = 0; e < 4; e++) {
+                            f[e] = scale;
+                            if constexpr (F8) f[e] *= pow2_of_byte((t.ks[T2] >> (8 * e)) & 0xFFu);
                         }
 #pragma unroll
-                    for (int e = 0; e < 8; e++) {
-                        float f = scale;
-                        if constexpr (F8) f *= pow2_of_byte((t.ks[e >> 2] >> (8 * (e & 3))) & 0xFFu);
+                        for (int rt = 0; rt < RT; rt++) {
+                            if (rt > 0 && !second) break;
+                            f32x4 st = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                        for (int rt = 0; rt < RT; rt++) x[rt][e] = st[rt][e >> 2][e & 3] * f;
+                            for (int s = 0; s < DH / 32; s++) st = mfma16(kf[s], RT == 1 ? qf[s] : s_q[q_off + (rt * (DH / 32) + s) * 64], st);
+#pragma unroll
+                            for (int e = 0; e < 4; e++) x[rt][4 * T2 + e] = st[e] * f[e];
+                        }
                     }
                 }
-                if (tile + 4 < c1) load_k(tile + 4);
+                if (decltype(always)::value || tile + 4 * NB < c1) load_k(t, tile + 4 * NB);
 
+                float fv[8];                                 // e4m3: the values' scales (of places that no row attends: 1, the bytes may be anything)
+                if constexpr (F8) {
+                    if (!whole) {
+                        const int n_in = t.here ? min(max(len - key, 0), 8) : 0;
+                        const uint64_t in = n_in == 8 ? ~0ull : (1ull << (8 * n_in)) - 1, ones = 0x7F7F7F7F7F7F7F7Full;
+                        const uint64_t v = (((uint64_t)t.vs[1] << 32 | t.vs[0]) & in) | (ones & ~in);
+                        t.vs = u32x2{(uint32_t)v, (uint32_t)(v >> 32)};
+                    }
+#pragma unroll
+                    for (int e = 0; e < 8; e++) fv[e] = pow2_of_byte((t.vs[e >> 2] >> (8 * (e & 3))) & 0xFFu);
+                }
                 u32x4 hi[RT], lo[RT];
                 uint32_t sees[RT];                           // bit e: the lane's row attends key + e
 #pragma unroll
                 for (int rt = 0; rt < RT; rt++) {
+                    if (rt > 0 && !second) break;
                     sees[rt] = 0xFFu;
                     if (!whole) {
                         const int n_see = t.here ? min(max(min(limit[rt] + 1, len) - key, 0), 8) : 0;
@@ -339,41 +360,71 @@ __global__ __launch_bounds__(256, RT == 1 ? 2 : 1) void k_paged_attn_few(PagedAt
                             const int e = 2 * i + o;
                             w[o] = __builtin_amdgcn_exp2f(x[rt][e] - ref);
                             l_run[rt] += w[o];
-                            if constexpr (F8) {              // (the byte of a place that nobody wrote may be anything)
-                                const float f = pow2_of_byte((t.vs[e >> 2] >> (8 * (e & 3))) & 0xFFu);
-                                w[o] = (sees[rt] >> e) & 1u ? w[o] * f : 0.f;
-                            }
+                            if constexpr (F8) w[o] *= fv[e];
                         }
                         hi[rt][i] = pack_bf16x2(w[0], w[1]);
-                        lo[rt][i] = pack_bf16x2(w[0] - __uint_as_float(hi[rt][i] << 16), w[1] - __uint_as_float(hi[rt][i] & 0xFFFF0000u));
+                        if constexpr (LO) lo[rt][i] = pack_bf16x2(w[0] - __uint_as_float(hi[rt][i] << 16), w[1] - __uint_as_float(hi[rt][i] & 0xFFFF0000u));
                     }
                 }
 
-                u32x4 vf[F];
-                v_operands<DH, F8>(t.v, vf);
-                if (!whole) {
-                    // keys behind the sequence's last are whatever the page holds, keys without a page somebody else's; and values that are not finite
-                    const int n_in = t.here ? min(max(len - key, 0), 8) : 0;
 #pragma unroll
-                    for (int i = 0; i < 4; i++) {
-                        const uint32_t keep = (2 * i < n_in ? 0xFFFFu : 0u) | (2 * i + 1 < n_in ? 0xFFFF0000u : 0u);
+                for (int y = 0; y < F; y += 4) {
+                    u32x4 vf[4];
+                    v_operands<DH, F8>(t.v, vf, y);
+                    if (!whole) {
+                        // keys behind the sequence's last are whatever the page holds, keys without a page somebody else's; and values that are not finite
+                        const int n_in = t.here ? min(max(len - key, 0), 8) : 0;
 #pragma unroll
-                        for (int j = 0; j < F; j++) {
-                            vf[j][i] &= keep;
-                            const uint32_t o = odd_halves(vf[j][i]);
-                            odd |= o;
-                            vf[j][i] &= ~o;
+                        for (int i = 0; i < 4; i++) {
+                            const uint32_t keep = (2 * i < n_in ? 0xFFFFu : 0u) | (2 * i + 1 < n_in ? 0xFFFF0000u : 0u);
+#pragma unroll
+                            for (int j = 0; j < 4; j++) {
+                                vf[j][i] &= keep;
+                                const uint32_t o = odd_halves(vf[j][i]);
+                                odd |= o;
+                                vf[j][i] &= ~o;
+                            }
+                        }
+                    }
+#pragma unroll
+                    for (int rt = 0; rt < RT; rt++) {
+                        if (rt > 0 && !second) break;
+#pragma unroll
+                        for (int j = 0; j < 4; j++) {
+                            acc[rt][y + j] = mfma16(vf[j], hi[rt], acc[rt][y + j]);
+                            if constexpr (LO) acc[rt][y + j] = mfma16(vf[j], lo[rt], acc[rt][y + j]);
                         }
                     }
                 }
+                if (decltype(always)::value || tile + 4 * NB < c1) load_v(t, tile + 4 * NB);
+            };
+            // (behind a load under a condition, the wait for an earlier one is a wait for all: the main part has none)
+            int tile = c0 + wave;
+            if (tile + 4 * (2 * NB - 1) < c1) {
 #pragma unroll
-                for (int rt = 0; rt < RT; rt++)
+                for (int x = 0; x < NB; x++) {
+                    load_k(ring[x], tile + 4 * x);
+                    load_v(ring[x], tile + 4 * x);
+                }
+#pragma unroll 1
+                do {
 #pragma unroll
-                    for (int j = 0; j < F; j++) {
-                        acc[rt][j] = mfma16(vf[j], hi[rt], acc[rt][j]);
-                        acc[rt][j] = mfma16(vf[j], lo[rt], acc[rt][j]);
+                    for (int x = 0; x < NB; x++) step(ring[x], tile + 4 * x, std::true_type{});
+                    tile += 4 * NB;
+                } while (tile + 4 * (2 * NB - 1) < c1);
+            } else {
+#pragma unroll
+                for (int x = 0; x < NB; x++)
+                    if (tile + 4 * x < c1) {
+                        load_k(ring[x], tile + 4 * x);
+                        load_v(ring[x], tile + 4 * x);
                     }
-                if (tile + 4 < c1) load_v(tile + 4);
+            }
+#pragma unroll 1
+            for (; tile < c1; tile += 4 * NB) {
+#pragma unroll
+                for (int x = 0; x < NB; x++)
+                    if (tile + 4 * x < c1) step(ring[x], tile + 4 * x, std::false_type{});
             }
             c0 = c1;
         }
@@ -390,15 +441,13 @@ __global__ __launch_bounds__(256, RT == 1 ? 2 : 1) void k_paged_attn_few(PagedAt
 #pragma unroll
                         for (int j = 0; j < F; j++)
 #pragma unroll
-                            for (int i = 0; i < 4; i++) {
-                                const float v = odd_value<F8>(row, F * (4 * g + i) + j);
-                                if (attends) acc[rt][j][i] += v;
-                            }
+                            for (int i = 0; i < 4; i++) acc[rt][j][i] += odd_value<F8>(row, F * (4 * g + i) + j, attends);
                     }
                 }
         }
 
         // ---- the four waves' results
+        if constexpr (RT > 1) __syncthreads();               // (the queries are no longer read)
 #pragma unroll
         for (int rt = 0; rt < RT; rt++) {
             l_run[rt] = groups_sum(l_run[rt]);
@@ -450,22 +499,22 @@ __global__ __launch_bounds__(256, RT == 1 ? 2 : 1) void k_paged_attn_few(PagedAt
             __syncthreads();
             if (s_last) {
                 auto at = [&](int i) { return part + (size_t)(2 * (w_first + i) + (i == 0 ? 1 : 0)) * R * PS; };
-                float *sums = &s_o[0][0][0];                 // (the waves' results are no longer needed)
+                float *sums = &s_o[0][0][0], *fades = sums + CSD_PAGED_FEW_PARTS * R;      // [part][row] (the waves' results are no longer needed)
                 for (int x = tid; x < parts * rows; x += 256) {
                     const int i = x / rows, r = x - i * rows;
                     const float2 ml = load_dev(at(i) + r * PS + DH);
-                    s_w[i][r] = ml.x;
+                    fades[i * R + r] = ml.x;
                     sums[i * R + r] = ml.y;
                 }
                 __syncthreads();
                 if (tid < rows) {
                     float m = -INFINITY, l = 0.f;
-                    for (int i = 0; i < parts; i++) m = fmaxf(m, s_w[i][tid]);
+                    for (int i = 0; i < parts; i++) m = fmaxf(m, fades[i * R + tid]);
                     const float ref = m == -INFINITY ? 0.f : m;
                     for (int i = 0; i < parts; i++) {
-                        const float f = __builtin_amdgcn_exp2f(s_w[i][tid] - ref);
+                        const float f = __builtin_amdgcn_exp2f(fades[i * R + tid] - ref);
                         l += f * sums[i * R + tid];
-                        s_w[i][tid] = f;
+                        fades[i * R + tid] = f;
                     }
                     s_m[0][tid] = m;
                     s_l[0][tid] = l;
@@ -480,7 +529,7 @@ __global__ __launch_bounds__(256, RT == 1 ? 2 : 1) void k_paged_attn_few(PagedAt
                         for (int k = 0; k < 8; k++) v[k] = load_dev(at(min(i0 + k, parts - 1)) + r * PS + c);
 #pragma unroll
                         for (int k = 0; k < 8; k++) {
-                            const float f = i0 + k < parts ? s_w[i0 + k][r] : 0.f;
+                            const float f = i0 + k < parts ? fades[(i0 + k) * R + r] : 0.f;
                             if (i0 + k < parts) {
                                 o0 += f * v[k].x;
                                 o1 += f * v[k].y;
@@ -501,7 +550,7 @@ __global__ __launch_bounds__(256, RT == 1 ? 2 : 1) void k_paged_attn_few(PagedAt
 
 template <int DH, bool F8, int RT>
 static void few_launch(const PagedAttn &a, hipStream_t st) {
-    hipLaunchKernelGGL((k_paged_attn_few<DH, F8, RT>), dim3(CSD_PAGED_FEW_GRID / RT), dim3(256), 0, st, a);
+    hipLaunchKernelGGL((k_paged_attn_few<DH, F8, RT>), dim3(CSD_PAGED_FEW_GRID), dim3(256), 0, st, a);
 }
 
 template <int DH, bool F8>

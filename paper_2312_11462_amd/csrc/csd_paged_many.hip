@@ -323,10 +323,7 @@ __global__ __launch_bounds__(256, 2) void k_paged_attn_many(PagedAttn a, int min
 #pragma unroll
                 for (int d = 0; d < DT; d++)
 #pragma unroll
-                    for (int e = 0; e < 16; e++) {
-                        const float v = odd_value<F8>(row, 32 * d + 8 * (e / 4) + 4 * h + e % 4);
-                        if (attends) acc[d][e] += v;
-                    }
+                    for (int e = 0; e < 16; e++) acc[d][e] += odd_value<F8>(row, 32 * d + 8 * (e / 4) + 4 * h + e % 4, attends);
             }
         }
     }
