@@ -352,7 +352,7 @@ typedef struct csd_paged_kv {
     void *k, *v;
     uint8_t *k_scale, *v_scale;
     const int32_t *table;
-    int32_t table_stride;          /* entries per sequence, >= 1; table_stride * page_rows < 2^31 */
+    int32_t table_stride;          /* entries per sequence, >= 1; table_stride * page_rows at most 2^30 */
 } csd_paged_kv;
 
 /* Write rows k_rows, v_rows (dtype CSD_DTYPE_FP32 or CSD_DTYPE_BF16; [rows][n_kv_heads][head_dim] with k_stride / v_stride elements from one

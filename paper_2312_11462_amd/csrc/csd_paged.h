@@ -3,7 +3,10 @@
 
 #include <type_traits>
 
+#include "csd_epilogue.h"
 #include "csd_internal.h"
+
+#define CSD_PAGED_COUNTER_BYTES 65536        /* the workspace begins with counters (zero between launches) */
 
 // The pool of one layer and the page table, by value in the kernels' arguments.
 struct PagedPool {
@@ -111,6 +114,17 @@ __device__ __forceinline__ float odd_value(const void *row, int c, bool attends)
     return fabsf(v) < INFINITY || !attends ? 0.f : v;
 }
 
+// The shares: T tiles over n workgroups, the first T % n of them one tile longer.
+struct PagedShares {
+    int q, r;
+    __device__ __forceinline__ PagedShares(int T, int n) : q(T / n), r(T % n) {}
+    __device__ __forceinline__ int first(int w) const { return w * q + min(w, r); }
+    __device__ __forceinline__ int owner(int tile) const {
+        const int wide = r * (q + 1);
+        return tile < wide ? tile / (q + 1) : r + (tile - wide) / q;
+    }
+};
+
 // One attention call.
 struct PagedAttn {
     PagedPool p;
@@ -123,23 +137,102 @@ struct PagedAttn {
     float scale;
     void *ws;
 };
+// Parts of items.  A workgroup has two at most that are not whole items: one that others began (its slot 0) and one that others end (slot 1).  A slot
+// holds R rows of DH outputs (weighted sums), their maximum and the sum of weights.  Slots are written and read within a launch by workgroups on
+// different compute dies: device scope (the stores write through).
+template <int DH> constexpr int part_stride() { return DH + 4; }     // floats per row, 16-byte pieces
+template <int DH, int R>
+struct PagedParts {
+    __amdgpu_buffer_rsrc_t r;
+    int w_first, parts;                                      // the workgroup that has the item's first part; how many there are
+    __device__ __forceinline__ PagedParts(void *ws, int wgs, int w_first_, int parts_) : w_first(w_first_), parts(parts_) {
+        r = ch_rsrc(reinterpret_cast<char *>(ws) + CSD_PAGED_COUNTER_BYTES, (size_t)2 * wgs * R * part_stride<DH>() * 4);
+    }
+    __device__ __forceinline__ int at(int part, int row, int c) const {
+        return (((2 * (w_first + part) + (part == 0 ? 1 : 0)) * R + row) * part_stride<DH>() + c) * 4;
+    }
+    __device__ __forceinline__ void store(int part, int row, int c, f32x4 v) const {
+        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, v), r, at(part, row, c), 0, CH_SC1);
+    }
+    __device__ __forceinline__ f32x4 load(int part, int row, int c) const {
+        return __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(r, at(part, row, c), 0, CH_SC1));
+    }
+    // Behind the stores of this workgroup's part: true in the workgroup that finishes last.  `flag`: LDS.
+    __device__ __forceinline__ bool arrive(void *ws, int *flag) const {
+        __builtin_amdgcn_s_waitcnt(0x0F70);                  // vmcnt(0): the stores are acknowledged before the counter moves
+        __syncthreads();
+        if (threadIdx.x == 0)
+            *flag = __hip_atomic_fetch_add(reinterpret_cast<unsigned *>(ws) + w_first, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (unsigned)(parts - 1);
+        __syncthreads();
+        return *flag != 0;
+    }
+    // The last one joins the parts, in their order: out = sum f_k o_k / sum f_k l_k with f_k = 2^(m_k - max m).  lds: (2 * parts + 1) * R floats.  `out` of a row:
+    // 256 threads, four features each; the first parts' outputs are requested along with the maxima.
+    template <typename OUT>
+    __device__ __forceinline__ void join(void *ws, float *lds, int rows, OUT out) const {
+        const int tid = threadIdx.x;
+        float *fade = lds, *sum = lds + parts * R, *inv = lds + 2 * parts * R;
+        constexpr int C = DH / 4;
+        f32x4 v[4];
+        auto request = [&](int x, int k0) {
+#pragma unroll
+            for (int k = 0; k < 4; k++)
+                if (k0 + k < parts && x < rows * C) v[k] = load(k0 + k, x / C, 4 * (x % C));
+        };
+        request(tid, 0);
+        for (int x = tid; x < parts * rows; x += 256) {
+            const int k = x / rows, row = x - k * rows;
+            const f32x4 ml = load(k, row, DH);
+            fade[k * R + row] = ml[0];
+            sum[k * R + row] = ml[1];
+        }
+        __syncthreads();
+        if (tid < rows) {
+            float m = -INFINITY, l = 0.f;
+            for (int k = 0; k < parts; k++) m = fmaxf(m, fade[k * R + tid]);
+            const float ref = m == -INFINITY ? 0.f : m;
+            for (int k = 0; k < parts; k++) {
+                const float f = __builtin_amdgcn_exp2f(fade[k * R + tid] - ref);
+                l += f * sum[k * R + tid];
+                fade[k * R + tid] = f;
+            }
+            inv[tid] = m == -INFINITY ? -1.f : 1.f / l;      // (-1: the row has nothing to attend)
+        }
+        __syncthreads();
+        for (int x = tid; x < rows * C; x += 256) {
+            const int row = x / C, c = 4 * (x % C);
+            f32x4 o = f32x4{0.f, 0.f, 0.f, 0.f};
+            for (int k0 = 0; k0 < parts; k0 += 4) {
+                if (x != tid || k0 != 0) request(x, k0);
+#pragma unroll
+                for (int k = 0; k < 4; k++)
+                    if (k0 + k < parts) o += v[k] * fade[(k0 + k) * R + row];
+            }
+            const float f = inv[row];
+            *reinterpret_cast<u32x2 *>(out(row) + c) = f == -1.f ? u32x2{0u, 0u} : u32x2{pack_bf16x2(o[0] * f, o[1] * f), pack_bf16x2(o[2] * f, o[3] * f)};
+        }
+        if (tid == 0) __hip_atomic_store(reinterpret_cast<unsigned *>(ws) + w_first, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);   // ready for the next launch
+    }
+};
+
 int32_t csd_paged_attention_enqueue(const PagedAttn &a, int32_t pool_dtype, int32_t q_dtype, hipStream_t st);
 
-// csd_paged_few.hip: sequences of up to 32 rows per key-value head.  The workspace holds counters (zero between launches) and behind
-// them the partial results, two of up to 32 rows per workgroup.
-#define CSD_PAGED_COUNTER_BYTES 65536
+// csd_paged_few.hip: sequences of up to 32 rows per key-value head.
 #define CSD_PAGED_FEW_GRID 512       /* two workgroups per compute unit */
 #define CSD_PAGED_FEW_SHARE 4        /* tiles of 32 keys per workgroup at least */
 #define CSD_PAGED_FEW_PARTS 64       /* parts of an item at most */
 #define CSD_PAGED_FEW_ROWS 32
-static_assert(CSD_PAGED_COUNTER_BYTES + 2ull * CSD_PAGED_FEW_GRID * CSD_PAGED_FEW_ROWS * 130 * 4 <= CSD_PAGED_WORKSPACE_BYTES, "");
+static_assert(CSD_PAGED_COUNTER_BYTES + 2ull * CSD_PAGED_FEW_GRID * CSD_PAGED_FEW_ROWS * 132 * 4 <= CSD_PAGED_WORKSPACE_BYTES, "");
 bool csd_paged_few_fits(const PagedAttn &a, int32_t pool_dtype, int32_t q_dtype);
 void csd_paged_few_enqueue(const PagedAttn &a, int rows, int32_t pool_dtype, hipStream_t st);
 
-// csd_paged_many.hip: the others, 128 rows per workgroup, in the same types and head sizes.
+// csd_paged_many.hip: the others, in the same types and head sizes, 128 rows per workgroup.
 #define CSD_PAGED_MANY_ROWS 128
 #define CSD_PAGED_MANY_SHARE 4       /* tiles of 64 keys per part of an item at least */
-#define CSD_PAGED_MANY_PARTS 8       /* parts of an item at most */
-#define CSD_PAGED_MANY_SLOTS 1024    /* items times parts at most, where items are split */
-static_assert(CSD_PAGED_COUNTER_BYTES + (size_t)CSD_PAGED_MANY_SLOTS * CSD_PAGED_MANY_ROWS * 130 * 4 <= CSD_PAGED_WORKSPACE_BYTES, "");
+#define CSD_PAGED_MANY_COST 4        /* what an item costs besides its keys, in such tiles */
+#define CSD_PAGED_MANY_PARTS 14      /* parts of an item at most */
+#define CSD_PAGED_MANY_GRID 512      /* two workgroups per compute unit, where they share the items' keys */
+#define CSD_PAGED_MANY_ITEMS 1024    /* row tiles times key-value heads at most for that */
+#define CSD_PAGED_MANY_BATCH 512     /* sequences at most for that */
+static_assert(CSD_PAGED_COUNTER_BYTES + 2ull * CSD_PAGED_MANY_GRID * CSD_PAGED_MANY_ROWS * 132 * 4 <= CSD_PAGED_WORKSPACE_BYTES, "");
 void csd_paged_many_enqueue(const PagedAttn &a, int min_rows, int32_t pool_dtype, hipStream_t st);

@@ -34,15 +34,15 @@ struct FewTile {
 template <int VW>
 __device__ __forceinline__ void load_words(const void *p, uint32_t (&w)[VW]) {
     if constexpr (VW == 4) {
-        const u32x4 x = *reinterpret_cast<const u32x4 *>(p);
+        const u32x4 x = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(p));
 #pragma unroll
         for (int i = 0; i < 4; i++) w[i] = x[i];
     } else if constexpr (VW == 2) {
-        const u32x2 x = *reinterpret_cast<const u32x2 *>(p);
+        const u32x2 x = __builtin_nontemporal_load(reinterpret_cast<const u32x2 *>(p));
         w[0] = x[0];
         w[1] = x[1];
     } else {
-        w[0] = *reinterpret_cast<const uint32_t *>(p);
+        w[0] = __builtin_nontemporal_load(reinterpret_cast<const uint32_t *>(p));
     }
 }
 
@@ -75,43 +75,24 @@ __device__ __forceinline__ void v_operands(const uint32_t (&v)[8][FewTile<DH, F8
     }
 }
 
-// The shares: T tiles over n workgroups, the first T % n of them one tile longer.
-struct FewShares {
-    int q, r;
-    __device__ __forceinline__ FewShares(int T, int n) : q(T / n), r(T % n) {}
-    __device__ __forceinline__ int first(int w) const { return w * q + min(w, r); }
-    __device__ __forceinline__ int owner(int tile) const {
-        const int wide = r * (q + 1);
-        return tile < wide ? tile / (q + 1) : r + (tile - wide) / q;
-    }
-};
-
 __device__ __forceinline__ f32x4 mfma16(u32x4 a, u32x4 b, f32x4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
-}
-
-// Partial results live in memory that other compute dies read within the same launch: stores and loads of device scope.
-__device__ __forceinline__ void store_dev(float *p, float a, float b) {
-    const uint64_t x = ((uint64_t)__float_as_uint(b) << 32) | __float_as_uint(a);
-    __hip_atomic_store(reinterpret_cast<uint64_t *>(p), x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-}
-__device__ __forceinline__ float2 load_dev(const float *p) {
-    const uint64_t x = __hip_atomic_load(reinterpret_cast<const uint64_t *>(p), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    return float2{__uint_as_float((uint32_t)x), __uint_as_float((uint32_t)(x >> 32))};
 }
 
 // RT: 16-row tiles of queries.
 template <int DH, bool F8, int RT>
 __global__ __launch_bounds__(256, 2) void k_paged_attn_few(PagedAttn a) {
     using Tile = FewTile<DH, F8>;
-    constexpr int F = DH / 16, R = 16 * RT, PS = DH + 2;     // PS: floats of a partial row: outputs, maximum, sum
+    constexpr int F = DH / 16, R = 16 * RT;
     constexpr bool LO = RT == 1;
-    constexpr int NB = F8 && (RT == 1 || DH == 64) ? 2 : 1;
+    constexpr int NB = (F8 && (RT == 1 || DH == 64) ? 2 : 1) + (DH == 64 ? 1 : 0);     // tiles in flight per wave, as registers allow
     constexpr int ES = F8 ? 1 : 2, kGrid = CSD_PAGED_FEW_GRID;
     __shared__ int s_pages[kFewPages];
     __shared__ __align__(16) float s_o[4][R][DH + 4];
     __shared__ float s_m[4][R], s_l[4][R];
-    static_assert(2 * CSD_PAGED_FEW_PARTS * R <= 4 * R * (DH + 4) && RT * (DH / 32) * 64 * 16 <= 4 * R * (DH + 4) * 4, "");
+    __shared__ int s_limit[R];                               // last position a row attends
+    __shared__ unsigned long long s_above[R];                // tree: its ancestors in the block
+    static_assert((2 * CSD_PAGED_FEW_PARTS + 1) * R <= 4 * R * (DH + 4) && RT * (DH / 32) * 64 * 16 <= 4 * R * (DH + 4) * 4, "");
     __shared__ int s_last;
     const PagedPool &p = a.p;
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, col = lane & 15, g = lane >> 4;
@@ -147,7 +128,7 @@ __global__ __launch_bounds__(256, 2) void k_paged_attn_few(PagedAttn a) {
     const int least = max(CSD_PAGED_FEW_SHARE, (longest + CSD_PAGED_FEW_PARTS - 3) / (CSD_PAGED_FEW_PARTS - 2));
     const int n_wg = min((int)kGrid, max(1, T / least));
     if ((int)blockIdx.x >= n_wg) return;
-    const FewShares shares(T, n_wg);
+    const PagedShares shares(T, n_wg);
     const int u_end = shares.first(blockIdx.x + 1);
 
     for (int u = shares.first(blockIdx.x); u < u_end;) {
@@ -183,8 +164,7 @@ __global__ __launch_bounds__(256, 2) void k_paged_attn_few(PagedAttn a) {
         // ---- queries: row r = token r / group, head r % group of the group
         u32x4 qf[RT == 1 ? DH / 32 : 1];                      // (two row tiles: in LDS, where the waves' results will be; the registers are needed)
         u32x4 *s_q = reinterpret_cast<u32x4 *>(&s_o[0][0][0]) + lane;
-        int limit[RT];                                       // last position the lane's row attends
-        unsigned long long above[RT];
+        const uint32_t flip = a.scale < 0.f ? 0x80008000u : 0u;
         unsigned long long anc = 1ull << lane;               // tree: ancestors of block row `lane`, by doubling the step up
         if (a.parent) {
             int up = 0;
@@ -203,11 +183,14 @@ __global__ __launch_bounds__(256, 2) void k_paged_attn_few(PagedAttn a) {
 #pragma unroll
         for (int rt = 0; rt < RT; rt++) {
             const int r = rt * 16 + col, i = r / a.group, h = r - i * a.group;
-            limit[rt] = seq.t + i;
-            above[rt] = 0;
+            unsigned long long above = 0;
             if (a.parent) {
                 const int src = min(i, 63);
-                above[rt] = ((unsigned long long)(unsigned)__shfl((unsigned)(anc >> 32), src, 64) << 32) | (unsigned)__shfl((unsigned)anc, src, 64);
+                above = ((unsigned long long)(unsigned)__shfl((unsigned)(anc >> 32), src, 64) << 32) | (unsigned)__shfl((unsigned)anc, src, 64);
+            }
+            if (wave == 0 && g == 0) {                       // (needed where rows differ only: not worth registers)
+                s_limit[r] = seq.t + i;
+                s_above[r] = above;
             }
             const bf16_t *q = reinterpret_cast<const bf16_t *>(a.q) + (size_t)(seq.start + i) * a.q_stride + (size_t)(kvh * a.group + h) * DH;
 #pragma unroll
@@ -215,12 +198,15 @@ __global__ __launch_bounds__(256, 2) void k_paged_attn_few(PagedAttn a) {
                 u32x4 x = u32x4{0u, 0u, 0u, 0u};
                 const int at = F8 ? 64 * (s / 2) + 16 * g + 8 * (s & 1) : 32 * s + 8 * g;      // features of the K operand's step s
                 if (r < rows) x = *reinterpret_cast<const u32x4 *>(q + at);
+#pragma unroll
+                for (int w = 0; w < 4; w++) x[w] ^= flip;
                 if constexpr (RT == 1) qf[s] = x;
                 else if (wave == 0) s_q[(rt * (DH / 32) + s) * 64] = x;
             }
         }
         const bool second = RT > 1 && rows > 16;             // the second row tile holds rows
-        const float scale = a.scale * 1.44269504088896f;     // scores in units of log2
+        // scores in units of log2; the sign is the queries' (the maximum needs scale >= 0), at least 1e-30 (a masked score of -inf has to stay one)
+        const float scale = fmaxf(fabsf(a.scale) * 1.44269504088896f, 1e-30f);
         f32x4 acc[RT][F];
         float m_run[RT], l_run[RT];
         uint32_t odd = 0;                                    // the wave took values out of its products
@@ -255,7 +241,7 @@ __global__ __launch_bounds__(256, 2) void k_paged_attn_few(PagedAttn a) {
 #pragma unroll
                 for (int T2 = 0; T2 < 2; T2++)
 #pragma unroll
-                    for (int s = 0; s < Tile::KV; s++) t.k[T2][s] = *reinterpret_cast<const u32x4 *>(kp + T2 * 4 * DH * ES + s * 64);
+                    for (int s = 0; s < Tile::KV; s++) t.k[T2][s] = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(kp + T2 * 4 * DH * ES + s * 64));
                 if constexpr (F8) {
                     const int key8 = tile * 32 + 8 * g;
                     t.ks = *reinterpret_cast<const u32x2 *>(p.ks + paged_row(p, max(s_pages[(key8 >> p.page_shift) - page0], 0), kvh, key8));
@@ -293,12 +279,6 @@ __global__ __launch_bounds__(256, 2) void k_paged_attn_few(PagedAttn a) {
                                 kf[s] = t.k[T2][s];
                             }
                         }
-                        float f[4];
-#pragma unroll
-                        for (int e = 0; e < 4; e++) {
-                            f[e] = scale;
-                            if constexpr (F8) f[e] *= pow2_of_byte((t.ks[T2] >> (8 * e)) & 0xFFu);
-                        }
 #pragma unroll
                         for (int rt = 0; rt < RT; rt++) {
                             if (rt > 0 && !second) break;
@@ -306,22 +286,19 @@ __global__ __launch_bounds__(256, 2) void k_paged_attn_few(PagedAttn a) {
 #pragma unroll
                             for (int s = 0; s < DH / 32; s++) st = mfma16(kf[s], RT == 1 ? qf[s] : s_q[q_off + (rt * (DH / 32) + s) * 64], st);
 #pragma unroll
-                            for (int e = 0; e < 4; e++) x[rt][4 * T2 + e] = st[e] * f[e];
+                            for (int e = 0; e < 4; e++) x[rt][4 * T2 + e] = F8 ? st[e] * pow2_of_byte((t.ks[T2] >> (8 * e)) & 0xFFu) : st[e];
                         }
                     }
                 }
                 if (decltype(always)::value || tile + 4 * NB < c1) load_k(t, tile + 4 * NB);
 
-                float fv[8];                                 // e4m3: the values' scales (of places that no row attends: 1, the bytes may be anything)
-                if constexpr (F8) {
+                if constexpr (F8) {                          // values' scales of places that no row attends: 1 (the bytes may be anything)
                     if (!whole) {
                         const int n_in = t.here ? min(max(len - key, 0), 8) : 0;
                         const uint64_t in = n_in == 8 ? ~0ull : (1ull << (8 * n_in)) - 1, ones = 0x7F7F7F7F7F7F7F7Full;
                         const uint64_t v = (((uint64_t)t.vs[1] << 32 | t.vs[0]) & in) | (ones & ~in);
                         t.vs = u32x2{(uint32_t)v, (uint32_t)(v >> 32)};
                     }
-#pragma unroll
-                    for (int e = 0; e < 8; e++) fv[e] = pow2_of_byte((t.vs[e >> 2] >> (8 * (e & 3))) & 0xFFu);
                 }
                 u32x4 hi[RT], lo[RT];
                 uint32_t sees[RT];                           // bit e: the lane's row attends key + e
@@ -330,11 +307,12 @@ __global__ __launch_bounds__(256, 2) void k_paged_attn_few(PagedAttn a) {
                     if (rt > 0 && !second) break;
                     sees[rt] = 0xFFu;
                     if (!whole) {
-                        const int n_see = t.here ? min(max(min(limit[rt] + 1, len) - key, 0), 8) : 0;
+                        const int n_see = t.here ? min(max(min(s_limit[rt * 16 + col] + 1, len) - key, 0), 8) : 0;
                         sees[rt] = (1u << n_see) - 1u;
                         if (a.parent) {
-                            const int d = key - seq.t;       // rows of the block lie at d .. d + 7 of `above`; keys before them are cached
-                            const unsigned long long m = d >= 0 ? (d < 64 ? above[rt] >> d : 0ull) : (above[rt] << min(-d, 8)) | ((1ull << min(-d, 8)) - 1);
+                            const int d = key - seq.t;       // rows of the block lie at d .. d + 7 of `up`; keys before them are cached
+                            const unsigned long long up = s_above[rt * 16 + col];
+                            const unsigned long long m = d >= 0 ? (d < 64 ? up >> d : 0ull) : (up << min(-d, 8)) | ((1ull << min(-d, 8)) - 1);
                             sees[rt] &= (uint32_t)m;
                         }
 #pragma unroll
@@ -343,8 +321,9 @@ __global__ __launch_bounds__(256, 2) void k_paged_attn_few(PagedAttn a) {
                     }
                     float top = fmaxf(fmaxf(fmaxf(x[rt][0], x[rt][1]), fmaxf(x[rt][2], x[rt][3])),
                                       fmaxf(fmaxf(x[rt][4], x[rt][5]), fmaxf(x[rt][6], x[rt][7])));
-                    top = groups_max(sees[rt] ? fmaxf(top, -3.0e38f) : top);     // -inf: nothing to attend yet (a score of -inf is something)
-                    if (__any(top > m_run[rt])) {
+                    top = groups_max(sees[rt] ? fmaxf(top * scale, -3.0e38f) : -INFINITY);   // -inf: nothing to attend yet (a score of -inf is something)
+                    // weights up to 2^8 are as good as weights up to 1: the outputs are rescaled only when the maximum has moved by more
+                    if (__any(top > m_run[rt] + 8.f)) {
                         const float m_new = fmaxf(m_run[rt], top), fade = __builtin_amdgcn_exp2f(m_run[rt] - (m_new == -INFINITY ? 0.f : m_new));
                         l_run[rt] *= fade;
 #pragma unroll
@@ -358,9 +337,9 @@ __global__ __launch_bounds__(256, 2) void k_paged_attn_few(PagedAttn a) {
 #pragma unroll
                         for (int o = 0; o < 2; o++) {
                             const int e = 2 * i + o;
-                            w[o] = __builtin_amdgcn_exp2f(x[rt][e] - ref);
+                            w[o] = __builtin_amdgcn_exp2f(fmaf(x[rt][e], scale, -ref));
                             l_run[rt] += w[o];
-                            if constexpr (F8) w[o] *= fv[e];
+                            if constexpr (F8) w[o] *= pow2_of_byte((t.vs[e >> 2] >> (8 * (e & 3))) & 0xFFu);
                         }
                         hi[rt][i] = pack_bf16x2(w[0], w[1]);
                         if constexpr (LO) lo[rt][i] = pack_bf16x2(w[0] - __uint_as_float(hi[rt][i] << 16), w[1] - __uint_as_float(hi[rt][i] & 0xFFFF0000u));
@@ -437,7 +416,7 @@ __global__ __launch_bounds__(256, 2) void k_paged_attn_few(PagedAttn a) {
                     const char *row = reinterpret_cast<const char *>(p.v) + paged_row(p, page, kvh, key) * (DH * ES);
 #pragma unroll
                     for (int rt = 0; rt < RT; rt++) {
-                        const bool attends = key <= limit[rt] && (!a.parent || key < seq.t || ((above[rt] >> min(key - seq.t, 63)) & 1ull));
+                        const bool attends = key <= s_limit[rt * 16 + col] && (!a.parent || key < seq.t || ((s_above[rt * 16 + col] >> min(key - seq.t, 63)) & 1ull));
 #pragma unroll
                         for (int j = 0; j < F; j++)
 #pragma unroll
@@ -463,87 +442,35 @@ __global__ __launch_bounds__(256, 2) void k_paged_attn_few(PagedAttn a) {
         __syncthreads();
         const int w_first = shares.owner(item), w_last = shares.owner(item + n - 1);
         const bool split = w_first != w_last;
-        float *part = reinterpret_cast<float *>(reinterpret_cast<char *>(a.ws) + CSD_PAGED_COUNTER_BYTES);
-        float *mine = part + (size_t)(2 * blockIdx.x + (w_first == (int)blockIdx.x ? 1 : 0)) * R * PS;
-        for (int x = tid; x < rows * (DH / 2); x += 256) {
-            const int r = x / (DH / 2), c = 2 * (x % (DH / 2));
+        const PagedParts<DH, R> parts(a.ws, CSD_PAGED_FEW_GRID, w_first, w_last - w_first + 1);
+        auto out_row = [&](int r) {
+            const int i = r / a.group, h = r - i * a.group;
+            return reinterpret_cast<bf16_t *>(a.out) + (((size_t)(seq.start + i) * p.Hkv + kvh) * a.group + h) * DH;
+        };
+        for (int x = tid; x < rows * (DH / 4); x += 256) {
+            const int r = x / (DH / 4), c = 4 * (x % (DH / 4));
             float m = s_m[0][r];
 #pragma unroll
             for (int w = 1; w < 4; w++) m = fmaxf(m, s_m[w][r]);
             const float ref = m == -INFINITY ? 0.f : m;
-            float l = 0.f, o0 = 0.f, o1 = 0.f;
+            float l = 0.f;
+            f32x4 o = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int w = 0; w < 4; w++) {
                 const float f = __builtin_amdgcn_exp2f(s_m[w][r] - ref);
                 l += f * s_l[w][r];
-                o0 += f * s_o[w][r][c];
-                o1 += f * s_o[w][r][c + 1];
+                o += *reinterpret_cast<const f32x4 *>(&s_o[w][r][c]) * f;
             }
             if (!split) {
-                const int i = r / a.group, h = r - i * a.group;
-                const float inv = m == -INFINITY ? 0.f : 1.f / l;
-                uint32_t *out = reinterpret_cast<uint32_t *>(a.out) + (((size_t)(seq.start + i) * p.Hkv + kvh) * a.group + h) * (DH / 2);
-                out[c / 2] = m == -INFINITY ? 0u : pack_bf16x2(o0 * inv, o1 * inv);
+                const float inv = 1.f / l;
+                *reinterpret_cast<u32x2 *>(out_row(r) + c) =
+                    m == -INFINITY ? u32x2{0u, 0u} : u32x2{pack_bf16x2(o[0] * inv, o[1] * inv), pack_bf16x2(o[2] * inv, o[3] * inv)};
             } else {
-                store_dev(mine + r * PS + c, o0, o1);
-                if (c == 0) store_dev(mine + r * PS + DH, m, l);
+                parts.store(blockIdx.x - w_first, r, c, o);
+                if (c == 0) parts.store(blockIdx.x - w_first, r, DH, f32x4{m, l, 0.f, 0.f});
             }
         }
-        if (split) {
-            // the stores above are acknowledged before the counter moves; whoever arrives last joins the parts, in their order
-            __builtin_amdgcn_s_waitcnt(0x0F70);              // vmcnt(0)
-            __syncthreads();
-            unsigned *count = reinterpret_cast<unsigned *>(a.ws) + w_first;
-            const int parts = w_last - w_first + 1;
-            if (tid == 0) s_last = __hip_atomic_fetch_add(count, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (unsigned)(parts - 1);
-            __syncthreads();
-            if (s_last) {
-                auto at = [&](int i) { return part + (size_t)(2 * (w_first + i) + (i == 0 ? 1 : 0)) * R * PS; };
-                float *sums = &s_o[0][0][0], *fades = sums + CSD_PAGED_FEW_PARTS * R;      // [part][row] (the waves' results are no longer needed)
-                for (int x = tid; x < parts * rows; x += 256) {
-                    const int i = x / rows, r = x - i * rows;
-                    const float2 ml = load_dev(at(i) + r * PS + DH);
-                    fades[i * R + r] = ml.x;
-                    sums[i * R + r] = ml.y;
-                }
-                __syncthreads();
-                if (tid < rows) {
-                    float m = -INFINITY, l = 0.f;
-                    for (int i = 0; i < parts; i++) m = fmaxf(m, fades[i * R + tid]);
-                    const float ref = m == -INFINITY ? 0.f : m;
-                    for (int i = 0; i < parts; i++) {
-                        const float f = __builtin_amdgcn_exp2f(fades[i * R + tid] - ref);
-                        l += f * sums[i * R + tid];
-                        fades[i * R + tid] = f;
-                    }
-                    s_m[0][tid] = m;
-                    s_l[0][tid] = l;
-                }
-                __syncthreads();
-                for (int x = tid; x < rows * (DH / 2); x += 256) {
-                    const int r = x / (DH / 2), c = 2 * (x % (DH / 2));
-                    float o0 = 0.f, o1 = 0.f;
-                    for (int i0 = 0; i0 < parts; i0 += 8) {
-                        float2 v[8];
-#pragma unroll
-                        for (int k = 0; k < 8; k++) v[k] = load_dev(at(min(i0 + k, parts - 1)) + r * PS + c);
-#pragma unroll
-                        for (int k = 0; k < 8; k++) {
-                            const float f = i0 + k < parts ? fades[(i0 + k) * R + r] : 0.f;
-                            if (i0 + k < parts) {
-                                o0 += f * v[k].x;
-                                o1 += f * v[k].y;
-                            }
-                        }
-                    }
-                    const int i = r / a.group, h = r - i * a.group;
-                    const float inv = 1.f / s_l[0][r];
-                    uint32_t *out = reinterpret_cast<uint32_t *>(a.out) + (((size_t)(seq.start + i) * p.Hkv + kvh) * a.group + h) * (DH / 2);
-                    out[c / 2] = s_m[0][r] == -INFINITY ? 0u : pack_bf16x2(o0 * inv, o1 * inv);
-                }
-                if (tid == 0) __hip_atomic_store(count, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);   // ready for the next launch
-            }
-        }
+        if (split && parts.arrive(a.ws, &s_last)) parts.join(a.ws, &s_o[0][0][0], rows, out_row);
         __syncthreads();
     }
 }
@@ -561,9 +488,9 @@ static void few_rows(const PagedAttn &a, int rows, hipStream_t st) {
 
 bool csd_paged_few_fits(const PagedAttn &a, int32_t pool_dtype, int32_t q_dtype) {
     if (q_dtype != CSD_DTYPE_BF16 || pool_dtype == CSD_DTYPE_FP32 || (a.p.D != 64 && a.p.D != 128)) return false;
-    // tiles are counted in 32 bits
-    const long long tiles = (((long long)a.p.table_stride << a.p.page_shift) + 31) / 32;
-    return tiles * a.p.Hkv * a.r.B < (1ll << 30) && (long long)a.r.rows * a.p.Hkv * a.group < (1ll << 30);
+    // tiles are counted in 32 bits, and so are the work items of a launch
+    const long long tiles = (((long long)a.p.table_stride << a.p.page_shift) + 31) / 32, heads = (long long)a.p.Hkv * a.group;
+    return tiles * a.p.Hkv * a.r.B < (1ll << 30) && (long long)a.r.rows * heads / 128 + (long long)a.r.B * a.p.Hkv < (1ll << 24);
 }
 
 void csd_paged_few_enqueue(const PagedAttn &a, int rows, int32_t pool_dtype, hipStream_t st) {

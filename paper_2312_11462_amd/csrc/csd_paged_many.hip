@@ -32,14 +32,6 @@ __device__ __forceinline__ float halves_sum(float v) {
     const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
     return __uint_as_float(a[0]) + __uint_as_float(a[1]);
 }
-__device__ __forceinline__ void store_dev2(float *p, float a, float b) {
-    const uint64_t x = ((uint64_t)__float_as_uint(b) << 32) | __float_as_uint(a);
-    __hip_atomic_store(reinterpret_cast<uint64_t *>(p), x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-}
-__device__ __forceinline__ float2 load_dev2(const float *p) {
-    const uint64_t x = __hip_atomic_load(reinterpret_cast<const uint64_t *>(p), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    return float2{__uint_as_float((uint32_t)x), __uint_as_float((uint32_t)(x >> 32))};
-}
 
 // 16-byte piece c of row `row` in a staged tile
 template <int DH> __device__ __forceinline__ int k_piece(int row, int c) { return row * (DH / 8) + (c ^ (row & (DH / 8 - 1))); }
@@ -47,66 +39,177 @@ template <int DH> __device__ __forceinline__ int v_piece(int row, int c) {
     return row * (DH / 8) + (c ^ (DH == 128 ? (row & 3) << 2 : ((row >> 1) & 1) << 2));
 }
 
-template <int DH, bool F8>
-__global__ __launch_bounds__(256, 2) void k_paged_attn_many(PagedAttn a, int min_rows, int splits) {
+// The key tiles that row tile rt of a sequence goes through: those up to the last position that one of its rows attends.
+__device__ __forceinline__ int row_tile_keys(int rt, int m, int t, int group, int cap) {
+    const int last = min(((rt + 1) * CSD_PAGED_MANY_ROWS - 1) / group, m - 1);
+    return (min(t + last + 1, cap) + kKeys - 1) / kKeys;
+}
+
+// SHARED: the grid is a fixed number of workgroups, which take equal, contiguous shares of all items' key tiles (as k_paged_attn_few does; the
+// parts of an item are joined by the workgroup that finishes last).  Else a workgroup is an item: where there are many of them, the parts'
+// way through memory costs more than the ends of the launch.
+template <int DH, bool F8, bool SHARED>
+__global__ __launch_bounds__(256, 2) void k_paged_attn_many(PagedAttn a, int min_rows) {
     constexpr int ES = F8 ? 1 : 2, LPR = DH * ES / 16;       // lanes that load a row
     constexpr int RPP = 256 / LPR, NP = kKeys / RPP;         // rows per pass of the workgroup, passes per tile
     constexpr int PIECES = kKeys * DH / 8;                   // 16-byte pieces of a staged tile
-    constexpr int ST = DH / 16, DT = DH / 32, PS = DH + 2, BM = CSD_PAGED_MANY_ROWS;
+    constexpr int ST = DH / 16, DT = DH / 32, BM = CSD_PAGED_MANY_ROWS, PARTS = CSD_PAGED_MANY_PARTS;
+    // what an item costs besides its keys, in tiles: the round trips to memory in front of its first tile and behind its last one
+    constexpr int COST = CSD_PAGED_MANY_COST;
     __shared__ u32x4 s_k[2][PIECES], s_v[2][PIECES];
     __shared__ int s_odd, s_last;
+    __shared__ int s_start[SHARED ? CSD_PAGED_MANY_BATCH : 1], s_m[SHARED ? CSD_PAGED_MANY_BATCH : 1], s_t[SHARED ? CSD_PAGED_MANY_BATCH : 1], s_units[SHARED ? CSD_PAGED_MANY_BATCH : 1];
     const PagedPool &p = a.p;
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, col = lane & 31, h = lane >> 5;
     const int cap = p.table_stride << p.page_shift;
 
-    // ---- which rows: key-value heads follow one another (workgroups of a die, every eighth, read the same keys), then the parts of an item,
-    // then the row tiles, the late ones with the most keys first
-    const int kvh = blockIdx.x % p.Hkv, part_no = (blockIdx.x / p.Hkv) % splits, tile_no = blockIdx.x / p.Hkv / splits;
-    int b = -1, rt = 0, total = 0, n_tiles = 0;
-    PagedSeq seq{0, 0, 0};
-    for (int pass = 0; pass < 2; pass++) {                   // count the tiles of all sequences, then find this one
-        int before = 0;
-        const int want = pass ? total - 1 - tile_no : 0;
-        if (pass && want < 0) return;
-        for (int b0 = 0; b0 < a.r.B; b0 += 64) {
-            PagedSeq s{0, 0, 0};
-            int n = 0;
-            if (b0 + lane < a.r.B) {
-                s = paged_seq(a.r, b0 + lane);
-                s.m = min(s.m, a.max_rows);
-                const int rows = s.m * a.group;
-                n = rows > min_rows ? (rows + BM - 1) / BM : 0;
-            }
-            int incl = n;
+    auto seq_of = [&](int b, PagedSeq &s) -> int {           // row tiles of a sequence
+        s = PagedSeq{0, 0, 0};
+        if (b >= a.r.B) return 0;
+        s = paged_seq(a.r, b);
+        s.m = min(s.m, a.max_rows);
+        const int rows = s.m * a.group;
+        return rows > min_rows ? (rows + BM - 1) / BM : 0;
+    };
+    auto scan = [&](int x) {                                 // inclusive, over the wave
 #pragma unroll
-            for (int o = 1; o < 64; o <<= 1) {
-                const int x = __shfl_up(incl, o, 64);
-                if (lane >= o) incl += x;
-            }
-            if (pass) {
-                const unsigned long long past = __ballot(before + incl > want);
-                if (past) {
-                    const int j = __ffsll((long long)past) - 1;
-                    b = b0 + j;
-                    n_tiles = __builtin_amdgcn_readlane(n, j);
-                    rt = want - (before + __builtin_amdgcn_readlane(incl, j) - n_tiles);
-                    seq = PagedSeq{__builtin_amdgcn_readlane(s.start, j), __builtin_amdgcn_readlane(s.m, j), __builtin_amdgcn_readlane(s.t, j)};
-                    break;
-                }
+        for (int o = 1; o < 64; o <<= 1) {
+            const int y = __shfl_up(x, o, 64);
+            if (lane >= o) x += y;
+        }
+        return x;
+    };
+
+    // ---- SHARED: this workgroup's share
+    int u = 0, u_end = 1, me = 0;
+    int T = 1, n_wg = 1;
+    if constexpr (SHARED) {
+        for (int b = tid; b < a.r.B; b += 256) {
+            PagedSeq s;
+            s_m[b] = seq_of(b, s) ? s.m : 0;
+            s_t[b] = s.t;
+            s_start[b] = s.start;
+        }
+        __syncthreads();
+        for (int b = wave; b < a.r.B; b += 4) {
+            const int m = s_m[b], t = s_t[b], n = (m * a.group + BM - 1) / BM;
+            int sum = 0;
+            for (int rt = lane; rt < n; rt += 64) sum += COST + row_tile_keys(rt, m, t, a.group, cap);
+#pragma unroll
+            for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o, 64);
+            if (lane == 0) s_units[b] = sum;
+        }
+        __syncthreads();
+        int sum = 0, longest = 0;
+        for (int b = lane; b < a.r.B; b += 64) {
+            sum += s_units[b];
+            if (s_m[b]) longest = max(longest, COST + (min(s_t[b] + s_m[b], cap) + kKeys - 1) / kKeys);
+        }
+#pragma unroll
+        for (int o = 32; o > 0; o >>= 1) {
+            sum += __shfl_xor(sum, o, 64);
+            longest = max(longest, __shfl_xor(longest, o, 64));
+        }
+        T = __builtin_amdgcn_readfirstlane(sum) * p.Hkv;
+        if (T == 0) return;
+        longest = __builtin_amdgcn_readfirstlane(longest);
+        const int least = max(CSD_PAGED_MANY_SHARE, (longest + PARTS - 3) / (PARTS - 2));
+        n_wg = min(CSD_PAGED_MANY_GRID, max(1, T / least));
+        // workgroups go to the compute dies in turn: a die's take neighbouring shares, which read the same keys
+        const int per_die = (n_wg + 7) / 8;
+        me = (blockIdx.x % 8) * per_die + blockIdx.x / 8;
+        if ((int)blockIdx.x / 8 >= per_die || me >= n_wg) return;
+        const PagedShares shares(T, n_wg);
+        u = shares.first(me);
+        u_end = shares.first(me + 1);
+    }
+    const PagedShares shares(T, n_wg);
+
+    while (u < u_end) {
+    // ---- the item: rows rt * BM .. of sequence b, key-value head kvh, key tiles kt0 .. kt1 of its n_kt
+    int b = -1, kvh = 0, rt = 0, kt0 = 0, item = 0;
+    PagedSeq seq{0, 0, 0};
+    if constexpr (SHARED) {
+        int before = 0;
+        for (int b0 = 0; b0 < a.r.B; b0 += 64) {
+            const int x = b0 + lane < a.r.B ? s_units[b0 + lane] * p.Hkv : 0, incl = scan(x);
+            const unsigned long long past = __ballot(before + incl > u);
+            if (past) {
+                const int j = __ffsll((long long)past) - 1;
+                b = b0 + j;
+                before += __builtin_amdgcn_readlane(incl, j) - __builtin_amdgcn_readlane(x, j);
+                break;
             }
             before += __builtin_amdgcn_readlane(incl, 63);
         }
-        total = before;
+        if (b < 0) return;                                   // (the lengths changed while they were read)
+        seq = PagedSeq{__builtin_amdgcn_readfirstlane(s_start[b]), __builtin_amdgcn_readfirstlane(s_m[b]), __builtin_amdgcn_readfirstlane(s_t[b])};
+        const int units = __builtin_amdgcn_readfirstlane(s_units[b]), n = (seq.m * a.group + BM - 1) / BM;
+        kvh = (u - before) / units;
+        int left = u - before - kvh * units;
+        rt = -1;
+        for (int r0 = 0; r0 < n; r0 += 64) {
+            const int x = r0 + lane < n ? COST + row_tile_keys(r0 + lane, seq.m, seq.t, a.group, cap) : 0, incl = scan(x);
+            const unsigned long long past = __ballot(incl > left);
+            if (past) {
+                const int j = __ffsll((long long)past) - 1;
+                rt = r0 + j;
+                kt0 = left - (__builtin_amdgcn_readlane(incl, j) - __builtin_amdgcn_readlane(x, j));
+                break;
+            }
+            left -= __builtin_amdgcn_readlane(incl, 63);
+        }
+        if (rt < 0) return;
+        item = u - kt0 + COST;                               // where its keys begin
+        kt0 -= COST;
+    } else {
+        // key-value heads follow one another (workgroups of a die, every eighth, read the same keys), then the row tiles, the late ones with
+        // the most keys first
+        kvh = blockIdx.x % p.Hkv;
+        int total = 0;
+        for (int pass = 0; pass < 2; pass++) {               // count the row tiles of all sequences, then find this one
+            int before = 0;
+            const int want = total - 1 - (int)(blockIdx.x / p.Hkv);
+            if (pass && want < 0) return;
+            for (int b0 = 0; b0 < a.r.B; b0 += 64) {
+                PagedSeq s;
+                const int n = seq_of(b0 + lane, s), incl = scan(n);
+                if (pass) {
+                    const unsigned long long past = __ballot(before + incl > want);
+                    if (past) {
+                        const int j = __ffsll((long long)past) - 1;
+                        b = b0 + j;
+                        rt = want - (before + __builtin_amdgcn_readlane(incl, j) - __builtin_amdgcn_readlane(n, j));
+                        seq = PagedSeq{__builtin_amdgcn_readlane(s.start, j), __builtin_amdgcn_readlane(s.m, j), __builtin_amdgcn_readlane(s.t, j)};
+                        break;
+                    }
+                }
+                before += __builtin_amdgcn_readlane(incl, 63);
+            }
+            total = before;
+        }
+        if (b < 0) return;
     }
-    if (b < 0) return;
     const int rows = min(seq.m * a.group - rt * BM, BM);     // of this item
-    const int i_first = rt * BM / a.group, i_last = (rt * BM + rows - 1) / a.group;
-    const int len = min(seq.t + i_last + 1, cap);            // keys that some row attends
-    const int n_kt = (len + kKeys - 1) / kKeys;
-    // an item's keys in equal parts of at least CSD_PAGED_MANY_SHARE tiles
-    const int parts = min(splits, max(1, n_kt / CSD_PAGED_MANY_SHARE));
-    if (part_no >= parts) return;
-    const int kt0 = (int)((long long)n_kt * part_no / parts), kt1 = (int)((long long)n_kt * (part_no + 1) / parts);
+    const int n_kt = row_tile_keys(rt, seq.m, seq.t, a.group, cap);
+    const int kt1 = SHARED ? min(n_kt, kt0 + u_end - u) : n_kt;
+    u += kt1 - kt0;
+    kt0 = max(kt0, 0);
+    if (kt1 <= 0) continue;                                  // (the share ends before the keys begin)
+    const int len = min(seq.t + (rt * BM + rows - 1) / a.group + 1, cap);      // keys that some row attends
+
+    // The page table, 16 tiles at a time: lane x holds where the x-th group of 16 keys from tile `base` on lies in the pools (bytes; one without a
+    // page: in page 0, which the masks leave out), and bit x of `here` says that it has a page.
+    struct Pages {
+        size_t at;
+        unsigned long long here;
+    };
+    auto pages_from = [&](int base) {
+        const int key = (base * 4 + lane) * 16;
+        const int page = paged_page(p, b, key);
+        return Pages{paged_row(p, max(page, 0), kvh, key) * (DH * ES), __ballot(page >= 0)};
+    };
+    Pages pages = pages_from(kt0), pages_next = pages_from(kt0 + 16);
 
     // ---- this lane's row
     const int r = rt * BM + wave * 32 + col, i = r / a.group, hq = r - i * a.group;
@@ -133,19 +236,16 @@ __global__ __launch_bounds__(256, 2) void k_paged_attn_many(PagedAttn a, int min
     u32x4 qf[ST];
     {
         const bf16_t *q = reinterpret_cast<const bf16_t *>(a.q) + (size_t)(seq.start + i) * a.q_stride + (size_t)(kvh * a.group + hq) * DH + 8 * h;
-        const uint32_t flip = a.scale < 0.f ? 0x80008000u : 0u;      // a negative scale turns the queries around: the maximum below needs scale >= 0
 #pragma unroll
         for (int s = 0; s < ST; s++) {
             qf[s] = u32x4{0u, 0u, 0u, 0u};
             if (live) qf[s] = *reinterpret_cast<const u32x4 *>(q + 16 * s);
-#pragma unroll
-            for (int w = 0; w < 4; w++) qf[s][w] ^= flip;
         }
     }
     // scores in units of log2 (at least 1e-30: a masked score of -inf has to stay one)
     const float scale = fmaxf(fabsf(a.scale) * 1.44269504088896f, 1e-30f);
     f32x16 acc[DT];
-    float m_run = -INFINITY, l_run = 0.f;
+    float m_run = -INFINITY;
 #pragma unroll
     for (int d = 0; d < DT; d++)
 #pragma unroll
@@ -153,168 +253,245 @@ __global__ __launch_bounds__(256, 2) void k_paged_attn_many(PagedAttn a, int min
 
     // ---- staging: in pass x a wave's rows lie in one group of 16 keys, so in one page
     const int row_in = tid / LPR, c_in = tid % LPR;
-    u32x4 kr[NP], vr[NP];
-    uint8_t ksr[NP], vsr[NP];
     auto group_of = [&](int x) { return (x * RPP + wave * (64 / LPR)) >> 4; };
-    auto load = [&](int kt) {
+    auto here_mask = [&](int kt) { return (unsigned)(pages.here >> (((kt - kt0) & 15) * 4)) & 0xFu; };
+    // A side (0: keys, 1: values) of a tile, pass by pass: to registers, then, converted, to LDS.
+    constexpr std::integral_constant<int, 0> K{};
+    constexpr std::integral_constant<int, 1> V{};
+    constexpr int SIDES = F8 ? 2 : 1;                        // bf16: both sides in the same registers, one after the other
+    u32x4 regs[SIDES][NP];
+    uint8_t scales[F8 ? 2 : 1][NP];
+    const unsigned lane_at = ((wave * (64 / LPR)) & 15) * (DH * ES) + lane * 16;       // a lane's place in the 16 keys of its pass
+    auto load = [&](int kt, int x, auto side) {
+        constexpr int S = decltype(side)::value;
+        const int from = ((kt - kt0) & 15) * 4 + group_of(x);
+        const size_t at = ((size_t)(unsigned)__builtin_amdgcn_readlane((int)(pages.at >> 32), from) << 32) | (unsigned)__builtin_amdgcn_readlane((int)pages.at, from);
+        regs[S % SIDES][x] = *reinterpret_cast<const u32x4 *>(reinterpret_cast<const char *>(S ? p.v : p.k) + at + lane_at);
+        if constexpr (F8) scales[S][x] = ((S ? p.vs : p.ks) + at / DH)[lane_at / DH];
+    };
+    auto stage = [&](int x, int buf, auto side) {
+        constexpr int S = decltype(side)::value, W = F8 ? 2 : 1;
+        const int row = x * RPP + row_in;
+        const u32x4 raw = regs[S % SIDES][x];
+        u32x4 v[W];
+        if constexpr (F8) {
+            const float f = pow2_of_byte(scales[S][x]);
 #pragma unroll
-        for (int x = 0; x < NP; x++) {
-            const int page = max(paged_page(p, b, kt * kKeys + 16 * group_of(x)), 0);     // (no page: rows of page 0, which the masks leave out)
-            const size_t row = paged_row(p, page, kvh, kt * kKeys + x * RPP + row_in);
-            kr[x] = *reinterpret_cast<const u32x4 *>(reinterpret_cast<const char *>(p.k) + row * (DH * ES) + c_in * 16);
-            vr[x] = *reinterpret_cast<const u32x4 *>(reinterpret_cast<const char *>(p.v) + row * (DH * ES) + c_in * 16);
-            if constexpr (F8) {
-                ksr[x] = p.ks[row];
-                vsr[x] = p.vs[row];
-            }
+            for (int w = 0; w < 2; w++)
+#pragma unroll
+                for (int y = 0; y < 2; y++) {
+                    v[w][2 * y] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(raw[2 * w + y], f, false));
+                    v[w][2 * y + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(raw[2 * w + y], f, true));
+                }
+        } else {
+            v[0] = raw;
+        }
+#pragma unroll
+        for (int w = 0; w < W; w++) {
+            if constexpr (S == 1) s_v[buf][v_piece<DH>(row, W * c_in + w)] = v[w];
+            else s_k[buf][k_piece<DH>(row, W * c_in + w)] = v[w];
         }
     };
-    auto here_mask = [&](int kt) {                           // bit g: keys 16 g .. 16 g + 15 of the tile have a page
-        unsigned m = 0;
-#pragma unroll
-        for (int g = 0; g < 4; g++) m |= (unsigned)(paged_page(p, b, kt * kKeys + 16 * g) >= 0) << g;
-        return (unsigned)__builtin_amdgcn_readfirstlane((int)m);
-    };
-    auto stage = [&](int kt, int buf, unsigned here) {
-        const bool edge = kt * kKeys + kKeys > seq.t || here != 0xFu;     // rows of the block, or places without a row, among the keys
+    // Where rows of the block, or places without a row, are among a tile's keys: values that no row attends are taken out of LDS again, and those
+    // that are not finite (see odd_halves).  A thread looks at what it stored.
+    auto mend = [&](int kt, int buf) {
+        const unsigned here = here_mask(kt);
+        if (kt * kKeys + kKeys <= seq.t && here == 0xFu) return;
+        constexpr int W = F8 ? 2 : 1;
+        bool odd = false;
 #pragma unroll
         for (int x = 0; x < NP; x++) {
             const int row = x * RPP + row_in;
-            u32x4 vv[F8 ? 2 : 1];
-            if constexpr (F8) {
-                const float fk = pow2_of_byte(ksr[x]), fv = pow2_of_byte(vsr[x]);
+            const bool out = kt * kKeys + row >= len || !((here >> group_of(x)) & 1u);
 #pragma unroll
-                for (int w = 0; w < 2; w++) {
-                    u32x4 kk;
+            for (int w = 0; w < W; w++) {
+                u32x4 v = s_v[buf][v_piece<DH>(row, W * c_in + w)];
 #pragma unroll
-                    for (int y = 0; y < 2; y++) {
-                        kk[2 * y] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(kr[x][2 * w + y], fk, false));
-                        kk[2 * y + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(kr[x][2 * w + y], fk, true));
-                        vv[w][2 * y] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(vr[x][2 * w + y], fv, false));
-                        vv[w][2 * y + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(vr[x][2 * w + y], fv, true));
-                    }
-                    s_k[buf][k_piece<DH>(row, 2 * c_in + w)] = kk;
+                for (int y = 0; y < 4; y++) {
+                    if (out) v[y] = 0u;
+                    const uint32_t o = odd_halves(v[y]);
+                    odd |= o != 0u;
+                    v[y] &= ~o;
                 }
-            } else {
-                s_k[buf][k_piece<DH>(row, c_in)] = kr[x];
-                vv[0] = vr[x];
+                s_v[buf][v_piece<DH>(row, W * c_in + w)] = v;
             }
-            if (edge) {
-                // values that no row attends are taken out, and those that are not finite (see odd_halves)
-                bool odd = false;
-                const bool out = kt * kKeys + row >= len || !((here >> group_of(x)) & 1u);
-#pragma unroll
-                for (int w = 0; w < (F8 ? 2 : 1); w++)
-#pragma unroll
-                    for (int y = 0; y < 4; y++) {
-                        if (out) vv[w][y] = 0u;
-                        const uint32_t o = odd_halves(vv[w][y]);
-                        odd |= o != 0u;
-                        vv[w][y] &= ~o;
-                    }
-                if (odd) s_odd = 1;
-            }
-#pragma unroll
-            for (int w = 0; w < (F8 ? 2 : 1); w++) s_v[buf][v_piece<DH>(row, (F8 ? 2 : 1) * c_in + w)] = vv[w];
         }
+        if (odd) s_odd = 1;
     };
-    // V^T operand: features 32 d .. 32 d + 31 of keys 16 u .. 16 u + 15, in the order of the weights
-    const int l16 = lane & 15;
-    auto v_operand = [&](int buf, int d, int u) {
-        uint64_t w[2];
-#pragma unroll
-        for (int y = 0; y < 2; y++) {
-            const int row = 16 * u + 8 * y + 4 * h + (l16 >> 2), piece = 4 * d + 2 * ((lane >> 4) & 1) + ((l16 >> 1) & 1);
-            char *at = reinterpret_cast<char *>(&s_v[buf][v_piece<DH>(row, piece)]) + 8 * (l16 & 1);
-            w[y] = __builtin_bit_cast(uint64_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)at));
-        }
-        return u32x4{(uint32_t)w[0], (uint32_t)(w[0] >> 32), (uint32_t)w[1], (uint32_t)(w[1] >> 32)};
-    };
-
     if (tid == 0) s_odd = 0;
-    load(kt0);
-    unsigned here = here_mask(kt0);
     __syncthreads();
-    stage(kt0, 0, here);
+    {
+        u32x4 first[NP];                                     // (both sides in flight)
+#pragma unroll
+        for (int x = 0; x < NP; x++) load(kt0, x, V);
+#pragma unroll
+        for (int x = 0; x < NP; x++) first[x] = regs[1 % SIDES][x];
+#pragma unroll
+        for (int x = 0; x < NP; x++) load(kt0, x, K);
+#pragma unroll
+        for (int x = 0; x < NP; x++) stage(x, 0, K);
+#pragma unroll
+        for (int x = 0; x < NP; x++) regs[1 % SIDES][x] = first[x];
+#pragma unroll
+        for (int x = 0; x < NP; x++) stage(x, 0, V);
+        mend(kt0, 0);
+    }
     __syncthreads();
+
+    if (a.scale < 0.f)                                       // a negative scale turns the queries around: the maximum below needs scale >= 0
+#pragma unroll
+        for (int s = 0; s < ST; s++) qf[s] ^= u32x4{0x80008000u, 0x80008000u, 0x80008000u, 0x80008000u};
     const int wave_first = seq.t + (rt * BM + wave * 32) / a.group;      // last position that the wave's first row attends
     const bool wave_live = wave * 32 < rows;
+    // where a lane reads: K row `col` (+ 32), pieces 2 s + h; V as LDS's transposing read wants it (the place of 4 features of a key), pieces 4 d + ..
+    const int l16 = lane & 15;
+    const int k_at = k_piece<DH>(col, h) * 16, v_row = 4 * h + (l16 >> 2);
+    const int v_at = v_piece<DH>(v_row, 2 * ((lane >> 4) & 1) + ((l16 >> 1) & 1)) * 16 + 8 * (l16 & 1);
+    float l_run = 0.f, l_more = 0.f;                         // the sum of weights, in two chains
+    int kt = kt0;
+    auto turn = [&](auto which) {
+        constexpr int buf = decltype(which)::value;
+        const int key0 = kt * kKeys, next = min(kt + 1, kt1 - 1);        // (the last turn brings its own tile once more: no branches)
+        const unsigned here = here_mask(kt);
+        if (((next - kt0) & 15) == 0 && next != kt) {
+            pages = pages_next;
+            pages_next = pages_from(next + 16);
+        }
+        if (!wave_live) {
+#pragma unroll
+            for (int x = 0; x < NP; x++) load(next, x, V);
+#pragma unroll
+            for (int x = 0; x < NP; x++) {
+                stage(x, buf ^ 1, V);
+                load(next, x, K);
+            }
+#pragma unroll
+            for (int x = 0; x < NP; x++) stage(x, buf ^ 1, K);
+            mend(next, buf ^ 1);
+            return;
+        }
+        // What is issued between the matrix instructions, which take as long as several others, is set down one by one: operands are read two
+        // products ahead; the next tile's values are requested first and stored (to the other buffer, last read a turn ago) beside the second
+        // products, its keys requested as registers become free and stored at the end.
+        int ka_at = k_at, va_at = v_at;
+        asm volatile("" : "+v"(ka_at), "+v"(va_at));         // (the xors below are made here, not kept in a register each)
+        f32x16 st[2];
+#pragma unroll
+        for (int e = 0; e < 16; e++) st[0][e] = st[1][e] = 0.f;
+        u32x4 ka[3][2];
+        auto read_k = [&](int s) {
+#pragma unroll
+            for (int T2 = 0; T2 < 2; T2++)
+                ka[s % 3][T2] = *reinterpret_cast<const u32x4 *>(reinterpret_cast<const char *>(&s_k[buf][0]) + (ka_at ^ (32 * s)) + T2 * 32 * DH * 2);
+        };
+        read_k(0);
+        read_k(1);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int s = 0; s < ST; s++) {
+            if (s + 2 < ST) read_k(s + 2);
+            st[0] = mfma32(ka[s % 3][0], qf[s], st[0]);
+            if (s < NP) load(next, s, V);
+            __builtin_amdgcn_sched_barrier(0);
+            st[1] = mfma32(ka[s % 3][1], qf[s], st[1]);
+            if (F8 && s < NP) load(next, s, K);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        // element e of half T2 is key 32 T2 + 8 (e / 4) + 4 h + e % 4
+        const bool whole = (a.parent ? key0 + kKeys <= seq.t : key0 + kKeys - 1 <= wave_first) && key0 + kKeys <= len && here == 0xFu;
+        bool sees = true;
+        if (!whole) {
+            const int n = min(limit, len - 1) - key0;        // attended: keys 0 .. n of the tile
+            unsigned long long m = n >= 63 ? ~0ull : n < 0 ? 0ull : (2ull << n) - 1;
+#pragma unroll
+            for (int g = 0; g < 4; g++)
+                if (!((here >> g) & 1u)) m &= ~(0xFFFFull << (16 * g));
+            if (a.parent) {
+                const int d = key0 - seq.t;                  // rows of the block lie at d .. of `above`; keys before them are cached
+                m &= d >= 0 ? (d < 64 ? above >> d : 0ull) : -d >= 64 ? ~0ull : (above << -d) | ((1ull << -d) - 1);
+            }
+            sees = m != 0;
+            m >>= 4 * h;
+#pragma unroll
+            for (int e = 0; e < 32; e++)
+                if (!((m >> (8 * (e / 4) + e % 4)) & 1u)) st[e >> 4][e & 15] = -INFINITY;
+        }
+        auto read_v = [&](int x) {                           // features 32 d .. of keys 16 u .., in the order of the weights
+            const int u = x / DT, d = x % DT;
+            uint64_t w[2];
+#pragma unroll
+            for (int y = 0; y < 2; y++) {
+                char *at = reinterpret_cast<char *>(&s_v[buf][0]) + (va_at ^ (64 * d)) + (16 * u + 8 * y) * DH * 2;
+                w[y] = __builtin_bit_cast(uint64_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)at));
+            }
+            return u32x4{(uint32_t)w[0], (uint32_t)(w[0] >> 32), (uint32_t)w[1], (uint32_t)(w[1] >> 32)};
+        };
+        u32x4 va[3];
+        va[0] = read_v(0);
+        va[1] = read_v(1);
+        float top = st[0][0];
+#pragma unroll
+        for (int e = 1; e < 31; e += 2) top = fmaxf(fmaxf(st[e >> 4][e & 15], st[(e + 1) >> 4][(e + 1) & 15]), top);
+        // (both halves of the lanes have the row's maximum; -inf: nothing to attend yet, a score of -inf is something)
+        top = halves_max(sees ? fmaxf(fmaxf(top, st[1][15]) * scale, -3.0e38f) : -INFINITY);
+        // weights up to 2^8 are as good as weights up to 1: the outputs are rescaled only when the maximum has moved by more
+        if (__any(top > m_run + 8.f)) {
+            const float m_new = fmaxf(m_run, top), fade = __builtin_amdgcn_exp2f(m_run - (m_new == -INFINITY ? 0.f : m_new));
+            l_run *= fade;
+            l_more *= fade;
+#pragma unroll
+            for (int d = 0; d < DT; d++) acc[d] *= fade;
+            m_run = m_new;
+        }
+        const float ref = m_run == -INFINITY ? 0.f : -m_run;
+        u32x4 pw[2];                                         // weights of keys 16 u .. 16 u + 15 at u % 2
+        auto weigh = [&](int e) {                            // elements e, e + 1
+            const float w0 = __builtin_amdgcn_exp2f(fmaf(st[e >> 4][e & 15], scale, ref)), w1 = __builtin_amdgcn_exp2f(fmaf(st[e >> 4][(e + 1) & 15], scale, ref));
+            l_run += w0;
+            l_more += w1;
+            pw[(e >> 3) & 1][(e & 7) >> 1] = pack_bf16x2(w0, w1);
+        };
+#pragma unroll
+        for (int e = 0; e < 8; e += 2) weigh(e);
+        __builtin_amdgcn_sched_barrier(0);
+        // The next 16 keys' weights are made beside the products of these.  (A wave here goes first: the matrix cores wait for nothing else; chunks of
+        // 2048 rows 550 -> 531 us, with the first products at that priority too 531.)
+        __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+        for (int x = 0; x < 4 * DT; x++) {
+            const int u = x / DT, d = x % DT;
+            if (x + 2 < 4 * DT) va[(x + 2) % 3] = read_v(x + 2);
+            acc[d] = mfma32(va[x % 3], pw[u & 1], acc[d]);
+            if (u < 3)
+#pragma unroll
+                for (int e = 0; e < 8 / DT; e += 2) weigh(8 * (u + 1) + 8 / DT * d + e);
+            __builtin_amdgcn_sched_barrier(0);
+            if (x < NP) {
+                stage(x, buf ^ 1, V);
+                if (!F8) load(next, x, K);
+            }
+            if (F8 && x >= 4 * DT - NP) stage(x - (4 * DT - NP), buf ^ 1, K);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        __builtin_amdgcn_s_setprio(0);
+        if (!F8)
+#pragma unroll
+            for (int x = 0; x < NP; x++) stage(x, buf ^ 1, K);
+        mend(next, buf ^ 1);
+    };
 #pragma unroll 1
-    for (int kt = kt0; kt < kt1; kt++) {
-        const int buf = (kt - kt0) & 1, key0 = kt * kKeys;
-        const bool more = kt + 1 < kt1;
-        unsigned here_next = 0xFu;
-        if (more) {
-            load(kt + 1);
-            here_next = here_mask(kt + 1);
-        }
-        if (wave_live) {
-            f32x16 st[2];
-#pragma unroll
-            for (int T2 = 0; T2 < 2; T2++) {
-#pragma unroll
-                for (int e = 0; e < 16; e++) st[T2][e] = 0.f;
-#pragma unroll
-                for (int s = 0; s < ST; s++) st[T2] = mfma32(s_k[buf][k_piece<DH>(32 * T2 + col, 2 * s + h)], qf[s], st[T2]);
-            }
-            // element e of half T2 is key 32 T2 + 8 (e / 4) + 4 h + e % 4
-            uint32_t sees = ~0u;
-            const bool whole = (a.parent ? key0 + kKeys <= seq.t : key0 + kKeys - 1 <= wave_first) && key0 + kKeys <= len && here == 0xFu;
-            if (!whole) {
-                const int n = min(limit, len - 1) - key0;    // attended: keys 0 .. n of the tile
-                unsigned long long m = n >= 63 ? ~0ull : n < 0 ? 0ull : (2ull << n) - 1;
-#pragma unroll
-                for (int g = 0; g < 4; g++)
-                    if (!((here >> g) & 1u)) m &= ~(0xFFFFull << (16 * g));
-                if (a.parent) {
-                    const int d = key0 - seq.t;              // rows of the block lie at d .. of `above`; keys before them are cached
-                    m &= d >= 0 ? (d < 64 ? above >> d : 0ull) : -d >= 64 ? ~0ull : (above << -d) | ((1ull << -d) - 1);
-                }
-                m >>= 4 * h;
-                sees = 0;
-#pragma unroll
-                for (int q = 0; q < 8; q++) sees |= (uint32_t)((m >> (8 * q)) & 0xFull) << (4 * q);
-#pragma unroll
-                for (int e = 0; e < 32; e++)
-                    if (!((sees >> e) & 1u)) st[e >> 4][e & 15] = -INFINITY;
-            }
-            float top = st[0][0];
-#pragma unroll
-            for (int e = 1; e < 32; e++) top = fmaxf(top, st[e >> 4][e & 15]);
-            top = halves_max(sees ? fmaxf(top * scale, -3.0e38f) : -INFINITY);   // -inf: nothing to attend yet (a score of -inf is something)
-            // weights up to 2^8 are as good as weights up to 1: the outputs are rescaled only when the maximum has moved by more
-            if (__any(top > m_run + 8.f)) {
-                const float m_new = fmaxf(m_run, top), fade = __builtin_amdgcn_exp2f(m_run - (m_new == -INFINITY ? 0.f : m_new));
-                l_run *= fade;
-#pragma unroll
-                for (int d = 0; d < DT; d++) acc[d] *= fade;
-                m_run = m_new;
-            }
-            const float ref = m_run == -INFINITY ? 0.f : m_run;
-            u32x4 pw[4];                                     // weights of keys 16 u .. 16 u + 15
-#pragma unroll
-            for (int e = 0; e < 32; e += 2) {
-                const float w0 = __builtin_amdgcn_exp2f(fmaf(st[e >> 4][e & 15], scale, -ref)), w1 = __builtin_amdgcn_exp2f(fmaf(st[e >> 4][(e + 1) & 15], scale, -ref));
-                l_run += w0;
-                l_run += w1;
-                pw[e >> 3][(e & 7) >> 1] = pack_bf16x2(w0, w1);
-            }
-#pragma unroll
-            for (int d = 0; d < DT; d++)
-#pragma unroll
-                for (int u = 0; u < 4; u++) acc[d] = mfma32(v_operand(buf, d, u), pw[u], acc[d]);
-        }
-        if (more) {
-            stage(kt + 1, buf ^ 1, here_next);               // (that buffer was last read a turn ago)
-            __syncthreads();
-            here = here_next;
-        }
+    while (true) {
+        turn(std::integral_constant<int, 0>{});
+        __syncthreads();
+        if (++kt == kt1) break;
+        turn(std::integral_constant<int, 1>{});
+        __syncthreads();
+        if (++kt == kt1) break;
     }
+    l_run = halves_sum(l_run + l_more);
 
     if (s_odd) {                                             // (uniform; the last tile was staged in front of a barrier)
-        for (int kt = kt0; kt < kt1; kt++) {
-            const unsigned m = here_mask(kt);
-            if (kt * kKeys + kKeys <= seq.t && m == 0xFu) continue;
+        for (kt = kt0; kt < kt1; kt++) {
             for (int key = kt * kKeys; key < min(kt * kKeys + kKeys, len); key++) {
                 const int page = paged_page(p, b, key);
                 if (page < 0) continue;
@@ -329,8 +506,8 @@ __global__ __launch_bounds__(256, 2) void k_paged_attn_many(PagedAttn a, int min
     }
 
     // ---- results: element e of acc[d] is feature 32 d + 8 (e / 4) + 4 h + e % 4 of the lane's row
-    l_run = halves_sum(l_run);
     const size_t out_row = ((size_t)(seq.start + i) * p.Hkv + kvh) * a.group + hq;
+    const int w_first = SHARED ? shares.owner(item) : 0, w_last = SHARED ? shares.owner(item + n_kt - 1) : 0, parts = w_last - w_first + 1;
     if (parts == 1) {
         if (live) {
             const float inv = 1.f / l_run;
@@ -343,83 +520,43 @@ __global__ __launch_bounds__(256, 2) void k_paged_attn_many(PagedAttn a, int min
                     *reinterpret_cast<u32x2 *>(reinterpret_cast<bf16_t *>(a.out) + out_row * DH + 32 * d + 8 * y + 4 * h) = o;
                 }
         }
-        return;
+        __syncthreads();
+        continue;
     }
-    const int item = tile_no * p.Hkv + kvh;
-    float *part = reinterpret_cast<float *>(reinterpret_cast<char *>(a.ws) + CSD_PAGED_COUNTER_BYTES) + (size_t)item * splits * BM * PS;
+    const PagedParts<DH, BM> split(a.ws, CSD_PAGED_MANY_GRID, w_first, parts);
     if (live) {
-        float *mine = part + ((size_t)part_no * BM + wave * 32 + col) * PS;
+        const int row = wave * 32 + col;
 #pragma unroll
         for (int d = 0; d < DT; d++)
 #pragma unroll
-            for (int y = 0; y < 4; y++) {
-                store_dev2(mine + 32 * d + 8 * y + 4 * h, acc[d][4 * y], acc[d][4 * y + 1]);
-                store_dev2(mine + 32 * d + 8 * y + 4 * h + 2, acc[d][4 * y + 2], acc[d][4 * y + 3]);
-            }
-        if (h == 0) store_dev2(mine + DH, m_run, l_run);
+            for (int y = 0; y < 4; y++)
+                split.store(me - w_first, row, 32 * d + 8 * y + 4 * h, f32x4{acc[d][4 * y], acc[d][4 * y + 1], acc[d][4 * y + 2], acc[d][4 * y + 3]});
+        if (h == 0) split.store(me - w_first, row, DH, f32x4{m_run, l_run, 0.f, 0.f});
     }
-    // the stores above are acknowledged before the counter moves; whoever arrives last joins the parts, in their order
-    __builtin_amdgcn_s_waitcnt(0x0F70);                      // vmcnt(0)
+    if (!split.arrive(a.ws, &s_last)) continue;
+    static_assert((2 * CSD_PAGED_MANY_PARTS + 1) * BM * 4 <= 2 * PIECES * 16, "");
+    split.join(a.ws, reinterpret_cast<float *>(&s_k[0][0]), rows, [&](int row) {
+        const int r_ = rt * BM + row, i_ = r_ / a.group, h_ = r_ - i_ * a.group;
+        return reinterpret_cast<bf16_t *>(a.out) + (((size_t)(seq.start + i_) * p.Hkv + kvh) * a.group + h_) * DH;
+    });
     __syncthreads();
-    unsigned *count = reinterpret_cast<unsigned *>(a.ws) + item;
-    if (tid == 0) s_last = __hip_atomic_fetch_add(count, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (unsigned)(parts - 1);
-    __syncthreads();
-    if (!s_last) return;
-    float *weight = reinterpret_cast<float *>(&s_k[0][0]);   // [parts][BM], then the rows' maxima and sums
-    float *sums = weight + CSD_PAGED_MANY_PARTS * BM;
-    if (tid < rows) {
-        float m = -INFINITY, l = 0.f;
-        float2 ml[CSD_PAGED_MANY_PARTS];
-#pragma unroll
-        for (int k = 0; k < CSD_PAGED_MANY_PARTS; k++) ml[k] = k < parts ? load_dev2(part + ((size_t)k * BM + tid) * PS + DH) : float2{-INFINITY, 0.f};
-#pragma unroll
-        for (int k = 0; k < CSD_PAGED_MANY_PARTS; k++) m = fmaxf(m, ml[k].x);
-        const float ref = m == -INFINITY ? 0.f : m;
-#pragma unroll
-        for (int k = 0; k < CSD_PAGED_MANY_PARTS; k++)
-            if (k < parts) {
-                const float f = __builtin_amdgcn_exp2f(ml[k].x - ref);
-                l += f * ml[k].y;
-                weight[k * BM + tid] = f;
-            }
-        sums[2 * tid] = m;
-        sums[2 * tid + 1] = l;
     }
-    __syncthreads();
-    for (int x = tid; x < rows * (DH / 2); x += 256) {
-        const int rr = x / (DH / 2), c = 2 * (x % (DH / 2));
-        float o0 = 0.f, o1 = 0.f;
-        float2 v[CSD_PAGED_MANY_PARTS];
-#pragma unroll
-        for (int k = 0; k < CSD_PAGED_MANY_PARTS; k++) v[k] = load_dev2(part + ((size_t)min(k, parts - 1) * BM + rr) * PS + c);
-#pragma unroll
-        for (int k = 0; k < CSD_PAGED_MANY_PARTS; k++)
-            if (k < parts) {
-                const float f = weight[k * BM + rr];
-                o0 += f * v[k].x;
-                o1 += f * v[k].y;
-            }
-        const int ro = rt * BM + rr, io = ro / a.group, ho = ro - io * a.group;
-        const float inv = 1.f / sums[2 * rr + 1];
-        uint32_t *out = reinterpret_cast<uint32_t *>(a.out) + (((size_t)(seq.start + io) * p.Hkv + kvh) * a.group + ho) * (DH / 2);
-        out[c / 2] = sums[2 * rr] == -INFINITY ? 0u : pack_bf16x2(o0 * inv, o1 * inv);
-    }
-    if (tid == 0) __hip_atomic_store(count, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);     // ready for the next launch
 }
 
 // min_rows: sequences of so many rows or fewer are another kernel's.
 void csd_paged_many_enqueue(const PagedAttn &a, int min_rows, int32_t pool_dtype, hipStream_t st) {
     // row tiles at most: full ones, and a last one per sequence
     const long long tiles = (long long)a.r.rows * a.group / CSD_PAGED_MANY_ROWS + a.r.B, items = tiles * a.p.Hkv;
-    // few items: their keys are split, as far as the chip (two workgroups per compute unit) and the workspace have room
-    int splits = 1;
-    while (splits * 2 <= CSD_PAGED_MANY_PARTS && items * splits * 2 <= CSD_PAGED_MANY_SLOTS) splits *= 2;
-    const dim3 grid((unsigned)(items * splits));
+    const long long keys = ((long long)a.p.table_stride << a.p.page_shift) / kKeys + 1 + CSD_PAGED_MANY_COST;      // (all key tiles are counted in 32 bits)
+    const bool shared = items <= CSD_PAGED_MANY_ITEMS && a.r.B <= CSD_PAGED_MANY_BATCH && items * keys < (1ll << 30);
+    const dim3 grid(shared ? CSD_PAGED_MANY_GRID : (unsigned)items);
+    auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, st, a, min_rows); };
+    const bool f8 = pool_dtype == CSD_DTYPE_FP8;
     if (a.p.D == 128) {
-        if (pool_dtype == CSD_DTYPE_FP8) hipLaunchKernelGGL((k_paged_attn_many<128, true>), grid, dim3(256), 0, st, a, min_rows, splits);
-        else hipLaunchKernelGGL((k_paged_attn_many<128, false>), grid, dim3(256), 0, st, a, min_rows, splits);
+        if (shared) f8 ? launch(k_paged_attn_many<128, true, true>) : launch(k_paged_attn_many<128, false, true>);
+        else f8 ? launch(k_paged_attn_many<128, true, false>) : launch(k_paged_attn_many<128, false, false>);
     } else {
-        if (pool_dtype == CSD_DTYPE_FP8) hipLaunchKernelGGL((k_paged_attn_many<64, true>), grid, dim3(256), 0, st, a, min_rows, splits);
-        else hipLaunchKernelGGL((k_paged_attn_many<64, false>), grid, dim3(256), 0, st, a, min_rows, splits);
+        if (shared) f8 ? launch(k_paged_attn_many<64, true, true>) : launch(k_paged_attn_many<64, false, true>);
+        else f8 ? launch(k_paged_attn_many<64, true, false>) : launch(k_paged_attn_many<64, false, false>);
     }
 }
