@@ -376,10 +376,11 @@ int32_t csd_paged_read(const csd_paged_kv *kv, int32_t layer, const int32_t *row
  * out = softmax(scale * q k^T) v, scores, maxima and sums in fp32; a row that has nothing to attend gives zeros, and what
  * a row does not attend never reaches it (not even infinities and NaN).  max_rows: at least the rows of the longest sequence of the batch
  * (a longer one is cut to it), 1 <= max_rows; CSD_ESHAPE for trees with max_rows > 64.
- * workspace: device, 256-byte aligned, CSD_PAGED_WORKSPACE_BYTES; zeroed before its first use; every call leaves what the next one
- * needs zeroed.  Calls that share it must not overlap.
+ * workspace: device, 256-byte aligned, CSD_PAGED_WORKSPACE_BYTES, of which the first CSD_PAGED_WORKSPACE_ZERO_BYTES are zeroed before its first use;
+ * every call leaves them zeroed.  Calls that share it must not overlap.
  */
-#define CSD_PAGED_WORKSPACE_BYTES (96u << 20)
+#define CSD_PAGED_WORKSPACE_BYTES (72u << 20)
+#define CSD_PAGED_WORKSPACE_ZERO_BYTES (64u << 10)
 int32_t csd_paged_attention(const csd_paged_kv *kv, int32_t layer, const int32_t *row_start, const int32_t *cache_len,
                             const int32_t *parent, int32_t B, int32_t rows, int32_t max_rows, const void *q, int64_t q_stride,
                             int32_t n_heads, int32_t dtype, float scale, void *out, void *workspace, void *stream);

@@ -58,7 +58,8 @@ _ARGTYPES = {"csd_paged_write": [_P, _I, _P, _P, _I, _I, _P, _L, _P, _L, _I, _P]
              "csd_paged_read": [_P, _I, _P, _P, _I, _I, _P, _L, _P, _L, _I, _P],
              "csd_paged_attention": [_P, _I, _P, _P, _P, _I, _I, _I, _P, _L, _I, _I, C.c_float, _P, _P, _P],
              "csd_paged_commit": [_P, _P, _P, _P, _I, _I, _P]}
-PAGED_WORKSPACE_BYTES = 96 << 20
+PAGED_WORKSPACE_BYTES, PAGED_WORKSPACE_ZERO_BYTES = 72 << 20, 64 << 10
+_ROWS = {torch.float32: 0, torch.bfloat16: 1}     # types of dense rows
 
 _lib = None
 
@@ -105,6 +106,10 @@ def _ptr(t, dtype=None):
 
 # (not a public name: a build of torch without it takes the public way)
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda device: torch.cuda.current_stream(device).cuda_stream)
+
+
+# (likewise: the public way also looks whether the runtime is up, which it is once there is a tensor)
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 
 
 def _stream():
@@ -271,106 +276,130 @@ class PagedKv:
         self.n_layers, self.n_pages, self.n_kv_heads, self.page_rows, self.head_dim = k.shape
         self._pool = PagedPool(self.n_layers, self.n_pages, self.page_rows, self.n_kv_heads, self.head_dim, types[k.dtype],
                                _ptr(k).value, _ptr(v).value, _ptr(k_scale, torch.uint8).value, _ptr(v_scale, torch.uint8).value, None, 0)
-        self._ref = C.addressof(self._pool)
+        self._ref, self._lib, self._device = C.addressof(self._pool), lib(), k.device
         if workspace is None:
-            self._check_device()
-            workspace = torch.zeros(PAGED_WORKSPACE_BYTES, dtype=torch.uint8, device=k.device)
+            self._check()
+            workspace = torch.empty(PAGED_WORKSPACE_BYTES, dtype=torch.uint8, device=k.device)
+            workspace[:PAGED_WORKSPACE_ZERO_BYTES].zero_()
             torch.cuda.current_stream().synchronize()     # zeroed for whatever stream the first call runs on
         elif workspace.numel() * workspace.element_size() < PAGED_WORKSPACE_BYTES:
-            raise ValueError(f"workspace: {PAGED_WORKSPACE_BYTES} bytes, zeroed")
+            raise ValueError(f"workspace: {PAGED_WORKSPACE_BYTES} bytes, the first {PAGED_WORKSPACE_ZERO_BYTES} of them zeroed")
         self.workspace = workspace
         self._ws = _ptr(workspace).value
 
-    def _check_device(self):
-        if torch.cuda.current_device() != self._dev:
+    def _check(self, **tensors):
+        """Raises for what is wrong with a call's tensors.  The methods look at everything in one expression and come here only if it does not hold
+        (which strides of dimensions of size one may also cause): checked one by one, in functions, they took as long as the smallest kernels."""
+        if _current_device() != self._dev:
             raise ValueError("the cache is on another device than the current one")
-
-    def _ints(self, t, n, what):
-        """Address of a contiguous int32 tensor with n elements on the cache's device."""
-        if t.get_device() != self._dev:
-            raise ValueError(f"{what}: a tensor on the cache's device is required")
-        if t.dtype is not torch.int32:
-            raise TypeError(f"{what}: expected torch.int32, got {t.dtype}")
-        if t.numel() != n or not t.is_contiguous():
-            raise ValueError(f"{what}: {n} contiguous elements are required")
-        return t.data_ptr()
-
-    def _rows(self, t, rows, heads, what, dtype=None):
-        """(address, elements from row to row, type) of a [rows][heads][head dim] tensor."""
-        if t.get_device() != self._dev:
-            raise ValueError(f"{what}: a tensor on the cache's device is required")
-        code = 1 if t.dtype is torch.bfloat16 else 0 if t.dtype is torch.float32 else -1
-        if code < 0 or (dtype is not None and code != dtype):
-            raise TypeError(f"{what}: rows are float32 or bfloat16, all of a call alike, got {t.dtype}")
-        d = self.head_dim
-        if t.ndim != 3 or t.shape[0] != rows or t.shape[1] != heads or t.shape[2] != d:
-            raise ValueError(f"{what}: [{rows}][{heads}][{d}] is required, got {list(t.shape)}")
-        if t.stride(2) != 1 or (heads > 1 and t.stride(1) != d):
-            raise ValueError(f"{what}: the elements of a row must be contiguous")
-        return t.data_ptr(), t.stride(0) if rows > 1 else heads * d, code
-
-    def _call(self, table, row_start, pos):
-        """Puts the table into the pool's description; (B, row_start, pos) of the call."""
-        if table.ndim != 2:
-            raise ValueError("table: [B][pages of a sequence]")
-        B, n = table.shape
-        self._check_device()
-        pool = self._pool
-        pool.table, pool.table_stride = self._ints(table, B * n, "table"), n
-        return B, self._ints(row_start, B + 1, "row_start") if row_start is not None else None, self._ints(pos, B, "cache_len")
+        dtype = None
+        for name, (t, want) in tensors.items():
+            if t.get_device() != self._dev:
+                raise ValueError(f"{name}: a tensor on the cache's device is required")
+            if isinstance(want, int):                      # int32, so many elements
+                if t.dtype is not torch.int32:
+                    raise TypeError(f"{name}: expected torch.int32, got {t.dtype}")
+                if t.numel() != want or not t.is_contiguous():
+                    raise ValueError(f"{name}: {want} contiguous elements are required")
+                continue
+            if t.dtype not in _ROWS or dtype not in (None, t.dtype):
+                raise TypeError(f"{name}: rows are float32 or bfloat16, all of a call alike, got {t.dtype}")
+            dtype = t.dtype
+            if tuple(t.shape) != want or (want[2] > 1 and t.stride(2) != 1) or (want[1] > 1 and t.stride(1) != want[2]):
+                raise ValueError(f"{name}: {list(want)} with contiguous rows is required, got {list(t.shape)} with strides {list(t.stride())}")
 
     def write(self, layer, table, row_start, cache_len, k_rows, v_rows):
         """csd_paged_write: row r of sequence b becomes position cache_len[b] + r - row_start[b]."""
-        B, start, pos = self._call(table, row_start, cache_len)
-        rows = k_rows.shape[0]
-        kp, ks, code = self._rows(k_rows, rows, self.n_kv_heads, "k_rows")
-        vp, vs, _ = self._rows(v_rows, rows, self.n_kv_heads, "v_rows", code)
-        rc = lib().csd_paged_write(self._ref, layer, start, pos, B, rows, kp, ks, vp, vs, code, _raw_stream(self._dev))
+        dev, i32, d, heads = self._dev, torch.int32, self.head_dim, self.n_kv_heads
+        B, n = table.shape
+        shape, dtype, ks, vs = k_rows.shape, k_rows.dtype, k_rows.stride(), v_rows.stride()
+        rows = shape[0]
+        if not (dev == table.get_device() == row_start.get_device() == cache_len.get_device() == k_rows.get_device() == v_rows.get_device()
+                and i32 is table.dtype is row_start.dtype is cache_len.dtype and table.is_contiguous() and row_start.is_contiguous()
+                and cache_len.is_contiguous() and row_start.numel() == B + 1 and cache_len.numel() == B and dtype in _ROWS
+                and v_rows.dtype is dtype and (rows, heads, d) == shape == v_rows.shape and (d, 1) == ks[1:] == vs[1:] and _current_device() == dev):
+            self._check(table=(table, B * n), row_start=(row_start, B + 1), cache_len=(cache_len, B), k_rows=(k_rows, (rows, heads, d)),
+                        v_rows=(v_rows, (rows, heads, d)))
+        pool = self._pool
+        pool.table, pool.table_stride = table.data_ptr(), n
+        rc = self._lib.csd_paged_write(self._ref, layer, row_start.data_ptr(), cache_len.data_ptr(), B, rows, k_rows.data_ptr(),
+                                       ks[0] if rows > 1 else heads * d, v_rows.data_ptr(), vs[0] if rows > 1 else heads * d, _ROWS[dtype],
+                                       _raw_stream(dev))
         if rc:
             _chk(rc, "csd_paged_write")
 
     def read(self, layer, table, row_start, cache_len, rows, dtype=torch.float32, out=None):
         """csd_paged_read: (k, v) [rows][kv heads][head dim], row r of sequence b from position cache_len[b] + r - row_start[b].
         out: the two tensors to fill; rows of no sequence are left as they are (undefined in new tensors)."""
-        B, start, pos = self._call(table, row_start, cache_len)
+        dev, i32, d, heads = self._dev, torch.int32, self.head_dim, self.n_kv_heads
+        B, n = table.shape
         if out is None:
-            shape = (rows, self.n_kv_heads, self.head_dim)
-            out = torch.empty((2,) + shape, dtype=dtype, device=self.k.device).unbind(0)
-        kp, ks, code = self._rows(out[0], rows, self.n_kv_heads, "out")
-        vp, vs, _ = self._rows(out[1], rows, self.n_kv_heads, "out", code)
-        rc = lib().csd_paged_read(self._ref, layer, start, pos, B, rows, kp, ks, vp, vs, code, _raw_stream(self._dev))
+            k = torch.empty(rows, heads, d, dtype=dtype, device=self._device)
+            v = torch.empty_like(k)
+            ok = dtype in _ROWS
+        else:
+            k, v = out
+            dtype = k.dtype
+            ok = (dev == k.get_device() == v.get_device() and dtype in _ROWS and v.dtype is dtype and (rows, heads, d) == k.shape == v.shape
+                  and (d, 1) == k.stride()[1:] == v.stride()[1:])
+        if not (ok and dev == table.get_device() == row_start.get_device() == cache_len.get_device()
+                and i32 is table.dtype is row_start.dtype is cache_len.dtype and table.is_contiguous() and row_start.is_contiguous()
+                and cache_len.is_contiguous() and row_start.numel() == B + 1 and cache_len.numel() == B and _current_device() == dev):
+            self._check(table=(table, B * n), row_start=(row_start, B + 1), cache_len=(cache_len, B), k=(k, (rows, heads, d)), v=(v, (rows, heads, d)))
+        pool = self._pool
+        pool.table, pool.table_stride = table.data_ptr(), n
+        rc = self._lib.csd_paged_read(self._ref, layer, row_start.data_ptr(), cache_len.data_ptr(), B, rows, k.data_ptr(),
+                                      k.stride(0) if rows > 1 else heads * d, v.data_ptr(), v.stride(0) if rows > 1 else heads * d, _ROWS[dtype],
+                                      _raw_stream(dev))
         if rc:
             _chk(rc, "csd_paged_read")
-        return out[0], out[1]
+        return k, v
 
     def attention(self, layer, table, row_start, cache_len, q, scale, max_rows=None, parent=None, out=None):
         """csd_paged_attention: q [rows][heads][head dim] -> out, contiguous and of q's type; rows of no sequence are left as they are
-        (undefined in a new tensor).
-        max_rows: at least the rows of the longest sequence of the batch (default: all rows of the call); parent: tree blocks."""
-        B, start, pos = self._call(table, row_start, cache_len)
-        rows, heads = q.shape[0], q.shape[1]
-        qp, qs, code = self._rows(q, rows, heads, "q")
+        (undefined in a new tensor).  max_rows: at least the rows of the longest sequence of the batch (default: all rows of the call);
+        parent: tree blocks."""
+        dev, i32, d = self._dev, torch.int32, self.head_dim
+        B, n = table.shape
+        rows, heads, width = q.shape
+        dtype, qs = q.dtype, q.stride()
+        if not (dev == table.get_device() == row_start.get_device() == cache_len.get_device() == q.get_device()
+                and i32 is table.dtype is row_start.dtype is cache_len.dtype and table.is_contiguous() and row_start.is_contiguous()
+                and cache_len.is_contiguous() and row_start.numel() == B + 1 and cache_len.numel() == B and dtype in _ROWS and width == d
+                and qs[1:] == (d, 1) and _current_device() == dev):
+            self._check(table=(table, B * n), row_start=(row_start, B + 1), cache_len=(cache_len, B), q=(q, (rows, heads, d)))
         if out is None:
-            out = torch.empty((rows, heads, self.head_dim), dtype=q.dtype, device=q.device)
+            out = torch.empty(rows, heads, d, dtype=dtype, device=self._device)
         else:
-            self._rows(out, rows, heads, "out", code)
+            self._check(q=(q, (rows, heads, d)), out=(out, (rows, heads, d)))
             if not out.is_contiguous():
                 raise ValueError("out: a contiguous tensor is required")
-        up = self._ints(parent, rows, "parent") if parent is not None else None
-        rc = lib().csd_paged_attention(self._ref, layer, start, pos, up, B, rows, rows or 1 if max_rows is None else max_rows, qp, qs, heads,
-                                       code, scale, out.data_ptr(), self._ws, _raw_stream(self._dev))
+        up = None
+        if parent is not None:
+            self._check(parent=(parent, rows))
+            up = parent.data_ptr()
+        pool = self._pool
+        pool.table, pool.table_stride = table.data_ptr(), n
+        rc = self._lib.csd_paged_attention(self._ref, layer, row_start.data_ptr(), cache_len.data_ptr(), up, B, rows,
+                                           (rows or 1) if max_rows is None else max_rows, q.data_ptr(), qs[0] if rows > 1 else heads * d, heads,
+                                           _ROWS[dtype], scale, out.data_ptr(), self._ws, _raw_stream(dev))
         if rc:
             _chk(rc, "csd_paged_attention")
         return out
 
     def commit(self, table, cache_len, path, n_accepted):
         """csd_paged_commit: the kept rows of a tree block, path[b][: n_accepted[b]], to positions cache_len[b] + 1 .., in all layers."""
-        B, _, pos = self._call(table, None, cache_len)
-        if path.ndim != 2:
-            raise ValueError("path: [B][rows of the tree]")
-        m = path.shape[1]
-        rc = lib().csd_paged_commit(self._ref, pos, self._ints(path, B * m, "path"), self._ints(n_accepted, B, "n_accepted"), B, m,
-                                    _raw_stream(self._dev))
+        dev, i32 = self._dev, torch.int32
+        B, n = table.shape
+        sequences, m = path.shape
+        if not (dev == table.get_device() == path.get_device() == cache_len.get_device() == n_accepted.get_device()
+                and i32 is table.dtype is path.dtype is cache_len.dtype is n_accepted.dtype and table.is_contiguous() and path.is_contiguous()
+                and cache_len.is_contiguous() and n_accepted.is_contiguous() and B == sequences == cache_len.numel() == n_accepted.numel()
+                and _current_device() == dev):
+            self._check(table=(table, B * n), cache_len=(cache_len, B), path=(path, B * m), n_accepted=(n_accepted, B))
+        pool = self._pool
+        pool.table, pool.table_stride = table.data_ptr(), n
+        rc = self._lib.csd_paged_commit(self._ref, cache_len.data_ptr(), path.data_ptr(), n_accepted.data_ptr(), B, m, _raw_stream(dev))
         if rc:
             _chk(rc, "csd_paged_commit")
 

@@ -6,7 +6,7 @@
 #include "csd_epilogue.h"
 #include "csd_internal.h"
 
-#define CSD_PAGED_COUNTER_BYTES 65536        /* the workspace begins with counters (zero between launches) */
+#define CSD_PAGED_COUNTER_BYTES CSD_PAGED_WORKSPACE_ZERO_BYTES      /* the workspace begins with counters, zero between launches */
 
 // The pool of one layer and the page table, by value in the kernels' arguments.
 struct PagedPool {

@@ -111,13 +111,14 @@ static void any_launch(const PagedAttn &a, hipStream_t st) {
 
 int32_t csd_paged_attention_enqueue(const PagedAttn &a, int32_t pool_dtype, int32_t q_dtype, hipStream_t st) {
     if (csd_paged_few_fits(a, pool_dtype, q_dtype)) {
-        // Sequences of few rows are bound by the cache's bytes, others by the products: a batch may hold both.
+        // Sequences of few rows are bound by the cache's bytes, others by the products.  A batch that may hold both takes both kernels, and
+        // the first one only for up to 16 rows (single tokens, mostly), where it has no second row tile to carry.
         const long long rows = (long long)a.max_rows * a.group;
         const bool many = rows > CSD_PAGED_FEW_ROWS;
         // (one sequence, or as many rows as B sequences of max_rows have: no sequence needs the other kernel)
         const bool few = !many || (a.r.B > 1 && a.r.rows < (long long)a.r.B * a.max_rows);
-        if (many) csd_paged_many_enqueue(a, few ? CSD_PAGED_FEW_ROWS : 0, pool_dtype, st);
-        if (few) csd_paged_few_enqueue(a, (int)(many ? CSD_PAGED_FEW_ROWS : rows), pool_dtype, st);
+        if (many) csd_paged_many_enqueue(a, few ? 16 : 0, pool_dtype, st);
+        if (few) csd_paged_few_enqueue(a, (int)(many ? 16 : rows), pool_dtype, st);
         CSD_LAUNCH_CHECK();
         return CSD_OK;
     }
