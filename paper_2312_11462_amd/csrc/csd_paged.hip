@@ -1,9 +1,7 @@
 // The paged KV cache: rows in (with quantisation), rows out, the commit of a tree's path, and the entry points' checks.
 //
 // All three move rows of D elements between dense rows and pages; they read and write each byte once and are bound by memory, or,
-// with few rows, by the chain row -> sequence -> page -> place of dependent reads.  A row of one head belongs to a group of W lanes
-// (W: the power of two from D / 8 up), eight elements per lane: the row's maximum stays inside the group, and groups that follow
-// one another are the heads of one row, whose dense elements are consecutive.
+// with few rows, by the chain row -> sequence -> page -> place of dependent reads.
 #include "csd_paged.h"
 
 static constexpr int kPagedThreads = 256;
@@ -39,98 +37,153 @@ __device__ __forceinline__ u32x2 quantise8(const float (&x)[8], int s) {
     return u32x2{c[0], c[1]};
 }
 
-// One lane's place in a move of rows: which row, head and eight elements, and where they are in the pool.
-struct RowPlace {
-    bool row_ok;      // the lane holds eight elements of a row of some sequence
-    int page;         // -1: a place without a row
-    int row, head, c; // c: first element / 8
-    size_t at;        // row index in the layer's pool
+// maximum over the 2^log_w neighbouring lanes of a row, in each of them (register moves up to sixteen lanes; a shuffle goes through LDS)
+template <int CTRL>
+__device__ __forceinline__ float max_dpp(float a) {
+    return fmaxf(a, __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(a), CTRL, 0xF, 0xF, false)));
+}
+__device__ __forceinline__ float row_max(float a, int log_w) {
+    if (log_w > 0) a = max_dpp<0xB1>(a);                     // lane ^ 1
+    if (log_w > 1) a = max_dpp<0x4E>(a);                     // lane ^ 2
+    if (log_w > 2) a = max_dpp<0x141>(a);                    // 7 - lane, of eight
+    if (log_w > 3) a = max_dpp<0x140>(a);                    // 15 - lane, of sixteen
+    if (log_w > 4) a = fmaxf(a, __shfl_xor(a, 16, 64));
+    return a;
+}
+
+// Eight elements of a dense row as they are in memory: bf16 one 16-byte piece, fp32 two.
+template <typename T> struct Raw8 {
+    u32x4 w[sizeof(T) / 2];
+    __device__ __forceinline__ void load(const T *p) {
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(T) / 2; i++) w[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(p) + i);
+    }
+    __device__ __forceinline__ void get(float (&x)[8]) const {
+#pragma unroll
+        for (int i = 0; i < 8; i++) {
+            if constexpr (sizeof(T) == 4) x[i] = __uint_as_float(w[i / 4][i % 4]);
+            else x[i] = __uint_as_float(i & 1 ? w[0][i / 2] & 0xFFFF0000u : w[0][i / 2] << 16);
+        }
+    }
 };
 
-// unit: index of the lane's group over (row, head); b: sequence of the wave's first row, moved on from there
-__device__ __forceinline__ RowPlace row_place(const PagedPool &p, const PagedRows &r, long long group, int c, int b) {
-    RowPlace o;
-    o.c = c;
-    o.row = (int)(group / p.Hkv);
-    o.head = (int)(group - (long long)o.row * p.Hkv);
-    o.row_ok = false;
-    o.page = -1;
-    o.at = 0;
-    if (o.row >= r.rows || c * 8 >= p.D) return o;
-    while (b < r.B && r.row_start[b + 1] <= o.row) b++;
-    if (b >= r.B) return o;
+// How the moves of rows are laid out.  A row of one head belongs to W lanes (W = 2^log_w: the power of two from D / 8 up), eight elements per lane, so its
+// maximum stays inside the lanes.  A wave takes 64 / W consecutive rows of U heads: in the pool consecutive rows of a head lie one behind
+// the other, their scale bytes too (with a wave on one row of 64 / W heads every scale byte was a store of its own: a prompt of 8198 rows of 32 heads of
+// 128 57 -> 46 us).  Everything that a lane loads is requested before anything is looked up or used.
+struct RowPlace {
+    bool ok;          // the lane holds eight elements of a row of some sequence
+    int page;         // -1: a place without a row
+    size_t at;        // row index in the layer's pool, of head 0
+};
+
+__device__ __forceinline__ RowPlace row_place(const PagedPool &p, const PagedRows &r, int first, int row, bool active, int log_w) {
+    const int lane = threadIdx.x & 63;
+    // the sequence of each row of the wave: how many sequences end at or before it (64 ends at a time; the sequences of a wave's rows are
+    // mostly the same)
+    int b = 0;
+    for (int b0 = 0; b0 < r.B; b0 += 64) {
+        const int end = b0 + lane < r.B ? r.row_start[b0 + lane + 1] : 0x7FFFFFFF;
+        const int before = __popcll(__ballot(end <= first));
+        b += before;
+        for (int j = 1; j < 64 >> log_w; j++) {              // rows that begin another sequence than the wave's first one
+            const int n = __popcll(__ballot(end <= first + j)) - before;
+            if (row - first == j) b += n;
+        }
+        if (__popcll(__ballot(end <= first + (64 >> log_w) - 1)) < 64) break;
+    }
+    RowPlace o{false, -1, 0};
+    if (!active || b >= r.B) return o;
     const PagedSeq s = paged_seq(r, b);
-    if (o.row < s.start) return o;
-    o.row_ok = true;
-    const int pos = s.t + (o.row - s.start);
+    if (row < s.start) return o;
+    o.ok = true;
+    const int pos = s.t + (row - s.start);
     o.page = paged_page(p, b, pos);
-    if (o.page >= 0) o.at = paged_row(p, o.page, o.head, pos);
+    if (o.page >= 0) o.at = paged_row(p, o.page, 0, pos);
     return o;
 }
 
-// TR: type of the dense rows, TP: of the pool (uint8_t: e4m3).
-template <typename TR, typename TP>
+// TR: type of the dense rows, TP: of the pool (uint8_t: e4m3), U: heads per wave.
+template <typename TR, typename TP, int U>
 __global__ __launch_bounds__(kPagedThreads) void k_paged_write(PagedPool p, PagedRows r, const TR *__restrict__ k, long long k_stride,
-                                                               const TR *__restrict__ v, long long v_stride, int log_w) {
-    const long long group = ((long long)blockIdx.x * kPagedThreads + threadIdx.x) >> log_w;
-    const long long first = ((long long)blockIdx.x * kPagedThreads + (threadIdx.x & ~63)) >> log_w;
-    const int first_row = (int)(first / p.Hkv);
-    if (first_row >= r.rows) return;
-    const int b = paged_find(r, first_row);
-    const RowPlace o = row_place(p, r, group, threadIdx.x & ((1 << log_w) - 1), b);
-    const bool live = o.row_ok && o.page >= 0;
+                                                               const TR *__restrict__ v, long long v_stride, int log_w, int head_blocks) {
+    const int wave = blockIdx.x * (kPagedThreads / 64) + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+    const int first = (wave / head_blocks) * (64 >> log_w), head0 = wave % head_blocks * U;
+    if (first >= r.rows) return;
+    const int row = first + (lane >> log_w), c = 8 * (lane & ((1 << log_w) - 1));
+    const bool active = row < r.rows && c < p.D;
+    Raw8<TR> raw[U][2];
 #pragma unroll
-    for (int side = 0; side < 2; side++) {
-        float x[8];
+    for (int u = 0; u < U; u++)
 #pragma unroll
-        for (int i = 0; i < 8; i++) x[i] = 0.f;
-        const size_t col = (size_t)o.head * p.D + o.c * 8;
-        if (live) load8<TR>((side ? v + o.row * v_stride : k + o.row * k_stride) + col, x);
-        TP *pool = reinterpret_cast<TP *>(side ? p.v : p.k);
-        if constexpr (sizeof(TP) == 1) {
-            float a = 0.f;
+        for (int side = 0; side < 2; side++) {
+            raw[u][side] = Raw8<TR>{};
+            if (active && head0 + u < p.Hkv) raw[u][side].load((side ? v + row * v_stride : k + row * k_stride) + (size_t)(head0 + u) * p.D + c);
+        }
+    const RowPlace o = row_place(p, r, first, row, active, log_w);
 #pragma unroll
-            for (int i = 0; i < 8; i++) {
-                const float f = fabsf(x[i]);
-                if (f < INFINITY) a = fmaxf(a, f);
+    for (int u = 0; u < U; u++) {
+        if (head0 + u >= p.Hkv) break;
+        const size_t at = o.at + ((size_t)(head0 + u) << p.page_shift);
+#pragma unroll
+        for (int side = 0; side < 2; side++) {
+            float x[8];
+            raw[u][side].get(x);
+            TP *to = reinterpret_cast<TP *>(side ? p.v : p.k) + at * p.D + c;
+            if constexpr (sizeof(TP) == 1) {
+                float a = 0.f;
+#pragma unroll
+                for (int i = 0; i < 8; i++) {
+                    const float f = fabsf(x[i]);
+                    a = f < INFINITY ? fmaxf(a, f) : a;
+                }
+                a = row_max(a, log_w);
+                const int s = scale_byte(a);
+                if (o.page >= 0) {
+                    *reinterpret_cast<u32x2 *>(to) = quantise8(x, s);
+                    if (c == 0) (side ? p.vs : p.ks)[at] = (uint8_t)s;
+                }
+            } else {
+                if (o.page >= 0) store8<TP>(to, x);
             }
-            for (int w = 1 << log_w >> 1; w > 0; w >>= 1) a = fmaxf(a, __shfl_xor(a, w, 64));
-            const int s = scale_byte(a);
-            if (live) {
-                *reinterpret_cast<u32x2 *>(pool + o.at * p.D + o.c * 8) = quantise8(x, s);
-                if (o.c == 0) (side ? p.vs : p.ks)[o.at] = (uint8_t)s;
-            }
-        } else {
-            if (live) store8<TP>(pool + o.at * p.D + o.c * 8, x);
         }
     }
 }
 
-template <typename TR, typename TP>
+template <typename TR, typename TP, int U>
 __global__ __launch_bounds__(kPagedThreads) void k_paged_read(PagedPool p, PagedRows r, TR *__restrict__ k, long long k_stride,
-                                                              TR *__restrict__ v, long long v_stride, int log_w) {
-    const long long group = ((long long)blockIdx.x * kPagedThreads + threadIdx.x) >> log_w;
-    const long long first = ((long long)blockIdx.x * kPagedThreads + (threadIdx.x & ~63)) >> log_w;
-    const int first_row = (int)(first / p.Hkv);
-    if (first_row >= r.rows) return;
-    const int b = paged_find(r, first_row);
-    const RowPlace o = row_place(p, r, group, threadIdx.x & ((1 << log_w) - 1), b);
-    if (!o.row_ok) return;
+                                                              TR *__restrict__ v, long long v_stride, int log_w, int head_blocks) {
+    const int wave = blockIdx.x * (kPagedThreads / 64) + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+    const int first = (wave / head_blocks) * (64 >> log_w), head0 = wave % head_blocks * U;
+    if (first >= r.rows) return;
+    const int row = first + (lane >> log_w), c = 8 * (lane & ((1 << log_w) - 1));
+    const RowPlace o = row_place(p, r, first, row, row < r.rows && c < p.D, log_w);
+    if (!o.ok) return;
+    float x[U][2][8], f[U][2];
 #pragma unroll
-    for (int side = 0; side < 2; side++) {
-        float x[8];
+    for (int u = 0; u < U; u++)
 #pragma unroll
-        for (int i = 0; i < 8; i++) x[i] = 0.f;
-        if (o.page >= 0) {
-            load8<TP>(reinterpret_cast<const TP *>(side ? p.v : p.k) + o.at * p.D + o.c * 8, x);
-            if constexpr (sizeof(TP) == 1) {
-                const float f = pow2_of_byte((side ? p.vs : p.ks)[o.at]);
+        for (int side = 0; side < 2; side++) {
 #pragma unroll
-                for (int i = 0; i < 8; i++) x[i] *= f;
+            for (int i = 0; i < 8; i++) x[u][side][i] = 0.f;
+            f[u][side] = 1.f;
+            if (o.page >= 0 && head0 + u < p.Hkv) {
+                const size_t at = o.at + ((size_t)(head0 + u) << p.page_shift);
+                load8<TP>(reinterpret_cast<const TP *>(side ? p.v : p.k) + at * p.D + c, x[u][side]);
+                if constexpr (sizeof(TP) == 1) f[u][side] = pow2_of_byte((side ? p.vs : p.ks)[at]);
             }
         }
-        store8<TR>((side ? v + o.row * v_stride : k + o.row * k_stride) + (size_t)o.head * p.D + o.c * 8, x);
-    }
+#pragma unroll
+    for (int u = 0; u < U; u++)
+#pragma unroll
+        for (int side = 0; side < 2; side++) {
+            if (head0 + u >= p.Hkv) break;
+            if constexpr (sizeof(TP) == 1) {
+#pragma unroll
+                for (int i = 0; i < 8; i++) x[u][side][i] *= f[u][side];
+            }
+            store8<TR>((side ? v + row * v_stride : k + row * k_stride) + (size_t)(head0 + u) * p.D + c, x[u][side]);
+        }
 }
 
 // The kept rows of a tree block to where a plain block would have put them.  A thread owns eight elements of one head of one
@@ -253,6 +306,23 @@ static void by_types(int32_t dense, int32_t pool, F f) {
     }
 }
 
+// Launches f for the types of a move of rows: four heads per wave where there are waves enough to fill the chip all the same, else one.
+template <typename F>
+static int32_t move_rows(const csd_paged_kv *kv, int32_t dtype, int32_t rows, F f) {
+    const int log_w = ilog2(kv->head_dim / 8), per_wave = 64 >> log_w;
+    const long long row_blocks = ((long long)rows + per_wave - 1) / per_wave;
+    const bool wide = row_blocks * kv->n_kv_heads >= 4 * 256 * 16;      // 16 waves per compute unit
+    const int head_blocks = wide ? (kv->n_kv_heads + 3) / 4 : kv->n_kv_heads;
+    const long long grid = (row_blocks * head_blocks + kPagedThreads / 64 - 1) / (kPagedThreads / 64);
+    if (grid > 0xFFFFFF) return CSD_ESHAPE;                  // (work items of a launch are counted in 32 bits)
+    by_types(dtype, kv->dtype, [&](auto *dense, auto *pool) {
+        if (wide) f(dense, pool, std::integral_constant<int, 4>{}, (unsigned)grid, log_w, head_blocks);
+        else f(dense, pool, std::integral_constant<int, 1>{}, (unsigned)grid, log_w, head_blocks);
+    });
+    CSD_LAUNCH_CHECK();
+    return CSD_OK;
+}
+
 extern "C" int32_t csd_paged_write(const csd_paged_kv *kv, int32_t layer, const int32_t *row_start, const int32_t *pos, int32_t B,
                                    int32_t rows, const void *k_rows, int64_t k_stride, const void *v_rows, int64_t v_stride,
                                    int32_t dtype, void *stream) {
@@ -263,18 +333,12 @@ extern "C" int32_t csd_paged_write(const csd_paged_kv *kv, int32_t layer, const 
     if (!row_stride_ok(kv, kv->n_kv_heads, k_stride, k_rows) || !row_stride_ok(kv, kv->n_kv_heads, v_stride, v_rows)) return CSD_EINVAL;
     const PagedPool p = csd_paged_layer(kv, layer);
     const PagedRows r{row_start, pos, B, rows};
-    const int log_w = ilog2(kv->head_dim / 8);
-    const long long threads = ((long long)rows * kv->n_kv_heads) << log_w;
-    const long long grid = (threads + kPagedThreads - 1) / kPagedThreads;
-    if (grid > 0xFFFFFF) return CSD_ESHAPE;                  // (work items of a launch are counted in 32 bits)
-    by_types(dtype, kv->dtype, [&](auto *dense, auto *pool) {
+    return move_rows(kv, dtype, rows, [&](auto *dense, auto *pool, auto u, unsigned grid, int log_w, int head_blocks) {
         using TR = std::remove_pointer_t<decltype(dense)>;
         using TP = std::remove_pointer_t<decltype(pool)>;
-        hipLaunchKernelGGL((k_paged_write<TR, TP>), dim3((unsigned)grid), dim3(kPagedThreads), 0, (hipStream_t)stream, p, r,
-                           (const TR *)k_rows, (long long)k_stride, (const TR *)v_rows, (long long)v_stride, log_w);
+        hipLaunchKernelGGL((k_paged_write<TR, TP, decltype(u)::value>), dim3(grid), dim3(kPagedThreads), 0, (hipStream_t)stream, p, r, (const TR *)k_rows,
+                           (long long)k_stride, (const TR *)v_rows, (long long)v_stride, log_w, head_blocks);
     });
-    CSD_LAUNCH_CHECK();
-    return CSD_OK;
 }
 
 extern "C" int32_t csd_paged_read(const csd_paged_kv *kv, int32_t layer, const int32_t *row_start, const int32_t *pos, int32_t B,
@@ -287,18 +351,12 @@ extern "C" int32_t csd_paged_read(const csd_paged_kv *kv, int32_t layer, const i
     if (!row_stride_ok(kv, kv->n_kv_heads, k_stride, k_rows) || !row_stride_ok(kv, kv->n_kv_heads, v_stride, v_rows)) return CSD_EINVAL;
     const PagedPool p = csd_paged_layer(kv, layer);
     const PagedRows r{row_start, pos, B, rows};
-    const int log_w = ilog2(kv->head_dim / 8);
-    const long long threads = ((long long)rows * kv->n_kv_heads) << log_w;
-    const long long grid = (threads + kPagedThreads - 1) / kPagedThreads;
-    if (grid > 0xFFFFFF) return CSD_ESHAPE;                  // (work items of a launch are counted in 32 bits)
-    by_types(dtype, kv->dtype, [&](auto *dense, auto *pool) {
+    return move_rows(kv, dtype, rows, [&](auto *dense, auto *pool, auto u, unsigned grid, int log_w, int head_blocks) {
         using TR = std::remove_pointer_t<decltype(dense)>;
         using TP = std::remove_pointer_t<decltype(pool)>;
-        hipLaunchKernelGGL((k_paged_read<TR, TP>), dim3((unsigned)grid), dim3(kPagedThreads), 0, (hipStream_t)stream, p, r,
-                           (TR *)k_rows, (long long)k_stride, (TR *)v_rows, (long long)v_stride, log_w);
+        hipLaunchKernelGGL((k_paged_read<TR, TP, decltype(u)::value>), dim3(grid), dim3(kPagedThreads), 0, (hipStream_t)stream, p, r, (TR *)k_rows,
+                           (long long)k_stride, (TR *)v_rows, (long long)v_stride, log_w, head_blocks);
     });
-    CSD_LAUNCH_CHECK();
-    return CSD_OK;
 }
 
 extern "C" int32_t csd_paged_commit(const csd_paged_kv *kv, const int32_t *cache_len, const int32_t *path, const int32_t *n_accepted,
