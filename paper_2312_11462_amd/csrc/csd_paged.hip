@@ -70,7 +70,7 @@ template <typename T> struct Raw8 {
 // How the moves of rows are laid out.  A row of one head belongs to W lanes (W = 2^log_w: the power of two from D / 8 up), eight elements per lane, so its
 // maximum stays inside the lanes.  A wave takes 64 / W consecutive rows of U heads: in the pool consecutive rows of a head lie one behind
 // the other, their scale bytes too (with a wave on one row of 64 / W heads every scale byte was a store of its own: a prompt of 8198 rows of 32 heads of
-// 128 57 -> 46 us).  Everything that a lane loads is requested before anything is looked up or used.
+// 128 56 -> 45 us).  Everything that a lane loads is requested before anything is looked up or used.
 struct RowPlace {
     bool ok;          // the lane holds eight elements of a row of some sequence
     int page;         // -1: a place without a row
