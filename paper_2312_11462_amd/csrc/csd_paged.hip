@@ -67,6 +67,16 @@ template <typename T> struct Raw8 {
     }
 };
 
+// Stores past the caches, for many dense rows: they are more than a cache level holds, and kept there they push out the pages still to be read (8198
+// rows of 32 heads of 128, e4m3 to bf16: 57 -> 34 us; with the loads of the pages past them too 52).
+template <typename T>
+__device__ __forceinline__ void store8_past(T *p, const float (&x)[8]) {
+    alignas(16) T t[8];
+    store8<T>(t, x);
+#pragma unroll
+    for (int i = 0; i < (int)sizeof(T) / 2; i++) __builtin_nontemporal_store(reinterpret_cast<u32x4 *>(t)[i], reinterpret_cast<u32x4 *>(p) + i);
+}
+
 // How the moves of rows are laid out.  A row of one head belongs to W lanes (W = 2^log_w: the power of two from D / 8 up), eight elements per lane, so its
 // maximum stays inside the lanes.  A wave takes 64 / W consecutive rows of U heads: in the pool consecutive rows of a head lie one behind
 // the other, their scale bytes too (with a wave on one row of 64 / W heads every scale byte was a store of its own: a prompt of 8198 rows of 32 heads of
@@ -182,7 +192,9 @@ __global__ __launch_bounds__(kPagedThreads) void k_paged_read(PagedPool p, Paged
 #pragma unroll
                 for (int i = 0; i < 8; i++) x[u][side][i] *= f[u][side];
             }
-            store8<TR>((side ? v + row * v_stride : k + row * k_stride) + (size_t)(head0 + u) * p.D + c, x[u][side]);
+            TR *to = (side ? v + row * v_stride : k + row * k_stride) + (size_t)(head0 + u) * p.D + c;
+            if constexpr (U > 1) store8_past<TR>(to, x[u][side]);
+            else store8<TR>(to, x[u][side]);
         }
 }
 
