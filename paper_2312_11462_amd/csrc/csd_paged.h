@@ -220,6 +220,7 @@ int32_t csd_paged_attention_enqueue(const PagedAttn &a, int32_t pool_dtype, int3
 // csd_paged_few.hip: sequences of up to 32 rows per key-value head.
 #define CSD_PAGED_FEW_GRID 512       /* two workgroups per compute unit */
 #define CSD_PAGED_FEW_SHARE 4        /* tiles of 32 keys per workgroup at least */
+#define CSD_PAGED_FEW_COST 8         /* what an item costs besides its keys, in such tiles */
 #define CSD_PAGED_FEW_PARTS 64       /* parts of an item at most */
 #define CSD_PAGED_FEW_ROWS 32
 static_assert(CSD_PAGED_COUNTER_BYTES + 2ull * CSD_PAGED_FEW_GRID * CSD_PAGED_FEW_ROWS * 132 * 4 <= CSD_PAGED_WORKSPACE_BYTES, "");

@@ -4,8 +4,9 @@
 // Every cached row is read once and takes part in few products, so the cache's bytes bound this: what matters is that all compute units
 // read all the time.  The tiles of 32 keys of all sequences and key-value heads are counted through, and every workgroup takes an
 // equal, contiguous share of them (sequences of very different length share the chip evenly, and nobody outside the device has to know the
-// lengths).  A share ends inside an item (sequence, key-value head) in general; the parts of such an item are joined by the workgroup
-// that finishes last.
+// lengths).  An item (sequence, key-value head) counts CSD_PAGED_FEW_COST tiles more than it has, for the trips to memory before its first key and behind
+// its last (5 rows of 16 ragged sequences, 8 heads of 128, e4m3: 112 us without, 104 for 4 tiles, 102 for 8 and for 12).  A share ends inside an
+// item in general; the parts of such an item are joined by the workgroup that finishes last.
 //
 // The four waves of a workgroup take the tiles of its share in turn.  Both
 // products are transposed so that nothing passes through LDS:
@@ -15,7 +16,8 @@
 //                  eight keys (a row of V is read by 16 neighbouring lanes) and transposes them in registers by byte permutations; A-row i of
 //                  product j is then feature DH / 16 * i + j.
 // e4m3 keys and values become bf16 without loss; the keys' scales multiply the scores, the values' scales the weights (powers of
-// two: exact).  Weights enter the second product as two bf16 planes (w = hi + lo, 16 bits): the matrix cores have time to spare here.
+// two: exact).  Up to 16 rows the weights enter the second product as two bf16 planes (w = hi + lo, 16 bits): the matrix cores have time to
+// spare there.  With 32 rows they enter as one (half a step: 2^-8 of a weight, random in sign; their sum is kept in fp32).
 #include "csd_paged.h"
 
 static constexpr int kFewPages = 1024;      // entries of the page table held in LDS at a time
@@ -86,7 +88,7 @@ __global__ __launch_bounds__(256, 2) void k_paged_attn_few(PagedAttn a) {
     constexpr int F = DH / 16, R = 16 * RT;
     constexpr bool LO = RT == 1;
     constexpr int NB = (F8 && (RT == 1 || DH == 64) ? 2 : 1) + (DH == 64 ? 1 : 0);     // tiles in flight per wave, as registers allow
-    constexpr int ES = F8 ? 1 : 2, kGrid = CSD_PAGED_FEW_GRID;
+    constexpr int ES = F8 ? 1 : 2, kGrid = CSD_PAGED_FEW_GRID, kCost = CSD_PAGED_FEW_COST;
     __shared__ int s_pages[kFewPages];
     __shared__ __align__(16) float s_o[4][R][DH + 4];
     __shared__ float s_m[4][R], s_l[4][R];
@@ -97,15 +99,17 @@ __global__ __launch_bounds__(256, 2) void k_paged_attn_few(PagedAttn a) {
     const PagedPool &p = a.p;
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, col = lane & 15, g = lane >> 4;
     const int cap = p.table_stride << p.page_shift;
+    const float per_group = 1.f / (float)a.group;
+    auto token_of = [&](int r) { return (int)(((float)r + 0.5f) * per_group); };     // r / group, r < 32: at least 1 / 64 from the next whole number
 
-    // ---- the tiles of every sequence
+    // ---- the tiles of every sequence, counted from what an item costs besides them
     auto seq_of = [&](int b, PagedSeq &s) -> int {
         s = PagedSeq{0, 0, 0};
         if (b >= a.r.B) return 0;
         s = paged_seq(a.r, b);
         s.m = min(s.m, a.max_rows);
         const int rows = s.m * a.group;
-        return rows >= 1 && rows <= R ? (min(s.t + s.m, cap) + 31) >> 5 : 0;
+        return rows >= 1 && rows <= R ? kCost + ((min(s.t + s.m, cap) + 31) >> 5) : 0;
     };
     PagedSeq s0;
     const int n0 = seq_of(lane, s0);                         // the first 64 sequences stay in registers
@@ -133,6 +137,7 @@ __global__ __launch_bounds__(256, 2) void k_paged_attn_few(PagedAttn a) {
 
     for (int u = shares.first(blockIdx.x); u < u_end;) {
         // ---- the item of tile u: sequence b, key-value head kvh, tiles t0 .. t1 of its n
+        const int u0 = u;
         int b = 0, n = 0, before = 0;
         PagedSeq seq{0, 0, 0};
         for (int b0 = 0; b0 < a.r.B; b0 += 64) {
@@ -156,12 +161,15 @@ __global__ __launch_bounds__(256, 2) void k_paged_attn_few(PagedAttn a) {
             before += __builtin_amdgcn_readlane(incl, 63);
         }
         if (n == 0) return;                                  // (the lengths changed while they were read)
-        const int kvh = (u - before) / n, t0 = u - before - kvh * n;
-        const int item = u - t0, t1 = min(n, t0 + u_end - u);
+        const int kvh = (u - before) / n, item = before + kvh * n + kCost;     // (where its tiles begin)
+        u = min(item - kCost + n, u_end);
+        n -= kCost;
+        const int t0 = max(u0 - item, 0), t1 = u - item;
+        if (t0 >= t1) continue;                              // (the share ends before the item's tiles begin)
         const int len = min(seq.t + seq.m, cap), rows = seq.m * a.group;
-        u += t1 - t0;
 
-        // ---- queries: row r = token r / group, head r % group of the group
+        // ---- the first pages and the queries are requested together; row r = token r / group, head r % group of the group
+        const int first_page = paged_page(p, b, ((((t0 * 32) >> p.page_shift) + tid)) << p.page_shift);
         u32x4 qf[RT == 1 ? DH / 32 : 1];                      // (two row tiles: in LDS, where the waves' results will be; the registers are needed)
         u32x4 *s_q = reinterpret_cast<u32x4 *>(&s_o[0][0][0]) + lane;
         const uint32_t flip = a.scale < 0.f ? 0x80008000u : 0u;
@@ -182,7 +190,7 @@ __global__ __launch_bounds__(256, 2) void k_paged_attn_few(PagedAttn a) {
         }
 #pragma unroll
         for (int rt = 0; rt < RT; rt++) {
-            const int r = rt * 16 + col, i = r / a.group, h = r - i * a.group;
+            const int r = rt * 16 + col, i = token_of(r), h = r - i * a.group;
             unsigned long long above = 0;
             if (a.parent) {
                 const int src = min(i, 63);
@@ -192,14 +200,13 @@ __global__ __launch_bounds__(256, 2) void k_paged_attn_few(PagedAttn a) {
                 s_limit[r] = seq.t + i;
                 s_above[r] = above;
             }
-            const bf16_t *q = reinterpret_cast<const bf16_t *>(a.q) + (size_t)(seq.start + i) * a.q_stride + (size_t)(kvh * a.group + h) * DH;
+            const bf16_t *q = reinterpret_cast<const bf16_t *>(a.q) + (size_t)(seq.start + min(i, seq.m - 1)) * a.q_stride + (size_t)(kvh * a.group + h) * DH;
 #pragma unroll
             for (int s = 0; s < DH / 32; s++) {
-                u32x4 x = u32x4{0u, 0u, 0u, 0u};
                 const int at = F8 ? 64 * (s / 2) + 16 * g + 8 * (s & 1) : 32 * s + 8 * g;      // features of the K operand's step s
-                if (r < rows) x = *reinterpret_cast<const u32x4 *>(q + at);
+                u32x4 x = *reinterpret_cast<const u32x4 *>(q + at);
 #pragma unroll
-                for (int w = 0; w < 4; w++) x[w] ^= flip;
+                for (int w = 0; w < 4; w++) x[w] = r < rows ? x[w] ^ flip : 0u;
                 if constexpr (RT == 1) qf[s] = x;
                 else if (wave == 0) s_q[(rt * (DH / 32) + s) * 64] = x;
             }
@@ -225,7 +232,12 @@ __global__ __launch_bounds__(256, 2) void k_paged_attn_few(PagedAttn a) {
             const int c1 = fits >= t1 ? t1 : t0 + (((int)fits - t0) & ~3);      // (a wave keeps its turn from piece to piece)
             const int n_pages = (((c1 * 32 - 1) >> p.page_shift) - page0) + 1;
             __syncthreads();
-            for (int i = tid; i < n_pages; i += 256) s_pages[i] = paged_page(p, b, (page0 + i) << p.page_shift);
+            if (c0 == t0) {
+                if (tid < n_pages) s_pages[tid] = first_page;
+                for (int i = tid + 256; i < n_pages; i += 256) s_pages[i] = paged_page(p, b, (page0 + i) << p.page_shift);
+            } else {
+                for (int i = tid; i < n_pages; i += 256) s_pages[i] = paged_page(p, b, (page0 + i) << p.page_shift);
+            }
             __syncthreads();
             // The queries have come too (before the table's entries, in order); said here, as otherwise the first product below waits for them, and
             // with them for every load in flight, at every turn.
@@ -444,7 +456,7 @@ __global__ __launch_bounds__(256, 2) void k_paged_attn_few(PagedAttn a) {
         const bool split = w_first != w_last;
         const PagedParts<DH, R> parts(a.ws, CSD_PAGED_FEW_GRID, w_first, w_last - w_first + 1);
         auto out_row = [&](int r) {
-            const int i = r / a.group, h = r - i * a.group;
+            const int i = token_of(r), h = r - i * a.group;
             return reinterpret_cast<bf16_t *>(a.out) + (((size_t)(seq.start + i) * p.Hkv + kvh) * a.group + h) * DH;
         };
         for (int x = tid; x < rows * (DH / 4); x += 256) {
@@ -490,7 +502,7 @@ bool csd_paged_few_fits(const PagedAttn &a, int32_t pool_dtype, int32_t q_dtype)
     if (q_dtype != CSD_DTYPE_BF16 || pool_dtype == CSD_DTYPE_FP32 || (a.p.D != 64 && a.p.D != 128)) return false;
     // tiles are counted in 32 bits, and so are the work items of a launch
     const long long tiles = (((long long)a.p.table_stride << a.p.page_shift) + 31) / 32, heads = (long long)a.p.Hkv * a.group;
-    return tiles * a.p.Hkv * a.r.B < (1ll << 30) && (long long)a.r.rows * heads / 128 + (long long)a.r.B * a.p.Hkv < (1ll << 24);
+    return (tiles + CSD_PAGED_FEW_COST) * a.p.Hkv * a.r.B < (1ll << 30) && (long long)a.r.rows * heads / 128 + (long long)a.r.B * a.p.Hkv < (1ll << 24);
 }
 
 void csd_paged_few_enqueue(const PagedAttn &a, int rows, int32_t pool_dtype, hipStream_t st) {
