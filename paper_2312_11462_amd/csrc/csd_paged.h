@@ -167,19 +167,28 @@ struct PagedParts {
         return *flag != 0;
     }
     // The last one joins the parts, in their order: out = sum f_k o_k / sum f_k l_k with f_k = 2^(m_k - max m).  lds: (2 * parts + 1) * R floats.  `out` of a row:
-    // 256 threads, four features each; the first parts' outputs are requested along with the maxima.
+    // 256 threads, four features each.  P such places of a thread and K parts are requested at once, the first of them along with the maxima:
+    // each round of requests is a trip to memory.
     template <typename OUT>
     __device__ __forceinline__ void join(void *ws, float *lds, int rows, OUT out) const {
-        const int tid = threadIdx.x;
+        int tid = threadIdx.x;
+        asm volatile("" : "+v"(tid));                        // (what follows from it is made here, not kept in registers from the kernel's start on)
         float *fade = lds, *sum = lds + parts * R, *inv = lds + 2 * parts * R;
-        constexpr int C = DH / 4;
-        f32x4 v[4];
-        auto request = [&](int x, int k0) {
+        constexpr int C = DH / 4, P = R * C / 256 < 1 ? 1 : R * C / 256 > 4 ? 4 : R * C / 256, K = 4;
+        f32x4 v[P][K];
+        auto request = [&](int x0, int k0) {
+            const int voff = ((x0 + tid) / C * part_stride<DH>() + 4 * (tid % C)) * 4;
 #pragma unroll
-            for (int k = 0; k < 4; k++)
-                if (k0 + k < parts && x < rows * C) v[k] = load(k0 + k, x / C, 4 * (x % C));
+            for (int k = 0; k < K; k++) {
+                if (k0 + k >= parts) break;
+                const int soff = __builtin_amdgcn_readfirstlane(at(k0 + k, 0, 0));
+#pragma unroll
+                for (int i = 0; i < P; i++)
+                    if (x0 + 256 * i + tid < rows * C)
+                        v[i][k] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(r, voff, soff + i * (256 / C) * part_stride<DH>() * 4, CH_SC1));
+            }
         };
-        request(tid, 0);
+        request(0, 0);
         for (int x = tid; x < parts * rows; x += 256) {
             const int k = x / rows, row = x - k * rows;
             const f32x4 ml = load(k, row, DH);
@@ -199,17 +208,28 @@ struct PagedParts {
             inv[tid] = m == -INFINITY ? -1.f : 1.f / l;      // (-1: the row has nothing to attend)
         }
         __syncthreads();
-        for (int x = tid; x < rows * C; x += 256) {
-            const int row = x / C, c = 4 * (x % C);
-            f32x4 o = f32x4{0.f, 0.f, 0.f, 0.f};
-            for (int k0 = 0; k0 < parts; k0 += 4) {
-                if (x != tid || k0 != 0) request(x, k0);
+        for (int x0 = 0; x0 < rows * C; x0 += 256 * P) {
+            f32x4 o[P];
 #pragma unroll
-                for (int k = 0; k < 4; k++)
-                    if (k0 + k < parts) o += v[k] * fade[(k0 + k) * R + row];
+            for (int i = 0; i < P; i++) o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+            const int row0 = (x0 + tid) / C;
+            for (int k0 = 0; k0 < parts; k0 += K) {
+                if (x0 + k0 > 0) request(x0, k0);
+#pragma unroll
+                for (int k = 0; k < K; k++) {
+                    if (k0 + k >= parts) break;
+#pragma unroll
+                    for (int i = 0; i < P; i++) o[i] += v[i][k] * fade[(k0 + k) * R + min(row0 + i * (256 / C), R - 1)];
+                }
             }
-            const float f = inv[row];
-            *reinterpret_cast<u32x2 *>(out(row) + c) = f == -1.f ? u32x2{0u, 0u} : u32x2{pack_bf16x2(o[0] * f, o[1] * f), pack_bf16x2(o[2] * f, o[3] * f)};
+#pragma unroll
+            for (int i = 0; i < P; i++) {
+                if (x0 + 256 * i + tid >= rows * C) continue;
+                const int row = row0 + i * (256 / C), c = 4 * (tid % C);
+                const float f = inv[row];
+                *reinterpret_cast<u32x2 *>(out(row) + c) =
+                    f == -1.f ? u32x2{0u, 0u} : u32x2{pack_bf16x2(o[i][0] * f, o[i][1] * f), pack_bf16x2(o[i][2] * f, o[i][3] * f)};
+            }
         }
         if (tid == 0) __hip_atomic_store(reinterpret_cast<unsigned *>(ws) + w_first, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);   // ready for the next launch
     }

@@ -56,7 +56,9 @@ __global__ __launch_bounds__(256, 2) void k_paged_attn_many(PagedAttn a, int min
     constexpr int ST = DH / 16, DT = DH / 32, BM = CSD_PAGED_MANY_ROWS, PARTS = CSD_PAGED_MANY_PARTS;
     // what an item costs besides its keys, in tiles: the round trips to memory in front of its first tile and behind its last one
     constexpr int COST = CSD_PAGED_MANY_COST;
-    __shared__ u32x4 s_k[2][PIECES], s_v[2][PIECES];
+    __shared__ u32x4 s_tiles[4][PIECES];
+    u32x4(&s_k)[2][PIECES] = *reinterpret_cast<u32x4(*)[2][PIECES]>(&s_tiles[0]), (&s_v)[2][PIECES] = *reinterpret_cast<u32x4(*)[2][PIECES]>(&s_tiles[2]);
+    __shared__ float s_max[BM], s_sum[BM];
     __shared__ int s_odd, s_last;
     __shared__ int s_start[SHARED ? CSD_PAGED_MANY_BATCH : 1], s_m[SHARED ? CSD_PAGED_MANY_BATCH : 1], s_t[SHARED ? CSD_PAGED_MANY_BATCH : 1], s_units[SHARED ? CSD_PAGED_MANY_BATCH : 1];
     const PagedPool &p = a.p;
@@ -91,13 +93,13 @@ __global__ __launch_bounds__(256, 2) void k_paged_attn_many(PagedAttn a, int min
             s_start[b] = s.start;
         }
         __syncthreads();
-        for (int b = wave; b < a.r.B; b += 4) {
+        for (int b = tid / 8; b < a.r.B; b += 32) {          // eight lanes per sequence
             const int m = s_m[b], t = s_t[b], n = (m * a.group + BM - 1) / BM;
             int sum = 0;
-            for (int rt = lane; rt < n; rt += 64) sum += COST + row_tile_keys(rt, m, t, a.group, cap);
+            for (int rt = tid % 8; rt < n; rt += 8) sum += COST + row_tile_keys(rt, m, t, a.group, cap);
 #pragma unroll
-            for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o, 64);
-            if (lane == 0) s_units[b] = sum;
+            for (int o = 4; o > 0; o >>= 1) sum += __shfl_xor(sum, o, 64);
+            if (tid % 8 == 0) s_units[b] = sum;
         }
         __syncthreads();
         int sum = 0, longest = 0;
@@ -505,40 +507,58 @@ __global__ __launch_bounds__(256, 2) void k_paged_attn_many(PagedAttn a, int min
         }
     }
 
-    // ---- results: element e of acc[d] is feature 32 d + 8 (e / 4) + 4 h + e % 4 of the lane's row
-    const size_t out_row = ((size_t)(seq.start + i) * p.Hkv + kvh) * a.group + hq;
+    // ---- results: element e of acc[d] is feature 32 d + 8 (e / 4) + 4 h + e % 4 of the lane's row.  Turned in LDS, where the key tiles were (16-byte pieces,
+    // their index xored by the row), so that whole rows are written one behind the other (with the join by 4 x 4 pieces, against 16-byte stores from here and
+    // a join by fours: a tree of 41 rows over 1024 keys, 32 heads of 128, 23.9 -> 21.5 us).
+    constexpr int C = DH / 4;
+    auto piece = [&](int row, int c) { return row * C + (c ^ (row & (C - 1))); };
+    u32x4 *s_o = &s_tiles[0][0];
+    {
+        int row = wave * 32 + col;
+        asm volatile("" : "+v"(row));
+#pragma unroll
+        for (int d = 0; d < DT; d++)
+#pragma unroll
+            for (int y = 0; y < 4; y++)
+                s_o[piece(row, 8 * d + 2 * y + h)] = __builtin_bit_cast(u32x4, f32x4{acc[d][4 * y], acc[d][4 * y + 1], acc[d][4 * y + 2], acc[d][4 * y + 3]});
+        if (h == 0) {
+            s_max[row] = m_run;
+            s_sum[row] = l_run;
+        }
+    }
+    __syncthreads();
+    int id = tid;
+    asm volatile("" : "+v"(id));                             // (what follows from it is made here, not kept in registers all along)
+    auto out_row = [&](int row) {
+        const int r_ = rt * BM + row, i_ = r_ / a.group, h_ = r_ - i_ * a.group;
+        return reinterpret_cast<bf16_t *>(a.out) + (((size_t)(seq.start + i_) * p.Hkv + kvh) * a.group + h_) * DH;
+    };
     const int w_first = SHARED ? shares.owner(item) : 0, w_last = SHARED ? shares.owner(item + n_kt - 1) : 0, parts = w_last - w_first + 1;
     if (parts == 1) {
-        if (live) {
-            const float inv = 1.f / l_run;
+        for (int x = id; x < rows * (C / 2); x += 256) {
+            const int row = x / (C / 2), c = x % (C / 2);
+            const float inv = 1.f / s_sum[row];
+            u32x4 o;
 #pragma unroll
-            for (int d = 0; d < DT; d++)
-#pragma unroll
-                for (int y = 0; y < 4; y++) {
-                    u32x2 o = u32x2{pack_bf16x2(acc[d][4 * y] * inv, acc[d][4 * y + 1] * inv), pack_bf16x2(acc[d][4 * y + 2] * inv, acc[d][4 * y + 3] * inv)};
-                    if (m_run == -INFINITY) o = u32x2{0u, 0u};
-                    *reinterpret_cast<u32x2 *>(reinterpret_cast<bf16_t *>(a.out) + out_row * DH + 32 * d + 8 * y + 4 * h) = o;
-                }
+            for (int y = 0; y < 2; y++) {
+                const f32x4 v = __builtin_bit_cast(f32x4, s_o[piece(row, 2 * c + y)]) * inv;
+                o[2 * y] = pack_bf16x2(v[0], v[1]);
+                o[2 * y + 1] = pack_bf16x2(v[2], v[3]);
+            }
+            if (s_max[row] == -INFINITY) o = u32x4{0u, 0u, 0u, 0u};
+            *reinterpret_cast<u32x4 *>(out_row(row) + 8 * c) = o;
         }
         __syncthreads();
         continue;
     }
     const PagedParts<DH, BM> split(a.ws, CSD_PAGED_MANY_GRID, w_first, parts);
-    if (live) {
-        const int row = wave * 32 + col;
-#pragma unroll
-        for (int d = 0; d < DT; d++)
-#pragma unroll
-            for (int y = 0; y < 4; y++)
-                split.store(me - w_first, row, 32 * d + 8 * y + 4 * h, f32x4{acc[d][4 * y], acc[d][4 * y + 1], acc[d][4 * y + 2], acc[d][4 * y + 3]});
-        if (h == 0) split.store(me - w_first, row, DH, f32x4{m_run, l_run, 0.f, 0.f});
+    for (int x = id; x < rows * (C + 1); x += 256) {
+        const int row = x / (C + 1), c = x % (C + 1);
+        split.store(me - w_first, row, 4 * c, c < C ? __builtin_bit_cast(f32x4, s_o[piece(row, c)]) : f32x4{s_max[row], s_sum[row], 0.f, 0.f});
     }
     if (!split.arrive(a.ws, &s_last)) continue;
-    static_assert((2 * CSD_PAGED_MANY_PARTS + 1) * BM * 4 <= 2 * PIECES * 16, "");
-    split.join(a.ws, reinterpret_cast<float *>(&s_k[0][0]), rows, [&](int row) {
-        const int r_ = rt * BM + row, i_ = r_ / a.group, h_ = r_ - i_ * a.group;
-        return reinterpret_cast<bf16_t *>(a.out) + (((size_t)(seq.start + i_) * p.Hkv + kvh) * a.group + h_) * DH;
-    });
+    static_assert((2 * PARTS + 1) * BM * 4 <= 4 * PIECES * 16 && BM * C <= 4 * PIECES, "");
+    split.join(a.ws, reinterpret_cast<float *>(s_o), rows, out_row);
     __syncthreads();
     }
 }
