@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import threading
 
 import torch
 
@@ -276,7 +277,7 @@ class PagedKv:
         self.n_layers, self.n_pages, self.n_kv_heads, self.page_rows, self.head_dim = k.shape
         self._pool = PagedPool(self.n_layers, self.n_pages, self.page_rows, self.n_kv_heads, self.head_dim, types[k.dtype],
                                _ptr(k).value, _ptr(v).value, _ptr(k_scale, torch.uint8).value, _ptr(v_scale, torch.uint8).value, None, 0)
-        self._ref, self._lib, self._device = C.addressof(self._pool), lib(), k.device
+        self._threads, self._lib, self._device = threading.local(), lib(), k.device
         if workspace is None:
             self._check()
             workspace = torch.empty(PAGED_WORKSPACE_BYTES, dtype=torch.uint8, device=k.device)
@@ -286,6 +287,15 @@ class PagedKv:
             raise ValueError(f"workspace: {PAGED_WORKSPACE_BYTES} bytes, the first {PAGED_WORKSPACE_ZERO_BYTES} of them zeroed")
         self.workspace = workspace
         self._ws = _ptr(workspace).value
+
+    def _mine(self):
+        """The call's description of the cache, whose page table a call sets: one per thread."""
+        try:
+            return self._threads.mine
+        except AttributeError:
+            pool = PagedPool.from_buffer_copy(self._pool)
+            self._threads.mine = pool, C.addressof(pool)
+            return self._threads.mine
 
     def _check(self, **tensors):
         """Raises for what is wrong with a call's tensors.  The methods look at everything in one expression and come here only if it does not hold
@@ -320,9 +330,9 @@ class PagedKv:
                 and v_rows.dtype is dtype and (rows, heads, d) == shape == v_rows.shape and (d, 1) == ks[1:] == vs[1:] and _current_device() == dev):
             self._check(table=(table, B * n), row_start=(row_start, B + 1), cache_len=(cache_len, B), k_rows=(k_rows, (rows, heads, d)),
                         v_rows=(v_rows, (rows, heads, d)))
-        pool = self._pool
+        pool, ref = self._mine()
         pool.table, pool.table_stride = table.data_ptr(), n
-        rc = self._lib.csd_paged_write(self._ref, layer, row_start.data_ptr(), cache_len.data_ptr(), B, rows, k_rows.data_ptr(),
+        rc = self._lib.csd_paged_write(ref, layer, row_start.data_ptr(), cache_len.data_ptr(), B, rows, k_rows.data_ptr(),
                                        ks[0] if rows > 1 else heads * d, v_rows.data_ptr(), vs[0] if rows > 1 else heads * d, _ROWS[dtype],
                                        _raw_stream(dev))
         if rc:
@@ -346,9 +356,9 @@ class PagedKv:
                 and i32 is table.dtype is row_start.dtype is cache_len.dtype and table.is_contiguous() and row_start.is_contiguous()
                 and cache_len.is_contiguous() and row_start.numel() == B + 1 and cache_len.numel() == B and _current_device() == dev):
             self._check(table=(table, B * n), row_start=(row_start, B + 1), cache_len=(cache_len, B), k=(k, (rows, heads, d)), v=(v, (rows, heads, d)))
-        pool = self._pool
+        pool, ref = self._mine()
         pool.table, pool.table_stride = table.data_ptr(), n
-        rc = self._lib.csd_paged_read(self._ref, layer, row_start.data_ptr(), cache_len.data_ptr(), B, rows, k.data_ptr(),
+        rc = self._lib.csd_paged_read(ref, layer, row_start.data_ptr(), cache_len.data_ptr(), B, rows, k.data_ptr(),
                                       k.stride(0) if rows > 1 else heads * d, v.data_ptr(), v.stride(0) if rows > 1 else heads * d, _ROWS[dtype],
                                       _raw_stream(dev))
         if rc:
@@ -378,9 +388,9 @@ class PagedKv:
         if parent is not None:
             self._check(parent=(parent, rows))
             up = parent.data_ptr()
-        pool = self._pool
+        pool, ref = self._mine()
         pool.table, pool.table_stride = table.data_ptr(), n
-        rc = self._lib.csd_paged_attention(self._ref, layer, row_start.data_ptr(), cache_len.data_ptr(), up, B, rows,
+        rc = self._lib.csd_paged_attention(ref, layer, row_start.data_ptr(), cache_len.data_ptr(), up, B, rows,
                                            (rows or 1) if max_rows is None else max_rows, q.data_ptr(), qs[0] if rows > 1 else heads * d, heads,
                                            _ROWS[dtype], scale, out.data_ptr(), self._ws, _raw_stream(dev))
         if rc:
@@ -397,9 +407,9 @@ class PagedKv:
                 and cache_len.is_contiguous() and n_accepted.is_contiguous() and B == sequences == cache_len.numel() == n_accepted.numel()
                 and _current_device() == dev):
             self._check(table=(table, B * n), cache_len=(cache_len, B), path=(path, B * m), n_accepted=(n_accepted, B))
-        pool = self._pool
+        pool, ref = self._mine()
         pool.table, pool.table_stride = table.data_ptr(), n
-        rc = self._lib.csd_paged_commit(self._ref, cache_len.data_ptr(), path.data_ptr(), n_accepted.data_ptr(), B, m, _raw_stream(dev))
+        rc = self._lib.csd_paged_commit(ref, cache_len.data_ptr(), path.data_ptr(), n_accepted.data_ptr(), B, m, _raw_stream(dev))
         if rc:
             _chk(rc, "csd_paged_commit")
 

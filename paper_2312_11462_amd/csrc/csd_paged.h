@@ -32,19 +32,6 @@ __device__ __forceinline__ PagedSeq paged_seq(const PagedRows &r, int b) {
     return PagedSeq{s, e - s, min(max(r.pos[b], 0), 0x3FFFFFFF)};
 }
 
-// The sequence of a row (uniform in the wave): how many sequences end at or before it.  64 ends are looked at at once; B if there is none.
-__device__ __forceinline__ int paged_find(const PagedRows &r, int row) {
-    const int lane = threadIdx.x & 63;
-    int b = 0;
-    for (int b0 = 0; b0 < r.B; b0 += 64) {
-        const bool ends = b0 + lane < r.B && r.row_start[b0 + lane + 1] <= row;
-        const int n = __popcll(__ballot(ends));
-        b += n;
-        if (n < 64) break;
-    }
-    return b;
-}
-
 // page of a position, -1: there is none
 __device__ __forceinline__ int paged_page(const PagedPool &p, int b, int pos) {
     const int i = pos >> p.page_shift;

@@ -334,9 +334,10 @@ __global__ __launch_bounds__(256, 2) void k_paged_attn_few(PagedAttn a) {
                     float top = fmaxf(fmaxf(fmaxf(x[rt][0], x[rt][1]), fmaxf(x[rt][2], x[rt][3])),
                                       fmaxf(fmaxf(x[rt][4], x[rt][5]), fmaxf(x[rt][6], x[rt][7])));
                     top = groups_max(sees[rt] ? fmaxf(top * scale, -3.0e38f) : -INFINITY);   // -inf: nothing to attend yet (a score of -inf is something)
-                    // weights up to 2^8 are as good as weights up to 1: the outputs are rescaled only when the maximum has moved by more
-                    if (__any(top > m_run[rt] + 8.f)) {
-                        const float m_new = fmaxf(m_run[rt], top), fade = __builtin_amdgcn_exp2f(m_run[rt] - (m_new == -INFINITY ? 0.f : m_new));
+                    // The reference of the weights is 8 above the maximum when it is set, and moves when a score passes it: the outputs are seldom rescaled, and
+                    // no weight is above 1 (a sum of large values has the room that the formula's has).
+                    if (__any(top > m_run[rt])) {
+                        const float m_new = top > m_run[rt] ? top + 8.f : m_run[rt], fade = __builtin_amdgcn_exp2f(m_run[rt] - (m_new == -INFINITY ? 0.f : m_new));
                         l_run[rt] *= fade;
 #pragma unroll
                         for (int j = 0; j < F; j++) acc[rt][j] *= fade;

@@ -4,7 +4,7 @@
 // The products of the scores and the weights bound this.  A workgroup of four waves takes 128 rows (rows of a sequence times the query heads that
 // share its keys) of one key-value head, 32 rows per wave, and goes through the keys in tiles of 64 that it stages in LDS as bf16, two tiles
 // deep: while a tile is worked on, the next one's loads are in flight to registers, from where it is stored (e4m3: converted, with its
-// scale, exactly) behind the work.  Two workgroups share a compute unit, so that one's matrix products run beside the other's exponentials.
+// scale, exactly) between the second products.  Two workgroups share a compute unit, so that one's matrix products run beside the other's exponentials.
 // Products are transposed:
 //   S^T = K q^T    A = K (32 keys x 16 features, one 16-byte read), B = q^T, in registers throughout
 //   O^T = V^T P^T  A = V^T (32 features x 16 keys, by LDS's transposing reads), B = P^T: a lane's scores of 16 keys are, in
@@ -436,9 +436,10 @@ __global__ __launch_bounds__(256, 2) void k_paged_attn_many(PagedAttn a, int min
         for (int e = 1; e < 31; e += 2) top = fmaxf(fmaxf(st[e >> 4][e & 15], st[(e + 1) >> 4][(e + 1) & 15]), top);
         // (both halves of the lanes have the row's maximum; -inf: nothing to attend yet, a score of -inf is something)
         top = halves_max(sees ? fmaxf(fmaxf(top, st[1][15]) * scale, -3.0e38f) : -INFINITY);
-        // weights up to 2^8 are as good as weights up to 1: the outputs are rescaled only when the maximum has moved by more
-        if (__any(top > m_run + 8.f)) {
-            const float m_new = fmaxf(m_run, top), fade = __builtin_amdgcn_exp2f(m_run - (m_new == -INFINITY ? 0.f : m_new));
+        // The reference of the weights is 8 above the maximum when it is set, and moves when a score passes it: the outputs are seldom rescaled, and no
+        // weight is above 1 (a sum of large values has the room that the formula's has).
+        if (__any(top > m_run)) {
+            const float m_new = top > m_run ? top + 8.f : m_run, fade = __builtin_amdgcn_exp2f(m_run - (m_new == -INFINITY ? 0.f : m_new));
             l_run *= fade;
             l_more *= fade;
 #pragma unroll

@@ -509,6 +509,166 @@ def test_a_models_sequence_is_parked_in_the_pool_and_taken_back():
     assert torch.equal(gm.verify_block(block, cl)[0], want)
 
 
+@pytest.mark.parametrize("rows,cache,d,kv_heads,n", [("bf16", "fp8", 256, 17, 1931), ("fp32", "fp8", 64, 5, 26250), ("bf16", "bf16", 8, 33, 31801), ("bf16", "fp8", 80, 6, 10931)])
+def test_many_rows_in_and_out(rows, cache, d, kv_heads, n):
+    """So many that a wave takes several heads; head counts that are no multiple of these, row counts that end inside a wave."""
+    c = Paged(cache, rows, [3, 0, 70], [n - 5, 0, 5], kv_heads=kv_heads, d=d, page=64, seed=d)
+    c.table[0, 2] = -1
+    c.dev[0].copy_(torch.tensor(c.table))
+    k, v = c.random_rows(n), c.random_rows(n)
+    before = [c.values(c.k, c.ks)[0], c.values(c.v, c.vs)[0]]
+    c.kv.write(0, *c.dev, k, v)
+    where = O.places(c.start, c.cached, c.table, c.page, c.n_pages, n)
+    for pool, scale, was, x in ((c.k, c.ks, before[0], k), (c.v, c.vs, before[1], v)):
+        dense = x.double().cpu().numpy()
+        O.write(was, O.quantise(dense)[0] if cache == "fp8" else dense, where)
+        got = c.values(pool, scale)[0]
+        used = np.unique([page for _, _, _, page, _ in where if page >= 0])
+        if cache == "fp8":                                              # (places that nobody wrote: NaN whatever their scale)
+            assert np.array_equal(got[used], was[used], equal_nan=True)
+        else:
+            assert np.array_equal(got, was, equal_nan=True)
+    back = c.kv.read(0, *c.dev, n, dtype=TORCH[rows])
+    for was, x in zip(before, back):
+        assert np.array_equal(x.double().cpu().numpy(), torch.tensor(O.read(was, where, n)).to(TORCH[rows]).double().numpy())
+
+
+@pytest.mark.parametrize("rows,cache,d", [("bf16", "bf16", 64), ("bf16", "fp8", 128), ("bf16", "fp8", 64), ("bf16", "bf16", 128)])
+def test_attention_of_more_sequences_than_share_their_keys(rows, cache, d):
+    """More than 512 sequences, and more row tiles than workgroups share; single tokens beside them, lengths of every kind."""
+    rng = np.random.default_rng(d)
+    cached, new = rng.integers(0, 70, 530), rng.choice([0, 1, 5, 9], 530)
+    cached[7], new[7] = 300, 41
+    c = Paged(cache, rows, cached, new, kv_heads=1, group=8, d=d, seed=5)
+    c.fill()
+    q = c.random_rows(c.total, 8)
+    c.check(c.attend(q, d ** -0.5, 41), q, d ** -0.5)
+    c = Paged(cache, rows, rng.integers(0, 40, 140), np.append(rng.integers(33, 40, 139), 150), kv_heads=8, d=d, seed=6)
+    c.fill()
+    q = c.random_rows(c.total, 8)
+    c.check(c.attend(q, d ** -0.5, 150), q, d ** -0.5)
+
+
+@pytest.mark.parametrize("rows,cache,d", SPREAD + [("bf16", "bf16", 64), ("bf16", "fp8", 128)])
+def test_attention_of_blocks_of_every_size_in_one_batch(rows, cache, d):
+    """1 .. 70 rows times two query heads: the sizes where one way of doing it ends and another begins; rows in front of the first sequence and behind
+    the last stay as they are."""
+    new = [1, 7, 8, 9, 15, 16, 17, 31, 33, 63, 64, 65, 70, 1]
+    c = Paged(cache, rows, [40 * i % 330 for i in range(len(new))], new, kv_heads=2, group=2, d=d, seed=9)
+    c.fill()
+    lead, tail = 3, 4
+    start = c.start + lead
+    c.dev[1].copy_(torch.tensor(start))
+    q = c.random_rows(c.total + lead + tail, 4)
+    out = torch.full_like(q, 5.0)
+    c.attend(q, d ** -0.5, 70, out=out)
+    c.check(out, q, d ** -0.5, start=start)
+    assert (out[:lead] == 5).all() and (out[-tail:] == 5).all()
+
+
+@pytest.mark.parametrize("cache", ["bf16", "fp8"])
+def test_a_million_cached_positions(cache):
+    """A share of the keys is longer than the pages that are held at a time; as a single token, and as a block of more rows."""
+    n = 1_100_000
+    c = Paged(cache, "bf16", [n], [1], kv_heads=1, d=64, page=16)
+    k, v = c.fill()
+    # feature f is large in the f-th of 64 stretches of the keys: a stretch left out, or taken twice, shows
+    v = (v * 0.1).to(torch.bfloat16) + 8 * torch.nn.functional.one_hot(torch.arange(n + 1, device="cuda") * 64 // (n + 1), 64).to(torch.bfloat16)[:, None]
+    c.kv.write(0, c.dev[0], torch.tensor([0, n + 1], dtype=torch.int32, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda"), k, v)
+    q = c.random_rows(1, 1)
+    whole = q * 0.125                                                   # (exact: a power of two)
+    x = (k[:, 0].double() if cache == "bf16" else torch.tensor(O.quantise(k[:, 0].double().cpu().numpy())[0]).cuda()) @ whole[0, 0].double()
+    vv = v[:, 0].double() if cache == "bf16" else torch.tensor(O.quantise(v[:, 0].double().cpu().numpy())[0]).cuda()
+    w = torch.softmax(x, 0)
+    want, size = w @ vv, w @ vv.abs()
+    dot = whole.double().norm() * k.double().norm(dim=-1).max()
+    # as in the head of this file; no sum runs over more than a tenth of the keys before it is joined with the others
+    tol = 2.0 ** -8 * want.abs() + 2 * (2.0 ** -8 + 68 * 2.0 ** -24 * dot + 2.0 ** -21 + n / 10 * 2.0 ** -24) * size
+    got = c.attend(q, 0.125, 1)
+    assert ((got[0, 0].double() - want).abs() <= tol).all()
+    # a block of 40 rows that ends there, row 39 the same query
+    c.dev[1].copy_(torch.tensor([0, 40]))
+    c.dev[2].copy_(torch.tensor([n - 39]))
+    block = c.random_rows(40, 1)
+    block[39] = q[0]
+    got = c.attend(block, 0.125, 40)
+    assert ((got[39, 0].double() - want).abs() <= tol).all()
+
+
+@pytest.mark.parametrize("rows,cache,d,m", [("bf16", "bf16", 128, 2), ("bf16", "bf16", 64, 40), ("bf16", "fp8", 64, 12), ("bf16", "fp8", 128, 40), ("fp32", "fp32", 32, 3)])
+def test_values_near_the_largest(rows, cache, d, m):
+    """Sums of weights times values stay in range where the values do: one of 2^120 among ordinary ones, a whole row of them, and their negatives."""
+    c = Paged(cache, rows, [50, 90], [m, m], kv_heads=2, d=d, seed=11)
+    c.fill()
+    one = torch.tensor([0, 1], dtype=torch.int32, device="cuda")
+    for at, x in ((3, 2.0 ** 120), (20, -2.0 ** 120), (49, 1.75 * 2.0 ** 119)):
+        kr, vr = c.random_rows(1), c.random_rows(1)
+        vr[:, :, :d if at == 49 else 1] = x
+        c.kv.write(0, c.dev[0][:1].contiguous(), one, torch.tensor([at], dtype=torch.int32, device="cuda"), kr, vr)
+    q = c.random_rows(2 * m, 2)
+    c.check(c.attend(q, d ** -0.5, m), q, d ** -0.5)
+
+
+def test_two_caches_on_two_streams_and_in_two_graphs():
+    """Each has its own workspace: work that overlaps gives what it gives alone."""
+    cs = [Paged("fp8", "bf16", [3000, 500], [m, m], kv_heads=4, group=2, d=128, width=1, seed=m) for m in (4, 40)]
+    qs, want, graphs, outs = [], [], [], []
+    for c, m in zip(cs, (4, 40)):
+        c.fill()
+        qs.append(c.random_rows(2 * m, 8))
+        want.append(c.attend(qs[-1], 0.09, m))
+        outs.append(torch.empty_like(qs[-1]))
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for c, m, q, out, s in zip(cs, (4, 40), qs, outs, streams):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=s):
+            for _ in range(5):
+                c.attend(q, 0.09, m, out=out)
+        graphs.append(g)
+    for _ in range(3):
+        for o in outs:
+            o.fill_(-1)
+        torch.cuda.synchronize()
+        for g, s in zip(graphs, streams):
+            with torch.cuda.stream(s):
+                g.replay()
+        for c, m, q, s in zip(cs, (4, 40), qs, streams):
+            with torch.cuda.stream(s):
+                late = [c.attend(q, 0.09, m) for _ in range(5)]
+            s.synchronize()
+            assert all(torch.equal(x, want[cs.index(c)]) for x in late)
+        torch.cuda.synchronize()
+        assert torch.equal(outs[0], want[0]) and torch.equal(outs[1], want[1])
+
+
+def test_threads_that_share_a_cache():
+    """Rows in and out from several threads, each with a page table of its own."""
+    import threading
+    c = Paged("bf16", "bf16", [0] * 4, [40] * 4, kv_heads=2, d=64)
+    c.fill()
+    start, zero = torch.tensor([0, 40], dtype=torch.int32, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda")
+    tables = [c.dev[0][b:b + 1].contiguous() for b in range(4)]
+    want = [c.kv.read(0, t, start, zero, 40) for t in tables]
+    torch.cuda.synchronize()
+    wrong = []
+
+    def work(b):
+        torch.cuda.set_device(0)
+        for _ in range(200):
+            k, v = c.kv.read(0, tables[b], start, zero, 40)
+            c.kv.write(0, tables[b], start, zero, k.to(torch.bfloat16), v.to(torch.bfloat16))
+        if not (torch.equal(k, want[b][0]) and torch.equal(v, want[b][1])):
+            wrong.append(b)
+
+    threads = [threading.Thread(target=work, args=(b,)) for b in range(4)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not wrong
+
+
 def test_refusals_of_the_binding():
     import paper_2312_11462_amd as P
     c = Paged("bf16", "bf16", [3], [2], kv_heads=2, group=2, d=64)
