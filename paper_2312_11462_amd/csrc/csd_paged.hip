@@ -67,8 +67,8 @@ template <typename T> struct Raw8 {
     }
 };
 
-// Stores past the caches, for many dense rows: they are more than a cache level holds, and kept there they push out the pages still to be read (8198
-// rows of 32 heads of 128, e4m3 to bf16: 57 -> 34 us; with the loads of the pages past them too 52).
+// Stores past the caches, for many dense rows: they are more than a cache level holds, and kept there they push out the pages still to be read (36004
+// rows of 8 heads of 128, e4m3 to bf16: 57 -> 34 us; with the loads of the pages past them too 52).
 template <typename T>
 __device__ __forceinline__ void store8_past(T *p, const float (&x)[8]) {
     alignas(16) T t[8];
