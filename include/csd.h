@@ -329,7 +329,7 @@ int32_t csd_tree_commit(const csd_model *model, void *kv, const int32_t *cache_l
  * A pool holds the rows of n_layers layers in n_pages pages of page_rows rows each (a power of two, 16 to 1024):
  *   k, v              [n_layers][n_pages][n_kv_heads][page_rows][head_dim] in dtype (head_dim a multiple of 8, 8 to 256)
  *   k_scale, v_scale  CSD_DTYPE_FP8: [n_layers][n_pages][n_kv_heads][page_rows]; NULL for the other types
- * Both pools are 16-byte aligned.  table[B][table_stride] names the pages of every sequence in order, the same in every
+ * Both pools are 16-byte aligned, the scales 8-byte aligned.  table[B][table_stride] names the pages of every sequence in order, the same in every
  * layer: position pos of sequence b is row pos % page_rows of page table[b][pos / page_rows].  An entry outside [0, n_pages), and every
  * position from table_stride * page_rows on, is a place without a row: what would be written there is dropped, it reads as zeros,
  * and the attention leaves it out (so pages that are no longer wanted may be given back and their entries set to -1).
@@ -343,7 +343,8 @@ int32_t csd_tree_commit(const csd_model *model, void *kv, const int32_t *cache_l
  * The rows of a batch are ragged: row r of a call, 0 <= r < rows, belongs to the sequence b with
  * row_start[b] <= r < row_start[b + 1] (row_start[B + 1], non-decreasing) and has position
  * pos[b] + r - row_start[b].  Rows of no sequence (before row_start[0], from row_start[B] on) are left alone, in outputs too.
- * row_start, pos and table are device arrays and are clamped to the call's buffers by the kernels.
+ * row_start, pos and table are device arrays and are clamped to the call's buffers by the kernels.  CSD_ESHAPE: more than 4096
+ * key-value heads, 2^22 rows or 2^20 sequences.
  * Pages that two sequences share may be read by both; two rows of one call, or of calls that overlap, must not be
  * written to the same place.
  */

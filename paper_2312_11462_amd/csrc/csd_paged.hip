@@ -266,7 +266,7 @@ static int32_t check_pool(const csd_paged_kv *kv) {
     if (kv->n_layers < 1 || kv->n_pages < 1 || kv->n_kv_heads < 1 || kv->table_stride < 1) return CSD_EINVAL;
     if (kv->head_dim < 8 || kv->head_dim > 256 || kv->head_dim % 8) return CSD_EINVAL;
     if (kv->page_rows < 16 || kv->page_rows > 1024 || (kv->page_rows & (kv->page_rows - 1))) return CSD_EINVAL;
-    if (((uintptr_t)kv->k | (uintptr_t)kv->v) % 16) return CSD_EINVAL;
+    if (((uintptr_t)kv->k | (uintptr_t)kv->v) % 16 || ((uintptr_t)kv->k_scale | (uintptr_t)kv->v_scale) % 8) return CSD_EINVAL;
     if ((long long)kv->table_stride * kv->page_rows > (1ll << 30) || kv->n_kv_heads > 4096) return CSD_ESHAPE;
     return CSD_OK;
 }

@@ -160,7 +160,7 @@ __global__ __launch_bounds__(256, 2) void k_paged_attn_few(PagedAttn a) {
             }
             before += __builtin_amdgcn_readlane(incl, 63);
         }
-        if (n == 0) return;                                  // (the lengths changed while they were read)
+        if (n == 0 || u - before >= n * p.Hkv) return;       // (the lengths changed while they were read)
         const int kvh = (u - before) / n, item = before + kvh * n + kCost;     // (where its tiles begin)
         u = min(item - kCost + n, u_end);
         n -= kCost;
@@ -206,14 +206,14 @@ __global__ __launch_bounds__(256, 2) void k_paged_attn_few(PagedAttn a) {
                 const int at = F8 ? 64 * (s / 2) + 16 * g + 8 * (s & 1) : 32 * s + 8 * g;      // features of the K operand's step s
                 u32x4 x = *reinterpret_cast<const u32x4 *>(q + at);
 #pragma unroll
-                for (int w = 0; w < 4; w++) x[w] = r < rows ? x[w] ^ flip : 0u;
+                for (int w = 0; w < 4; w++) x[w] = r < rows && a.scale != 0.f ? x[w] ^ flip : 0u;
                 if constexpr (RT == 1) qf[s] = x;
                 else if (wave == 0) s_q[(rt * (DH / 32) + s) * 64] = x;
             }
         }
         const bool second = RT > 1 && rows > 16;             // the second row tile holds rows
-        // scores in units of log2; the sign is the queries' (the maximum needs scale >= 0), at least 1e-30 (a masked score of -inf has to stay one)
-        const float scale = fmaxf(fabsf(a.scale) * 1.44269504088896f, 1e-30f);
+        // scores in units of log2; the sign is the queries' (the maximum needs scale >= 0), and so is a scale of 0 (a masked score of -inf has to stay one)
+        const float scale = fmaxf(fabsf(a.scale) * 1.44269504088896f, 1e-37f);
         f32x4 acc[RT][F];
         float m_run[RT], l_run[RT];
         uint32_t odd = 0;                                    // the wave took values out of its products

@@ -148,6 +148,7 @@ __global__ __launch_bounds__(256, 2) void k_paged_attn_many(PagedAttn a, int min
         seq = PagedSeq{__builtin_amdgcn_readfirstlane(s_start[b]), __builtin_amdgcn_readfirstlane(s_m[b]), __builtin_amdgcn_readfirstlane(s_t[b])};
         const int units = __builtin_amdgcn_readfirstlane(s_units[b]), n = (seq.m * a.group + BM - 1) / BM;
         kvh = (u - before) / units;
+        if (kvh >= p.Hkv) return;
         int left = u - before - kvh * units;
         rt = -1;
         for (int r0 = 0; r0 < n; r0 += 64) {
@@ -241,11 +242,11 @@ __global__ __launch_bounds__(256, 2) void k_paged_attn_many(PagedAttn a, int min
 #pragma unroll
         for (int s = 0; s < ST; s++) {
             qf[s] = u32x4{0u, 0u, 0u, 0u};
-            if (live) qf[s] = *reinterpret_cast<const u32x4 *>(q + 16 * s);
+            if (live && a.scale != 0.f) qf[s] = *reinterpret_cast<const u32x4 *>(q + 16 * s);
         }
     }
-    // scores in units of log2 (at least 1e-30: a masked score of -inf has to stay one)
-    const float scale = fmaxf(fabsf(a.scale) * 1.44269504088896f, 1e-30f);
+    // scores in units of log2 (more than 0, so that a masked score of -inf stays one; with a scale of 0 the queries are)
+    const float scale = fmaxf(fabsf(a.scale) * 1.44269504088896f, 1e-37f);
     f32x16 acc[DT];
     float m_run = -INFINITY;
 #pragma unroll

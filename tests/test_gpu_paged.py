@@ -595,6 +595,18 @@ def test_a_million_cached_positions(cache):
     assert ((got[39, 0].double() - want).abs() <= tol).all()
 
 
+@pytest.mark.parametrize("rows,cache,d", SPREAD + [("bf16", "bf16", 64), ("bf16", "fp8", 128)])
+@pytest.mark.parametrize("m", [3, 40])
+def test_a_scale_of_zero_weighs_all_alike(rows, cache, d, m):
+    """However large the products of queries and keys are."""
+    c = Paged(cache, rows, [70, 0], [m, m], kv_heads=2, group=2, d=d, seed=m)
+    k, v = c.fill()
+    start = torch.tensor([0, 70 + m, 70 + 2 * m], dtype=torch.int32, device="cuda")
+    c.kv.write(0, c.dev[0], start, torch.zeros(2, dtype=torch.int32, device="cuda"), k * 2.0 ** 56, v)
+    q = c.random_rows(2 * m, 4) * 2.0 ** 56
+    c.check(c.attend(q, 0.0, m), q, 0.0)
+
+
 @pytest.mark.parametrize("rows,cache,d,m", [("bf16", "bf16", 128, 2), ("bf16", "bf16", 64, 40), ("bf16", "fp8", 64, 12), ("bf16", "fp8", 128, 40), ("fp32", "fp32", 32, 3)])
 def test_values_near_the_largest(rows, cache, d, m):
     """Sums of weights times values stay in range where the values do: one of 2^120 among ordinary ones, a whole row of them, and their negatives."""

@@ -76,7 +76,7 @@ EINVAL, ESHAPE, ENULL = -1, -2, -3
 POOL_REFUSALS = [(dict(k=None), ENULL), (dict(v=None), ENULL), (dict(table=None), ENULL), (dict(k_scale=None), ENULL), (dict(v_scale=None), ENULL),
                  (dict(dtype=3), EINVAL), (dict(dtype=-1), EINVAL), (dict(n_layers=0), EINVAL), (dict(n_pages=0), EINVAL), (dict(n_kv_heads=0), EINVAL),
                  (dict(head_dim=0), EINVAL), (dict(head_dim=12), EINVAL), (dict(head_dim=264), EINVAL), (dict(page_rows=8), EINVAL),
-                 (dict(page_rows=24), EINVAL), (dict(page_rows=2048), EINVAL), (dict(table_stride=0), EINVAL), (dict(k=260), EINVAL),
+                 (dict(page_rows=24), EINVAL), (dict(page_rows=2048), EINVAL), (dict(table_stride=0), EINVAL), (dict(k=260), EINVAL), (dict(k_scale=257), EINVAL), (dict(v_scale=260), EINVAL),
                  (dict(table_stride=1 << 27), ESHAPE)]
 
 
