@@ -234,13 +234,17 @@ static_assert(CSD_PAGED_COUNTER_BYTES + 2ull * CSD_PAGED_FEW_GRID * CSD_PAGED_FE
 bool csd_paged_few_fits(const PagedAttn &a, int32_t pool_dtype, int32_t q_dtype);
 void csd_paged_few_enqueue(const PagedAttn &a, int rows, int32_t pool_dtype, hipStream_t st);
 
-// csd_paged_many.hip: the others, in the same types and head sizes, 128 rows per workgroup.
+// csd_paged_many.hip: the others, in the same types and head sizes, 128 rows per workgroup and item.
 #define CSD_PAGED_MANY_ROWS 128
 #define CSD_PAGED_MANY_SHARE 4       /* tiles of 64 keys per part of an item at least */
 #define CSD_PAGED_MANY_COST 4        /* what an item costs besides its keys, in such tiles */
 #define CSD_PAGED_MANY_PARTS 14      /* parts of an item at most */
-#define CSD_PAGED_MANY_GRID 512      /* two workgroups per compute unit, where they share the items' keys */
-#define CSD_PAGED_MANY_ITEMS 1024    /* row tiles times key-value heads at most for that */
-#define CSD_PAGED_MANY_BATCH 512     /* sequences at most for that */
+#define CSD_PAGED_MANY_GRID 512      /* two workgroups per compute unit */
+#define CSD_PAGED_MANY_BATCH 512     /* sequences at most */
+// Row tiles times key-value heads at most: above, csd_paged_chunk.hip takes over, a workgroup of 256 rows per item.  (8 x 4 heads of 128, bf16: 40 sequences of 64 rows over
+// 0 to 3000 keys, 960 items, 123 us against 142; 5 of 300 rows, 32 heads, 512 items, 100 against 119; 2 of 2048 rows, 1040 items, 455 against 415.)
+#define CSD_PAGED_MANY_ITEMS 1024
 static_assert(CSD_PAGED_COUNTER_BYTES + 2ull * CSD_PAGED_MANY_GRID * CSD_PAGED_MANY_ROWS * 132 * 4 <= CSD_PAGED_WORKSPACE_BYTES, "");
+// min_rows: sequences of so many rows or fewer are another kernel's.
 void csd_paged_many_enqueue(const PagedAttn &a, int min_rows, int32_t pool_dtype, hipStream_t st);
+void csd_paged_chunk_enqueue(const PagedAttn &a, int min_rows, int32_t pool_dtype, hipStream_t st);

@@ -1,4 +1,4 @@
-// Attention of many rows (chunks of a prompt, large trees, many query heads per key-value head) over a paged KV cache: bf16 queries, heads of
+// Attention of many rows (chunks of prompts beside other sequences, large trees, many query heads per key-value head) over a paged KV cache: bf16 queries, heads of
 // 64 or 128, bf16 or e4m3 pools.
 //
 // The products of the scores and the weights bound this.  A workgroup of four waves takes 128 rows (rows of a sequence times the query heads that
@@ -13,42 +13,11 @@
 // is kept in fp32): a second plane of them would be a third more matrix instructions, which bound this kernel.
 // Rows of 16-byte pieces are stored with the piece index xored by the row, K and V in different ways, so that each kind of read
 // spreads over all banks.
-#include "csd_paged.h"
+#include "csd_paged_tiles.h"
 
-typedef float f32x16 __attribute__((ext_vector_type(16)));
-typedef short s16x4 __attribute__((ext_vector_type(4)));
-typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
-
-static constexpr int kKeys = 64;                             // keys per tile
-
-__device__ __forceinline__ f32x16 mfma32(u32x4 a, u32x4 b, f32x16 c) {
-    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
-}
-__device__ __forceinline__ float halves_max(float v) {
-    const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-    return fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
-}
-__device__ __forceinline__ float halves_sum(float v) {
-    const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-    return __uint_as_float(a[0]) + __uint_as_float(a[1]);
-}
-
-// 16-byte piece c of row `row` in a staged tile
-template <int DH> __device__ __forceinline__ int k_piece(int row, int c) { return row * (DH / 8) + (c ^ (row & (DH / 8 - 1))); }
-template <int DH> __device__ __forceinline__ int v_piece(int row, int c) {
-    return row * (DH / 8) + (c ^ (DH == 128 ? (row & 3) << 2 : ((row >> 1) & 1) << 2));
-}
-
-// The key tiles that row tile rt of a sequence goes through: those up to the last position that one of its rows attends.
-__device__ __forceinline__ int row_tile_keys(int rt, int m, int t, int group, int cap) {
-    const int last = min(((rt + 1) * CSD_PAGED_MANY_ROWS - 1) / group, m - 1);
-    return (min(t + last + 1, cap) + kKeys - 1) / kKeys;
-}
-
-// SHARED: the grid is a fixed number of workgroups, which take equal, contiguous shares of all items' key tiles (as k_paged_attn_few does; the
-// parts of an item are joined by the workgroup that finishes last).  Else a workgroup is an item: where there are many of them, the parts'
-// way through memory costs more than the ends of the launch.
-template <int DH, bool F8, bool SHARED>
+// The grid is a fixed number of workgroups, which take equal, contiguous shares of all items' key tiles (as k_paged_attn_few does; the parts of an item
+// are joined by the workgroup that finishes last).
+template <int DH, bool F8>
 __global__ __launch_bounds__(256, 2) void k_paged_attn_many(PagedAttn a, int min_rows) {
     constexpr int ES = F8 ? 1 : 2, LPR = DH * ES / 16;       // lanes that load a row
     constexpr int RPP = 256 / LPR, NP = kKeys / RPP;         // rows per pass of the workgroup, passes per tile
@@ -60,7 +29,7 @@ __global__ __launch_bounds__(256, 2) void k_paged_attn_many(PagedAttn a, int min
     u32x4(&s_k)[2][PIECES] = *reinterpret_cast<u32x4(*)[2][PIECES]>(&s_tiles[0]), (&s_v)[2][PIECES] = *reinterpret_cast<u32x4(*)[2][PIECES]>(&s_tiles[2]);
     __shared__ float s_max[BM], s_sum[BM];
     __shared__ int s_odd, s_last;
-    __shared__ int s_start[SHARED ? CSD_PAGED_MANY_BATCH : 1], s_m[SHARED ? CSD_PAGED_MANY_BATCH : 1], s_t[SHARED ? CSD_PAGED_MANY_BATCH : 1], s_units[SHARED ? CSD_PAGED_MANY_BATCH : 1];
+    __shared__ int s_start[CSD_PAGED_MANY_BATCH], s_m[CSD_PAGED_MANY_BATCH], s_t[CSD_PAGED_MANY_BATCH], s_units[CSD_PAGED_MANY_BATCH];
     const PagedPool &p = a.p;
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, col = lane & 31, h = lane >> 5;
     const int cap = p.table_stride << p.page_shift;
@@ -82,120 +51,84 @@ __global__ __launch_bounds__(256, 2) void k_paged_attn_many(PagedAttn a, int min
         return x;
     };
 
-    // ---- SHARED: this workgroup's share
-    int u = 0, u_end = 1, me = 0;
-    int T = 1, n_wg = 1;
-    if constexpr (SHARED) {
-        for (int b = tid; b < a.r.B; b += 256) {
-            PagedSeq s;
-            s_m[b] = seq_of(b, s) ? s.m : 0;
-            s_t[b] = s.t;
-            s_start[b] = s.start;
-        }
-        __syncthreads();
-        for (int b = tid / 8; b < a.r.B; b += 32) {          // eight lanes per sequence
-            const int m = s_m[b], t = s_t[b], n = (m * a.group + BM - 1) / BM;
-            int sum = 0;
-            for (int rt = tid % 8; rt < n; rt += 8) sum += COST + row_tile_keys(rt, m, t, a.group, cap);
-#pragma unroll
-            for (int o = 4; o > 0; o >>= 1) sum += __shfl_xor(sum, o, 64);
-            if (tid % 8 == 0) s_units[b] = sum;
-        }
-        __syncthreads();
-        int sum = 0, longest = 0;
-        for (int b = lane; b < a.r.B; b += 64) {
-            sum += s_units[b];
-            if (s_m[b]) longest = max(longest, COST + (min(s_t[b] + s_m[b], cap) + kKeys - 1) / kKeys);
-        }
-#pragma unroll
-        for (int o = 32; o > 0; o >>= 1) {
-            sum += __shfl_xor(sum, o, 64);
-            longest = max(longest, __shfl_xor(longest, o, 64));
-        }
-        T = __builtin_amdgcn_readfirstlane(sum) * p.Hkv;
-        if (T == 0) return;
-        longest = __builtin_amdgcn_readfirstlane(longest);
-        const int least = max(CSD_PAGED_MANY_SHARE, (longest + PARTS - 3) / (PARTS - 2));
-        n_wg = min(CSD_PAGED_MANY_GRID, max(1, T / least));
-        // workgroups go to the compute dies in turn: a die's take neighbouring shares, which read the same keys
-        const int per_die = (n_wg + 7) / 8;
-        me = (blockIdx.x % 8) * per_die + blockIdx.x / 8;
-        if ((int)blockIdx.x / 8 >= per_die || me >= n_wg) return;
-        const PagedShares shares(T, n_wg);
-        u = shares.first(me);
-        u_end = shares.first(me + 1);
+    // ---- this workgroup's share
+    for (int b = tid; b < a.r.B; b += 256) {
+        PagedSeq s;
+        s_m[b] = seq_of(b, s) ? s.m : 0;
+        s_t[b] = s.t;
+        s_start[b] = s.start;
     }
+    __syncthreads();
+    for (int b = tid / 8; b < a.r.B; b += 32) {              // eight lanes per sequence
+        const int m = s_m[b], t = s_t[b], n = (m * a.group + BM - 1) / BM;
+        int sum = 0;
+        for (int rt = tid % 8; rt < n; rt += 8) sum += COST + row_tile_keys(rt, m, t, a.group, cap);
+#pragma unroll
+        for (int o = 4; o > 0; o >>= 1) sum += __shfl_xor(sum, o, 64);
+        if (tid % 8 == 0) s_units[b] = sum;
+    }
+    __syncthreads();
+    int sum = 0, longest = 0;
+    for (int b = lane; b < a.r.B; b += 64) {
+        sum += s_units[b];
+        if (s_m[b]) longest = max(longest, COST + (min(s_t[b] + s_m[b], cap) + kKeys - 1) / kKeys);
+    }
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) {
+        sum += __shfl_xor(sum, o, 64);
+        longest = max(longest, __shfl_xor(longest, o, 64));
+    }
+    const int T = __builtin_amdgcn_readfirstlane(sum) * p.Hkv;
+    if (T == 0) return;
+    longest = __builtin_amdgcn_readfirstlane(longest);
+    const int least = max(CSD_PAGED_MANY_SHARE, (longest + PARTS - 3) / (PARTS - 2));
+    const int n_wg = min(CSD_PAGED_MANY_GRID, max(1, T / least));
+    // workgroups go to the compute dies in turn: a die's take neighbouring shares, which read the same keys
+    const int per_die = (n_wg + 7) / 8;
+    const int me = (int)(blockIdx.x % 8) * per_die + (int)(blockIdx.x / 8);
+    if ((int)blockIdx.x / 8 >= per_die || me >= n_wg) return;
     const PagedShares shares(T, n_wg);
+    int u = shares.first(me);
+    const int u_end = shares.first(me + 1);
 
     while (u < u_end) {
     // ---- the item: rows rt * BM .. of sequence b, key-value head kvh, key tiles kt0 .. kt1 of its n_kt
-    int b = -1, kvh = 0, rt = 0, kt0 = 0, item = 0;
-    PagedSeq seq{0, 0, 0};
-    if constexpr (SHARED) {
-        int before = 0;
-        for (int b0 = 0; b0 < a.r.B; b0 += 64) {
-            const int x = b0 + lane < a.r.B ? s_units[b0 + lane] * p.Hkv : 0, incl = scan(x);
-            const unsigned long long past = __ballot(before + incl > u);
-            if (past) {
-                const int j = __ffsll((long long)past) - 1;
-                b = b0 + j;
-                before += __builtin_amdgcn_readlane(incl, j) - __builtin_amdgcn_readlane(x, j);
-                break;
-            }
-            before += __builtin_amdgcn_readlane(incl, 63);
+    int b = -1, before = 0;
+    for (int b0 = 0; b0 < a.r.B; b0 += 64) {
+        const int x = b0 + lane < a.r.B ? s_units[b0 + lane] * p.Hkv : 0, incl = scan(x);
+        const unsigned long long past = __ballot(before + incl > u);
+        if (past) {
+            const int j = __ffsll((long long)past) - 1;
+            b = b0 + j;
+            before += __builtin_amdgcn_readlane(incl, j) - __builtin_amdgcn_readlane(x, j);
+            break;
         }
-        if (b < 0) return;                                   // (the lengths changed while they were read)
-        seq = PagedSeq{__builtin_amdgcn_readfirstlane(s_start[b]), __builtin_amdgcn_readfirstlane(s_m[b]), __builtin_amdgcn_readfirstlane(s_t[b])};
-        const int units = __builtin_amdgcn_readfirstlane(s_units[b]), n = (seq.m * a.group + BM - 1) / BM;
-        kvh = (u - before) / units;
-        if (kvh >= p.Hkv) return;
-        int left = u - before - kvh * units;
-        rt = -1;
-        for (int r0 = 0; r0 < n; r0 += 64) {
-            const int x = r0 + lane < n ? COST + row_tile_keys(r0 + lane, seq.m, seq.t, a.group, cap) : 0, incl = scan(x);
-            const unsigned long long past = __ballot(incl > left);
-            if (past) {
-                const int j = __ffsll((long long)past) - 1;
-                rt = r0 + j;
-                kt0 = left - (__builtin_amdgcn_readlane(incl, j) - __builtin_amdgcn_readlane(x, j));
-                break;
-            }
-            left -= __builtin_amdgcn_readlane(incl, 63);
-        }
-        if (rt < 0) return;
-        item = u - kt0 + COST;                               // where its keys begin
-        kt0 -= COST;
-    } else {
-        // key-value heads follow one another (workgroups of a die, every eighth, read the same keys), then the row tiles, the late ones with
-        // the most keys first
-        kvh = blockIdx.x % p.Hkv;
-        int total = 0;
-        for (int pass = 0; pass < 2; pass++) {               // count the row tiles of all sequences, then find this one
-            int before = 0;
-            const int want = total - 1 - (int)(blockIdx.x / p.Hkv);
-            if (pass && want < 0) return;
-            for (int b0 = 0; b0 < a.r.B; b0 += 64) {
-                PagedSeq s;
-                const int n = seq_of(b0 + lane, s), incl = scan(n);
-                if (pass) {
-                    const unsigned long long past = __ballot(before + incl > want);
-                    if (past) {
-                        const int j = __ffsll((long long)past) - 1;
-                        b = b0 + j;
-                        rt = want - (before + __builtin_amdgcn_readlane(incl, j) - __builtin_amdgcn_readlane(n, j));
-                        seq = PagedSeq{__builtin_amdgcn_readlane(s.start, j), __builtin_amdgcn_readlane(s.m, j), __builtin_amdgcn_readlane(s.t, j)};
-                        break;
-                    }
-                }
-                before += __builtin_amdgcn_readlane(incl, 63);
-            }
-            total = before;
-        }
-        if (b < 0) return;
+        before += __builtin_amdgcn_readlane(incl, 63);
     }
+    if (b < 0) return;                                       // (the lengths changed while they were read)
+    const PagedSeq seq{__builtin_amdgcn_readfirstlane(s_start[b]), __builtin_amdgcn_readfirstlane(s_m[b]), __builtin_amdgcn_readfirstlane(s_t[b])};
+    const int units = __builtin_amdgcn_readfirstlane(s_units[b]), n = (seq.m * a.group + BM - 1) / BM;
+    const int kvh = (u - before) / units;
+    if (kvh >= p.Hkv) return;
+    int left = u - before - kvh * units;
+    int rt = -1, kt0 = 0;
+    for (int r0 = 0; r0 < n; r0 += 64) {
+        const int x = r0 + lane < n ? COST + row_tile_keys(r0 + lane, seq.m, seq.t, a.group, cap) : 0, incl = scan(x);
+        const unsigned long long past = __ballot(incl > left);
+        if (past) {
+            const int j = __ffsll((long long)past) - 1;
+            rt = r0 + j;
+            kt0 = left - (__builtin_amdgcn_readlane(incl, j) - __builtin_amdgcn_readlane(x, j));
+            break;
+        }
+        left -= __builtin_amdgcn_readlane(incl, 63);
+    }
+    if (rt < 0) return;
+    const int item = u - kt0 + COST;                         // where its keys begin
+    kt0 -= COST;
     const int rows = min(seq.m * a.group - rt * BM, BM);     // of this item
     const int n_kt = row_tile_keys(rt, seq.m, seq.t, a.group, cap);
-    const int kt1 = SHARED ? min(n_kt, kt0 + u_end - u) : n_kt;
+    const int kt1 = min(n_kt, kt0 + u_end - u);
     u += kt1 - kt0;
     kt0 = max(kt0, 0);
     if (kt1 <= 0) continue;                                  // (the share ends before the keys begin)
@@ -345,7 +278,6 @@ __global__ __launch_bounds__(256, 2) void k_paged_attn_many(PagedAttn a, int min
 #pragma unroll
         for (int s = 0; s < ST; s++) qf[s] ^= u32x4{0x80008000u, 0x80008000u, 0x80008000u, 0x80008000u};
     const int wave_first = seq.t + (rt * BM + wave * 32) / a.group;      // last position that the wave's first row attends
-    const bool wave_live = wave * 32 < rows;
     // where a lane reads: K row `col` (+ 32), pieces 2 s + h; V as LDS's transposing read wants it (the place of 4 features of a key), pieces 4 d + ..
     const int l16 = lane & 15;
     const int k_at = k_piece<DH>(col, h) * 16, v_row = 4 * h + (l16 >> 2);
@@ -359,19 +291,6 @@ __global__ __launch_bounds__(256, 2) void k_paged_attn_many(PagedAttn a, int min
         if (((next - kt0) & 15) == 0 && next != kt) {
             pages = pages_next;
             pages_next = pages_from(next + 16);
-        }
-        if (!wave_live) {
-#pragma unroll
-            for (int x = 0; x < NP; x++) load(next, x, V);
-#pragma unroll
-            for (int x = 0; x < NP; x++) {
-                stage(x, buf ^ 1, V);
-                load(next, x, K);
-            }
-#pragma unroll
-            for (int x = 0; x < NP; x++) stage(x, buf ^ 1, K);
-            mend(next, buf ^ 1);
-            return;
         }
         // What is issued between the matrix instructions, which take as long as several others, is set down one by one: operands are read two
         // products ahead; the next tile's values are requested first and stored (to the other buffer, last read a turn ago) beside the second
@@ -535,7 +454,7 @@ __global__ __launch_bounds__(256, 2) void k_paged_attn_many(PagedAttn a, int min
         const int r_ = rt * BM + row, i_ = r_ / a.group, h_ = r_ - i_ * a.group;
         return reinterpret_cast<bf16_t *>(a.out) + (((size_t)(seq.start + i_) * p.Hkv + kvh) * a.group + h_) * DH;
     };
-    const int w_first = SHARED ? shares.owner(item) : 0, w_last = SHARED ? shares.owner(item + n_kt - 1) : 0, parts = w_last - w_first + 1;
+    const int w_first = shares.owner(item), w_last = shares.owner(item + n_kt - 1), parts = w_last - w_first + 1;
     if (parts == 1) {
         for (int x = id; x < rows * (C / 2); x += 256) {
             const int row = x / (C / 2), c = x % (C / 2);
@@ -565,20 +484,14 @@ __global__ __launch_bounds__(256, 2) void k_paged_attn_many(PagedAttn a, int min
     }
 }
 
-// min_rows: sequences of so many rows or fewer are another kernel's.
 void csd_paged_many_enqueue(const PagedAttn &a, int min_rows, int32_t pool_dtype, hipStream_t st) {
     // row tiles at most: full ones, and a last one per sequence
     const long long tiles = (long long)a.r.rows * a.group / CSD_PAGED_MANY_ROWS + a.r.B, items = tiles * a.p.Hkv;
     const long long keys = ((long long)a.p.table_stride << a.p.page_shift) / kKeys + 1 + CSD_PAGED_MANY_COST;      // (all key tiles are counted in 32 bits)
     const bool shared = items <= CSD_PAGED_MANY_ITEMS && a.r.B <= CSD_PAGED_MANY_BATCH && items * keys < (1ll << 30);
-    const dim3 grid(shared ? CSD_PAGED_MANY_GRID : (unsigned)items);
-    auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, st, a, min_rows); };
+    if (!shared) return csd_paged_chunk_enqueue(a, min_rows, pool_dtype, st);
+    auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(CSD_PAGED_MANY_GRID), dim3(256), 0, st, a, min_rows); };
     const bool f8 = pool_dtype == CSD_DTYPE_FP8;
-    if (a.p.D == 128) {
-        if (shared) f8 ? launch(k_paged_attn_many<128, true, true>) : launch(k_paged_attn_many<128, false, true>);
-        else f8 ? launch(k_paged_attn_many<128, true, false>) : launch(k_paged_attn_many<128, false, false>);
-    } else {
-        if (shared) f8 ? launch(k_paged_attn_many<64, true, true>) : launch(k_paged_attn_many<64, false, true>);
-        else f8 ? launch(k_paged_attn_many<64, true, false>) : launch(k_paged_attn_many<64, false, false>);
-    }
+    if (a.p.D == 128) f8 ? launch(k_paged_attn_many<128, true>) : launch(k_paged_attn_many<128, false>);
+    else f8 ? launch(k_paged_attn_many<64, true>) : launch(k_paged_attn_many<64, false>);
 }

@@ -549,6 +549,66 @@ def test_attention_of_more_sequences_than_share_their_keys(rows, cache, d):
     c.check(c.attend(q, d ** -0.5, 150), q, d ** -0.5)
 
 
+FULL = [("bf16", "bf16", 64), ("bf16", "bf16", 128), ("bf16", "fp8", 64), ("bf16", "fp8", 128)]
+IDLE = 520                                                              # sequences without rows: so many that the keys are not shared out
+
+
+@pytest.mark.parametrize("rows,cache,d", FULL)
+@pytest.mark.parametrize("page", [16, 128])
+def test_chunks_beside_idle_sequences(rows, cache, d, page):
+    """Whole workgroups of rows: lengths of one tile to fifty, row counts around a wave and a workgroup, negative scales, rows in a wider buffer."""
+    cached, new = [3000, 3, 1500, 1023, 64, 0, 447, 512], [130, 129, 20, 64, 1, 257, 65, 16]
+    c = Paged(cache, rows, cached + [0] * IDLE, new + [0] * IDLE, kv_heads=2, group=2, d=d, page=page, seed=page)
+    c.fill()
+    wide = torch.randn(c.total, 4 * d + 24, device="cuda").to(TORCH[rows])
+    q = wide[:, 8:8 + 4 * d].unflatten(1, (4, d))
+    out = c.attend(q, d ** -0.5, 257)
+    c.check(out, q, d ** -0.5)
+    for _ in range(3):
+        assert torch.equal(c.attend(q, d ** -0.5, 257), out)
+    c.check(c.attend(q, -0.3, 257), q, -0.3)
+
+
+@pytest.mark.parametrize("rows,cache,d", FULL)
+@pytest.mark.parametrize("m", [33, 41, 64])
+def test_trees_beside_idle_sequences(rows, cache, d, m):
+    rng = np.random.default_rng(m)
+    n = 3
+    c = Paged(cache, rows, [0, 601, 130] + [0] * IDLE, [m] * n + [0] * IDLE, kv_heads=2, group=4, d=d, seed=m)
+    c.fill()
+    c.table[1, 3:6] = -1
+    c.dev[0].copy_(torch.tensor(c.table))
+    parent = np.concatenate([[int(rng.integers(max(0, i - 9), i)) if i else -1 for i in range(m)] for _ in range(n)]).astype(np.int32)
+    q = c.random_rows(c.total, 8)
+    c.check(c.attend(q, d ** -0.5, m, parent), q, d ** -0.5, parent)
+    c.check(c.attend(q, 0.0, m, parent), q, 0.0, parent)
+
+
+@pytest.mark.parametrize("rows,cache,d", FULL)
+@pytest.mark.parametrize("tree", [False, True])
+@pytest.mark.parametrize("what", [math.nan, math.inf, -math.inf])
+def test_values_that_are_not_finite_beside_idle_sequences(rows, cache, d, tree, what):
+    """In front of the block, in it, and behind it on the last page; a sequence whose pages are all gone."""
+    m = 50
+    c = Paged(cache, rows, [700, 0, 90] + [0] * IDLE, [m, m, m] + [0] * IDLE, kv_heads=2, group=2, d=d, seed=m)
+    c.fill()
+    one = torch.tensor([0, 1], dtype=torch.int32, device="cuda")
+    for b, at, entry in ((0, 730, 3), (1, 20, d - 1)):
+        kr, vr = c.random_rows(1), c.random_rows(1)
+        vr[0, 1, entry] = what
+        c.kv.write(0, c.dev[0][b:b + 1].contiguous(), one, torch.tensor([at], dtype=torch.int32, device="cuda"), kr, vr)
+    kr, vr = c.random_rows(1), c.random_rows(1)
+    kr[0, 0, 1] = what                                                  # a key
+    c.kv.write(0, c.dev[0][0:1].contiguous(), one, torch.tensor([745], dtype=torch.int32, device="cuda"), kr, vr)
+    c.table[2] = -1
+    c.dev[0].copy_(torch.tensor(c.table))
+    parent = np.concatenate([[-1] + [i // 2 for i in range(m - 1)]] * 3).astype(np.int32) if tree else None
+    q = c.random_rows(c.total, 4)
+    with np.errstate(invalid="ignore"):
+        want = c.check(c.attend(q, 0.2, m, parent), q, 0.2, parent)
+    assert (want[2 * m:] == 0).all() and np.isfinite(want[:10]).all() and not np.isfinite(want).all()
+
+
 @pytest.mark.parametrize("rows,cache,d", SPREAD + [("bf16", "bf16", 64), ("bf16", "fp8", 128)])
 def test_attention_of_blocks_of_every_size_in_one_batch(rows, cache, d):
     """1 .. 70 rows times two query heads: the sizes where one way of doing it ends and another begins; rows in front of the first sequence and behind
