@@ -1,21 +1,70 @@
 // Attention of new rows over a paged KV cache.
 #include "csd_paged.h"
 
-// Any types and head sizes: one workgroup per (row, query head).  The four waves take 64 keys in turn, a key per lane for the scores;
-// for the products with the values the lanes are W features (the power of two from D up, 64 at most) of 64 / W keys at a time, eight such steps
-// requested together, the first eight along with the keys.  Running maximum, sum and output per wave are joined at the end.  Only keys
-// that the row attends are looked at in the second half, so that nothing else reaches it.  All arithmetic is in fp32.  Small models' calls are bound by
-// the chain rows -> page table -> keys and values (five rows of 4 heads of 16 over 32 cached keys, fp32: 10.1 -> 7.1 us with each of these
-// asked for at once).
+// Four consecutive elements of a pool's row as they are in memory.
+template <typename T> struct Raw4 {
+    uint32_t w[sizeof(T)];
+    __device__ __forceinline__ void load(const T *p) {
+        if constexpr (sizeof(T) == 4) *reinterpret_cast<u32x4 *>(w) = *reinterpret_cast<const u32x4 *>(p);
+        else if constexpr (sizeof(T) == 2) *reinterpret_cast<u32x2 *>(w) = *reinterpret_cast<const u32x2 *>(p);
+        else w[0] = *reinterpret_cast<const uint32_t *>(p);
+    }
+    __device__ __forceinline__ void get(float (&x)[4]) const {
+        if constexpr (sizeof(T) == 4) {
+#pragma unroll
+            for (int e = 0; e < 4; e++) x[e] = __uint_as_float(w[e]);
+        } else if constexpr (sizeof(T) == 2) {
+#pragma unroll
+            for (int e = 0; e < 4; e++) x[e] = __uint_as_float(e & 1 ? w[e / 2] & 0xFFFF0000u : w[e / 2] << 16);
+        } else {
+            const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[0], false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[0], true);
+            x[0] = lo[0];
+            x[1] = lo[1];
+            x[2] = hi[0];
+            x[3] = hi[1];
+        }
+    }
+};
+
+// sum over the 2^log_w neighbouring lanes, in each of them
+template <int CTRL>
+__device__ __forceinline__ float add_dpp(float a) {
+    return a + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(a), CTRL, 0xF, 0xF, false));
+}
+__device__ __forceinline__ float lanes_sum(float a, int log_w) {
+    if (log_w > 0) a = add_dpp<0xB1>(a);                     // lane ^ 1
+    if (log_w > 1) a = add_dpp<0x4E>(a);                     // lane ^ 2
+    if (log_w > 2) a = add_dpp<0x141>(a);                    // 7 - lane, of eight
+    if (log_w > 3) a = add_dpp<0x140>(a);                    // 15 - lane, of sixteen
+    if (log_w > 4) a += __shfl_xor(a, 16, 64);
+    if (log_w > 5) a += __shfl_xor(a, 32, 64);
+    return a;
+}
+
+// Any types and head sizes: one workgroup per (row, query head).  Its waves take 64 keys in turn.  For the products the lanes are W = 2^log_w pieces of four
+// features (the power of two from D / 4 up) of 64 / W keys at a time, eight such steps of keys and the first eight of values requested at once; for the
+// softmax a lane is a key.  Running maximum, sum and output per wave are joined at the end.  Only keys that the row attends are looked at.  All
+// arithmetic is in fp32.  Small models' calls are bound by the chain rows -> page table -> keys and values: so as many waves as the page table has
+// room for 64 keys each, four or eight.  (fp32: twelve rows of 4 heads of 64 over 761 keys 18 us, a tree of 41 rows over 445 11; with a lane per key in the scores and a
+// feature per lane behind them 63 and 38.  Five rows of 4 heads of 16 over 32 keys 7.4.)
+static constexpr int kAnyWaves = 8;
+
 template <typename TQ, typename TP>
-__global__ __launch_bounds__(256) void k_paged_attn_any(PagedAttn a, int log_w) {
-    __shared__ float s_q[256], s_o[4][256], s_m[4], s_l[4], s_w[4][64];
-    __shared__ size_t s_at[4][64];
+__global__ __launch_bounds__(64 * kAnyWaves) void k_paged_attn_any(PagedAttn a, int log_w) {
+    __shared__ float s_o[kAnyWaves][256], s_m[kAnyWaves], s_l[kAnyWaves], s_w[kAnyWaves][64];
+    __shared__ size_t s_at[kAnyWaves][64];
     const int row = blockIdx.x, head = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int waves = blockDim.x >> 6;
     const PagedPool &p = a.p;
     const int D = p.D, kvh = head / a.group;
-    const TQ *q = reinterpret_cast<const TQ *>(a.q) + (size_t)row * a.q_stride + (size_t)head * D;
-    const float q_mine = tid < D ? to_f32<TQ>(q[tid]) : 0.f;
+    const int per_step = 64 >> log_w, key_in = lane >> log_w, c = 4 * (lane & ((1 << log_w) - 1));
+    float q[4] = {0.f, 0.f, 0.f, 0.f};
+    if (c < D) {
+        const TQ *qp = reinterpret_cast<const TQ *>(a.q) + (size_t)row * a.q_stride + (size_t)head * D + c;
+        Raw4<TQ> raw;
+        raw.load(qp);
+        raw.get(q);
+    }
     // ---- the row's sequence
     PagedSeq s{0, 0, 0};
     int b = -1;
@@ -47,13 +96,10 @@ __global__ __launch_bounds__(256) void k_paged_attn_any(PagedAttn a, int log_w) 
             above |= 1ull << x;
         }
     }
-    if (tid < D) s_q[tid] = q_mine;
-    __syncthreads();
     constexpr float kLog2e = 1.44269504088896f;
-    const int per_step = 64 >> log_w, key_in = lane >> log_w, feature = lane & ((1 << log_w) - 1);
     float m_run = -INFINITY, l_run = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
     const int keys = min(s.t + i + 1, p.table_stride << p.page_shift);
-    for (int key0 = wave * 64; key0 < keys; key0 += 256) {
+    for (int key0 = wave * 64; key0 < keys; key0 += 64 * waves) {
         const int key = key0 + lane;
         int page = key < keys ? paged_page(p, b, key) : -1;
         if (a.parent && key >= s.t && !((above >> min(key - s.t, 63)) & 1ull)) page = -1;
@@ -62,44 +108,37 @@ __global__ __launch_bounds__(256) void k_paged_attn_any(PagedAttn a, int log_w) 
         if (!seen) continue;
         s_at[wave][lane] = at;
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        // values of steps st .. st + 7: element e of step j is feature 64 e + `feature` of key (st + j) * per_step + key_in
-        const int steps = min(64, keys - key0 + per_step - 1) >> (6 - log_w);
-        float v[8][4];
-        auto values = [&](int st) {
+        // step j: keys j * per_step + key_in of the 64
+        const int steps = (min(64, keys - key0) + per_step - 1) >> (6 - log_w);
+        auto has = [&](int j) { return j < steps && ((seen >> (j * per_step + key_in)) & 1ull); };
+        Raw4<TP> k[8], v[8];
+        auto request = [&](Raw4<TP> (&r)[8], const void *pool, int first) {
 #pragma unroll
             for (int j = 0; j < 8; j++) {
-                const int x = (st + j) * per_step + key_in;
-                const bool there = st + j < steps && x < 64 && ((seen >> (x & 63)) & 1ull);
-                const TP *vp = reinterpret_cast<const TP *>(p.v) + s_at[wave][x & 63] * D;
-#pragma unroll
-                for (int e = 0; e < 4; e++) {
-                    v[j][e] = 0.f;
-                    if (there && (e == 0 || D > 64 * e) && 64 * e + feature < D) {
-                        if constexpr (sizeof(TP) == 1) v[j][e] = __builtin_amdgcn_cvt_f32_fp8((int)vp[64 * e + feature], 0);
-                        else v[j][e] = to_f32<TP>(vp[64 * e + feature]);
-                    }
-                }
+                r[j] = Raw4<TP>{};
+                if (has(first + j) && c < D) r[j].load(reinterpret_cast<const TP *>(pool) + s_at[wave][(first + j) * per_step + key_in] * D + c);
             }
         };
-        values(0);
-        float v_scale = 1.f, score = -INFINITY;
-        if (page >= 0) {
-            const TP *kp = reinterpret_cast<const TP *>(p.k) + at * D;
-            float k_scale = 1.f;
-            if constexpr (sizeof(TP) == 1) {
+        request(k, p.k, 0);
+        request(v, p.v, 0);
+        float k_scale = 1.f, v_scale = 1.f;
+        if constexpr (sizeof(TP) == 1)
+            if (page >= 0) {
                 k_scale = pow2_of_byte(p.ks[at]);
                 v_scale = pow2_of_byte(p.vs[at]);
             }
-            float dot = 0.f;
-#pragma unroll 4
-            for (int c = 0; c < D; c += 8) {
-                float x[8];
-                load8<TP>(kp + c, x);
+        for (int first = 0; first < steps; first += 8) {
+            if (first) request(k, p.k, first);
 #pragma unroll
-                for (int e = 0; e < 8; e++) dot = fmaf(x[e], s_q[c + e], dot);
+            for (int j = 0; j < 8; j++) {
+                float x[4];
+                k[j].get(x);
+                const float dot = lanes_sum(fmaf(x[0], q[0], fmaf(x[1], q[1], fmaf(x[2], q[2], x[3] * q[3]))), log_w);
+                if (c == 0 && has(first + j)) s_w[wave][(first + j) * per_step + key_in] = dot;
             }
-            score = dot * k_scale * a.scale;
         }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        const float score = page >= 0 ? s_w[wave][lane] * k_scale * a.scale : -INFINITY;
         const float m_new = fmaxf(m_run, wave_max(score)), m_ref = m_new == -INFINITY ? 0.f : m_new;
         const float w = page >= 0 ? exp2f((score - m_ref) * kLog2e) : 0.f, fade = exp2f((m_run - m_ref) * kLog2e);
         l_run = l_run * fade + wave_sum(w);
@@ -108,25 +147,25 @@ __global__ __launch_bounds__(256) void k_paged_attn_any(PagedAttn a, int log_w) 
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 #pragma unroll
         for (int e = 0; e < 4; e++) o[e] *= fade;
-        for (int st = 0; st < steps; st += 8) {
-            if (st) values(st);
+        for (int first = 0; first < steps; first += 8) {
+            if (first) request(v, p.v, first);
 #pragma unroll
-            for (int j = 0; j < 8; j++) {
-                const int x = (st + j) * per_step + key_in;
-                if (st + j < steps && x < 64 && ((seen >> x) & 1ull)) {
-                    const float f = s_w[wave][x];
+            for (int j = 0; j < 8; j++)
+                if (has(first + j)) {
+                    const float f = s_w[wave][(first + j) * per_step + key_in];
+                    float x[4];
+                    v[j].get(x);
 #pragma unroll
-                    for (int e = 0; e < 4; e++) o[e] = fmaf(f, v[j][e], o[e]);
+                    for (int e = 0; e < 4; e++) o[e] = fmaf(f, x[e], o[e]);
                 }
-            }
         }
     }
-    for (int x = 32; x >= 1 << log_w; x >>= 1)               // (the lanes that hold the same feature)
+    for (int x = 32; x >= 1 << log_w; x >>= 1)               // (the lanes that hold the same features)
 #pragma unroll
         for (int e = 0; e < 4; e++) o[e] += __shfl_xor(o[e], x, 64);
     if (key_in == 0)
 #pragma unroll
-        for (int e = 0; e < 4; e++) s_o[wave][e * 64 + feature] = o[e];
+        for (int e = 0; e < 4; e++) s_o[wave][c + e] = o[e];
     if (lane == 0) {
         s_m[wave] = m_run;
         s_l[wave] = l_run;
@@ -134,10 +173,10 @@ __global__ __launch_bounds__(256) void k_paged_attn_any(PagedAttn a, int log_w) 
     __syncthreads();
     if (tid >= D) return;
     float m_all = s_m[0];
-    for (int w = 1; w < 4; w++) m_all = fmaxf(m_all, s_m[w]);
+    for (int w = 1; w < waves; w++) m_all = fmaxf(m_all, s_m[w]);
     if (m_all == -INFINITY) m_all = 0.f;
     float l = 0.f, x = 0.f;
-    for (int w = 0; w < 4; w++) {
+    for (int w = 0; w < waves; w++) {
         const float f = exp2f((s_m[w] - m_all) * kLog2e);
         l += f * s_l[w];
         x += f * s_o[w][tid];
@@ -154,8 +193,9 @@ __global__ __launch_bounds__(256) void k_paged_attn_any(PagedAttn a, int log_w) 
 template <typename TQ, typename TP>
 static void any_launch(const PagedAttn &a, hipStream_t st) {
     int log_w = 0;
-    while (log_w < 6 && (1 << log_w) < a.p.D) log_w++;
-    hipLaunchKernelGGL((k_paged_attn_any<TQ, TP>), dim3(a.r.rows, a.p.Hkv * a.group), dim3(256), 0, st, a, log_w);
+    while (4 << log_w < a.p.D) log_w++;
+    const int keys = a.p.table_stride << a.p.page_shift, waves = keys > 4 * 64 ? 8 : 4;
+    hipLaunchKernelGGL((k_paged_attn_any<TQ, TP>), dim3(a.r.rows, a.p.Hkv * a.group), dim3(64 * waves), 0, st, a, log_w);
 }
 
 int32_t csd_paged_attention_enqueue(const PagedAttn &a, int32_t pool_dtype, int32_t q_dtype, hipStream_t st) {
