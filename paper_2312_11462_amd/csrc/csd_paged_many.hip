@@ -488,8 +488,9 @@ void csd_paged_many_enqueue(const PagedAttn &a, int min_rows, int32_t pool_dtype
     // row tiles at most: full ones, and a last one per sequence
     const long long tiles = (long long)a.r.rows * a.group / CSD_PAGED_MANY_ROWS + a.r.B, items = tiles * a.p.Hkv;
     const long long keys = ((long long)a.p.table_stride << a.p.page_shift) / kKeys + 1 + CSD_PAGED_MANY_COST;      // (all key tiles are counted in 32 bits)
-    const bool shared = items <= CSD_PAGED_MANY_ITEMS && a.r.B <= CSD_PAGED_MANY_BATCH && items * keys < (1ll << 30);
-    if (!shared) return csd_paged_chunk_enqueue(a, min_rows, pool_dtype, st);
+    const bool fits = a.r.B <= CSD_PAGED_MANY_BATCH && items * keys < (1ll << 30);
+    if (!fits || (items > CSD_PAGED_MANY_ITEMS && (long long)a.max_rows * a.group >= CSD_PAGED_CHUNK_ROWS))
+        return csd_paged_chunk_enqueue(a, min_rows, pool_dtype, st);
     auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(CSD_PAGED_MANY_GRID), dim3(256), 0, st, a, min_rows); };
     const bool f8 = pool_dtype == CSD_DTYPE_FP8;
     if (a.p.D == 128) f8 ? launch(k_paged_attn_many<128, true>) : launch(k_paged_attn_many<128, false>);

@@ -535,7 +535,7 @@ def test_many_rows_in_and_out(rows, cache, d, kv_heads, n):
 
 @pytest.mark.parametrize("rows,cache,d", [("bf16", "bf16", 64), ("bf16", "fp8", 128), ("bf16", "fp8", 64), ("bf16", "bf16", 128)])
 def test_attention_of_more_sequences_than_share_their_keys(rows, cache, d):
-    """More than 512 sequences, and more row tiles than workgroups share; single tokens beside them, lengths of every kind."""
+    """More than 512 sequences; many row tiles of short blocks, and of longer ones; single tokens beside them, lengths of every kind."""
     rng = np.random.default_rng(d)
     cached, new = rng.integers(0, 70, 530), rng.choice([0, 1, 5, 9], 530)
     cached[7], new[7] = 300, 41
@@ -547,6 +547,10 @@ def test_attention_of_more_sequences_than_share_their_keys(rows, cache, d):
     c.fill()
     q = c.random_rows(c.total, 8)
     c.check(c.attend(q, d ** -0.5, 150), q, d ** -0.5)
+    c = Paged(cache, rows, [40, 0, 9], [200, 1, 130], kv_heads=96, group=4, d=d, page=32, seed=7)
+    c.fill()
+    q = c.random_rows(c.total, 384)
+    c.check(c.attend(q, d ** -0.5, 200), q, d ** -0.5)
 
 
 FULL = [("bf16", "bf16", 64), ("bf16", "bf16", 128), ("bf16", "fp8", 64), ("bf16", "fp8", 128)]
