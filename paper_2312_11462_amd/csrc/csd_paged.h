@@ -32,6 +32,27 @@ __device__ __forceinline__ PagedSeq paged_seq(const PagedRows &r, int b) {
     return PagedSeq{s, e - s, min(max(r.pos[b], 0), 0x3FFFFFFF)};
 }
 
+// Tree blocks (64 rows at most): the rows of the sequence's block that row `lane` continues, and itself, one bit each, by doubling the step up; a parent
+// outside [0, row) is row 0.
+__device__ __forceinline__ unsigned long long lane_of(unsigned long long v, int lane) {
+    return ((unsigned long long)(unsigned)__shfl((unsigned)(v >> 32), lane, 64) << 32) | (unsigned)__shfl((unsigned)v, lane, 64);
+}
+__device__ __forceinline__ unsigned long long paged_ancestors(const int32_t *parent, const PagedSeq &s, int lane) {
+    unsigned long long anc = 1ull << lane;
+    int up = 0;
+    if (lane < s.m && lane > 0) {
+        up = parent[s.start + lane];
+        if (up < 0 || up >= lane) up = 0;
+    }
+    anc |= 1ull << up;
+#pragma unroll
+    for (int k = 0; k < 6; k++) {
+        anc |= lane_of(anc, up);
+        up = __shfl(up, up, 64);
+    }
+    return anc;
+}
+
 // page of a position, -1: there is none
 __device__ __forceinline__ int paged_page(const PagedPool &p, int b, int pos) {
     const int i = pos >> p.page_shift;

@@ -86,16 +86,7 @@ __global__ __launch_bounds__(64 * kAnyWaves) void k_paged_attn_any(PagedAttn a, 
     if (b < 0 || b >= a.r.B) return;
     const int i = row - s.start;
     if (i < 0 || i >= min(s.m, a.max_rows)) return;
-    // the row's ancestors in its block, one bit each
-    unsigned long long above = ~0ull;
-    if (a.parent) {
-        above = 1ull << i;
-        for (int x = i; x > 0;) {
-            const int up = a.parent[s.start + x];
-            x = up >= 0 && up < x ? up : 0;
-            above |= 1ull << x;
-        }
-    }
+    const unsigned long long above = a.parent ? lane_of(paged_ancestors(a.parent, s, lane), i) : ~0ull;      // (trees: max_rows <= 64)
     constexpr float kLog2e = 1.44269504088896f;
     float m_run = -INFINITY, l_run = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
     const int keys = min(s.t + i + 1, p.table_stride << p.page_shift);

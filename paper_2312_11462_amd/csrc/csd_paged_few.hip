@@ -173,29 +173,11 @@ __global__ __launch_bounds__(256, 2) void k_paged_attn_few(PagedAttn a) {
         u32x4 qf[RT == 1 ? DH / 32 : 1];                      // (two row tiles: in LDS, where the waves' results will be; the registers are needed)
         u32x4 *s_q = reinterpret_cast<u32x4 *>(&s_o[0][0][0]) + lane;
         const uint32_t flip = a.scale < 0.f ? 0x80008000u : 0u;
-        unsigned long long anc = 1ull << lane;               // tree: ancestors of block row `lane`, by doubling the step up
-        if (a.parent) {
-            int up = 0;
-            if (lane < seq.m && lane > 0) {
-                up = a.parent[seq.start + lane];
-                if (up < 0 || up >= lane) up = 0;
-            }
-            anc |= 1ull << up;
-#pragma unroll
-            for (int i = 0; i < 6; i++) {
-                const unsigned lo = __shfl((unsigned)anc, up, 64), hi = __shfl((unsigned)(anc >> 32), up, 64);
-                anc |= ((unsigned long long)hi << 32) | lo;
-                up = __shfl(up, up, 64);
-            }
-        }
+        const unsigned long long anc = a.parent ? paged_ancestors(a.parent, seq, lane) : 0ull;
 #pragma unroll
         for (int rt = 0; rt < RT; rt++) {
             const int r = rt * 16 + col, i = token_of(r), h = r - i * a.group;
-            unsigned long long above = 0;
-            if (a.parent) {
-                const int src = min(i, 63);
-                above = ((unsigned long long)(unsigned)__shfl((unsigned)(anc >> 32), src, 64) << 32) | (unsigned)__shfl((unsigned)anc, src, 64);
-            }
+            const unsigned long long above = a.parent ? lane_of(anc, min(i, 63)) : 0ull;
             if (wave == 0 && g == 0) {                       // (needed where rows differ only: not worth registers)
                 s_limit[r] = seq.t + i;
                 s_above[r] = above;

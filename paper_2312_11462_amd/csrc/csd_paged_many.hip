@@ -152,23 +152,7 @@ __global__ __launch_bounds__(256, 2) void k_paged_attn_many(PagedAttn a, int min
     const bool live = wave * 32 + col < rows;
     const int limit = seq.t + i;                             // last position it attends
     unsigned long long above = 0;
-    if (a.parent) {                                          // ancestors of block row `lane`, by doubling the step up; then those of this lane's row
-        unsigned long long anc = 1ull << lane;
-        int up = 0;
-        if (lane < seq.m && lane > 0) {
-            up = a.parent[seq.start + lane];
-            if (up < 0 || up >= lane) up = 0;
-        }
-        anc |= 1ull << up;
-#pragma unroll
-        for (int k = 0; k < 6; k++) {
-            const unsigned lo = __shfl((unsigned)anc, up, 64), hi = __shfl((unsigned)(anc >> 32), up, 64);
-            anc |= ((unsigned long long)hi << 32) | lo;
-            up = __shfl(up, up, 64);
-        }
-        const int src = min(i, 63);
-        above = ((unsigned long long)(unsigned)__shfl((unsigned)(anc >> 32), src, 64) << 32) | (unsigned)__shfl((unsigned)anc, src, 64);
-    }
+    if (a.parent) above = lane_of(paged_ancestors(a.parent, seq, lane), min(i, 63));
     u32x4 qf[ST];
     {
         const bf16_t *q = reinterpret_cast<const bf16_t *>(a.q) + (size_t)(seq.start + i) * a.q_stride + (size_t)(kvh * a.group + hq) * DH + 8 * h;
