@@ -148,9 +148,7 @@ __global__ __launch_bounds__(512, 2) void k_paged_attn_chunk(PagedAttn a, int mi
                 v[0] = regs[S][x];
             }
 #pragma unroll
-            for (int w = 0; w < W; w++) {
-                s_tiles[buf][S ? v_piece<DH>(row, W * c_in + w) : k_piece<DH>(row, W * c_in + w)] = v[w];
-            }
+            for (int w = 0; w < W; w++) s_tiles[buf][S ? v_piece<DH>(row, W * c_in + w) : k_piece<DH>(row, W * c_in + w)] = v[w];
         }
     };
     // Where rows of the block, or places without a row, are among a tile's keys: values that no row attends are taken out of LDS again, and those
@@ -257,7 +255,7 @@ __global__ __launch_bounds__(512, 2) void k_paged_attn_chunk(PagedAttn a, int mi
             for (int e = 0; e < 32; e++)
                 if (!((m >> (8 * (e / 4) + e % 4)) & 1u)) st[e >> 4][e & 15] = -INFINITY;
         }
-                };
+    };
     // its weights, and their products with the values
     auto products = [&](int v_this) {
         int va_at = v_at + (2 + v_this) * PIECES * 16;
@@ -277,29 +275,29 @@ __global__ __launch_bounds__(512, 2) void k_paged_attn_chunk(PagedAttn a, int mi
         va[1] = read_v(1);
         float top = st[0][0];
 #pragma unroll
-                    for (int e = 1; e < 31; e += 2) top = fmaxf(fmaxf(st[e >> 4][e & 15], st[(e + 1) >> 4][(e + 1) & 15]), top);
-                    // (both halves of the lanes have the row's maximum; -inf: nothing to attend yet, a score of -inf is something)
-                    top = halves_max(sees ? fmaxf(fmaxf(top, st[1][15]) * scale, -3.0e38f) : -INFINITY);
-                    // The reference of the weights is 8 above the maximum when it is set, and moves when a score passes it: the outputs are seldom rescaled, and no
-                    // weight is above 1 (a sum of large values has the room that the formula's has).
-                    if (__any(top > m_run)) {
-                        const float m_new = top > m_run ? top + 8.f : m_run, fade = __builtin_amdgcn_exp2f(m_run - (m_new == -INFINITY ? 0.f : m_new));
-                        l_run *= fade;
-                        l_more *= fade;
+        for (int e = 1; e < 31; e += 2) top = fmaxf(fmaxf(st[e >> 4][e & 15], st[(e + 1) >> 4][(e + 1) & 15]), top);
+        // (both halves of the lanes have the row's maximum; -inf: nothing to attend yet, a score of -inf is something)
+        top = halves_max(sees ? fmaxf(fmaxf(top, st[1][15]) * scale, -3.0e38f) : -INFINITY);
+        // The reference of the weights is 8 above the maximum when it is set, and moves when a score passes it: the outputs are seldom rescaled, and no
+        // weight is above 1 (a sum of large values has the room that the formula's has).
+        if (__any(top > m_run)) {
+            const float m_new = top > m_run ? top + 8.f : m_run, fade = __builtin_amdgcn_exp2f(m_run - (m_new == -INFINITY ? 0.f : m_new));
+            l_run *= fade;
+            l_more *= fade;
 #pragma unroll
-                        for (int d = 0; d < DT; d++) acc[d] *= fade;
-                        m_run = m_new;
-                    }
-                    const float ref = m_run == -INFINITY ? 0.f : -m_run;
-                    u32x4 pw[4];                                     // weights of keys 16 u .. 16 u + 15
-                    auto weigh = [&](int e) {                        // elements e, e + 1
-                        const float w0 = __builtin_amdgcn_exp2f(fmaf(st[e >> 4][e & 15], scale, ref)), w1 = __builtin_amdgcn_exp2f(fmaf(st[e >> 4][(e + 1) & 15], scale, ref));
-                        l_run += w0;
-                        l_more += w1;
-                        pw[e >> 3][(e & 7) >> 1] = pack_bf16x2(w0, w1);
-                    };
+            for (int d = 0; d < DT; d++) acc[d] *= fade;
+            m_run = m_new;
+        }
+        const float ref = m_run == -INFINITY ? 0.f : -m_run;
+        u32x4 pw[4];                                         // weights of keys 16 u .. 16 u + 15
+        auto weigh = [&](int e) {                            // elements e, e + 1
+            const float w0 = __builtin_amdgcn_exp2f(fmaf(st[e >> 4][e & 15], scale, ref)), w1 = __builtin_amdgcn_exp2f(fmaf(st[e >> 4][(e + 1) & 15], scale, ref));
+            l_run += w0;
+            l_more += w1;
+            pw[e >> 3][(e & 7) >> 1] = pack_bf16x2(w0, w1);
+        };
 #pragma unroll
-                    for (int e = 0; e < 8; e += 2) weigh(e);
+        for (int e = 0; e < 8; e += 2) weigh(e);
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int x = 0; x < 4 * DT; x++) {                   // the next 16 keys' weights are made beside the products of these
