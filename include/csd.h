@@ -376,7 +376,7 @@ int32_t csd_paged_read(const csd_paged_kv *kv, int32_t layer, const int32_t *row
  * 16-byte aligned, not overlapping); n_heads a multiple of n_kv_heads, query head h reads key-value head h / (n_heads / n_kv_heads).
  * out = softmax(scale * q k^T) v, scores, maxima and sums in fp32; a row that has nothing to attend gives zeros, and what
  * a row does not attend never reaches it (not even infinities and NaN).  max_rows: at least the rows of the longest sequence of the batch
- * (a longer one is cut to it), 1 <= max_rows; CSD_ESHAPE for trees with max_rows > 64.
+ * (a longer one is cut to it: its rows behind are left as they were; the kernels are chosen by it), 1 <= max_rows; CSD_ESHAPE for trees with max_rows > 64.
  * workspace: device, 256-byte aligned, CSD_PAGED_WORKSPACE_BYTES, of which the first CSD_PAGED_WORKSPACE_ZERO_BYTES are zeroed before its first use;
  * every call leaves them zeroed.  Calls that share it must not overlap.
  */

@@ -367,8 +367,8 @@ class PagedKv:
 
     def attention(self, layer, table, row_start, cache_len, q, scale, max_rows=None, parent=None, out=None):
         """csd_paged_attention: q [rows][heads][head dim] -> out, contiguous and of q's type; rows of no sequence are left as they are
-        (undefined in a new tensor).  max_rows: at least the rows of the longest sequence of the batch (default: all rows of the call);
-        parent: tree blocks."""
+        (undefined in a new tensor).  max_rows: at least the rows of the longest sequence of the batch (default: all rows of the call;
+        the kernels are chosen by it, so single tokens and short blocks are served best where it is given); parent: tree blocks."""
         dev, i32, d = self._dev, torch.int32, self.head_dim
         B, n = table.shape
         rows, heads, width = q.shape

@@ -176,13 +176,14 @@ struct PagedParts {
     }
     // The last one joins the parts, in their order: out = sum f_k o_k / sum f_k l_k with f_k = 2^(m_k - max m).  lds: (2 * parts + 1) * R floats.  `out` of a row:
     // 256 threads, four features each.  P such places of a thread and K parts are requested at once, the first of them along with the maxima:
-    // each round of requests is a trip to memory.
+    // each round of requests is a trip to memory (two rows of 4 heads of 64 over 3000 keys, up to twenty parts: 11.6 us by fours, 10.5 by sixteen; as
+    // many in flight again spill).
     template <typename OUT>
     __device__ __forceinline__ void join(void *ws, float *lds, int rows, OUT out) const {
         int tid = threadIdx.x;
         asm volatile("" : "+v"(tid));                        // (what follows from it is made here, not kept in registers from the kernel's start on)
         float *fade = lds, *sum = lds + parts * R, *inv = lds + 2 * parts * R;
-        constexpr int C = DH / 4, P = R * C / 256 < 1 ? 1 : R * C / 256 > 4 ? 4 : R * C / 256, K = 4;
+        constexpr int C = DH / 4, P = R * C / 256 < 1 ? 1 : R * C / 256 > 4 ? 4 : R * C / 256, K = 16 / P;
         f32x4 v[P][K];
         auto request = [&](int x0, int k0) {
             const int voff = ((x0 + tid) / C * part_stride<DH>() + 4 * (tid % C)) * 4;
