@@ -614,6 +614,24 @@ def test_values_that_are_not_finite_beside_idle_sequences(rows, cache, d, tree, 
 
 
 @pytest.mark.parametrize("rows,cache,d", SPREAD + [("bf16", "bf16", 64), ("bf16", "fp8", 128)])
+@pytest.mark.parametrize("most,idle", [(1, 0), (5, 0), (40, 0), (40, IDLE)])
+def test_sequences_longer_than_said_are_cut(rows, cache, d, most, idle):
+    """Their first rows are what they are, the others stay as they were."""
+    new = [60, 3, 41, 1]
+    c = Paged(cache, rows, [100, 0, 31, 7] + [0] * idle, new + [0] * idle, kv_heads=2, group=2, d=d, seed=most)
+    c.fill()
+    q = c.random_rows(c.total, 4)
+    out = torch.full_like(q, 3.0)
+    c.attend(q, d ** -0.5, most, out=out)
+    kept = np.concatenate([np.arange(m) < most for m in new])
+    assert (out[torch.tensor(~kept).cuda()] == 3).all()
+    whole = c.attend(q, d ** -0.5, 60)
+    c.check(whole, q, d ** -0.5)
+    whole[torch.tensor(kept).cuda()] = out[torch.tensor(kept).cuda()]
+    c.check(whole, q, d ** -0.5)
+
+
+@pytest.mark.parametrize("rows,cache,d", SPREAD + [("bf16", "bf16", 64), ("bf16", "fp8", 128)])
 def test_attention_of_blocks_of_every_size_in_one_batch(rows, cache, d):
     """1 .. 70 rows times two query heads: the sizes where one way of doing it ends and another begins; rows in front of the first sequence and behind
     the last stay as they are."""
