@@ -380,10 +380,9 @@ class PagedKv:
             self._check(table=(table, B * n), row_start=(row_start, B + 1), cache_len=(cache_len, B), q=(q, (rows, heads, d)))
         if out is None:
             out = torch.empty(rows, heads, d, dtype=dtype, device=self._device)
-        else:
+        elif not (out.dtype is dtype and out.shape == q.shape and out.get_device() == dev and out.is_contiguous()):
             self._check(q=(q, (rows, heads, d)), out=(out, (rows, heads, d)))
-            if not out.is_contiguous():
-                raise ValueError("out: a contiguous tensor is required")
+            raise ValueError("out: a contiguous tensor is required")
         up = None
         if parent is not None:
             self._check(parent=(parent, rows))
