@@ -114,6 +114,7 @@ __global__ __launch_bounds__(256, 2) void k_paged_attn_few(PagedAttn a) {
     PagedSeq s0;
     const int n0 = seq_of(lane, s0);                         // the first 64 sequences stay in registers
     int sum = n0, longest = n0;
+#pragma unroll 4
     for (int b0 = 64; b0 < a.r.B; b0 += 64) {
         PagedSeq s;
         const int n = seq_of(b0 + lane, s);
@@ -135,35 +136,48 @@ __global__ __launch_bounds__(256, 2) void k_paged_attn_few(PagedAttn a) {
     const PagedShares shares(T, n_wg);
     const int u_end = shares.first(blockIdx.x + 1);
 
-    for (int u = shares.first(blockIdx.x); u < u_end;) {
-        // ---- the item of tile u: sequence b, key-value head kvh, tiles t0 .. t1 of its n
-        const int u0 = u;
-        int b = 0, n = 0, before = 0;
-        PagedSeq seq{0, 0, 0};
-        for (int b0 = 0; b0 < a.r.B; b0 += 64) {
-            PagedSeq s = s0;
-            const int nn = b0 == 0 ? n0 : seq_of(b0 + lane, s);
-            int incl = nn * p.Hkv;
+    // The sequences of a share follow one another: 64 of them are held (lane x: sequence block + x), lane j is the one at hand, whose tiles begin at `before`.
+    int u = shares.first(blockIdx.x), block = 0, j = 0, before = 0, n = 0;
+    PagedSeq held = s0;
+    int held_n = n0;
+    for (;; block += 64) {
+        if (block >= a.r.B) return;                          // (the lengths changed while they were read)
+        if (block) held_n = seq_of(block + lane, held);
+        int incl = held_n * p.Hkv;
 #pragma unroll
-            for (int o = 1; o < 64; o <<= 1) {
-                const int x = __shfl_up(incl, o, 64);
-                if (lane >= o) incl += x;
-            }
-            const unsigned long long past = __ballot(before + incl > u);
-            if (past) {
-                const int j = __ffsll((long long)past) - 1;
-                b = b0 + j;
-                n = __builtin_amdgcn_readlane(nn, j);
-                before += __builtin_amdgcn_readlane(incl, j) - n * p.Hkv;
-                seq = PagedSeq{__builtin_amdgcn_readlane(s.start, j), __builtin_amdgcn_readlane(s.m, j), __builtin_amdgcn_readlane(s.t, j)};
-                break;
-            }
-            before += __builtin_amdgcn_readlane(incl, 63);
+        for (int o = 1; o < 64; o <<= 1) {
+            const int x = __shfl_up(incl, o, 64);
+            if (lane >= o) incl += x;
         }
-        if (n == 0 || u - before >= n * p.Hkv) return;       // (the lengths changed while they were read)
-        const int kvh = (u - before) / n, item = before + kvh * n + kCost;     // (where its tiles begin)
-        u = min(item - kCost + n, u_end);
-        n -= kCost;
+        const unsigned long long past = __ballot(before + incl > u);
+        if (past) {
+            j = __ffsll((long long)past) - 1;
+            n = __builtin_amdgcn_readlane(held_n, j);
+            before += __builtin_amdgcn_readlane(incl, j) - n * p.Hkv;
+            break;
+        }
+        before += __builtin_amdgcn_readlane(incl, 63);
+    }
+
+    while (u < u_end) {
+        // ---- the item of tile u: sequence b, key-value head kvh, tiles t0 .. t1 of its n
+        while (u >= before + n * p.Hkv) {                    // the next sequence that has tiles
+            before += n * p.Hkv;
+            const unsigned long long next = __ballot(held_n > 0) & ~((2ull << j) - 1);
+            if (next) {
+                j = __ffsll((long long)next) - 1;
+            } else {
+                block += 64;
+                if (block >= a.r.B) return;
+                held_n = seq_of(block + lane, held);
+                j = 0;
+            }
+            n = __builtin_amdgcn_readlane(held_n, j);
+        }
+        const int b = block + j;
+        const PagedSeq seq{__builtin_amdgcn_readlane(held.start, j), __builtin_amdgcn_readlane(held.m, j), __builtin_amdgcn_readlane(held.t, j)};
+        const int u0 = u, kvh = (u - before) / n, item = before + kvh * n + kCost, tiles = n - kCost;      // (where its tiles begin, how many there are)
+        u = min(item + tiles, u_end);
         const int t0 = max(u0 - item, 0), t1 = u - item;
         if (t0 >= t1) continue;                              // (the share ends before the item's tiles begin)
         const int len = min(seq.t + seq.m, cap), rows = seq.m * a.group;
@@ -435,7 +449,7 @@ __global__ __launch_bounds__(256, 2) void k_paged_attn_few(PagedAttn a) {
                 for (int i = 0; i < 4; i++) s_o[wave][rt * 16 + col][F * (4 * g + i) + j] = acc[rt][j][i];
         }
         __syncthreads();
-        const int w_first = shares.owner(item), w_last = shares.owner(item + n - 1);
+        const int w_first = shares.owner(item), w_last = shares.owner(item + tiles - 1);
         const bool split = w_first != w_last;
         const PagedParts<DH, R> parts(a.ws, CSD_PAGED_FEW_GRID, w_first, w_last - w_first + 1);
         auto out_row = [&](int r) {
