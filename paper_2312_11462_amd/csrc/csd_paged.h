@@ -262,14 +262,18 @@ void csd_paged_few_enqueue(const PagedAttn &a, int rows, int32_t pool_dtype, hip
 #define CSD_PAGED_MANY_COST 4        /* what an item costs besides its keys, in such tiles */
 #define CSD_PAGED_MANY_PARTS 14      /* parts of an item at most */
 #define CSD_PAGED_MANY_GRID 512      /* two workgroups per compute unit */
-#define CSD_PAGED_MANY_BATCH 512     /* sequences at most */
-// With more items (row tiles times key-value heads) than this, and sequences of as many rows as the second (times the query heads that share keys; fewer leave more than
+#define CSD_PAGED_MANY_BATCH 512     /* sequences that take part at most */
+// With more items (row tiles times key-value heads, as far as the host can tell) than this, and sequences of as many rows as the second (times the query heads that share keys; fewer leave more than
 // a quarter of the workgroups' rows idle), csd_paged_chunk.hip takes over, a workgroup of 256 rows per item.  us here and there, heads of 128 in bf16: 8 x 4 heads, 40 sequences of
 // 64 rows over 0 to 3000 keys, 960 items, 123 and 142; 5 of 300 rows, 32 heads, 512 items, 100 and 119; 2 of 2048 rows, 8 x 4 heads, 1040 items, 526 and 418; 42 of 328
 // rows, 8 heads, 1200 items, 119 and 134; 8 of 512 rows, 32 heads, 1280 items, 161 and 146; trees of 41 rows, 32 heads, 1856 items, 123 and 168.
 #define CSD_PAGED_MANY_ITEMS 1024
 #define CSD_PAGED_CHUNK_ROWS 384
 static_assert(CSD_PAGED_COUNTER_BYTES + 2ull * CSD_PAGED_MANY_GRID * CSD_PAGED_MANY_ROWS * 132 * 4 <= CSD_PAGED_WORKSPACE_BYTES, "");
-// min_rows: sequences of so many rows or fewer are another kernel's.
+// min_rows: sequences of so many rows (times the query heads that share keys) or fewer are another kernel's.  How many can have more:
+static inline long long csd_paged_batch(const PagedAttn &a, int min_rows) {
+    const long long most = (long long)a.r.rows * a.group / (min_rows + 1);
+    return most < a.r.B ? most : a.r.B;
+}
 void csd_paged_many_enqueue(const PagedAttn &a, int min_rows, int32_t pool_dtype, hipStream_t st);
 void csd_paged_chunk_enqueue(const PagedAttn &a, int min_rows, int32_t pool_dtype, hipStream_t st);

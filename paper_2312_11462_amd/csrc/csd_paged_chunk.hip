@@ -380,8 +380,8 @@ __global__ __launch_bounds__(512, 2) void k_paged_attn_chunk(PagedAttn a, int mi
 }
 
 void csd_paged_chunk_enqueue(const PagedAttn &a, int min_rows, int32_t pool_dtype, hipStream_t st) {
-    // row tiles at most: full ones, and a last one per sequence
-    const long long items = ((long long)a.r.rows * a.group / kChunkRows + a.r.B) * a.p.Hkv;
+    // row tiles at most: full ones, and a last one per sequence that takes part
+    const long long items = ((long long)a.r.rows * a.group / kChunkRows + csd_paged_batch(a, min_rows)) * a.p.Hkv;
     auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)items), dim3(512), 0, st, a, min_rows); };
     const bool f8 = pool_dtype == CSD_DTYPE_FP8;
     if (a.p.D == 128) f8 ? launch(k_paged_attn_chunk<128, true>) : launch(k_paged_attn_chunk<128, false>);

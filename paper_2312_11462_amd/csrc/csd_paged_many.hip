@@ -29,7 +29,8 @@ __global__ __launch_bounds__(256, 2) void k_paged_attn_many(PagedAttn a, int min
     u32x4(&s_k)[2][PIECES] = *reinterpret_cast<u32x4(*)[2][PIECES]>(&s_tiles[0]), (&s_v)[2][PIECES] = *reinterpret_cast<u32x4(*)[2][PIECES]>(&s_tiles[2]);
     __shared__ float s_max[BM], s_sum[BM];
     __shared__ int s_odd, s_last;
-    __shared__ int s_start[CSD_PAGED_MANY_BATCH], s_m[CSD_PAGED_MANY_BATCH], s_t[CSD_PAGED_MANY_BATCH], s_units[CSD_PAGED_MANY_BATCH];
+    __shared__ int s_b[CSD_PAGED_MANY_BATCH], s_start[CSD_PAGED_MANY_BATCH], s_m[CSD_PAGED_MANY_BATCH], s_t[CSD_PAGED_MANY_BATCH], s_units[CSD_PAGED_MANY_BATCH];
+    __shared__ int s_count[4];
     const PagedPool &p = a.p;
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, col = lane & 31, h = lane >> 5;
     const int cap = p.table_stride << p.page_shift;
@@ -51,15 +52,31 @@ __global__ __launch_bounds__(256, 2) void k_paged_attn_many(PagedAttn a, int min
         return x;
     };
 
-    // ---- this workgroup's share
-    for (int b = tid; b < a.r.B; b += 256) {
+    // ---- the sequences that take part, in order
+    int batch = 0;
+    for (int b0 = 0; b0 < a.r.B; b0 += 256) {
         PagedSeq s;
-        s_m[b] = seq_of(b, s) ? s.m : 0;
-        s_t[b] = s.t;
-        s_start[b] = s.start;
+        const bool in = seq_of(b0 + tid, s) > 0;
+        const unsigned long long all = __ballot(in);
+        if (lane == 0) s_count[wave] = __popcll(all);
+        __syncthreads();
+        int at = batch + __popcll(all & ((1ull << lane) - 1));
+        for (int w = 0; w < 4; w++) {
+            if (w < wave) at += s_count[w];
+            batch += s_count[w];
+        }
+        if (in && at < CSD_PAGED_MANY_BATCH) {
+            s_b[at] = b0 + tid;
+            s_m[at] = s.m;
+            s_t[at] = s.t;
+            s_start[at] = s.start;
+        }
+        __syncthreads();
     }
-    __syncthreads();
-    for (int b = tid / 8; b < a.r.B; b += 32) {              // eight lanes per sequence
+    batch = min(__builtin_amdgcn_readfirstlane(batch), CSD_PAGED_MANY_BATCH);
+
+    // ---- this workgroup's share
+    for (int b = tid / 8; b < batch; b += 32) {              // eight lanes per sequence
         const int m = s_m[b], t = s_t[b], n = (m * a.group + BM - 1) / BM;
         int sum = 0;
         for (int rt = tid % 8; rt < n; rt += 8) sum += COST + row_tile_keys(rt, m, t, a.group, cap);
@@ -69,9 +86,9 @@ __global__ __launch_bounds__(256, 2) void k_paged_attn_many(PagedAttn a, int min
     }
     __syncthreads();
     int sum = 0, longest = 0;
-    for (int b = lane; b < a.r.B; b += 64) {
+    for (int b = lane; b < batch; b += 64) {
         sum += s_units[b];
-        if (s_m[b]) longest = max(longest, COST + (min(s_t[b] + s_m[b], cap) + kKeys - 1) / kKeys);
+        longest = max(longest, COST + (min(s_t[b] + s_m[b], cap) + kKeys - 1) / kKeys);
     }
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) {
@@ -93,21 +110,22 @@ __global__ __launch_bounds__(256, 2) void k_paged_attn_many(PagedAttn a, int min
 
     while (u < u_end) {
     // ---- the item: rows rt * BM .. of sequence b, key-value head kvh, key tiles kt0 .. kt1 of its n_kt
-    int b = -1, before = 0;
-    for (int b0 = 0; b0 < a.r.B; b0 += 64) {
-        const int x = b0 + lane < a.r.B ? s_units[b0 + lane] * p.Hkv : 0, incl = scan(x);
+    int at = -1, before = 0;
+    for (int b0 = 0; b0 < batch; b0 += 64) {
+        const int x = b0 + lane < batch ? s_units[b0 + lane] * p.Hkv : 0, incl = scan(x);
         const unsigned long long past = __ballot(before + incl > u);
         if (past) {
             const int j = __ffsll((long long)past) - 1;
-            b = b0 + j;
+            at = b0 + j;
             before += __builtin_amdgcn_readlane(incl, j) - __builtin_amdgcn_readlane(x, j);
             break;
         }
         before += __builtin_amdgcn_readlane(incl, 63);
     }
-    if (b < 0) return;                                       // (the lengths changed while they were read)
-    const PagedSeq seq{__builtin_amdgcn_readfirstlane(s_start[b]), __builtin_amdgcn_readfirstlane(s_m[b]), __builtin_amdgcn_readfirstlane(s_t[b])};
-    const int units = __builtin_amdgcn_readfirstlane(s_units[b]), n = (seq.m * a.group + BM - 1) / BM;
+    if (at < 0) return;                                      // (the lengths changed while they were read)
+    const PagedSeq seq{__builtin_amdgcn_readfirstlane(s_start[at]), __builtin_amdgcn_readfirstlane(s_m[at]), __builtin_amdgcn_readfirstlane(s_t[at])};
+    const int b = __builtin_amdgcn_readfirstlane(s_b[at]);
+    const int units = __builtin_amdgcn_readfirstlane(s_units[at]), n = (seq.m * a.group + BM - 1) / BM;
     const int kvh = (u - before) / units;
     if (kvh >= p.Hkv) return;
     int left = u - before - kvh * units;
@@ -469,12 +487,14 @@ __global__ __launch_bounds__(256, 2) void k_paged_attn_many(PagedAttn a, int min
 }
 
 void csd_paged_many_enqueue(const PagedAttn &a, int min_rows, int32_t pool_dtype, hipStream_t st) {
-    // row tiles at most: full ones, and a last one per sequence
-    const long long tiles = (long long)a.r.rows * a.group / CSD_PAGED_MANY_ROWS + a.r.B, items = tiles * a.p.Hkv;
+    // row tiles at most: full ones, and a last one per sequence that takes part
+    const long long rows = (long long)a.r.rows * a.group, batch = csd_paged_batch(a, min_rows), items = (rows / CSD_PAGED_MANY_ROWS + batch) * a.p.Hkv;
     const long long keys = ((long long)a.p.table_stride << a.p.page_shift) / kKeys + 1 + CSD_PAGED_MANY_COST;      // (all key tiles are counted in 32 bits)
-    const bool fits = a.r.B <= CSD_PAGED_MANY_BATCH && items * keys < (1ll << 30);
-    if (!fits || (items > CSD_PAGED_MANY_ITEMS && (long long)a.max_rows * a.group >= CSD_PAGED_CHUNK_ROWS))
-        return csd_paged_chunk_enqueue(a, min_rows, pool_dtype, st);
+    const bool fits = batch <= CSD_PAGED_MANY_BATCH && items * keys < (1ll << 30);
+    // row tiles if some sequences have max_rows rows and the others one
+    const long long most = a.max_rows, full = most > 1 ? (a.r.rows - (long long)a.r.B + most - 2) / (most - 1) : a.r.B;
+    const long long likely = (full * most * a.group / CSD_PAGED_MANY_ROWS + full) * a.p.Hkv;
+    if (!fits || (likely > CSD_PAGED_MANY_ITEMS && most * a.group >= CSD_PAGED_CHUNK_ROWS)) return csd_paged_chunk_enqueue(a, min_rows, pool_dtype, st);
     auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(CSD_PAGED_MANY_GRID), dim3(256), 0, st, a, min_rows); };
     const bool f8 = pool_dtype == CSD_DTYPE_FP8;
     if (a.p.D == 128) f8 ? launch(k_paged_attn_many<128, true>) : launch(k_paged_attn_many<128, false>);

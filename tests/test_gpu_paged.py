@@ -553,16 +553,29 @@ def test_attention_of_more_sequences_than_share_their_keys(rows, cache, d):
     c.check(c.attend(q, d ** -0.5, 200), q, d ** -0.5)
 
 
+@pytest.mark.parametrize("rows,cache,d", [("bf16", "bf16", 64), ("bf16", "bf16", 128), ("bf16", "fp8", 64), ("bf16", "fp8", 128)])
+def test_chunks_far_apart_in_a_large_batch(rows, cache, d):
+    """Hundreds of single tokens, and sequences without rows, between the few sequences of many rows."""
+    rng = np.random.default_rng(d)
+    cached, new = rng.integers(0, 60, 1300), (rng.random(1300) < 0.7).astype(int)
+    for b, t, m in ((5, 400, 70), (300, 0, 33), (640, 1000, 129), (1299, 10, 17)):
+        cached[b], new[b] = t, m
+    c = Paged(cache, rows, cached, new, kv_heads=2, d=d, seed=12)
+    c.fill()
+    q = c.random_rows(c.total, 2)
+    c.check(c.attend(q, d ** -0.5, 129), q, d ** -0.5)
+
+
 FULL = [("bf16", "bf16", 64), ("bf16", "bf16", 128), ("bf16", "fp8", 64), ("bf16", "fp8", 128)]
-IDLE = 520                                                              # sequences without rows: so many that the keys are not shared out
+MORE = 520                                                              # short sequences beside the ones at hand: too many for the keys to be shared out
 
 
 @pytest.mark.parametrize("rows,cache,d", FULL)
 @pytest.mark.parametrize("page", [16, 128])
-def test_chunks_beside_idle_sequences(rows, cache, d, page):
+def test_chunks_beside_many_short_ones(rows, cache, d, page):
     """Whole workgroups of rows: lengths of one tile to fifty, row counts around a wave and a workgroup, negative scales, rows in a wider buffer."""
     cached, new = [3000, 3, 1500, 1023, 64, 0, 447, 512], [130, 129, 20, 64, 1, 257, 65, 16]
-    c = Paged(cache, rows, cached + [0] * IDLE, new + [0] * IDLE, kv_heads=2, group=2, d=d, page=page, seed=page)
+    c = Paged(cache, rows, cached + [0] * MORE, new + [9] * MORE, kv_heads=2, group=2, d=d, page=page, seed=page)
     c.fill()
     wide = torch.randn(c.total, 4 * d + 24, device="cuda").to(TORCH[rows])
     q = wide[:, 8:8 + 4 * d].unflatten(1, (4, d))
@@ -575,14 +588,14 @@ def test_chunks_beside_idle_sequences(rows, cache, d, page):
 
 @pytest.mark.parametrize("rows,cache,d", FULL)
 @pytest.mark.parametrize("m", [33, 41, 64])
-def test_trees_beside_idle_sequences(rows, cache, d, m):
+def test_trees_beside_many_short_ones(rows, cache, d, m):
     rng = np.random.default_rng(m)
     n = 3
-    c = Paged(cache, rows, [0, 601, 130] + [0] * IDLE, [m] * n + [0] * IDLE, kv_heads=2, group=4, d=d, seed=m)
+    c = Paged(cache, rows, [0, 601, 130] + [0] * MORE, [m] * n + [5] * MORE, kv_heads=2, group=4, d=d, seed=m)
     c.fill()
     c.table[1, 3:6] = -1
     c.dev[0].copy_(torch.tensor(c.table))
-    parent = np.concatenate([[int(rng.integers(max(0, i - 9), i)) if i else -1 for i in range(m)] for _ in range(n)]).astype(np.int32)
+    parent = np.concatenate([[int(rng.integers(max(0, i - 9), i)) if i else -1 for i in range(m)] for _ in range(n)] + [[-1, 0, 0, 1, 3]] * MORE).astype(np.int32)
     q = c.random_rows(c.total, 8)
     c.check(c.attend(q, d ** -0.5, m, parent), q, d ** -0.5, parent)
     c.check(c.attend(q, 0.0, m, parent), q, 0.0, parent)
@@ -591,10 +604,10 @@ def test_trees_beside_idle_sequences(rows, cache, d, m):
 @pytest.mark.parametrize("rows,cache,d", FULL)
 @pytest.mark.parametrize("tree", [False, True])
 @pytest.mark.parametrize("what", [math.nan, math.inf, -math.inf])
-def test_values_that_are_not_finite_beside_idle_sequences(rows, cache, d, tree, what):
+def test_values_that_are_not_finite_beside_many_short_ones(rows, cache, d, tree, what):
     """In front of the block, in it, and behind it on the last page; a sequence whose pages are all gone."""
     m = 50
-    c = Paged(cache, rows, [700, 0, 90] + [0] * IDLE, [m, m, m] + [0] * IDLE, kv_heads=2, group=2, d=d, seed=m)
+    c = Paged(cache, rows, [700, 0, 90] + [0] * MORE, [m, m, m] + [9] * MORE, kv_heads=2, group=2, d=d, seed=m)
     c.fill()
     one = torch.tensor([0, 1], dtype=torch.int32, device="cuda")
     for b, at, entry in ((0, 730, 3), (1, 20, d - 1)):
@@ -606,19 +619,19 @@ def test_values_that_are_not_finite_beside_idle_sequences(rows, cache, d, tree, 
     c.kv.write(0, c.dev[0][0:1].contiguous(), one, torch.tensor([745], dtype=torch.int32, device="cuda"), kr, vr)
     c.table[2] = -1
     c.dev[0].copy_(torch.tensor(c.table))
-    parent = np.concatenate([[-1] + [i // 2 for i in range(m - 1)]] * 3).astype(np.int32) if tree else None
+    parent = np.concatenate([[-1] + [i // 2 for i in range(m - 1)]] * 3 + [np.arange(9) - 1] * MORE).astype(np.int32) if tree else None
     q = c.random_rows(c.total, 4)
     with np.errstate(invalid="ignore"):
         want = c.check(c.attend(q, 0.2, m, parent), q, 0.2, parent)
-    assert (want[2 * m:] == 0).all() and np.isfinite(want[:10]).all() and not np.isfinite(want).all()
+    assert (want[2 * m:3 * m] == 0).all() and np.isfinite(want[:10]).all() and not np.isfinite(want).all()
 
 
 @pytest.mark.parametrize("rows,cache,d", SPREAD + [("bf16", "bf16", 64), ("bf16", "fp8", 128)])
-@pytest.mark.parametrize("most,idle", [(1, 0), (5, 0), (40, 0), (40, IDLE)])
-def test_sequences_longer_than_said_are_cut(rows, cache, d, most, idle):
+@pytest.mark.parametrize("most,others", [(1, 0), (5, 0), (40, 0), (40, MORE)])
+def test_sequences_longer_than_said_are_cut(rows, cache, d, most, others):
     """Their first rows are what they are, the others stay as they were."""
-    new = [60, 3, 41, 1]
-    c = Paged(cache, rows, [100, 0, 31, 7] + [0] * idle, new + [0] * idle, kv_heads=2, group=2, d=d, seed=most)
+    new = [60, 3, 41, 1] + [9] * others
+    c = Paged(cache, rows, [100, 0, 31, 7] + [0] * others, new, kv_heads=2, group=2, d=d, seed=most)
     c.fill()
     q = c.random_rows(c.total, 4)
     out = torch.full_like(q, 3.0)
