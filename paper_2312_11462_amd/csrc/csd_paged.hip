@@ -77,6 +77,20 @@ __device__ __forceinline__ void store8_past(T *p, const float (&x)[8]) {
     for (int i = 0; i < (int)sizeof(T) / 2; i++) __builtin_nontemporal_store(reinterpret_cast<u32x4 *>(t)[i], reinterpret_cast<u32x4 *>(p) + i);
 }
 
+// Where to begin to look for the sequence of a row, 64 sequences at a time: all those before end at or before it (4096 sequences a step; uniform in the
+// wave; 1024 single rows in, 8 heads of 128: 8.2 -> 6.4 us).
+__device__ __forceinline__ int paged_block(const PagedRows &r, int row) {
+    const int lane = threadIdx.x & 63;
+    int b0 = 0;
+    for (int g = 0; g + 64 < r.B; g += 4096) {
+        const int e = g + (lane + 1) * 64;
+        const int n = __popcll(__ballot(e <= r.B && r.row_start[min(e, r.B)] <= row));
+        b0 = g + 64 * n;
+        if (n < 64) break;
+    }
+    return b0;
+}
+
 // How the moves of rows are laid out.  A row of one head belongs to W lanes (W = 2^log_w: the power of two from D / 8 up), eight elements per lane, so its
 // maximum stays inside the lanes.  A wave takes 64 / W consecutive rows of U heads: in the pool consecutive rows of a head lie one behind
 // the other, their scale bytes too (with a wave on one row of 64 / W heads every scale byte was a store of its own: a prompt of 8198 rows of 32 heads of
@@ -91,8 +105,8 @@ __device__ __forceinline__ RowPlace row_place(const PagedPool &p, const PagedRow
     const int lane = threadIdx.x & 63;
     // the sequence of each row of the wave: how many sequences end at or before it (64 ends at a time; the sequences of a wave's rows are
     // mostly the same)
-    int b = 0;
-    for (int b0 = 0; b0 < r.B; b0 += 64) {
+    int b = paged_block(r, first);
+    for (int b0 = b; b0 < r.B; b0 += 64) {
         const int end = b0 + lane < r.B ? r.row_start[b0 + lane + 1] : 0x7FFFFFFF;
         const int before = __popcll(__ballot(end <= first));
         b += before;

@@ -203,6 +203,24 @@ def test_rows_without_a_place_and_rows_of_no_sequence():
     assert (out[0][pad + 16:pad + 20] == 0).all() and (out[0][pad + 26:pad + 50] == 0).all()
 
 
+@pytest.mark.parametrize("rows,cache", [("bf16", "fp8"), ("fp32", "fp32")])
+def test_rows_of_thousands_of_sequences(rows, cache):
+    """None, one or a few each; in, out, and as single tokens attended."""
+    rng = np.random.default_rng(3)
+    new = rng.choice([0, 0, 1, 1, 1, 3, 20], 9001)
+    new[:70], new[4200:4400] = 0, 0                                    # (whole groups of sequences without rows)
+    c = Paged(cache, rows, rng.integers(0, 5, 9001), new, kv_heads=1, d=64, seed=13)
+    k, v = c.random_rows(c.total), c.random_rows(c.total)
+    c.kv.write(0, *c.dev, k, v)
+    got = c.kv.read(0, *c.dev, c.total, dtype=TORCH[rows])
+    for x, y in zip((k, v), got):
+        want = O.quantise(x.double().cpu().numpy())[0] if cache == "fp8" else x.double().cpu().numpy()
+        assert np.array_equal(y.double().cpu().numpy(), want)
+    c.fill()
+    q = c.random_rows(c.total, 2)
+    c.check(c.attend(q, 0.125, 20), q, 0.125)
+
+
 HEADS = [(1, 1), (2, 4), (8, 1), (1, 8), (4, 3)]
 
 
