@@ -122,6 +122,21 @@ __device__ __forceinline__ float odd_value(const void *row, int c, bool attends)
     return fabsf(v) < INFINITY || !attends ? 0.f : v;
 }
 
+// A pair of weights as two bf16 planes {hi, lo}, w = hi + lo, off by at most 2^-15 of w.  An infinite value has to stay one under both: so hi is w cut
+// off, and lo not negative; and where the pool's type has infinities (INF), lo is at least 2^-16 of hi, so not zero either (a weight below 2^-110 may have 0).
+typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+template <bool INF>
+__device__ __forceinline__ u32x2 two_planes(float w0, float w1) {
+    const uint32_t h0 = __float_as_uint(w0) & 0xFFFF0000u, h1 = __float_as_uint(w1) & 0xFFFF0000u;
+    const uint32_t hi = __builtin_amdgcn_perm(h1, h0, 0x07060302u);
+    uint32_t lo = pack_bf16x2(w0 - __uint_as_float(h0), w1 - __uint_as_float(h1));
+    if constexpr (INF) {
+        const u16x2 least = __builtin_elementwise_sub_sat(__builtin_bit_cast(u16x2, hi), u16x2{16 << 7, 16 << 7});
+        lo = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, lo), least));
+    }
+    return u32x2{hi, lo};
+}
+
 // The shares: T tiles over n workgroups, the first T % n of them one tile longer.
 struct PagedShares {
     int q, r;

@@ -350,8 +350,13 @@ __global__ __launch_bounds__(256, 2) void k_paged_attn_few(PagedAttn a) {
                             l_run[rt] += w[o];
                             if constexpr (F8) w[o] *= pow2_of_byte((t.vs[e >> 2] >> (8 * (e & 3))) & 0xFFu);
                         }
-                        hi[rt][i] = pack_bf16x2(w[0], w[1]);
-                        if constexpr (LO) lo[rt][i] = pack_bf16x2(w[0] - __uint_as_float(hi[rt][i] << 16), w[1] - __uint_as_float(hi[rt][i] & 0xFFFF0000u));
+                        if constexpr (LO) {
+                            const u32x2 planes = two_planes<!F8>(w[0], w[1]);
+                            hi[rt][i] = planes[0];
+                            lo[rt][i] = planes[1];
+                        } else {
+                            hi[rt][i] = pack_bf16x2(w[0], w[1]);
+                        }
                     }
                 }
 

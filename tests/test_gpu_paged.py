@@ -839,3 +839,26 @@ def test_refusals_of_the_binding():
     assert c.kv.attention(0, t, none, cl, q[:0], 0.1).shape == (0, 4, 64)
     c.kv.write(0, t, none, cl, k[:0], k[:0])
     assert c.kv.read(0, t, none, cl, 0)[0].shape == (0, 2, 64)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("m,group,others", [(1, 1, 0), (16, 1, 0), (2, 4, 0), (5, 5, 0), (32, 1, 0), (41, 1, 0), (9, 8, 0), (70, 1, 0), (64, 4, MORE), (150, 4, MORE)])
+def test_infinite_values_among_the_cached_rows(d, m, group, others):
+    """Every row attends them, whatever its weight for each: an infinity of that sign, NaN where both signs meet; in tiles that lie far before the block, and beside it."""
+    c = Paged("bf16", "bf16", [500, 90] + [0] * others, [m, m] + [9] * others, kv_heads=2, group=group, d=d, seed=m)
+    k, v = c.fill()
+    places = c.rng.permutation(490)[:24].tolist() + [497, 499]
+    features = c.rng.permutation(d)[:26].tolist()
+    for x, (at, f) in enumerate(zip(places, features)):
+        v[at, :, f] = math.inf if x % 2 else -math.inf
+    v[places[0], :, features[1]] = -math.inf                            # (there is an infinity of the other sign)
+    whole = torch.tensor(np.concatenate([[0], np.cumsum([t + n for t, n in zip(c.cached, c.new)])]), dtype=torch.int32, device="cuda")
+    c.kv.write(0, c.dev[0], whole, torch.zeros(len(c.cached), dtype=torch.int32, device="cuda"), k, v)
+    q = c.random_rows(c.total, 2 * group)
+    out = c.attend(q, 0.05, m)
+    with np.errstate(invalid="ignore"):
+        want = c.check(out, q, 0.05)
+    got = out.double().cpu().numpy()
+    odd = ~np.isfinite(want)
+    assert odd[:m].sum() == m * 2 * group * 26 and np.isnan(want).any()
+    assert np.array_equal(got[odd], want[odd], equal_nan=True)
