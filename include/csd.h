@@ -374,8 +374,9 @@ int32_t csd_paged_read(const csd_paged_kv *kv, int32_t layer, const int32_t *row
  * a value outside that range is read as 0) it attends the cached positions [0, cache_len[b]), the rows above it in the tree and itself.
  * q, out: [rows][n_heads][head_dim] of dtype (q_stride elements from one row to the next, a multiple of 8; out is contiguous;
  * 16-byte aligned, not overlapping); n_heads a multiple of n_kv_heads, query head h reads key-value head h / (n_heads / n_kv_heads).
- * out = softmax(scale * q k^T) v, scores, maxima and sums in fp32; a row that has nothing to attend gives zeros, and what
- * a row does not attend never reaches it (not even infinities and NaN).  max_rows: at least the rows of the longest sequence of the batch
+ * out = softmax(scale * q k^T) v, scores, maxima and sums in fp32; on their way into the product with v the weights of a sequence of up to 64 rows are rounded to 16
+ * bits, those of longer chunks to bf16 (bf16 queries, heads of 64 or 128, a pool of bf16 or e4m3; else not at all).  A row that has nothing to attend gives zeros, and what
+ * a row does not attend never reaches it (not even infinities and NaN; an attended infinity under a weight below 2^-100 may give NaN).  max_rows: at least the rows of the longest sequence of the batch
  * (a longer one is cut to it: its rows behind are left as they were; the kernels are chosen by it), 1 <= max_rows; CSD_ESHAPE for trees with max_rows > 64.
  * workspace: device, 256-byte aligned, CSD_PAGED_WORKSPACE_BYTES, of which the first CSD_PAGED_WORKSPACE_ZERO_BYTES are zeroed before its first use;
  * every call leaves them zeroed.  Calls that share it must not overlap.

@@ -9,7 +9,7 @@
 // and each stages its part of tile k + 1 beside its scores, from registers that were requested a tile earlier.  Values of three tiles and keys of two are in LDS.
 // (2 chunks of 2048 rows, 8 x 4 heads of 128, 10239 and 4096 keys, bf16: 415 us, 993 TFLOP/s; two independent workgroups of four waves and 128 rows
 // per compute unit took 455; e4m3 406 against 433; heads of 64 256 against 284; a barrier behind each half of a tile instead: 411, but one fresh prompt of
-// 4099 rows, 32 heads, 215 instead of 193.)
+// 4099 rows, 32 heads, 215 instead of 193.)  Weights in two planes, as those of blocks of up to 64 rows are, would take 542 us, e4m3 531, heads of 64 348.
 #include "csd_paged_tiles.h"
 
 static constexpr int kChunkRows = 256;
@@ -199,7 +199,7 @@ __global__ __launch_bounds__(512, 2) void k_paged_attn_chunk(PagedAttn a, int mi
     f32x16 st[2];
     bool sees = true;
     // the scores of tile kt, masked; the next tile to LDS
-    auto scores = [&](int kt, int v_next) {
+    auto scores = [&](int kt, int v_next) __attribute__((always_inline)) {
         const int key0 = kt * kKeys;
         if ((kt & 7) == 0 && kt != 0) {
             pages = pages_next;
@@ -257,7 +257,8 @@ __global__ __launch_bounds__(512, 2) void k_paged_attn_chunk(PagedAttn a, int mi
         }
     };
     // its weights, and their products with the values
-    auto products = [&](int v_this) {
+    auto products = [&](int v_this, auto planes) __attribute__((always_inline)) {
+        constexpr bool TWO = decltype(planes)::value;        // weights in two bf16 planes
         int va_at = v_at + (2 + v_this) * PIECES * 16;
         asm volatile("" : "+v"(va_at));
         auto read_v = [&](int x) {                           // features 32 d .. of keys 16 u .., in the order of the weights
@@ -289,12 +290,18 @@ __global__ __launch_bounds__(512, 2) void k_paged_attn_chunk(PagedAttn a, int mi
             m_run = m_new;
         }
         const float ref = m_run == -INFINITY ? 0.f : -m_run;
-        u32x4 pw[4];                                         // weights of keys 16 u .. 16 u + 15
+        u32x4 pw[2], pl[2];                                  // weights of keys 16 u .. 16 u + 15 at u % 2
         auto weigh = [&](int e) {                            // elements e, e + 1
             const float w0 = __builtin_amdgcn_exp2f(fmaf(st[e >> 4][e & 15], scale, ref)), w1 = __builtin_amdgcn_exp2f(fmaf(st[e >> 4][(e + 1) & 15], scale, ref));
             l_run += w0;
             l_more += w1;
-            pw[e >> 3][(e & 7) >> 1] = pack_bf16x2(w0, w1);
+            if constexpr (TWO) {
+                const u32x2 w = two_planes<!F8>(w0, w1);
+                pw[(e >> 3) & 1][(e & 7) >> 1] = w[0];
+                pl[(e >> 3) & 1][(e & 7) >> 1] = w[1];
+            } else {
+                pw[(e >> 3) & 1][(e & 7) >> 1] = pack_bf16x2(w0, w1);
+            }
         };
 #pragma unroll
         for (int e = 0; e < 8; e += 2) weigh(e);
@@ -303,7 +310,8 @@ __global__ __launch_bounds__(512, 2) void k_paged_attn_chunk(PagedAttn a, int mi
         for (int x = 0; x < 4 * DT; x++) {                   // the next 16 keys' weights are made beside the products of these
             const int u = x / DT, d = x % DT;
             if (x + 2 < 4 * DT) va[(x + 2) % 3] = read_v(x + 2);
-            acc[d] = mfma32(va[x % 3], pw[u], acc[d]);
+            acc[d] = mfma32(va[x % 3], pw[u & 1], acc[d]);
+            if constexpr (TWO) acc[d] = mfma32(va[x % 3], pl[u & 1], acc[d]);
             if (u < 3)
 #pragma unroll
                 for (int e = 0; e < 8 / DT; e += 2) weigh(8 * (u + 1) + 8 / DT * d + e);
@@ -315,24 +323,28 @@ __global__ __launch_bounds__(512, 2) void k_paged_attn_chunk(PagedAttn a, int mi
         v_this = v_next;
         v_next = v_next == 2 ? 0 : v_next + 1;
     };
-    if (!late) {
+    auto tiles = [&](auto planes) __attribute__((always_inline)) {
+        if (!late) {
 #pragma unroll 1
-        for (int kt = 0; kt < n_kt; kt++, on()) {
-            scores(kt, v_next);
-            products(v_this);
+            for (int kt = 0; kt < n_kt; kt++, on()) {
+                scores(kt, v_next);
+                products(v_this, planes);
+                __syncthreads();
+            }
+        } else {
+            scores(0, 1);
             __syncthreads();
-        }
-    } else {
-        scores(0, 1);
-        __syncthreads();
 #pragma unroll 1
-        for (int kt = 1; kt < n_kt; kt++, on()) {
-            products(v_this);
-            scores(kt, v_next == 2 ? 0 : v_next + 1);
-            __syncthreads();
+            for (int kt = 1; kt < n_kt; kt++, on()) {
+                products(v_this, planes);
+                scores(kt, v_next == 2 ? 0 : v_next + 1);
+                __syncthreads();
+            }
+            products(v_this, planes);
         }
-        products(v_this);
-    }
+    };
+    if (seq.m <= CSD_PAGED_FINE_ROWS) tiles(std::true_type{});
+    else tiles(std::false_type{});
     __syncthreads();
     l_run = halves_sum(l_run + l_more);
 

@@ -16,8 +16,8 @@
 //                  eight keys (a row of V is read by 16 neighbouring lanes) and transposes them in registers by byte permutations; A-row i of
 //                  product j is then feature DH / 16 * i + j.
 // e4m3 keys and values become bf16 without loss; the keys' scales multiply the scores, the values' scales the weights (powers of
-// two: exact).  Up to 16 rows the weights enter the second product as two bf16 planes (w = hi + lo, 16 bits): the matrix cores have time to
-// spare there.  With 32 rows they enter as one (half a step: 2^-8 of a weight, random in sign; their sum is kept in fp32).
+// two: exact).  The weights enter the second product as two bf16 planes (w = hi + lo, 16 bits): the matrix cores have time to spare (20 rows of 16 ragged
+// sequences, 8 heads of 128: bf16 100 us with either, e4m3 100 with one plane and 101 to 103 with two; heads of 64, e4m3: 61 and 67).
 #include "csd_paged.h"
 
 static constexpr int kFewPages = 1024;      // entries of the page table held in LDS at a time
@@ -86,7 +86,6 @@ template <int DH, bool F8, int RT>
 __global__ __launch_bounds__(256, 2) void k_paged_attn_few(PagedAttn a) {
     using Tile = FewTile<DH, F8>;
     constexpr int F = DH / 16, R = 16 * RT;
-    constexpr bool LO = RT == 1;
     constexpr int NB = (F8 && (RT == 1 || DH == 64) ? 2 : 1) + (DH == 64 ? 1 : 0);     // tiles in flight per wave, as registers allow
     constexpr int ES = F8 ? 1 : 2, kGrid = CSD_PAGED_FEW_GRID, kCost = CSD_PAGED_FEW_COST;
     __shared__ int s_pages[kFewPages];
@@ -350,13 +349,9 @@ __global__ __launch_bounds__(256, 2) void k_paged_attn_few(PagedAttn a) {
                             l_run[rt] += w[o];
                             if constexpr (F8) w[o] *= pow2_of_byte((t.vs[e >> 2] >> (8 * (e & 3))) & 0xFFu);
                         }
-                        if constexpr (LO) {
-                            const u32x2 planes = two_planes<!F8>(w[0], w[1]);
-                            hi[rt][i] = planes[0];
-                            lo[rt][i] = planes[1];
-                        } else {
-                            hi[rt][i] = pack_bf16x2(w[0], w[1]);
-                        }
+                        const u32x2 planes = two_planes<!F8>(w[0], w[1]);
+                        hi[rt][i] = planes[0];
+                        lo[rt][i] = planes[1];
                     }
                 }
 
@@ -385,7 +380,7 @@ __global__ __launch_bounds__(256, 2) void k_paged_attn_few(PagedAttn a) {
 #pragma unroll
                         for (int j = 0; j < 4; j++) {
                             acc[rt][y + j] = mfma16(vf[j], hi[rt], acc[rt][y + j]);
-                            if constexpr (LO) acc[rt][y + j] = mfma16(vf[j], lo[rt], acc[rt][y + j]);
+                            acc[rt][y + j] = mfma16(vf[j], lo[rt], acc[rt][y + j]);
                         }
                     }
                 }

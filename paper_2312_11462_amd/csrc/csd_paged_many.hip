@@ -9,8 +9,9 @@
 //   S^T = K q^T    A = K (32 keys x 16 features, one 16-byte read), B = q^T, in registers throughout
 //   O^T = V^T P^T  A = V^T (32 features x 16 keys, by LDS's transposing reads), B = P^T: a lane's scores of 16 keys are, in
 //                  order, keys 4 h .. 4 h + 3 and 8 + 4 h .. 8 + 4 h + 3 (h = lane / 32), and A's columns are read in that order
-// so that the weights never move between lanes.  The weights enter as bf16 (half a step: 2^-8 of a weight, random in sign; the sum of the weights
-// is kept in fp32): a second plane of them would be a third more matrix instructions, which bound this kernel.
+// so that the weights never move between lanes.  The weights of sequences of up to 64 rows enter as two bf16 planes, those of longer chunks as one: a second plane
+// is half as many matrix instructions more, which bound this kernel (with it and without: a tree of 41 rows 22.4 and 21.4 us; 50 trees 112 and 105; 5 rows of 12 ragged
+// sequences over up to 30000 keys, 8 x 8 heads of 128, e4m3 150 and 125; 4 chunks of 250 rows, 8 x 4 heads of 64, and 20 tokens 100 and 88).
 // Rows of 16-byte pieces are stored with the piece index xored by the row, K and V in different ways, so that each kind of read
 // spreads over all banks.
 #include "csd_paged_tiles.h"
@@ -286,8 +287,9 @@ __global__ __launch_bounds__(256, 2) void k_paged_attn_many(PagedAttn a, int min
     const int v_at = v_piece<DH>(v_row, 2 * ((lane >> 4) & 1) + ((l16 >> 1) & 1)) * 16 + 8 * (l16 & 1);
     float l_run = 0.f, l_more = 0.f;                         // the sum of weights, in two chains
     int kt = kt0;
-    auto turn = [&](auto which) {
+    auto turn = [&](auto which, auto planes) {
         constexpr int buf = decltype(which)::value;
+        constexpr bool TWO = decltype(planes)::value;        // weights in two bf16 planes
         const int key0 = kt * kKeys, next = min(kt + 1, kt1 - 1);        // (the last turn brings its own tile once more: no branches)
         const unsigned here = here_mask(kt);
         if (((next - kt0) & 15) == 0 && next != kt) {
@@ -369,12 +371,18 @@ __global__ __launch_bounds__(256, 2) void k_paged_attn_many(PagedAttn a, int min
             m_run = m_new;
         }
         const float ref = m_run == -INFINITY ? 0.f : -m_run;
-        u32x4 pw[2];                                         // weights of keys 16 u .. 16 u + 15 at u % 2
+        u32x4 pw[2], pl[2];                                  // weights of keys 16 u .. 16 u + 15 at u % 2
         auto weigh = [&](int e) {                            // elements e, e + 1
             const float w0 = __builtin_amdgcn_exp2f(fmaf(st[e >> 4][e & 15], scale, ref)), w1 = __builtin_amdgcn_exp2f(fmaf(st[e >> 4][(e + 1) & 15], scale, ref));
             l_run += w0;
             l_more += w1;
-            pw[(e >> 3) & 1][(e & 7) >> 1] = pack_bf16x2(w0, w1);
+            if constexpr (TWO) {
+                const u32x2 w = two_planes<!F8>(w0, w1);
+                pw[(e >> 3) & 1][(e & 7) >> 1] = w[0];
+                pl[(e >> 3) & 1][(e & 7) >> 1] = w[1];
+            } else {
+                pw[(e >> 3) & 1][(e & 7) >> 1] = pack_bf16x2(w0, w1);
+            }
         };
 #pragma unroll
         for (int e = 0; e < 8; e += 2) weigh(e);
@@ -387,6 +395,7 @@ __global__ __launch_bounds__(256, 2) void k_paged_attn_many(PagedAttn a, int min
             const int u = x / DT, d = x % DT;
             if (x + 2 < 4 * DT) va[(x + 2) % 3] = read_v(x + 2);
             acc[d] = mfma32(va[x % 3], pw[u & 1], acc[d]);
+            if constexpr (TWO) acc[d] = mfma32(va[x % 3], pl[u & 1], acc[d]);
             if (u < 3)
 #pragma unroll
                 for (int e = 0; e < 8 / DT; e += 2) weigh(8 * (u + 1) + 8 / DT * d + e);
@@ -404,15 +413,19 @@ __global__ __launch_bounds__(256, 2) void k_paged_attn_many(PagedAttn a, int min
             for (int x = 0; x < NP; x++) stage(x, buf ^ 1, K);
         mend(next, buf ^ 1);
     };
+    auto turns = [&](auto planes) {
 #pragma unroll 1
-    while (true) {
-        turn(std::integral_constant<int, 0>{});
-        __syncthreads();
-        if (++kt == kt1) break;
-        turn(std::integral_constant<int, 1>{});
-        __syncthreads();
-        if (++kt == kt1) break;
-    }
+        while (true) {
+            turn(std::integral_constant<int, 0>{}, planes);
+            __syncthreads();
+            if (++kt == kt1) break;
+            turn(std::integral_constant<int, 1>{}, planes);
+            __syncthreads();
+            if (++kt == kt1) break;
+        }
+    };
+    if (seq.m <= CSD_PAGED_FINE_ROWS) turns(std::true_type{});
+    else turns(std::false_type{});
     l_run = halves_sum(l_run + l_more);
 
     if (s_odd) {                                             // (uniform; the last tile was staged in front of a barrier)

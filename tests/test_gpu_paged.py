@@ -862,3 +862,54 @@ def test_infinite_values_among_the_cached_rows(d, m, group, others):
     odd = ~np.isfinite(want)
     assert odd[:m].sum() == m * 2 * group * 26 and np.isnan(want).any()
     assert np.array_equal(got[odd], want[odd], equal_nan=True)
+
+
+def check_closely(c, out, q, scale, u_p, parent=None, sequences=None):
+    """As Paged.check, for the rows of these sequences, with the weights off by u_p of themselves: the bound of the kernels that do not round weights to bf16 (0, all in fp32),
+    or keep them in two bf16 planes (2^-15: the second plane is off by 2^-8 of itself, and it is at most 2^-7 of the weight)."""
+    start, cached, table = c.start, c.cached, c.table
+    some = range(len(cached)) if sequences is None else sequences
+    k, v = c.values(c.k, c.ks)[0], c.values(c.v, c.vs)[0]
+    dev, qq = out.double().cpu().numpy(), q.double().cpu().numpy()
+    live = k[np.isfinite(k).all(-1)]
+    worst = 0.0
+    for b in some:
+        a, z = int(start[b]), int(start[b + 1])
+        up = parent[a:z] if parent is not None else None
+        args = table[b:b + 1], np.array([0, z - a]), cached[b:b + 1], qq[a:z], scale, up
+        want, size = O.attention(k, v, *args), O.attention(k, np.abs(v), *args)
+        n = cached[b] + z - a
+        dot = abs(scale) * np.sqrt((qq[a:z] ** 2).sum(-1)).max(initial=0) * np.sqrt((live ** 2).sum(-1)).max(initial=0)
+        e = (c.d + 4) * 2.0 ** -24 * dot + 2.0 ** -21 + n * 2.0 ** -24
+        tol = (2.0 ** -8 if c.rows == "bf16" else 2.0 ** -24) * np.abs(want) + 2 * (u_p + e) * size
+        worst = max(worst, (np.abs(dev[a:z] - want) / np.maximum(tol, 1e-300)).max(initial=0))
+    assert worst <= 1, f"off by {worst:.2f} times the bound"
+
+
+CLOSE = [("bf16", "bf16", 64, 2.0 ** -15), ("bf16", "bf16", 128, 2.0 ** -15), ("bf16", "fp8", 64, 2.0 ** -15), ("bf16", "fp8", 128, 2.0 ** -15),
+         ("bf16", "bf16", 80, 0.0), ("bf16", "fp32", 64, 0.0), ("fp32", "fp32", 64, 0.0), ("fp32", "fp8", 128, 0.0)]
+
+
+@pytest.mark.parametrize("rows,cache,d,u_p", CLOSE)
+@pytest.mark.parametrize("m,group,tree,others", [(1, 1, False, 0), (1, 8, False, 0), (5, 3, False, 0), (16, 1, False, 0), (5, 4, False, 0), (17, 1, True, 0), (32, 1, False, 0), (33, 1, False, 0),
+                                                 (5, 8, False, 0), (41, 1, True, 0), (64, 2, False, 0), (41, 4, True, MORE), (64, 4, False, MORE)])
+def test_weights_of_reviews_are_not_rounded_to_bf16(rows, cache, d, u_p, m, group, tree, others):
+    """Single tokens, blocks and trees of up to 64 rows: outputs small beside the values that they are sums of, in which a rounded weight shows."""
+    c = Paged(cache, rows, [700, 230] + [0] * others, [m, m] + [9] * others, kv_heads=2, group=group, d=d, seed=m)
+    c.fill()
+    parent = np.concatenate([[-1] + [(i - 1) // 2 for i in range(1, n)] for n in c.new]).astype(np.int32) if tree else None
+    q = c.random_rows(c.total, 2 * group, loud=False) * 0.25
+    out = c.attend(q, d ** -0.5, m, parent)
+    check_closely(c, out, q, d ** -0.5, u_p, parent, [0, 1, len(c.cached) - 1])
+
+
+@pytest.mark.parametrize("cache,d", [("bf16", 64), ("fp8", 128)])
+@pytest.mark.parametrize("group,chunk,others", [(1, 65, 0), (4, 300, 0), (8, 100, 0), (2, 300, MORE)])
+def test_a_blocks_weights_do_not_depend_on_its_company(cache, d, group, chunk, others):
+    """Blocks and single tokens beside a chunk, whose own weights may be rounded to bf16."""
+    c = Paged(cache, "bf16", [300, 700, 40, 500, 64] + [0] * others, [1, 5, 64, chunk, 20] + [9] * others, kv_heads=2, group=group, d=d, seed=chunk)
+    c.fill()
+    q = c.random_rows(c.total, 2 * group, loud=False) * 0.25
+    out = c.attend(q, d ** -0.5, chunk)
+    check_closely(c, out, q, d ** -0.5, 2.0 ** -15, None, [0, 1, 2, 4])
+    check_closely(c, out, q, d ** -0.5, 2.0 ** -8, None, [3])
