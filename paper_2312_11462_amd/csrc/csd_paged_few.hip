@@ -48,11 +48,15 @@ __device__ __forceinline__ void load_words(const void *p, uint32_t (&w)[VW]) {
     }
 }
 
-// two e4m3 codes (the low or the high half of w) as bf16, exact
+// two e4m3 codes (the low or the high half of w) times `scale`, a power of two, as bf16, exact
 template <bool HI>
-__device__ __forceinline__ uint32_t bf16x2_of_fp8(uint32_t w) {
-    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, HI));
+__device__ __forceinline__ uint32_t bf16x2_of_fp8(uint32_t w, float scale = 1.0f) {
+    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, HI));
 }
+// Weights are multiplied by their values' scales, 2^-126 to 2^120, before they are rounded to bf16.  So that products with the smallest scales do not end below bf16's
+// normal values, the weights get 2^kUp more (2^127 at most) and the codes as much less (20 rows over e4m3
+// caches: heads of 128 as before, heads of 64 66.5 -> 67.3 us).
+static constexpr int kUp = 7;
 
 // V^T operands of features y .. y + 3 (of the lane's DH / 16) from the eight keys' words: dword i holds keys 2 i, 2 i + 1
 template <int DH, bool F8>
@@ -63,10 +67,11 @@ __device__ __forceinline__ void v_operands(const uint32_t (&v)[8][FewTile<DH, F8
         if constexpr (F8) {
             const int w = y / 4;
             const uint32_t lo = __builtin_amdgcn_perm(b[w], a[w], 0x05010400u), hi = __builtin_amdgcn_perm(b[w], a[w], 0x07030602u);
-            f[0][i] = bf16x2_of_fp8<false>(lo);
-            f[1][i] = bf16x2_of_fp8<true>(lo);
-            f[2][i] = bf16x2_of_fp8<false>(hi);
-            f[3][i] = bf16x2_of_fp8<true>(hi);
+            constexpr float down = 1.0f / (1 << kUp);
+            f[0][i] = bf16x2_of_fp8<false>(lo, down);
+            f[1][i] = bf16x2_of_fp8<true>(lo, down);
+            f[2][i] = bf16x2_of_fp8<false>(hi, down);
+            f[3][i] = bf16x2_of_fp8<true>(hi, down);
         } else {
 #pragma unroll
             for (int w = 0; w < 2; w++) {
@@ -347,7 +352,7 @@ __global__ __launch_bounds__(256, 2) void k_paged_attn_few(PagedAttn a) {
                             const int e = 2 * i + o;
                             w[o] = __builtin_amdgcn_exp2f(fmaf(x[rt][e], scale, -ref));
                             l_run[rt] += w[o];
-                            if constexpr (F8) w[o] *= pow2_of_byte((t.vs[e >> 2] >> (8 * (e & 3))) & 0xFFu);
+                            if constexpr (F8) w[o] *= pow2_of_byte(((t.vs[e >> 2] >> (8 * (e & 3))) & 0xFFu) + kUp);
                         }
                         const u32x2 planes = two_planes<!F8>(w[0], w[1]);
                         hi[rt][i] = planes[0];

@@ -913,3 +913,25 @@ def test_a_blocks_weights_do_not_depend_on_its_company(cache, d, group, chunk, o
     out = c.attend(q, d ** -0.5, chunk)
     check_closely(c, out, q, d ** -0.5, 2.0 ** -15, None, [0, 1, 2, 4])
     check_closely(c, out, q, d ** -0.5, 2.0 ** -8, None, [3])
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("m,group", [(1, 1), (5, 2), (5, 4), (41, 1), (70, 2)])
+@pytest.mark.parametrize("power", [-117, -113, 110])
+def test_values_whose_scale_is_near_the_ends(d, m, group, power):
+    """e4m3 rows of values around 2^power: the scales reach from 2^-126 to 2^120, and the weights are multiplied by them.  In bf16, subnormal from 2^-126 down in steps
+    of 2^-133, a product of weight and scale is off by half a step per plane, times codes of at most 3.5, over a sum of weights of at least 2^-8: 2^-123 per key."""
+    c = Paged("fp8", "bf16", [20, 9], [m, m], kv_heads=2, group=group, d=d, seed=m)
+    n = 29 + 2 * m
+    k, v = (torch.tensor(c.rng.standard_normal((n, 2, d)), dtype=torch.float32).to(torch.bfloat16).cuda() for _ in range(2))
+    start = torch.tensor([0, 20 + m, n], dtype=torch.int32, device="cuda")
+    c.kv.write(0, c.dev[0], start, torch.zeros(2, dtype=torch.int32, device="cuda"), k, v * 2.0 ** (power - 2))
+    q = c.random_rows(2 * m, 2 * group)
+    out = c.attend(q, d ** -0.5, m)
+    kk, vv = c.values(c.k, c.ks)[0], c.values(c.v, c.vs)[0]
+    args = c.table, c.start, c.cached, q.double().cpu().numpy(), d ** -0.5
+    want, size = O.attention(kk, vv, *args), O.attention(kk, np.abs(vv), *args)
+    u_p = 2.0 ** -15 if m <= 64 else 2.0 ** -8
+    tol = 2.0 ** -8 * np.abs(want) + 2 * (u_p + 2.0 ** -15) * size + (20 + m) * 2.0 ** -123      # (scores up to 30: their error is below 2^-15)
+    worst = (np.abs(out.double().cpu().numpy() - want) / tol).max()
+    assert worst <= 1 and np.median(size) > 2.0 ** (power - 5), f"off by {worst:.2f} times the bound"
