@@ -377,7 +377,8 @@ int32_t csd_paged_read(const csd_paged_kv *kv, int32_t layer, const int32_t *row
  * out = softmax(scale * q k^T) v, scores, maxima and sums in fp32; on their way into the product with v the weights of a sequence of up to 64 rows are rounded to 16
  * bits, those of longer chunks to bf16 (bf16 queries, heads of 64 or 128, a pool of bf16 or e4m3; else not at all).  A row that has nothing to attend gives zeros, and what
  * a row does not attend never reaches it (not even infinities and NaN; an attended infinity under a weight below 2^-100 may give NaN).  max_rows: at least the rows of the longest sequence of the batch
- * (a longer one is cut to it: its rows behind are left as they were; the kernels are chosen by it), 1 <= max_rows; CSD_ESHAPE for trees with max_rows > 64.
+ * (a longer one is cut to it: its rows behind are left as they were; the kernels are chosen by it), 1 <= max_rows; CSD_ESHAPE for trees
+ * where it and `rows` are above 64.
  * workspace: device, 256-byte aligned, CSD_PAGED_WORKSPACE_BYTES, of which the first CSD_PAGED_WORKSPACE_ZERO_BYTES are zeroed before its first use;
  * every call leaves them zeroed.  Calls that share it must not overlap.
  */

@@ -367,8 +367,9 @@ class PagedKv:
 
     def attention(self, layer, table, row_start, cache_len, q, scale, max_rows=None, parent=None, out=None):
         """csd_paged_attention: q [rows][heads][head dim] -> out, contiguous and of q's type; rows of no sequence are left as they are
-        (undefined in a new tensor).  max_rows: at least the rows of the longest sequence of the batch (default: all rows of the call;
-        the kernels are chosen by it, so single tokens and short blocks are served best where it is given); parent: tree blocks."""
+        (undefined in a new tensor).  max_rows: at least the rows of the longest sequence of the batch (default: all rows of the call, for
+        several trees 64 at most; the kernels are chosen by it, so single tokens and short blocks are served best where it is given);
+        parent: tree blocks, of 64 rows at most."""
         dev, i32, d = self._dev, torch.int32, self.head_dim
         B, n = table.shape
         rows, heads, width = q.shape
@@ -387,6 +388,8 @@ class PagedKv:
         if parent is not None:
             self._check(parent=(parent, rows))
             up = parent.data_ptr()
+            if max_rows is None and B > 1:
+                max_rows = min(rows, 64) or 1
         pool, ref = self._mine()
         pool.table, pool.table_stride = table.data_ptr(), n
         rc = self._lib.csd_paged_attention(ref, layer, row_start.data_ptr(), cache_len.data_ptr(), up, B, rows,

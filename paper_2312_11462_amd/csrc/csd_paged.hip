@@ -408,11 +408,12 @@ extern "C" int32_t csd_paged_attention(const csd_paged_kv *kv, int32_t layer, co
     int32_t rc = check_rows(kv, layer, row_start, cache_len, B, rows, dtype);
     if (rc != CSD_OK) return rc;
     if (max_rows < 1 || n_heads < 1 || n_heads % kv->n_kv_heads || !(fabsf(scale) < INFINITY)) return CSD_EINVAL;
-    if (n_heads > 65535 || (parent && max_rows > 64)) return CSD_ESHAPE;
+    const int32_t most = max_rows < rows ? max_rows : rows;
+    if (n_heads > 65535 || (parent && most > 64)) return CSD_ESHAPE;
     if (rows == 0) return CSD_OK;
     if (!q || !out || !workspace) return CSD_ENULL;
     if (!row_stride_ok(kv, n_heads, q_stride, q) || (uintptr_t)out % 16 || (uintptr_t)workspace % 256) return CSD_EINVAL;
-    const PagedAttn a{csd_paged_layer(kv, layer), PagedRows{row_start, cache_len, B, rows}, parent, max_rows < rows ? max_rows : rows,
+    const PagedAttn a{csd_paged_layer(kv, layer), PagedRows{row_start, cache_len, B, rows}, parent, most,
                       n_heads / kv->n_kv_heads, q, (long long)q_stride, out, scale, workspace};
     return csd_paged_attention_enqueue(a, kv->dtype, dtype, (hipStream_t)stream);
 }

@@ -935,3 +935,20 @@ def test_values_whose_scale_is_near_the_ends(d, m, group, power):
     tol = 2.0 ** -8 * np.abs(want) + 2 * (u_p + 2.0 ** -15) * size + (20 + m) * 2.0 ** -123      # (scores up to 30: their error is below 2^-15)
     worst = (np.abs(out.double().cpu().numpy() - want) / tol).max()
     assert worst <= 1 and np.median(size) > 2.0 ** (power - 5), f"off by {worst:.2f} times the bound"
+
+
+@pytest.mark.parametrize("rows,cache,d", SPREAD)
+def test_trees_without_a_word_on_their_size(rows, cache, d):
+    """A batch of more than 64 rows whose trees are within 64 each; a single tree of more is refused."""
+    import paper_2312_11462_amd as P
+    rng = np.random.default_rng(1)
+    c = Paged(cache, rows, [70, 0, 33], [41, 9, 64], kv_heads=2, d=d, seed=3)
+    c.fill()
+    parent = np.concatenate([[int(rng.integers(max(0, i - 9), i)) if i else -1 for i in range(m)] for m in c.new]).astype(np.int32)
+    q = c.random_rows(c.total, 2)
+    c.check(c.attend(q, d ** -0.5, None, parent), q, d ** -0.5, parent)
+    one = Paged(cache, rows, [5], [65], kv_heads=2, d=d, seed=3)
+    one.fill()
+    with pytest.raises(P.CsdError) as e:
+        one.attend(one.random_rows(65, 2), 0.1, None, np.zeros(65, dtype=np.int32))
+    assert e.value.status == -2

@@ -144,3 +144,11 @@ def test_binding_refuses_host_tensors_and_wrong_pools():
         P.PagedKv(k, k, k_scale=torch.zeros(1, 2, 4, 16, dtype=torch.uint8))
     with pytest.raises(ValueError):
         P.PagedKv(k.to(torch.float8_e4m3fn), k.to(torch.float8_e4m3fn))
+
+
+def test_attention_over_trees_goes_by_the_rows_there_are(L):
+    """max_rows is cut to the rows of the call before it is held against the 64 rows of a tree (the output's address is refused behind that)."""
+    ref, keep = _pool()
+    for rows, most, code in ((40, 100, EINVAL), (64, 65, EINVAL), (65, 64, EINVAL), (65, 65, ESHAPE), (100, 1 << 20, ESHAPE)):
+        assert L.csd_paged_attention(ref, 0, 256, 256, 256, 1, rows, most, 256, 512, 8, 1, 0.125, 264, 256, None) == code, (rows, most)
+    assert L.csd_paged_attention(ref, 0, 256, 256, 256, 1, 0, 100, None, 0, 8, 1, 0.125, None, None, None) == 0
