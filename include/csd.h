@@ -396,6 +396,10 @@ int32_t csd_paged_attention(const csd_paged_kv *kv, int32_t layer, const int32_t
 int32_t csd_paged_commit(const csd_paged_kv *kv, const int32_t *cache_len, const int32_t *path, const int32_t *n_accepted,
                          int32_t B, int32_t m, void *stream);
 
+/* Whether the stream is being captured into a graph: *id is 0, or a number that no other capture has.  For callers that keep workspaces: graphs that may be
+ * replayed side by side must not share one. */
+int32_t csd_stream_capture(void *stream, uint64_t *id);
+
 /* Test hook: when trace != NULL the next verify calls also copy the residual stream of all
  * B*m rows after the embedding and after every layer to trace[(n_layers+1)][B*m][d] (fp32). */
 int32_t csd_debug_set_trace(csd_model *model, float *trace);

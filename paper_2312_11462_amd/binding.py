@@ -18,7 +18,7 @@ _LIB_PATH = os.path.join(_HERE, "libcsd.so")
 EXPORTS = ["csd_version", "csd_last_hip_error", "csd_model_create", "csd_model_destroy", "csd_kv_bytes",
            "csd_kv_write", "csd_kv_read", "csd_cross_kv_init", "csd_bigram_fit", "csd_bigram_draft", "csd_maxgram_draft", "csd_verify_block",
            "csd_accept", "csd_verify_accept", "csd_verify_accept_static", "csd_review_ctx", "csd_bigram_draft_append", "csd_cascade_gate", "csd_verify_tree", "csd_tree_accept", "csd_tree_commit",
-           "csd_paged_write", "csd_paged_read", "csd_paged_attention", "csd_paged_commit", "csd_debug_set_trace", "csd_debug_path", "csd_debug_gemm_plan", "csd_debug_tall_plan", "csd_debug_copy", "csd_debug_read", "csd_debug_mfma",
+           "csd_paged_write", "csd_paged_read", "csd_paged_attention", "csd_paged_commit", "csd_stream_capture", "csd_debug_set_trace", "csd_debug_path", "csd_debug_gemm_plan", "csd_debug_tall_plan", "csd_debug_copy", "csd_debug_read", "csd_debug_mfma",
            "csd_prof_enable", "csd_prof_read"]
 
 _STATUS = {-1: "CSD_EINVAL", -2: "CSD_ESHAPE", -3: "CSD_ENULL", -4: "CSD_EHIP", -5: "CSD_EUNSUPPORTED"}
@@ -58,7 +58,8 @@ _P, _I, _L = C.c_void_p, C.c_int32, C.c_int64
 _ARGTYPES = {"csd_paged_write": [_P, _I, _P, _P, _I, _I, _P, _L, _P, _L, _I, _P],
              "csd_paged_read": [_P, _I, _P, _P, _I, _I, _P, _L, _P, _L, _I, _P],
              "csd_paged_attention": [_P, _I, _P, _P, _P, _I, _I, _I, _P, _L, _I, _I, C.c_float, _P, _P, _P],
-             "csd_paged_commit": [_P, _P, _P, _P, _I, _I, _P]}
+             "csd_paged_commit": [_P, _P, _P, _P, _I, _I, _P],
+             "csd_stream_capture": [_P, _P]}
 PAGED_WORKSPACE_BYTES, PAGED_WORKSPACE_ZERO_BYTES = 72 << 20, 64 << 10
 _ROWS = {torch.float32: 0, torch.bfloat16: 1}     # types of dense rows
 
@@ -111,6 +112,9 @@ _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda de
 
 # (likewise: the public way also looks whether the runtime is up, which it is once there is a tensor)
 _current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+
+
+_capturing = getattr(torch._C, "_cuda_isCurrentStreamCapturing", None) or torch.cuda.is_current_stream_capturing
 
 
 def _stream():
@@ -258,8 +262,9 @@ class PagedKv:
     Every call takes the page table [B][n] int32 (entries outside [0, pages): no rows there) and the ragged rows of a batch: row_start
     [B + 1] int32, and a position [B] int32 for each sequence's first row.  Rows are [rows][heads][head dim], float32 or bfloat16,
     with any distance between rows that is a multiple of 8 elements.  All tensors are on the pools' device, which has to be the current one,
-    and the work is enqueued on its current stream.  The attention's workspace belongs to this object: calls of attention() that
-    may overlap (other streams or threads, captured graphs that are replayed side by side) need an object of their own."""
+    and the work is enqueued on its current stream.  The attention has a workspace (PAGED_WORKSPACE_BYTES) for every stream that it is called on and for
+    every capture, made at the first call there, so that calls on several streams and graphs that are replayed side by side may overlap.
+    A workspace that is given serves all calls, which then must not overlap."""
 
     def __init__(self, k, v, k_scale=None, v_scale=None, workspace=None):
         types = {torch.float32: 0, torch.bfloat16: 1, torch.float8_e4m3fn: 2}
@@ -278,15 +283,29 @@ class PagedKv:
         self._pool = PagedPool(self.n_layers, self.n_pages, self.page_rows, self.n_kv_heads, self.head_dim, types[k.dtype],
                                _ptr(k).value, _ptr(v).value, _ptr(k_scale, torch.uint8).value, _ptr(v_scale, torch.uint8).value, None, 0)
         self._threads, self._lib, self._device = threading.local(), lib(), k.device
-        if workspace is None:
-            self._check()
-            workspace = torch.empty(PAGED_WORKSPACE_BYTES, dtype=torch.uint8, device=k.device)
-            workspace[:PAGED_WORKSPACE_ZERO_BYTES].zero_()
-            torch.cuda.current_stream().synchronize()     # zeroed for whatever stream the first call runs on
-        elif workspace.numel() * workspace.element_size() < PAGED_WORKSPACE_BYTES:
+        if workspace is not None and workspace.numel() * workspace.element_size() < PAGED_WORKSPACE_BYTES:
             raise ValueError(f"workspace: {PAGED_WORKSPACE_BYTES} bytes, the first {PAGED_WORKSPACE_ZERO_BYTES} of them zeroed")
         self.workspace = workspace
         self._ws = _ptr(workspace).value
+        self._eager, self._captured = {}, {}              # by stream: (address, tensor), (capture, address, tensor)
+
+    def _workspace_of(self, stream):
+        """The address of the current stream's own workspace.  While the stream is captured, that of the capture, from the graph's memory and zeroed
+        by the graph; the one of the stream's last capture is let go of (its memory stays with its graph)."""
+        if not _capturing():
+            held = self._eager.get(stream)
+            return (held or self._eager.setdefault(stream, self._new_workspace()))[0]
+        capture = C.c_uint64()
+        _chk(self._lib.csd_stream_capture(stream, C.addressof(capture)), "csd_stream_capture")
+        held = self._captured.get(stream)
+        if held is None or held[0] != capture.value:
+            held = self._captured[stream] = (capture.value, *self._new_workspace())
+        return held[1]
+
+    def _new_workspace(self):
+        workspace = torch.empty(PAGED_WORKSPACE_BYTES, dtype=torch.uint8, device=self._device)
+        workspace[:PAGED_WORKSPACE_ZERO_BYTES].zero_()
+        return workspace.data_ptr(), workspace
 
     def _mine(self):
         """The call's description of the cache, whose page table a call sets: one per thread."""
@@ -392,9 +411,10 @@ class PagedKv:
                 max_rows = min(rows, 64) or 1
         pool, ref = self._mine()
         pool.table, pool.table_stride = table.data_ptr(), n
+        stream = _raw_stream(dev)
         rc = self._lib.csd_paged_attention(ref, layer, row_start.data_ptr(), cache_len.data_ptr(), up, B, rows,
                                            (rows or 1) if max_rows is None else max_rows, q.data_ptr(), qs[0] if rows > 1 else heads * d, heads,
-                                           _ROWS[dtype], scale, out.data_ptr(), self._ws, _raw_stream(dev))
+                                           _ROWS[dtype], scale, out.data_ptr(), self._ws or self._workspace_of(stream), stream)
         if rc:
             _chk(rc, "csd_paged_attention")
         return out

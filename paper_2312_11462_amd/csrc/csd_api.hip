@@ -11,6 +11,14 @@ thread_local int32_t g_csd_last_hip_error = 0;
 
 extern "C" const char *csd_version(void) { return "csd-mi355x 0.1 (gfx950)"; }
 extern "C" int32_t csd_last_hip_error(void) { return g_csd_last_hip_error; }
+extern "C" int32_t csd_stream_capture(void *stream, uint64_t *id) {
+    if (!id) return CSD_ENULL;
+    hipStreamCaptureStatus status = hipStreamCaptureStatusNone;
+    unsigned long long capture = 0;
+    CSD_HIP(hipStreamGetCaptureInfo((hipStream_t)stream, &status, &capture));
+    *id = status == hipStreamCaptureStatusNone ? 0 : capture + 1;
+    return CSD_OK;
+}
 
 static bool env_is(const char *name, const char *val) {
     const char *e = getenv(name);

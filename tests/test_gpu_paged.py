@@ -952,3 +952,77 @@ def test_trees_without_a_word_on_their_size(rows, cache, d):
     with pytest.raises(P.CsdError) as e:
         one.attend(one.random_rows(65, 2), 0.1, None, np.zeros(65, dtype=np.int32))
     assert e.value.status == -2
+
+
+@pytest.mark.parametrize("cache,m", [("fp8", 4), ("bf16", 40)])
+def test_one_cache_on_two_streams_and_in_two_graphs(cache, m):
+    """Sequences that several workgroups share: calls that overlap, eager and replayed, on two streams, give what one alone gives; so do later ones."""
+    c = Paged(cache, "bf16", [3000, 500], [m, m], kv_heads=4, group=2, d=128, seed=m)
+    c.fill()
+    q = [c.random_rows(2 * m, 8) for _ in range(2)]
+    want = [c.attend(x, 0.09, m) for x in q]
+    outs = [torch.empty_like(x) for x in q]
+    torch.cuda.synchronize()
+    graphs = []
+    for x, out in zip(q, outs):
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            for _ in range(8):
+                c.attend(x, 0.09, m, out=out)
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for _ in range(3):
+        for out in outs:
+            out.fill_(-1)
+        torch.cuda.synchronize()
+        late = [[], []]
+        for _ in range(8):
+            for i, s in enumerate(streams):
+                with torch.cuda.stream(s):
+                    late[i].append(c.attend(q[i], 0.09, m))
+        for g, s in zip(graphs, streams):
+            with torch.cuda.stream(s):
+                g.replay()
+        torch.cuda.synchronize()
+        for i in range(2):
+            assert torch.equal(outs[i], want[i]) and all(torch.equal(x, want[i]) for x in late[i])
+            assert torch.equal(c.attend(q[i], 0.09, m), want[i])
+
+
+def test_threads_that_attend_one_cache():
+    """Each on a stream of its own, or all on one."""
+    import threading
+    m = 4
+    c = Paged("bf16", "bf16", [3000, 500], [m, m], kv_heads=4, group=2, d=128, seed=m)
+    c.fill()
+    q = [c.random_rows(2 * m, 8) for _ in range(4)]
+    want = [c.attend(x, 0.09, m) for x in q]
+    torch.cuda.synchronize()
+    wrong = []
+
+    def work(i, stream):
+        torch.cuda.set_device(0)
+        with torch.cuda.stream(stream):
+            for _ in range(50):
+                if not torch.equal(c.attend(q[i], 0.09, m), want[i]):
+                    wrong.append(i)
+
+    one = torch.cuda.Stream()
+    for streams in ([torch.cuda.Stream() for _ in range(4)], [one] * 4):
+        threads = [threading.Thread(target=work, args=(i, s)) for i, s in enumerate(streams)]
+        for t in threads:
+            t.start()
+        for t in threads:
+            t.join()
+        assert not wrong
+
+
+def test_a_workspace_that_is_given_is_the_one_that_is_used():
+    import paper_2312_11462_amd as P
+    from paper_2312_11462_amd.binding import PAGED_WORKSPACE_BYTES
+    c = Paged("bf16", "bf16", [3000], [4], kv_heads=4, d=64, seed=1)
+    c.fill()
+    q = c.random_rows(4, 4)
+    want = c.attend(q, 0.1, 4)
+    w = torch.zeros(PAGED_WORKSPACE_BYTES, dtype=torch.uint8, device="cuda")
+    kv = P.PagedKv(c.k, c.v, workspace=w)
+    assert torch.equal(kv.attention(0, *c.dev, q, 0.1, 4), want) and w.any()      # (parts of the split sequence lie there)

@@ -152,3 +152,7 @@ def test_attention_over_trees_goes_by_the_rows_there_are(L):
     for rows, most, code in ((40, 100, EINVAL), (64, 65, EINVAL), (65, 64, EINVAL), (65, 65, ESHAPE), (100, 1 << 20, ESHAPE)):
         assert L.csd_paged_attention(ref, 0, 256, 256, 256, 1, rows, most, 256, 512, 8, 1, 0.125, 264, 256, None) == code, (rows, most)
     assert L.csd_paged_attention(ref, 0, 256, 256, 256, 1, 0, 100, None, 0, 8, 1, 0.125, None, None, None) == 0
+
+
+def test_capture_of_a_stream_needs_a_place_for_the_answer(L):
+    assert L.csd_stream_capture(None, None) == ENULL
