@@ -380,7 +380,7 @@ int32_t csd_paged_read(const csd_paged_kv *kv, int32_t layer, const int32_t *row
  * (a longer one is cut to it: its rows behind are left as they were; the kernels are chosen by it), 1 <= max_rows; CSD_ESHAPE for trees
  * where it and `rows` are above 64.
  * workspace: device, 256-byte aligned, CSD_PAGED_WORKSPACE_BYTES, of which the first CSD_PAGED_WORKSPACE_ZERO_BYTES are zeroed before its first use;
- * every call leaves them zeroed.  Calls that share it must not overlap.
+ * every call leaves them zeroed.  Calls that share it must not overlap.  It is used, and may not be NULL, for bf16 queries, heads of 64 or 128 and a pool of bf16 or e4m3.
  */
 #define CSD_PAGED_WORKSPACE_BYTES (72u << 20)
 #define CSD_PAGED_WORKSPACE_ZERO_BYTES (64u << 10)

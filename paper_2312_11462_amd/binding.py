@@ -262,8 +262,8 @@ class PagedKv:
     Every call takes the page table [B][n] int32 (entries outside [0, pages): no rows there) and the ragged rows of a batch: row_start
     [B + 1] int32, and a position [B] int32 for each sequence's first row.  Rows are [rows][heads][head dim], float32 or bfloat16,
     with any distance between rows that is a multiple of 8 elements.  All tensors are on the pools' device, which has to be the current one,
-    and the work is enqueued on its current stream.  The attention has a workspace (PAGED_WORKSPACE_BYTES) for every stream that it is called on and for
-    every capture, made at the first call there, so that calls on several streams and graphs that are replayed side by side may overlap.
+    and the work is enqueued on its current stream.  The attention has a workspace (PAGED_WORKSPACE_BYTES; for bf16 queries, heads of 64 or 128, pools
+    of bf16 or e4m3) for every stream that it is called on and for every capture, made at the first call there, so that calls on several streams and graphs that are replayed side by side may overlap.
     A workspace that is given serves all calls, which then must not overlap."""
 
     def __init__(self, k, v, k_scale=None, v_scale=None, workspace=None):
@@ -287,6 +287,7 @@ class PagedKv:
             raise ValueError(f"workspace: {PAGED_WORKSPACE_BYTES} bytes, the first {PAGED_WORKSPACE_ZERO_BYTES} of them zeroed")
         self.workspace = workspace
         self._ws = _ptr(workspace).value
+        self._split = self.head_dim in (64, 128) and k.dtype is not torch.float32      # (with bf16 queries: the work of a call may be split, in a workspace)
         self._eager, self._captured = {}, {}              # by stream: (address, tensor), (capture, address, tensor)
 
     def _workspace_of(self, stream):
@@ -414,7 +415,8 @@ class PagedKv:
         stream = _raw_stream(dev)
         rc = self._lib.csd_paged_attention(ref, layer, row_start.data_ptr(), cache_len.data_ptr(), up, B, rows,
                                            (rows or 1) if max_rows is None else max_rows, q.data_ptr(), qs[0] if rows > 1 else heads * d, heads,
-                                           _ROWS[dtype], scale, out.data_ptr(), self._ws or self._workspace_of(stream), stream)
+                                           _ROWS[dtype], scale, out.data_ptr(),
+                                           self._ws or (self._workspace_of(stream) if self._split and dtype is torch.bfloat16 else None), stream)
         if rc:
             _chk(rc, "csd_paged_attention")
         return out

@@ -272,6 +272,10 @@ int32_t csd_paged_attention_enqueue(const PagedAttn &a, int32_t pool_dtype, int3
 #define CSD_PAGED_FEW_PARTS 64       /* parts of an item at most */
 #define CSD_PAGED_FEW_ROWS 32
 static_assert(CSD_PAGED_COUNTER_BYTES + 2ull * CSD_PAGED_FEW_GRID * CSD_PAGED_FEW_ROWS * 132 * 4 <= CSD_PAGED_WORKSPACE_BYTES, "");
+// the types and head sizes of the kernels that split their work over workgroups
+static inline bool csd_paged_few_types(int32_t head_dim, int32_t pool_dtype, int32_t q_dtype) {
+    return q_dtype == CSD_DTYPE_BF16 && pool_dtype != CSD_DTYPE_FP32 && (head_dim == 64 || head_dim == 128);
+}
 bool csd_paged_few_fits(const PagedAttn &a, int32_t pool_dtype, int32_t q_dtype);
 void csd_paged_few_enqueue(const PagedAttn &a, int rows, int32_t pool_dtype, hipStream_t st);
 

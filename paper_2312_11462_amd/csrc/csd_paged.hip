@@ -411,7 +411,7 @@ extern "C" int32_t csd_paged_attention(const csd_paged_kv *kv, int32_t layer, co
     const int32_t most = max_rows < rows ? max_rows : rows;
     if (n_heads > 65535 || (parent && most > 64)) return CSD_ESHAPE;
     if (rows == 0) return CSD_OK;
-    if (!q || !out || !workspace) return CSD_ENULL;
+    if (!q || !out || (!workspace && csd_paged_few_types(kv->head_dim, kv->dtype, dtype))) return CSD_ENULL;
     if (!row_stride_ok(kv, n_heads, q_stride, q) || (uintptr_t)out % 16 || (uintptr_t)workspace % 256) return CSD_EINVAL;
     const PagedAttn a{csd_paged_layer(kv, layer), PagedRows{row_start, cache_len, B, rows}, parent, most,
                       n_heads / kv->n_kv_heads, q, (long long)q_stride, out, scale, workspace};

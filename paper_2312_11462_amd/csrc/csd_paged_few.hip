@@ -501,7 +501,7 @@ static void few_rows(const PagedAttn &a, int rows, hipStream_t st) {
 }
 
 bool csd_paged_few_fits(const PagedAttn &a, int32_t pool_dtype, int32_t q_dtype) {
-    if (q_dtype != CSD_DTYPE_BF16 || pool_dtype == CSD_DTYPE_FP32 || (a.p.D != 64 && a.p.D != 128)) return false;
+    if (!csd_paged_few_types(a.p.D, pool_dtype, q_dtype)) return false;
     // tiles are counted in 32 bits, and so are the work items of a launch
     const long long tiles = (((long long)a.p.table_stride << a.p.page_shift) + 31) / 32, heads = (long long)a.p.Hkv * a.group;
     return (tiles + CSD_PAGED_FEW_COST) * a.p.Hkv * a.r.B < (1ll << 30) && (long long)a.r.rows * heads / 128 + (long long)a.r.B * a.p.Hkv < (1ll << 23);

@@ -1026,3 +1026,16 @@ def test_a_workspace_that_is_given_is_the_one_that_is_used():
     w = torch.zeros(PAGED_WORKSPACE_BYTES, dtype=torch.uint8, device="cuda")
     kv = P.PagedKv(c.k, c.v, workspace=w)
     assert torch.equal(kv.attention(0, *c.dev, q, 0.1, 4), want) and w.any()      # (parts of the split sequence lie there)
+
+
+@pytest.mark.parametrize("rows,cache,d,made", [("fp32", "fp32", 64, 0), ("fp32", "fp8", 64, 0), ("bf16", "bf16", 80, 0), ("bf16", "fp32", 64, 0), ("bf16", "bf16", 64, 1), ("bf16", "fp8", 128, 1)])
+def test_a_cache_has_a_workspace_only_where_its_attention_uses_one(rows, cache, d, made):
+    from paper_2312_11462_amd.binding import PAGED_WORKSPACE_BYTES
+    c = Paged(cache, rows, [40], [3], kv_heads=2, d=d)
+    c.fill()
+    q = c.random_rows(3, 2)
+    torch.cuda.synchronize()
+    before = torch.cuda.memory_allocated()
+    out = c.attend(q, 0.1, 3)
+    del out
+    assert (torch.cuda.memory_allocated() - before) // PAGED_WORKSPACE_BYTES == made

@@ -156,3 +156,10 @@ def test_attention_over_trees_goes_by_the_rows_there_are(L):
 
 def test_capture_of_a_stream_needs_a_place_for_the_answer(L):
     assert L.csd_stream_capture(None, None) == ENULL
+
+
+def test_a_workspace_is_asked_for_where_it_is_used(L):
+    """(the queries' distance is refused behind that)"""
+    for pool, heads_of, dtype, code in ((2, 64, 1, ENULL), (1, 128, 1, ENULL), (0, 64, 1, EINVAL), (1, 64, 0, EINVAL), (2, 80, 1, EINVAL), (0, 16, 0, EINVAL)):
+        ref, keep = _pool(dtype=pool, head_dim=heads_of)
+        assert L.csd_paged_attention(ref, 0, 256, 256, None, 1, 4, 4, 256, 4, 8, dtype, 0.125, 256, None, None) == code, (pool, heads_of, dtype)
