@@ -53,6 +53,7 @@ template <typename TQ, typename TP>
 __global__ __launch_bounds__(64 * kAnyWaves) void k_paged_attn_any(PagedAttn a, int log_w) {
     __shared__ float s_o[kAnyWaves][256], s_m[kAnyWaves], s_l[kAnyWaves], s_w[kAnyWaves][64];
     __shared__ size_t s_at[kAnyWaves][64];
+    __shared__ bool s_any[kAnyWaves];                        // the wave has met a key that the row attends
     const int row = blockIdx.x, head = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int waves = blockDim.x >> 6;
     const PagedPool &p = a.p;
@@ -89,6 +90,7 @@ __global__ __launch_bounds__(64 * kAnyWaves) void k_paged_attn_any(PagedAttn a, 
     const unsigned long long above = a.parent ? lane_of(paged_ancestors(a.parent, s, lane), i) : ~0ull;      // (trees: max_rows <= 64)
     constexpr float kLog2e = 1.44269504088896f;
     float m_run = -INFINITY, l_run = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
+    bool any = false;
     const int keys = min(s.t + i + 1, p.table_stride << p.page_shift);
     for (int key0 = wave * 64; key0 < keys; key0 += 64 * waves) {
         const int key = key0 + lane;
@@ -97,6 +99,7 @@ __global__ __launch_bounds__(64 * kAnyWaves) void k_paged_attn_any(PagedAttn a, 
         const size_t at = page >= 0 ? paged_row(p, page, kvh, key) : 0;
         const unsigned long long seen = __ballot(page >= 0);
         if (!seen) continue;
+        any = true;
         s_at[wave][lane] = at;
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         // step j: keys j * per_step + key_in of the 64
@@ -160,6 +163,7 @@ __global__ __launch_bounds__(64 * kAnyWaves) void k_paged_attn_any(PagedAttn a, 
     if (lane == 0) {
         s_m[wave] = m_run;
         s_l[wave] = l_run;
+        s_any[wave] = any;
     }
     __syncthreads();
     if (tid >= D) return;
@@ -167,16 +171,14 @@ __global__ __launch_bounds__(64 * kAnyWaves) void k_paged_attn_any(PagedAttn a, 
     for (int w = 1; w < waves; w++) m_all = fmaxf(m_all, s_m[w]);
     if (m_all == -INFINITY) m_all = 0.f;
     float l = 0.f, x = 0.f;
+    any = false;
     for (int w = 0; w < waves; w++) {
         const float f = exp2f((s_m[w] - m_all) * kLog2e);
         l += f * s_l[w];
         x += f * s_o[w][tid];
+        any |= s_any[w];
     }
     // nothing to attend: zeros (0 / 0 where there are keys but all scores are -inf, as the formula has it)
-    bool any = l != 0.f;
-    if (!any)
-        for (int key = 0; key < keys && !any; key++)
-            any = paged_page(p, b, key) >= 0 && (!a.parent || key < s.t || ((above >> min(key - s.t, 63)) & 1ull));
     TQ *out = reinterpret_cast<TQ *>(a.out) + ((size_t)row * p.Hkv * a.group + head) * D;
     out[tid] = from_f32<TQ>(any ? x / l : 0.f);
 }

@@ -1039,3 +1039,22 @@ def test_a_cache_has_a_workspace_only_where_its_attention_uses_one(rows, cache, 
     out = c.attend(q, 0.1, 3)
     del out
     assert (torch.cuda.memory_allocated() - before) // PAGED_WORKSPACE_BYTES == made
+
+
+@pytest.mark.parametrize("rows,cache,d", [("fp32", "fp32", 32), ("bf16", "bf16", 80), ("bf16", "bf16", 64), ("bf16", "bf16", 128)])
+@pytest.mark.parametrize("m", [2, 40, 70])
+def test_rows_whose_scores_are_all_minus_infinity(rows, cache, d, m):
+    """0 / 0, as the formula has it, however many pages are gone; a row without any key left is zero, without a search for one."""
+    c = Paged(cache, rows, [300, 300, 300], [m, m, m], kv_heads=2, d=d, seed=m)
+    k, v = c.fill()
+    k[:300 + m, 1, 3] = -math.inf                                       # the first sequence's second head
+    whole = torch.arange(4, dtype=torch.int32, device="cuda") * (300 + m)
+    c.kv.write(0, c.dev[0], whole, torch.zeros(3, dtype=torch.int32, device="cuda"), k, v)
+    c.table[0, 3:15] = -1
+    c.table[1] = -1
+    c.dev[0].copy_(torch.tensor(c.table))
+    q = c.random_rows(3 * m, 2).abs()
+    out = c.attend(q, d ** -0.5, m)
+    with np.errstate(invalid="ignore"):
+        want = c.check(out, q, d ** -0.5)
+    assert np.isnan(want[:m, 1]).all() and torch.isnan(out[:m, 1]).all() and (out[m:2 * m] == 0).all() and torch.isfinite(out[2 * m:]).all()
