@@ -1058,3 +1058,65 @@ def test_rows_whose_scores_are_all_minus_infinity(rows, cache, d, m):
     with np.errstate(invalid="ignore"):
         want = c.check(out, q, d ** -0.5)
     assert np.isnan(want[:m, 1]).all() and torch.isnan(out[:m, 1]).all() and (out[m:2 * m] == 0).all() and torch.isfinite(out[2 * m:]).all()
+
+
+EVERY = FULL + [("fp32", "fp32", 64), ("fp32", "fp8", 64), ("bf16", "bf16", 80)]
+
+
+@pytest.mark.parametrize("rows,cache,d", EVERY)
+@pytest.mark.parametrize("m,group,others", [(1, 1, 0), (1, 8, 0), (5, 4, 0), (9, 2, 0), (40, 1, 0), (64, 2, 0), (130, 1, 0), (40, 4, MORE), (150, 4, MORE)])
+def test_every_key_counts_once(rows, cache, d, m, group, others):
+    """All weights alike, and of each stretch of 32 keys a feature that is 1 while the others are 0 (the first head counts the stretches by d, the second their rounds): an output
+    is the share of its stretches' keys.  Weights and their sums are exact then, and a key left out at a border of tiles, pages, shares or parts, or taken twice, changes
+    its share by more than the output's rounding (one of 141 keys at least) or is in a share that has to be 0."""
+    lens = [9001, 3, 4097, 0, 1333]
+    c = Paged(cache, rows, lens + [0] * others, [m] * 5 + [9] * others, kv_heads=2, group=group, d=d, page=16 if m % 2 else 64, seed=m)
+    k, _ = c.fill()
+    whole = [t + n for t, n in zip(c.cached, c.new)]
+    stretch = np.concatenate([np.arange(n) for n in whole]) // 32
+    feature = np.stack([stretch % d, stretch // d % d], 1)
+    v = torch.nn.functional.one_hot(torch.tensor(feature), d).to(TORCH[rows]).cuda()
+    start = torch.tensor(np.concatenate([[0], np.cumsum(whole)]), dtype=torch.int32, device="cuda")
+    c.kv.write(0, c.dev[0], start, torch.zeros(len(whole), dtype=torch.int32, device="cuda"), k, v)
+    lost = range(20, 23)
+    c.table[4, lost] = -1
+    c.dev[0].copy_(torch.tensor(c.table))
+    q = c.random_rows(c.total, 2 * group)
+    got = c.attend(q, 0.0, m).double().cpu().numpy()
+    for b, t in enumerate(lens):
+        there = np.ones(t + m)
+        if b == 4:
+            there[20 * c.page:23 * c.page] = 0
+        at = np.arange(t + m) // 32
+        for head, f in enumerate((at % d, at // d % d)):
+            counts = np.zeros((t + m, d))
+            counts[np.arange(t + m), f] = there
+            want = np.cumsum(counts, 0)[t:] / np.cumsum(there)[t:, None]
+            off = np.abs(got[c.start[b]:c.start[b + 1], head * group:(head + 1) * group] - want[:, None])
+            assert (off <= (2.0 ** -8 if rows == "bf16" else 2.0 ** -24) * 1.001 * want[:, None] + 2.0 ** -22 * want[:, None]).all(), (b, head)
+
+
+@pytest.mark.parametrize("rows,cache,d", EVERY)
+@pytest.mark.parametrize("m,group,others", [(1, 2, 0), (5, 4, 0), (64, 1, 0), (129, 1, 0), (200, 2, MORE)])
+def test_errors_are_those_of_the_roundings(rows, cache, d, m, group, others):
+    """Over all outputs.  Roundings to bf16 are off by 2^-8 / sqrt(3) of the step's lower end at most in the mean square, independently of one another: the output's, of itself, and in chunks of
+    more than 64 rows each weight's, of p v.  With the mean over the step's mantissas (1 / m^2 over m in 1 .. 2, density 1 / (m ln 2): 0.54) that is 0.42 of 2^-8; held to 0.55."""
+    c = Paged(cache, rows, [9001, 1200] + [0] * others, [m] * 2 + [9] * others, kv_heads=2, group=group, d=d, seed=m)
+    c.fill()
+    q = c.random_rows(c.total, 2 * group, loud=False)
+    got = c.attend(q, d ** -0.5, m).double().cpu()
+    kk, vv = (torch.tensor(c.values(pool, scale)[0]) for pool, scale in ((c.k, c.ks), (c.v, c.vs)))
+    rounded = 2.0 ** -8 if rows == "bf16" else 0.0
+    weights = rounded if m > 64 and d in (64, 128) and rows == "bf16" else 2.0 ** -14 if rows == "bf16" else 2.0 ** -16
+    err = room = 0.0
+    for b in range(2):
+        n = c.cached[b] + m
+        page, slot = torch.tensor(c.table[b])[torch.arange(n) // c.page].long(), torch.arange(n) % c.page
+        hidden = torch.arange(n)[None] > c.cached[b] + torch.arange(m)[:, None]
+        for h in range(2 * group):
+            k, v = kk[page, h // group, slot], vv[page, h // group, slot]
+            p = ((q[c.start[b]:c.start[b + 1], h].double().cpu() @ k.t().contiguous()) * d ** -0.5).masked_fill(hidden, -math.inf).softmax(-1)
+            want = p @ v
+            err += ((got[c.start[b]:c.start[b + 1], h] - want) ** 2).sum().item()
+            room += (0.55 ** 2 * (rounded ** 2 * want ** 2 + weights ** 2 * (p ** 2 @ v ** 2))).sum().item()
+    assert err <= room, f"{math.sqrt(err / room):.2f} times the bound"
