@@ -1120,3 +1120,52 @@ def test_errors_are_those_of_the_roundings(rows, cache, d, m, group, others):
             err += ((got[c.start[b]:c.start[b + 1], h] - want) ** 2).sum().item()
             room += (0.55 ** 2 * (rounded ** 2 * want ** 2 + weights ** 2 * (p ** 2 @ v ** 2))).sum().item()
     assert err <= room, f"{math.sqrt(err / room):.2f} times the bound"
+
+
+@pytest.mark.parametrize("tree", [False, True])
+@pytest.mark.parametrize("rows", ["fp32", "bf16"])
+def test_attention_over_a_models_rows_is_the_models_own(rows, tree):
+    """Its first layer computed in 64 bits around the attention over pages that hold its cached rows, against what the model itself computed.  With fp32 queries both attentions
+    are exact but for 2^-15 or so (the model's products take two bf16 planes); bf16 queries and outputs are off by 2^-9 in the mean."""
+    import csd_inputs as I
+    import paper_2312_11462_amd as P
+    H, dh, n, m = 4, 64, 96, 7
+    shape = I.ModelShape("own", 0, "bf16", 1, 256, H, dh, 512, 1024)
+    weights = I.make_weights(shape, 5, device="cuda", std=0.08)
+    gm = P.Model(shape, weights, max_batch=1, max_seq=160, max_block=8)
+    toks = I.token_ids(120, shape.vocab, 5, 1).cuda()
+    for pos in range(0, n, 8):
+        gm.verify_block(toks[None, pos:pos + 8].contiguous(), torch.full((1,), pos, dtype=torch.int32, device="cuda"))
+    trace = torch.zeros((2, m, 256), device="cuda")
+    block, at = toks[None, n:n + m].contiguous(), torch.full((1,), n, dtype=torch.int32, device="cuda")
+    parent = torch.tensor([0, 0, 0, 1, 1, 2, 4], dtype=torch.int32, device="cuda")
+    depth = torch.tensor([0, 1, 1, 2, 2, 2, 3] if tree else range(m))
+    gm.set_trace(trace)
+    if tree:
+        gm.verify_tree(block, parent[None].contiguous(), at)
+    else:
+        gm.verify_block(block, at)
+    gm.set_trace(None)
+    pool = torch.zeros((1, 8, H, 16, dh), dtype=torch.bfloat16, device="cuda")
+    kv = P.PagedKv(pool, torch.zeros_like(pool))
+    table = torch.tensor([[5, 0, 7, 2, 1, 6, 3]], dtype=torch.int32, device="cuda")
+    K, V = gm.kv_read(0, 0, 0, n + m)
+    zero = torch.zeros(1, dtype=torch.int32, device="cuda")
+    kv.write(0, table, torch.tensor([0, n + m], dtype=torch.int32, device="cuda"), zero, K.view(n + m, H, dh), V.view(n + m, H, dh))
+    embed, norm, wq, _, _, wo, norm2, gate, up, down = (w.double().cpu() for w in weights[:10])
+
+    def rms(x, g):
+        return x / (x.square().mean(-1, keepdim=True) + shape.rms_eps).sqrt() * g
+
+    x = embed[block[0].long().cpu()]
+    q = (rms(x, norm) @ wq).view(m, H, dh)
+    angle = (n + depth.double())[:, None] * shape.rope_theta ** (-2 * torch.arange(dh // 2, dtype=torch.float64) / dh)
+    a, b = q.chunk(2, -1)
+    cos, sin = angle.cos()[:, None], angle.sin()[:, None]
+    q = torch.cat([a * cos - b * sin, a * sin + b * cos], -1)
+    out = kv.attention(0, table, torch.tensor([0, m], dtype=torch.int32, device="cuda"), at, q.to(TORCH[rows]).cuda(), dh ** -0.5, m, parent=parent if tree else None)
+    x = x + out.double().cpu().reshape(m, H * dh) @ wo
+    h = rms(x, norm2)
+    x = x + (torch.nn.functional.silu(h @ gate) * (h @ up)) @ down
+    far = ((trace[1].double().cpu() - x).norm() / (x - trace[0].double().cpu()).norm()).item()
+    assert far < (2.0 ** -12 if rows == "fp32" else 2.0 ** -7), far
