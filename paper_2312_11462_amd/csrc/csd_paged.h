@@ -287,9 +287,10 @@ void csd_paged_few_enqueue(const PagedAttn &a, int rows, int32_t pool_dtype, hip
 #define CSD_PAGED_MANY_GRID 512      /* two workgroups per compute unit */
 #define CSD_PAGED_MANY_BATCH 512     /* sequences that take part at most */
 // With more items (row tiles times key-value heads, as far as the host can tell) than this, and sequences of as many rows as the second (times the query heads that share keys; fewer leave more than
-// a quarter of the workgroups' rows idle), csd_paged_chunk.hip takes over, a workgroup of 256 rows per item.  us here and there, heads of 128 in bf16: 8 x 4 heads, 40 sequences of
-// 64 rows over 0 to 3000 keys, 960 items, 123 and 142; 5 of 300 rows, 32 heads, 512 items, 100 and 119; 2 of 2048 rows, 8 x 4 heads, 1040 items, 526 and 418; 42 of 328
-// rows, 8 heads, 1200 items, 119 and 134; 8 of 512 rows, 32 heads, 1280 items, 161 and 146; trees of 41 rows, 32 heads, 1856 items, 123 and 168.
+// a quarter of the workgroups' rows idle), csd_paged_chunk.hip takes over, a workgroup of 256 rows per item; but not for blocks of up to CSD_PAGED_FINE_ROWS rows.  us here and there, heads of
+// 128 in bf16: 5 sequences of 300 rows over 0 to 1400 keys, 32 heads, 512 items, 66 and 76; 2 of 2048 rows over 2048 and 8191, 8 x 4 heads, 1040 items, 519 and 418; 42 of 328 rows over 0 to
+// 1000, 8 heads, 1200 items, 104 and 119; 8 of 512 rows over 0 to 700, 32 heads, 1280 items, 103 and 88; blocks: 40 of 64 rows over 0 to 3000, 8 x 4 heads, 960 items, 137 and 178; 44 trees of 41 rows
+// over 0 to 1400, 32 heads, 1856 items, 149 and 247; 150 of 48 rows over 100 to 400, 4 x 8 heads, 2400 items, 116 and 127 (e4m3 107 and 122, heads of 64 71 and 92).
 #define CSD_PAGED_MANY_ITEMS 1024
 #define CSD_PAGED_CHUNK_ROWS 384
 static_assert(CSD_PAGED_COUNTER_BYTES + 2ull * CSD_PAGED_MANY_GRID * CSD_PAGED_MANY_ROWS * 132 * 4 <= CSD_PAGED_WORKSPACE_BYTES, "");

@@ -387,8 +387,8 @@ __global__ __launch_bounds__(256, 2) void k_paged_attn_many(PagedAttn a, int min
 #pragma unroll
         for (int e = 0; e < 8; e += 2) weigh(e);
         __builtin_amdgcn_sched_barrier(0);
-        // The next 16 keys' weights are made beside the products of these.  (A wave here goes first: the matrix cores wait for nothing else; chunks of
-        // 2048 rows 550 -> 531 us, with the first products at that priority too 531.)
+        // The next 16 keys' weights are made beside the products of these.  (A wave here goes first: the matrix cores wait for nothing else; 4 chunks of 250 rows
+        // and 20 tokens, 8 x 4 heads of 64, 94.7 -> 87.5 us, 300 rows over 8000 keys, heads of 128, 76.9 -> 74.2.)
         __builtin_amdgcn_s_setprio(1);
 #pragma unroll
         for (int x = 0; x < 4 * DT; x++) {
@@ -445,7 +445,7 @@ __global__ __launch_bounds__(256, 2) void k_paged_attn_many(PagedAttn a, int min
 
     // ---- results: element e of acc[d] is feature 32 d + 8 (e / 4) + 4 h + e % 4 of the lane's row.  Turned in LDS, where the key tiles were (16-byte pieces,
     // their index xored by the row), so that whole rows are written one behind the other (with the join by 4 x 4 pieces, against 16-byte stores from here and
-    // a join by fours: a tree of 41 rows over 1024 keys, 32 heads of 128, 23.9 -> 21.5 us).
+    // a join by fours: a tree of 41 rows over 1024 keys, 32 heads of 128, 23.9 -> 21.5 us; 22.6 with weights in two planes).
     constexpr int C = DH / 4;
     auto piece = [&](int row, int c) { return row * C + (c ^ (row & (C - 1))); };
     u32x4 *s_o = &s_tiles[0][0];
@@ -507,7 +507,8 @@ void csd_paged_many_enqueue(const PagedAttn &a, int min_rows, int32_t pool_dtype
     // row tiles if some sequences have max_rows rows and the others one
     const long long most = a.max_rows, full = most > 1 ? (a.r.rows - (long long)a.r.B + most - 2) / (most - 1) : a.r.B;
     const long long likely = (full * most * a.group / CSD_PAGED_MANY_ROWS + full) * a.p.Hkv;
-    if (!fits || (likely > CSD_PAGED_MANY_ITEMS && most * a.group >= CSD_PAGED_CHUNK_ROWS)) return csd_paged_chunk_enqueue(a, min_rows, pool_dtype, st);
+    if (!fits || (likely > CSD_PAGED_MANY_ITEMS && most > CSD_PAGED_FINE_ROWS && most * a.group >= CSD_PAGED_CHUNK_ROWS))
+        return csd_paged_chunk_enqueue(a, min_rows, pool_dtype, st);
     auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(CSD_PAGED_MANY_GRID), dim3(256), 0, st, a, min_rows); };
     const bool f8 = pool_dtype == CSD_DTYPE_FP8;
     if (a.p.D == 128) f8 ? launch(k_paged_attn_many<128, true>) : launch(k_paged_attn_many<128, false>);
