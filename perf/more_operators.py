@@ -274,10 +274,10 @@ def _plain_pages(s):
     at = torch.arange(room, device="cuda")
     # the step's rows enter
     wanted = (s.cache_len + s.new_rows + c.page - 1) // c.page
-    need = (wanted - s.held).clamp(min=0)
-    run = torch.cumsum(need, 0)
-    served = (wanted <= room) & ((need == 0) | (run <= s.n_free)) & ((s.new_rows == 0) | (torch.cumsum(s.new_rows, 0) <= s.total))
-    need, rows = need * served, s.new_rows * served
+    fits = wanted <= room
+    need, rows = (wanted - s.held).clamp(min=0) * fits, s.new_rows * fits
+    served = fits & ((need == 0) | (torch.cumsum(need, 0) <= s.n_free)) & ((rows == 0) | (torch.cumsum(rows, 0) <= s.total))
+    need, rows = need * served, rows * served
     rank = torch.cumsum(need, 0) - need
     fresh = (at >= s.held[:, None]) & (at < (s.held + need)[:, None])
     take = s.n_free - 1 - (rank[:, None] + at - s.held[:, None])
