@@ -396,6 +396,91 @@ int32_t csd_paged_attention(const csd_paged_kv *kv, int32_t layer, const int32_t
 int32_t csd_paged_commit(const csd_paged_kv *kv, const int32_t *cache_len, const int32_t *path, const int32_t *n_accepted,
                          int32_t B, int32_t m, void *stream);
 
+/*
+ * Cross-attention over pages (the encoder-decoder reviewers of Section 5.1, in batches of different lengths): position j of a sequence is row j of its encoder's
+ * projected states, written once per prompt with csd_paged_write, and every row of the block or chunk attends positions 0 .. enc_len[b], those
+ * excluded that have no page.  The rows of the call themselves are in no page.  A sequence with enc_len[b] <= 0 gives zeros.  Everything else is as for
+ * csd_paged_attention: types, head sizes, strides, ragged rows, rounding, workspace, errors.
+ */
+int32_t csd_paged_cross_attention(const csd_paged_kv *kv, int32_t layer, const int32_t *row_start, const int32_t *enc_len, int32_t B,
+                                  int32_t rows, int32_t max_rows, const void *q, int64_t q_stride, int32_t n_heads, int32_t dtype,
+                                  float scale, void *out, void *workspace, void *stream);
+
+/*
+ * Which sequence holds which pages.  The calls below keep, on the device, what the paged calls take: page tables that follow the sequences' lengths, the row
+ * starts of a step's batch, and the place of every row.  All arrays belong to the caller, who sets them up once (table and held as the
+ * sequences stand, at first -1 and 0; free_pages[0 .. *n_free) the pages of nobody; users[page] how many tables name a page):
+ *   table[n_sequences][table_stride]   pages of every sequence in order, the paged calls' table
+ *   held[n_sequences]                  entries in use
+ *   free_pages[n_pages], n_free[1]     a stack: pages are taken from its end
+ *   users[n_pages]                     tables that name a page; 0 for those in the stack
+ * page_rows as in csd_paged_kv.  Lengths that are negative count as 0, n_free and held are cut to their ranges, entries that name no page are passed over.
+ * Calls on the same arrays must not overlap.  CSD_ESHAPE: more than 2^20 sequences, 2^30 table entries or pages, table_stride * page_rows above 2^30.
+ */
+typedef struct csd_pages {
+    int32_t n_pages, page_rows, n_sequences, table_stride;
+    int32_t *table, *held, *free_pages, *n_free, *users;
+} csd_pages;
+
+/*
+ * Before a step: sequence b has cache_len[b] rows and gets new_rows[b] more.  Its table is continued to hold them all, by pages from the stack's end on, in
+ * order of (sequence, place), each with one user.  served[b] is 1, or 0 where the rows cannot be had: they do not fit the
+ * table (such a sequence counts for nothing below); pages are missing and the pages wanted up to and with sequence b are more than there are; or there are rows and
+ * the rows up to and with it are more than `rows`.  A sequence that is not served keeps what it holds and has no rows in this step.
+ *   row_start[n_sequences + 1]  sums of the served sequences' rows, as the paged calls take them
+ *   sequence, position[rows], slot[rows] (int64)   of every row: its sequence, its position and where its place lies, page * page_rows + position % page_rows
+ *     (-1: the place has no page); -1 in all three behind the last row
+ */
+int32_t csd_pages_plan(const csd_pages *pages, const int32_t *cache_len, const int32_t *new_rows, int32_t rows, int32_t *row_start,
+                       int32_t *sequence, int32_t *position, int64_t *slot, int32_t *served, void *stream);
+
+/*
+ * After a step: sequence b keeps its first keep_len[b] rows (0: it has ended; negative: it is left alone).  Pages behind them leave its table (-1)
+ * and lose a user; those without any go back to the stack, in an order in which the next plan takes them by (sequence, place) again.  A page that
+ * two sequences give up in one call goes back once.
+ */
+int32_t csd_pages_release(const csd_pages *pages, const int32_t *keep_len, void *stream);
+
+/*
+ * A common prompt: sequence b, which holds nothing yet, takes over the pages of the first length[b] / page_rows * page_rows rows of sequence source[b] (whole
+ * pages only, and as many as that one holds), which get one user more.  source[b] outside [0, n_sequences), or b itself, or a sequence that has a
+ * source of its own in this call: left alone.
+ */
+int32_t csd_pages_share(const csd_pages *pages, const int32_t *source, const int32_t *length, void *stream);
+
+/*
+ * Draws from logits, and the probabilities of such draws (what csd_accept and csd_tree_accept take as p and q when the reviewer and the drafts are to be sampled
+ * by top-k, top-p or min-p).  For a row of logits with the largest one M, w_v = exp((l_v - M) / temperature); tokens are ranked by logit, of equal
+ * ones the lowest first.
+ *   top_k        the first top_k of the ranking stay (<= 0, or more than there are: all)
+ *   top_p        of these the shortest start that has at least top_p of their weight, one token at least (>= 1: all)
+ *   min_p        of these the tokens with w_v >= min_p (values above 1 count as 1)
+ *   temperature  0 (or anything that is not positive): the first of the ranking alone
+ * A token that stays has the probability w_v / (sum of w over those that stay), the others 0.  The token drawn by u in [0, 1) is the lowest one at which the
+ * running sum of the weights that stay, by token, passes u times their sum.  Weights are summed as whole numbers of 2^-45 (rounded to nearest; a
+ * token of less than 2^-46 has none), so the result does not depend on how a row is spread over the chip.  NaN counts as -inf; infinite logits share the
+ * weight; a row without any logit above -inf gives token -1 and probabilities of 0.
+ * Each parameter is an array [rows / rows_each] on the device, for rows_each consecutive rows an entry, or NULL: then the number beside it goes for all rows
+ * (CSD_EINVAL: temperature_all or top_p_all negative or NaN, min_p_all outside [0, 1]).
+ */
+typedef struct csd_filter {
+    const float *temperature;
+    const int32_t *top_k;
+    const float *top_p, *min_p;
+    float temperature_all;
+    int32_t top_k_all;
+    float top_p_all, min_p_all;
+    int32_t rows_each;             /* >= 1 */
+} csd_filter;
+
+/* logits: [rows][V] of dtype CSD_DTYPE_FP32 or CSD_DTYPE_BF16, `stride` elements (>= V) from one row to the next, any alignment that the type has.  u[rows], tokens[rows];
+ * probs: [rows][V] fp32, or NULL.  CSD_ESHAPE: V above 2^18, more than 2^22 rows. */
+int32_t csd_sample(const csd_filter *filter, const void *logits, int64_t stride, int32_t dtype, int32_t rows, int32_t V, const float *u,
+                   int32_t *tokens, float *probs, void *stream);
+/* The probabilities alone. */
+int32_t csd_filter_probs(const csd_filter *filter, const void *logits, int64_t stride, int32_t dtype, int32_t rows, int32_t V, float *probs,
+                         void *stream);
+
 /* Whether the stream is being captured into a graph: *id is 0, or a number that no other capture has.  For callers that keep workspaces: graphs that may be
  * replayed side by side must not share one. */
 int32_t csd_stream_capture(void *stream, uint64_t *id);

@@ -18,7 +18,7 @@ _LIB_PATH = os.path.join(_HERE, "libcsd.so")
 EXPORTS = ["csd_version", "csd_last_hip_error", "csd_model_create", "csd_model_destroy", "csd_kv_bytes",
            "csd_kv_write", "csd_kv_read", "csd_cross_kv_init", "csd_bigram_fit", "csd_bigram_draft", "csd_maxgram_draft", "csd_verify_block",
            "csd_accept", "csd_verify_accept", "csd_verify_accept_static", "csd_review_ctx", "csd_bigram_draft_append", "csd_cascade_gate", "csd_verify_tree", "csd_tree_accept", "csd_tree_commit",
-           "csd_paged_write", "csd_paged_read", "csd_paged_attention", "csd_paged_commit", "csd_stream_capture", "csd_debug_set_trace", "csd_debug_path", "csd_debug_gemm_plan", "csd_debug_tall_plan", "csd_debug_copy", "csd_debug_read", "csd_debug_mfma",
+           "csd_paged_write", "csd_paged_read", "csd_paged_attention", "csd_paged_commit", "csd_paged_cross_attention", "csd_pages_plan", "csd_pages_release", "csd_pages_share", "csd_sample", "csd_filter_probs", "csd_stream_capture", "csd_debug_set_trace", "csd_debug_path", "csd_debug_gemm_plan", "csd_debug_tall_plan", "csd_debug_copy", "csd_debug_read", "csd_debug_mfma",
            "csd_prof_enable", "csd_prof_read"]
 
 _STATUS = {-1: "CSD_EINVAL", -2: "CSD_ESHAPE", -3: "CSD_ENULL", -4: "CSD_EHIP", -5: "CSD_EUNSUPPORTED"}
@@ -53,12 +53,30 @@ class PagedPool(C.Structure):
                [(n, C.c_void_p) for n in ("k", "v", "k_scale", "v_scale", "table")] + [("table_stride", C.c_int32)]
 
 
+class PageTable(C.Structure):
+    """csd_pages: which sequence holds which pages."""
+    _fields_ = [(n, C.c_int32) for n in ("n_pages", "page_rows", "n_sequences", "table_stride")] + \
+               [(n, C.c_void_p) for n in ("table", "held", "free_pages", "n_free", "users")]
+
+
+class Filter(C.Structure):
+    """csd_filter: the parameters of draws from logits."""
+    _fields_ = [(n, C.c_void_p) for n in ("temperature", "top_k", "top_p", "min_p")] + \
+               [("temperature_all", C.c_float), ("top_k_all", C.c_int32), ("top_p_all", C.c_float), ("min_p_all", C.c_float), ("rows_each", C.c_int32)]
+
+
 _P, _I, _L = C.c_void_p, C.c_int32, C.c_int64
 # the paged calls are short: ctypes converts plain integers by these, without an object per argument
 _ARGTYPES = {"csd_paged_write": [_P, _I, _P, _P, _I, _I, _P, _L, _P, _L, _I, _P],
              "csd_paged_read": [_P, _I, _P, _P, _I, _I, _P, _L, _P, _L, _I, _P],
              "csd_paged_attention": [_P, _I, _P, _P, _P, _I, _I, _I, _P, _L, _I, _I, C.c_float, _P, _P, _P],
              "csd_paged_commit": [_P, _P, _P, _P, _I, _I, _P],
+             "csd_paged_cross_attention": [_P, _I, _P, _P, _I, _I, _I, _P, _L, _I, _I, C.c_float, _P, _P, _P],
+             "csd_pages_plan": [_P, _P, _P, _I, _P, _P, _P, _P, _P, _P],
+             "csd_pages_release": [_P, _P, _P],
+             "csd_pages_share": [_P, _P, _P, _P],
+             "csd_sample": [_P, _P, _L, _I, _I, _I, _P, _P, _P, _P],
+             "csd_filter_probs": [_P, _P, _L, _I, _I, _I, _P, _P],
              "csd_stream_capture": [_P, _P]}
 PAGED_WORKSPACE_BYTES, PAGED_WORKSPACE_ZERO_BYTES = 72 << 20, 64 << 10
 _ROWS = {torch.float32: 0, torch.bfloat16: 1}     # types of dense rows
@@ -421,6 +439,33 @@ class PagedKv:
             _chk(rc, "csd_paged_attention")
         return out
 
+    def cross_attention(self, layer, table, row_start, enc_len, q, scale, max_rows=None, out=None):
+        """csd_paged_cross_attention: every row of sequence b attends the enc_len[b] rows that its table names (an encoder's projected states, written once with
+        `write`); q, out, scale and max_rows as for `attention`."""
+        dev, i32, d = self._dev, torch.int32, self.head_dim
+        B, n = table.shape
+        rows, heads, width = q.shape
+        dtype, qs = q.dtype, q.stride()
+        if not (dev == table.get_device() == row_start.get_device() == enc_len.get_device() == q.get_device()
+                and i32 is table.dtype is row_start.dtype is enc_len.dtype and table.is_contiguous() and row_start.is_contiguous()
+                and enc_len.is_contiguous() and row_start.numel() == B + 1 and enc_len.numel() == B and dtype in _ROWS and width == d
+                and qs[1:] == (d, 1) and _current_device() == dev):
+            self._check(table=(table, B * n), row_start=(row_start, B + 1), enc_len=(enc_len, B), q=(q, (rows, heads, d)))
+        if out is None:
+            out = torch.empty(rows, heads, d, dtype=dtype, device=self._device)
+        elif not (out.dtype is dtype and out.shape == q.shape and out.get_device() == dev and out.is_contiguous()):
+            self._check(q=(q, (rows, heads, d)), out=(out, (rows, heads, d)))
+            raise ValueError("out: a contiguous tensor is required")
+        pool, ref = self._mine()
+        pool.table, pool.table_stride = table.data_ptr(), n
+        stream = _raw_stream(dev)
+        rc = self._lib.csd_paged_cross_attention(ref, layer, row_start.data_ptr(), enc_len.data_ptr(), B, rows, (rows or 1) if max_rows is None else max_rows,
+                                                 q.data_ptr(), qs[0] if rows > 1 else heads * d, heads, _ROWS[dtype], scale, out.data_ptr(),
+                                                 self._ws or (self._workspace_of(stream) if self._split and dtype is torch.bfloat16 else None), stream)
+        if rc:
+            _chk(rc, "csd_paged_cross_attention")
+        return out
+
     def commit(self, table, cache_len, path, n_accepted):
         """csd_paged_commit: the kept rows of a tree block, path[b][: n_accepted[b]], to positions cache_len[b] + 1 .., in all layers."""
         dev, i32 = self._dev, torch.int32
@@ -436,6 +481,160 @@ class PagedKv:
         rc = self._lib.csd_paged_commit(ref, cache_len.data_ptr(), path.data_ptr(), n_accepted.data_ptr(), B, m, _raw_stream(dev))
         if rc:
             _chk(rc, "csd_paged_commit")
+
+
+class Pages:
+    """Which sequence holds which pages of a paged cache, on the device (csd_pages): table [sequences][entries], held [sequences], free [pages], n_free [1], users
+    [pages], all int32, contiguous and on one device; the caller made and owns them, and may read them between calls.  `Pages.new` makes them for
+    sequences that hold nothing.  The calls enqueue on the current stream of the arrays' device, which has to be the current one, and change the arrays in place:
+    calls on the same arrays must not overlap."""
+
+    def __init__(self, table, held, free, n_free, users, page_rows):
+        self._dev, self._device = table.get_device(), table.device
+        if table.ndim != 2 or users.shape != free.shape:
+            raise ValueError("table: [sequences][entries]; free and users: [pages]")
+        self.n_sequences, n = table.shape
+        self.n_pages, self.page_rows = free.numel(), page_rows
+        for name, t, count in (("table", table, self.n_sequences * n), ("held", held, self.n_sequences), ("free", free, self.n_pages),
+                               ("n_free", n_free, 1), ("users", users, self.n_pages)):
+            self._check(name, t, count)
+        self.table, self.held, self.free, self.n_free, self.users = table, held, free, n_free, users
+        self._lib = lib()
+        self._arrays = PageTable(self.n_pages, page_rows, self.n_sequences, n, *(t.data_ptr() for t in (table, held, free, n_free, users)))
+        self._ref = C.addressof(self._arrays)
+
+    @classmethod
+    def new(cls, n_pages, page_rows, sequences, entries, device="cuda"):
+        """For so many sequences of up to `entries` pages each, none of which holds any yet; pages are taken from 0 on."""
+        i32 = dict(dtype=torch.int32, device=device)
+        return cls(torch.full((sequences, entries), -1, **i32), torch.zeros(sequences, **i32), torch.arange(n_pages - 1, -1, -1, **i32),
+                   torch.full((1,), n_pages, **i32), torch.zeros(n_pages, **i32), page_rows)
+
+    def _check(self, name, t, count):
+        if t.get_device() != self._dev or self._dev < 0:
+            raise ValueError(f"{name}: a tensor on the arrays' device is required")
+        if t.dtype is not torch.int32:
+            raise TypeError(f"{name}: expected torch.int32, got {t.dtype}")
+        if t.numel() != count or not t.is_contiguous():
+            raise ValueError(f"{name}: {count} contiguous elements are required")
+
+    def _given(self, **tensors):
+        if _current_device() != self._dev:
+            raise ValueError("the arrays are on another device than the current one")
+        for name, t in tensors.items():
+            self._check(name, t, self.n_sequences)
+
+    def plan(self, cache_len, new_rows, rows):
+        """csd_pages_plan: (row_start [sequences + 1], sequence [rows], position [rows], slot [rows] int64, served [sequences]); rows: the most rows of the step."""
+        self._given(cache_len=cache_len, new_rows=new_rows)
+        n = self.n_sequences
+        row_start = torch.empty(n + 1, dtype=torch.int32, device=self._device)
+        served = torch.empty(n, dtype=torch.int32, device=self._device)
+        sequence = torch.empty(rows, dtype=torch.int32, device=self._device)
+        position = torch.empty(rows, dtype=torch.int32, device=self._device)
+        slot = torch.empty(rows, dtype=torch.int64, device=self._device)
+        rc = self._lib.csd_pages_plan(self._ref, cache_len.data_ptr(), new_rows.data_ptr(), rows, row_start.data_ptr(), sequence.data_ptr(),
+                                      position.data_ptr(), slot.data_ptr(), served.data_ptr(), _raw_stream(self._dev))
+        if rc:
+            _chk(rc, "csd_pages_plan")
+        return row_start, sequence, position, slot, served
+
+    def release(self, keep_len):
+        """csd_pages_release: sequence b keeps its first keep_len[b] rows (0: it has ended; negative: it is left alone)."""
+        self._given(keep_len=keep_len)
+        rc = self._lib.csd_pages_release(self._ref, keep_len.data_ptr(), _raw_stream(self._dev))
+        if rc:
+            _chk(rc, "csd_pages_release")
+
+    def share(self, source, length):
+        """csd_pages_share: sequences that hold nothing take over the whole pages of the first length[b] rows of source[b] (negative: none)."""
+        self._given(source=source, length=length)
+        rc = self._lib.csd_pages_share(self._ref, source.data_ptr(), length.data_ptr(), _raw_stream(self._dev))
+        if rc:
+            _chk(rc, "csd_pages_share")
+
+
+def _filter(logits, temperature, top_k, top_p, min_p):
+    """(csd_filter, rows, elements between rows) of a call; raises for what is wrong with its tensors."""
+    dev, shape, stride = logits.get_device(), logits.shape, logits.stride()
+    if dev < 0:
+        raise ValueError("logits: a device tensor is required")
+    if _current_device() != dev:
+        raise ValueError("logits: on another device than the current one")
+    if logits.dtype not in _ROWS:
+        raise TypeError(f"logits are float32 or bfloat16, got {logits.dtype}")
+    V = shape[-1]
+    rows = 1
+    step = V                                              # rows are the leading dimensions, which have to be one run of equal steps
+    for size, by in zip(reversed(shape[:-1]), reversed(stride[:-1])):
+        if size > 1:
+            if rows == 1:
+                step = by
+            elif by != step * rows:
+                raise ValueError("logits: rows at equal distances are required")
+        rows *= size
+    if V > 1 and stride[-1] != 1:
+        raise ValueError("logits: contiguous rows are required")
+    f = Filter(None, None, None, None, 1.0, 0, 1.0, 0.0, 1)
+    sets = 0
+    for name, value, dtype in (("temperature", temperature, torch.float32), ("top_k", top_k, torch.int32), ("top_p", top_p, torch.float32),
+                               ("min_p", min_p, torch.float32)):
+        if isinstance(value, torch.Tensor):
+            if value.get_device() != dev:
+                raise ValueError(f"{name}: a tensor on the logits' device is required")
+            if value.dtype is not dtype:
+                raise TypeError(f"{name}: expected {dtype}, got {value.dtype}")
+            n = value.numel()
+            if not value.is_contiguous() or (rows and (n == 0 or rows % n)) or sets not in (0, n):
+                raise ValueError(f"{name}: contiguous, one entry for each row or for each of the same number of consecutive rows, all parameters alike")
+            sets = n
+            setattr(f, name, value.data_ptr())
+        elif value is not None:
+            setattr(f, name + "_all", value)
+    if sets:
+        f.rows_each = rows // sets or 1
+    return f, rows, step
+
+
+def sample(logits, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, probs=None, out=None):
+    """csd_sample: logits [..., V] float32 or bfloat16, u [...] float32 in [0, 1) -> tokens [...] int32 (-1 for a row without a logit above -inf).  The parameters are numbers,
+    or tensors with an entry for every row or for every so many consecutive rows (a sequence's block); None: not set.  probs: a float32
+    tensor [..., V] that takes the probabilities too."""
+    f, rows, step = _filter(logits, temperature, top_k, top_p, min_p)
+    shape, V = logits.shape[:-1], logits.shape[-1]
+    if out is None:
+        out = torch.empty(shape, dtype=torch.int32, device=logits.device)
+    for name, t, want, dtype in (("u", u, shape, torch.float32), ("out", out, shape, torch.int32), ("probs", probs, logits.shape, torch.float32)):
+        if t is not None:
+            _given(name, t, want, dtype, logits)
+    rc = lib().csd_sample(C.addressof(f), logits.data_ptr(), step, _ROWS[logits.dtype], rows, V, u.data_ptr(), out.data_ptr(),
+                          probs.data_ptr() if probs is not None else None, _raw_stream(logits.get_device()))
+    if rc:
+        _chk(rc, "csd_sample")
+    return out
+
+
+def filter_probs(logits, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, out=None):
+    """csd_filter_probs: the probabilities [..., V] float32 of the draws that `sample` makes with these parameters, as `accept` and `tree_accept` take them."""
+    f, rows, step = _filter(logits, temperature, top_k, top_p, min_p)
+    if out is None:
+        out = torch.empty(logits.shape, dtype=torch.float32, device=logits.device)
+    else:
+        _given("out", out, logits.shape, torch.float32, logits)
+    rc = lib().csd_filter_probs(C.addressof(f), logits.data_ptr(), step, _ROWS[logits.dtype], rows, logits.shape[-1], out.data_ptr(),
+                                _raw_stream(logits.get_device()))
+    if rc:
+        _chk(rc, "csd_filter_probs")
+    return out
+
+
+def _given(name, t, shape, dtype, like):
+    if t.get_device() != like.get_device():
+        raise ValueError(f"{name}: a tensor on the logits' device is required")
+    if t.dtype is not dtype:
+        raise TypeError(f"{name}: expected {dtype}, got {t.dtype}")
+    if t.shape != shape or not t.is_contiguous():
+        raise ValueError(f"{name}: {list(shape)}, contiguous, is required")
 
 
 def debug_copy(dst, src):

@@ -8,7 +8,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libcsd.so")
 SOURCES = ["csd_api.hip", "csd_draft.hip", "csd_accept.hip", "csd_forward.hip", "csd_attention.hip", "csd_chain.hip", "csd_rows.hip", "csd_tall.hip", "csd_f32.hip",
-           "csd_paged.hip", "csd_paged_attn.hip", "csd_paged_few.hip", "csd_paged_many.hip", "csd_paged_chunk.hip"]
+           "csd_paged.hip", "csd_paged_attn.hip", "csd_paged_few.hip", "csd_paged_many.hip", "csd_paged_chunk.hip", "csd_pages.hip", "csd_sample.hip"]
 
 
 def hipcc() -> str:

@@ -163,6 +163,11 @@ struct PagedAttn {
     void *out;
     float scale;
     void *ws;
+    int32_t cross;                // the sequences' positions are an encoder's rows (pos[b] of them): every row attends them all, and no row of the call is one
+
+    // the last position that row i of a sequence at t attends, and (cross: there may be none) the positions up to it
+    __device__ __forceinline__ int last(int t, int i) const { return cross ? t - 1 : t + i; }
+    __device__ __forceinline__ int keys(int t, int i) const { return min(last(t, i) + 1, p.table_stride << p.page_shift); }
 };
 // Parts of items.  A workgroup has two at most that are not whole items: one that others began (its slot 0) and one that others end (slot 1).  A slot
 // holds R rows of DH outputs (weighted sums), their maximum and the sum of weights.  Slots are written and read within a launch by workgroups on

@@ -401,10 +401,9 @@ extern "C" int32_t csd_paged_commit(const csd_paged_kv *kv, const int32_t *cache
     return CSD_OK;
 }
 
-extern "C" int32_t csd_paged_attention(const csd_paged_kv *kv, int32_t layer, const int32_t *row_start, const int32_t *cache_len,
-                                       const int32_t *parent, int32_t B, int32_t rows, int32_t max_rows, const void *q,
-                                       int64_t q_stride, int32_t n_heads, int32_t dtype, float scale, void *out, void *workspace,
-                                       void *stream) {
+static int32_t attention(const csd_paged_kv *kv, int32_t layer, const int32_t *row_start, const int32_t *cache_len, const int32_t *parent, int32_t cross, int32_t B,
+                         int32_t rows, int32_t max_rows, const void *q, int64_t q_stride, int32_t n_heads, int32_t dtype, float scale, void *out,
+                         void *workspace, void *stream) {
     int32_t rc = check_rows(kv, layer, row_start, cache_len, B, rows, dtype);
     if (rc != CSD_OK) return rc;
     if (max_rows < 1 || n_heads < 1 || n_heads % kv->n_kv_heads || !(fabsf(scale) < INFINITY)) return CSD_EINVAL;
@@ -414,6 +413,19 @@ extern "C" int32_t csd_paged_attention(const csd_paged_kv *kv, int32_t layer, co
     if (!q || !out || (!workspace && csd_paged_few_types(kv->head_dim, kv->dtype, dtype))) return CSD_ENULL;
     if (!row_stride_ok(kv, n_heads, q_stride, q) || (uintptr_t)out % 16 || (uintptr_t)workspace % 256) return CSD_EINVAL;
     const PagedAttn a{csd_paged_layer(kv, layer), PagedRows{row_start, cache_len, B, rows}, parent, most,
-                      n_heads / kv->n_kv_heads, q, (long long)q_stride, out, scale, workspace};
+                      n_heads / kv->n_kv_heads, q, (long long)q_stride, out, scale, workspace, cross};
     return csd_paged_attention_enqueue(a, kv->dtype, dtype, (hipStream_t)stream);
+}
+
+extern "C" int32_t csd_paged_attention(const csd_paged_kv *kv, int32_t layer, const int32_t *row_start, const int32_t *cache_len,
+                                       const int32_t *parent, int32_t B, int32_t rows, int32_t max_rows, const void *q,
+                                       int64_t q_stride, int32_t n_heads, int32_t dtype, float scale, void *out, void *workspace,
+                                       void *stream) {
+    return attention(kv, layer, row_start, cache_len, parent, 0, B, rows, max_rows, q, q_stride, n_heads, dtype, scale, out, workspace, stream);
+}
+
+extern "C" int32_t csd_paged_cross_attention(const csd_paged_kv *kv, int32_t layer, const int32_t *row_start, const int32_t *enc_len, int32_t B,
+                                             int32_t rows, int32_t max_rows, const void *q, int64_t q_stride, int32_t n_heads, int32_t dtype,
+                                             float scale, void *out, void *workspace, void *stream) {
+    return attention(kv, layer, row_start, enc_len, nullptr, 1, B, rows, max_rows, q, q_stride, n_heads, dtype, scale, out, workspace, stream);
 }

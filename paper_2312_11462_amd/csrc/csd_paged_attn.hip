@@ -91,7 +91,7 @@ __global__ __launch_bounds__(64 * kAnyWaves) void k_paged_attn_any(PagedAttn a, 
     constexpr float kLog2e = 1.44269504088896f;
     float m_run = -INFINITY, l_run = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
     bool any = false;
-    const int keys = min(s.t + i + 1, p.table_stride << p.page_shift);
+    const int keys = a.keys(s.t, i);
     for (int key0 = wave * 64; key0 < keys; key0 += 64 * waves) {
         const int key = key0 + lane;
         int page = key < keys ? paged_page(p, b, key) : -1;

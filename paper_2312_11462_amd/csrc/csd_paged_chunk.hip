@@ -67,8 +67,8 @@ __global__ __launch_bounds__(512, 2) void k_paged_attn_chunk(PagedAttn a, int mi
     }
     if (b < 0) return;
     const int rows = min(seq.m * a.group - rt * BM, BM);     // of this item
-    const int len = min(seq.t + (rt * BM + rows - 1) / a.group + 1, cap);      // keys that some row attends
-    const int n_kt = (len + kKeys - 1) / kKeys;
+    const int len = a.keys(seq.t, (rt * BM + rows - 1) / a.group);      // keys that some row attends
+    const int n_kt = tiles_of(len);
 
     // The page table, 16 tiles at a time: lane x holds where the x-th group of 16 keys from tile `base` on lies in the pools (bytes; one without a
     // page: in page 0, which the masks leave out), and bit x of `here` says that it has a page.  The window moves by eight tiles.
@@ -87,7 +87,7 @@ __global__ __launch_bounds__(512, 2) void k_paged_attn_chunk(PagedAttn a, int mi
     // ---- this lane's row
     const int r = rt * BM + wave * 32 + col, i = r / a.group, hq = r - i * a.group;
     const bool live = wave * 32 + col < rows;
-    const int limit = seq.t + i;                             // last position it attends
+    const int limit = a.last(seq.t, i);                             // last position it attends
     unsigned long long above = 0;
     if (a.parent) above = lane_of(paged_ancestors(a.parent, seq, lane), min(i, 63));
     u32x4 qf[ST];
@@ -187,7 +187,7 @@ __global__ __launch_bounds__(512, 2) void k_paged_attn_chunk(PagedAttn a, int mi
     load(1, K);
     load(1, V);
 
-    const int wave_first = seq.t + (rt * BM + wave * 32) / a.group;      // last position that the wave's first row attends
+    const int wave_first = a.last(seq.t, (rt * BM + wave * 32) / a.group);      // last position that the wave's first row attends
     // where a lane reads: K row `col` (+ 32), pieces 2 s + h; V as LDS's transposing read wants it (the place of 4 features of a key), pieces 4 d + ..
     const int l16 = lane & 15;
     const int k_at = k_piece<DH>(col, h) * 16, v_row = 4 * h + (l16 >> 2);

@@ -102,7 +102,6 @@ __global__ __launch_bounds__(256, 2) void k_paged_attn_few(PagedAttn a) {
     __shared__ int s_last;
     const PagedPool &p = a.p;
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, col = lane & 15, g = lane >> 4;
-    const int cap = p.table_stride << p.page_shift;
     const float per_group = 1.f / (float)a.group;
     auto token_of = [&](int r) { return (int)(((float)r + 0.5f) * per_group); };     // r / group, r < 32: at least 1 / 64 from the next whole number
 
@@ -113,7 +112,7 @@ __global__ __launch_bounds__(256, 2) void k_paged_attn_few(PagedAttn a) {
         s = paged_seq(a.r, b);
         s.m = min(s.m, a.max_rows);
         const int rows = s.m * a.group;
-        return rows >= 1 && rows <= R ? kCost + ((min(s.t + s.m, cap) + 31) >> 5) : 0;
+        return rows >= 1 && rows <= R ? kCost + max((a.keys(s.t, s.m - 1) + 31) >> 5, 1) : 0;      // (nothing to attend: one, left out by the masks)
     };
     PagedSeq s0;
     const int n0 = seq_of(lane, s0);                         // the first 64 sequences stay in registers
@@ -184,7 +183,7 @@ __global__ __launch_bounds__(256, 2) void k_paged_attn_few(PagedAttn a) {
         u = min(item + tiles, u_end);
         const int t0 = max(u0 - item, 0), t1 = u - item;
         if (t0 >= t1) continue;                              // (the share ends before the item's tiles begin)
-        const int len = min(seq.t + seq.m, cap), rows = seq.m * a.group;
+        const int len = a.keys(seq.t, seq.m - 1), rows = seq.m * a.group;
 
         // ---- the first pages and the queries are requested together; row r = token r / group, head r % group of the group
         const int first_page = paged_page(p, b, ((((t0 * 32) >> p.page_shift) + tid)) << p.page_shift);
@@ -197,7 +196,7 @@ __global__ __launch_bounds__(256, 2) void k_paged_attn_few(PagedAttn a) {
             const int r = rt * 16 + col, i = token_of(r), h = r - i * a.group;
             const unsigned long long above = a.parent ? lane_of(anc, min(i, 63)) : 0ull;
             if (wave == 0 && g == 0) {                       // (needed where rows differ only: not worth registers)
-                s_limit[r] = seq.t + i;
+                s_limit[r] = a.last(seq.t, i);
                 s_above[r] = above;
             }
             const bf16_t *q = reinterpret_cast<const bf16_t *>(a.q) + (size_t)(seq.start + min(i, seq.m - 1)) * a.q_stride + (size_t)(kvh * a.group + h) * DH;

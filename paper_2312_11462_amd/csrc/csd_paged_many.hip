@@ -34,7 +34,6 @@ __global__ __launch_bounds__(256, 2) void k_paged_attn_many(PagedAttn a, int min
     __shared__ int s_count[4];
     const PagedPool &p = a.p;
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, col = lane & 31, h = lane >> 5;
-    const int cap = p.table_stride << p.page_shift;
 
     auto seq_of = [&](int b, PagedSeq &s) -> int {           // row tiles of a sequence
         s = PagedSeq{0, 0, 0};
@@ -80,7 +79,7 @@ __global__ __launch_bounds__(256, 2) void k_paged_attn_many(PagedAttn a, int min
     for (int b = tid / 8; b < batch; b += 32) {              // eight lanes per sequence
         const int m = s_m[b], t = s_t[b], n = (m * a.group + BM - 1) / BM;
         int sum = 0;
-        for (int rt = tid % 8; rt < n; rt += 8) sum += COST + row_tile_keys(rt, m, t, a.group, cap);
+        for (int rt = tid % 8; rt < n; rt += 8) sum += COST + row_tile_keys(a, rt, m, t);
 #pragma unroll
         for (int o = 4; o > 0; o >>= 1) sum += __shfl_xor(sum, o, 64);
         if (tid % 8 == 0) s_units[b] = sum;
@@ -89,7 +88,7 @@ __global__ __launch_bounds__(256, 2) void k_paged_attn_many(PagedAttn a, int min
     int sum = 0, longest = 0;
     for (int b = lane; b < batch; b += 64) {
         sum += s_units[b];
-        longest = max(longest, COST + (min(s_t[b] + s_m[b], cap) + kKeys - 1) / kKeys);
+        longest = max(longest, COST + tiles_of(a.keys(s_t[b], s_m[b] - 1)));
     }
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) {
@@ -132,7 +131,7 @@ __global__ __launch_bounds__(256, 2) void k_paged_attn_many(PagedAttn a, int min
     int left = u - before - kvh * units;
     int rt = -1, kt0 = 0;
     for (int r0 = 0; r0 < n; r0 += 64) {
-        const int x = r0 + lane < n ? COST + row_tile_keys(r0 + lane, seq.m, seq.t, a.group, cap) : 0, incl = scan(x);
+        const int x = r0 + lane < n ? COST + row_tile_keys(a, r0 + lane, seq.m, seq.t) : 0, incl = scan(x);
         const unsigned long long past = __ballot(incl > left);
         if (past) {
             const int j = __ffsll((long long)past) - 1;
@@ -146,12 +145,12 @@ __global__ __launch_bounds__(256, 2) void k_paged_attn_many(PagedAttn a, int min
     const int item = u - kt0 + COST;                         // where its keys begin
     kt0 -= COST;
     const int rows = min(seq.m * a.group - rt * BM, BM);     // of this item
-    const int n_kt = row_tile_keys(rt, seq.m, seq.t, a.group, cap);
+    const int n_kt = row_tile_keys(a, rt, seq.m, seq.t);
     const int kt1 = min(n_kt, kt0 + u_end - u);
     u += kt1 - kt0;
     kt0 = max(kt0, 0);
     if (kt1 <= 0) continue;                                  // (the share ends before the keys begin)
-    const int len = min(seq.t + (rt * BM + rows - 1) / a.group + 1, cap);      // keys that some row attends
+    const int len = a.keys(seq.t, (rt * BM + rows - 1) / a.group);      // keys that some row attends
 
     // The page table, 16 tiles at a time: lane x holds where the x-th group of 16 keys from tile `base` on lies in the pools (bytes; one without a
     // page: in page 0, which the masks leave out), and bit x of `here` says that it has a page.
@@ -169,7 +168,7 @@ __global__ __launch_bounds__(256, 2) void k_paged_attn_many(PagedAttn a, int min
     // ---- this lane's row
     const int r = rt * BM + wave * 32 + col, i = r / a.group, hq = r - i * a.group;
     const bool live = wave * 32 + col < rows;
-    const int limit = seq.t + i;                             // last position it attends
+    const int limit = a.last(seq.t, i);                             // last position it attends
     unsigned long long above = 0;
     if (a.parent) above = lane_of(paged_ancestors(a.parent, seq, lane), min(i, 63));
     u32x4 qf[ST];
@@ -280,7 +279,7 @@ __global__ __launch_bounds__(256, 2) void k_paged_attn_many(PagedAttn a, int min
     if (a.scale < 0.f)                                       // a negative scale turns the queries around: the maximum below needs scale >= 0
 #pragma unroll
         for (int s = 0; s < ST; s++) qf[s] ^= u32x4{0x80008000u, 0x80008000u, 0x80008000u, 0x80008000u};
-    const int wave_first = seq.t + (rt * BM + wave * 32) / a.group;      // last position that the wave's first row attends
+    const int wave_first = a.last(seq.t, (rt * BM + wave * 32) / a.group);      // last position that the wave's first row attends
     // where a lane reads: K row `col` (+ 32), pieces 2 s + h; V as LDS's transposing read wants it (the place of 4 features of a key), pieces 4 d + ..
     const int l16 = lane & 15;
     const int k_at = k_piece<DH>(col, h) * 16, v_row = 4 * h + (l16 >> 2);

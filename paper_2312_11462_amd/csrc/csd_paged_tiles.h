@@ -27,8 +27,9 @@ template <int DH> __device__ __forceinline__ int v_piece(int row, int c) {
     return row * (DH / 8) + (c ^ (DH == 128 ? (row & 3) << 2 : ((row >> 1) & 1) << 2));
 }
 
+// The key tiles of so many keys; rows that have nothing to attend go through one.
+__device__ __forceinline__ int tiles_of(int keys) { return max((keys + kKeys - 1) / kKeys, 1); }
 // The key tiles that row tile rt of a sequence goes through: those up to the last position that one of its rows attends.
-__device__ __forceinline__ int row_tile_keys(int rt, int m, int t, int group, int cap) {
-    const int last = min(((rt + 1) * CSD_PAGED_MANY_ROWS - 1) / group, m - 1);
-    return (min(t + last + 1, cap) + kKeys - 1) / kKeys;
+__device__ __forceinline__ int row_tile_keys(const PagedAttn &a, int rt, int m, int t) {
+    return tiles_of(a.keys(t, min(((rt + 1) * CSD_PAGED_MANY_ROWS - 1) / a.group, m - 1)));
 }
