@@ -1,20 +1,27 @@
 // Draws from logits by temperature, top-k, top-p and min-p, and the probabilities of such draws.
 //
 // With M the largest logit of a row and w_v = 2^((l_v - M) log2(e) / T), every weight is the whole number round(w_v 2^45): sums do not depend on their
-// order, so neither do the sets that they bound nor the tokens (2^18 of them fit 63 bits; what a weight of 64 bits would add to the sums decides
+// order, so neither do the sets that they bound nor the tokens (2^18 of them fit 63 bits; what weights of 64 bits would add to the sums decides
 // for uniform numbers within 2^-38 or so of a border).  Tokens are ranked by (logit, lowest token first), which is the order of one 64-bit number, key << 32 | ~token.
 // Each parameter keeps a start of the ranking, so together they keep the tokens from a least such number on:
 //   top-k   the first k
 //   top-p   of those the shortest start with at least p of their weight
 //   min-p   of those the ones with w >= p
-// The least number is found by a histogram of counts and weights over 2048 steps of the logit (46 octaves of weight below M; lower ones have weight 0), and in
-// the step that holds the border by ranking its tokens against one another.  Steps with too many for that are divided again by their keys, until
-// few are left or all are equal.  The draw descends the row: sixteen ranges, the one that holds the border, sixteen ranges of that.
 //
-// A workgroup per row, which goes over it four to six times.
+// A workgroup per row.  Three ways, by what a row asks for:
+//   few tokens   a logit that all tokens that stay reach is known beforehand: the k-th largest of the lanes' own largest ones, or M + T ln(min-p).  The
+//                tokens that reach it go to a list and are ranked, weighed and drawn there, each against each; no other weight is ever made.
+//   a share      the weights of all tokens are added up in steps of 1/32 octave; the step that holds the border is ranked, or divided again by the bits of
+//                its logits until few tokens are left or all are equal.  What stays is then a list as above or, if there are too many, goes
+//   all          by the sum over the row, and the draw descends it: the wave's range that holds the border, a range of each wave in it, a tile.
 #include "csd_internal.h"
 
-static constexpr int kBins = 2048, kList = 256;              // steps of the histogram; tokens that are ranked against one another at most
+typedef unsigned long long u64;
+
+static constexpr int kList = 256;                            // tokens that are ranked against one another at most
+static constexpr int kBins = 2048;                           // counters of a histogram
+static constexpr int kPerOctave = 32, kSteps = 46 * kPerOctave + 1;      // steps of the weight, from M down (lower weights round to 0)
+static constexpr float kMost = 3.402823466e38f;
 
 struct SampleRows {
     const void *logits;
@@ -29,8 +36,6 @@ struct SampleRows {
     int32_t top_k_all;
 };
 
-typedef unsigned long long u64;
-
 // ---------------------------------------------------------------------------------------- numbers
 
 // NaN counts as -inf, -0 as 0
@@ -39,40 +44,47 @@ __device__ __forceinline__ uint32_t key_of(float v) {
     const uint32_t b = __float_as_uint(v);
     return b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);
 }
+__device__ __forceinline__ float logit_of(uint32_t key) { return __uint_as_float(key & 0x80000000u ? key ^ 0x80000000u : ~key); }
 __device__ __forceinline__ u64 rank_of(uint32_t key, int v) { return (u64)key << 32 | (uint32_t)~v; }
 
-// 2^x for x in [-46, 0] to 2^-47 of itself: the powers of ln 2 over the factorials, for the part of x within half of a whole number
-__device__ __forceinline__ double exp2_of(double x) {
-    const double n = rint(x), f = x - n;
-    double p = 4.4455382718708116e-10;
-    p = fma(p, f, 7.054911620801123e-09);
-    p = fma(p, f, 1.01780860092397e-07);
-    p = fma(p, f, 1.321548679014431e-06);
-    p = fma(p, f, 1.5252733804059841e-05);
-    p = fma(p, f, 0.0001540353039338161);
-    p = fma(p, f, 0.0013333558146428443);
-    p = fma(p, f, 0.009618129107628477);
-    p = fma(p, f, 0.05550410866482158);
-    p = fma(p, f, 0.2402265069591007);
-    p = fma(p, f, 0.6931471805599453);
-    p = fma(p, f, 1.0);
-    return ldexp(p, (int)n);
-}
-
-// Weights of a row.
+// Weights of a row.  x = (l - M) c, c = log2(e) / T, is cut to [-48, 0]; n = round(32 x) is the token's step (negative), and with f = x - n / 32,
+// |f| <= 1 / 64, 2^x = 2^(n / 32) 2^f: a table of 2^(i / 32) and the powers of ln 2 over the factorials up to the fifth (off by 2^-48).
 struct Weights {
-    float top;                    // M
-    double c;                     // log2(e) / T
-    __device__ __forceinline__ double real(float v) const {
-        const double x = v == top ? 0.0 : ((double)v - (double)top) * c;
-        return x >= -46.0 ? exp2_of(x) : 0.0;                // (also for NaN: 0 times -inf)
+    double top, c;
+    const double *roots;          // 2^(i / 32), in LDS
+    __device__ __forceinline__ double exponent(float l) const {
+        const double d = fmin((double)l - top, 0.0);         // (inf - inf: 0)
+        return fmax(d * c, -48.0);                           // (-inf * 0: -48)
+    }
+    static constexpr double kRound = 1.5 * (1ull << 47);     // a number of this size has steps of 1 / 32
+    static __device__ __forceinline__ int step(double x) { return -(int)(uint32_t)__double_as_longlong(x + kRound); }
+    __device__ __forceinline__ double real(double x) const {
+        const double t = x + kRound, f = x - (t - kRound);
+        const int n = (int)(uint32_t)__double_as_longlong(t);
+        double p = 0.0013333558146428443;
+        p = fma(p, f, 0.009618129107628477);
+        p = fma(p, f, 0.05550410866482158);
+        p = fma(p, f, 0.2402265069591007);
+        p = fma(p, f, 0.6931471805599453);
+        p = fma(p, f, 1.0);
+        const u64 w = (u64)__double_as_longlong(p * roots[n & (kPerOctave - 1)]);
+        return __longlong_as_double((long long)(w + ((u64)(uint32_t)((n >> 5) << 20) << 32)));       // times 2^(n / 32, rounded down)
     }
     // times 2^45, to the nearest whole number: 128 + w has steps of 2^-45
     static __device__ __forceinline__ u64 whole(double w) { return (u64)__double_as_longlong(w + 128.0) & ((1ull << 52) - 1); }
-    __device__ __forceinline__ u64 operator()(float v) const { return whole(real(v)); }
+    __device__ __forceinline__ u64 operator()(float l) const { return whole(real(exponent(l))); }
+    // A logit that every token within x octaves of M reaches, and few others; one that no token further down than x octaves passes.
+    __device__ __forceinline__ float reach(float x) const {
+        const double l = top - (double)x / c;
+        return top == INFINITY ? INFINITY : fmaxf((float)(l - fmax(fabs(l), fabs(top)) * 0x1p-20), -kMost);
+    }
+    __device__ __forceinline__ float below(float x) const {
+        const double l = x > 0.f ? top - (double)x / c : top;
+        return top == INFINITY ? INFINITY : fminf((float)(l + fmax(fabs(l), fabs(top)) * 0x1p-20), kMost);
+    }
 };
 
-// floor(a z) and ceil(a z) for a in [0, 1)
+// floor(a z) or, `up`, ceil(a z), for a in [0, 1)
 __device__ __forceinline__ u64 share_of(float a, u64 z, bool up) {
     if (!(a > 0.f)) return 0;
     const uint32_t b = __float_as_uint(a), e = b >> 23;
@@ -84,13 +96,55 @@ __device__ __forceinline__ u64 share_of(float a, u64 z, bool up) {
     return q + (up && ((unsigned __int128)q << s) != y ? 1 : 0);
 }
 
+// ---------------------------------------------------------------------------------------- lanes
+
+// what another lane of the wave has, by data-parallel moves; `old` where there is none
+template <int CTRL, int ROWS>
+__device__ __forceinline__ uint32_t moved(uint32_t old, uint32_t v) {
+    return (uint32_t)__builtin_amdgcn_update_dpp((int)old, (int)v, CTRL, ROWS, 0xF, false);
+}
+template <int CTRL, int ROWS>
+__device__ __forceinline__ u64 moved(u64 old, u64 v) {
+    return (u64)moved<CTRL, ROWS>((uint32_t)(old >> 32), (uint32_t)(v >> 32)) << 32 | moved<CTRL, ROWS>((uint32_t)old, (uint32_t)v);
+}
+// inclusive running sum over the wave: within sixteen lanes, then from row to row
+template <typename U>
+__device__ __forceinline__ U wave_scan(U v) {
+    v += moved<0x111, 0xF>((U)0, v);
+    v += moved<0x112, 0xF>((U)0, v);
+    v += moved<0x114, 0xF>((U)0, v);
+    v += moved<0x118, 0xF>((U)0, v);
+    v += moved<0x142, 0xA>((U)0, v);
+    v += moved<0x143, 0xC>((U)0, v);
+    return v;
+}
+__device__ __forceinline__ uint32_t from_lane(uint32_t v, int lane) { return (uint32_t)__builtin_amdgcn_readlane((int)v, lane); }
+__device__ __forceinline__ u64 from_lane(u64 v, int lane) { return (u64)from_lane((uint32_t)(v >> 32), lane) << 32 | from_lane((uint32_t)v, lane); }
+template <typename U>
+__device__ __forceinline__ U wave_total(U v) { return from_lane(wave_scan(v), 63); }
+__device__ __forceinline__ float wave_largest(float v) {
+    auto step = [&](float o) { v = fmaxf(v, o); };
+#define CSD_MOVED(CTRL, ROWS) __uint_as_float(moved<CTRL, ROWS>(__float_as_uint(v), __float_as_uint(v)))
+    step(CSD_MOVED(0x111, 0xF));
+    step(CSD_MOVED(0x112, 0xF));
+    step(CSD_MOVED(0x114, 0xF));
+    step(CSD_MOVED(0x118, 0xF));
+    step(CSD_MOVED(0x142, 0xA));
+    step(CSD_MOVED(0x143, 0xC));
+#undef CSD_MOVED
+    return __uint_as_float(from_lane(__float_as_uint(v), 63));
+}
+
 // ---------------------------------------------------------------------------------------- a row, by N threads
 
-template <typename T, int N>
+// Wave w has the w-th range of the row, tile by tile (a tile: 16 bytes of each lane).  NV tiles of a wave stay in registers, for the passes that do little with a
+// token; the others read the row again (so the code stays small).  NV = 0: all do.
+template <typename T, int N, int NV>
 struct Row {
     static constexpr int VE = 16 / sizeof(T), W = N / 64, TILE = 64 * VE, AHEAD = 4;
     const T *x;
     int V;
+    u32x4 kept[NV ? NV : 1];
 
     // rows start at any element
     struct __attribute__((packed, aligned(sizeof(T)))) Raw {
@@ -140,119 +194,151 @@ struct Row {
             for (int e = 0; e < VE; e++) f(at + e, get(r, e));
         });
     }
-    // the ranges of the waves
+    // tokens of a wave's range of n
     static __device__ __forceinline__ int range(int n) { return (n + W * TILE - 1) / (W * TILE) * TILE; }
+    static __device__ __forceinline__ int wave() { return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); }
+    __device__ __forceinline__ void keep() {
+        if constexpr (NV > 0) {
+            const int c = range(V);
+#pragma unroll
+            for (int j = 0; j < NV; j++) {
+                const int at = wave() * c + j * TILE + (threadIdx.x & 63) * VE;
+                kept[j] = u32x4{0xFF80FF80u, 0xFF80FF80u, 0xFF80FF80u, 0xFF80FF80u};      // (-inf, or, in fp32, NaN, which counts as that)
+                if (j * TILE < c && at < V) kept[j] = load(at);
+            }
+        }
+    }
+    // passes that do much, and little, with a token
     template <typename F>
     __device__ __forceinline__ void all(F f) const {
-        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = range(V);
-        tokens(min(wave * c, V), min(wave * c + c, V), f);
+        const int c = range(V);
+        tokens(min(wave() * c, V), min(wave() * c + c, V), f);
     }
+    template <typename F>
+    __device__ __forceinline__ void all_kept(F f) {
+        if constexpr (NV > 0) {
+            const int c = range(V), at = wave() * c + (threadIdx.x & 63) * VE;
+#pragma unroll
+            for (int j = 0; j < NV; j++) {
+                asm volatile("" : "+v"(kept[j]));            // (nothing that one pass makes of them is kept for the next)
+                if (j * TILE < c)
+#pragma unroll
+                    for (int e = 0; e < VE; e++) f(at + j * TILE + e, get(kept[j], e));
+            }
+        } else {
+            all(f);
+        }
+    }
+};
+
+struct Ranked {
+    u64 rank, mass;
 };
 
 struct SampleShared {
-    uint32_t count[kBins];
+    Ranked list[kList];
     u64 mass[kBins];
-    u64 list_rank[kList], list_mass[kList];
-    u64 part[32];
-    uint32_t part32[32];
+    uint32_t count[kBins], octave[64];
+    u64 stay_mass[kList];
+    double roots[kPerOctave];
+    u64 part[16];
+    uint32_t part32[16];
     float top[16];
-    uint32_t bin, base_count, n_list, key_lo, key_hi;
-    u64 base_mass, least, sum;
+    uint32_t n_list;
+    u64 least, sum, stay;
     int token;
 };
 
-__device__ __forceinline__ u64 wave_sum64(u64 v) {
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
-    return v;
-}
-__device__ __forceinline__ u64 wave_scan64(u64 v) {      // inclusive
-    const int lane = threadIdx.x & 63;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-        const u64 x = __shfl_up(v, o, 64);
-        if (lane >= o) v += x;
-    }
-    return v;
-}
-// sum over the workgroup, in every thread
 template <int N>
-__device__ __forceinline__ u64 group_sum64(SampleShared &S, u64 v) {
-    v = wave_sum64(v);
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) S.part[threadIdx.x >> 6] = v;
-    __syncthreads();
-    u64 t = 0;
-#pragma unroll
-    for (int i = 0; i < N / 64; i++) t += S.part[i];
-    return t;
+__device__ __forceinline__ void clear_counters(SampleShared &S, bool masses) {
+    for (int i = threadIdx.x; i < kBins / 4; i += N) reinterpret_cast<u32x4 *>(S.count)[i] = u32x4{0u, 0u, 0u, 0u};
+    if (masses)
+        for (int i = threadIdx.x; i < kBins / 2; i += N) reinterpret_cast<u32x4 *>(S.mass)[i] = u32x4{0u, 0u, 0u, 0u};
+    if (threadIdx.x < 64) S.octave[threadIdx.x] = 0;
 }
 
-// What the threads know of the histogram: thread t has kBins / N neighbouring steps, what they hold and what lies before them.
-template <int N>
-struct Steps {
-    static constexpr int B = kBins / N;
-    uint32_t count[B], before;
-    u64 mass[B], mass_before;
-
-    __device__ __forceinline__ void read(SampleShared &S) {
-        const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-        uint32_t n = 0;
-        u64 m = 0;
-#pragma unroll
-        for (int i = 0; i < B; i++) {
-            count[i] = S.count[tid * B + i];
-            mass[i] = S.mass[tid * B + i];
-            n += count[i];
-            m += mass[i];
-        }
-        const u64 ni = wave_scan64(n), mi = wave_scan64(m);
-        __syncthreads();
-        if (lane == 63) {
-            S.part32[wave] = (uint32_t)ni;
-            S.part[wave] = mi;
-        }
-        __syncthreads();
-        before = (uint32_t)ni - n;
-        mass_before = mi - m;
-        for (int i = 0; i < wave; i++) {
-            before += S.part32[i];
-            mass_before += S.part[i];
-        }
-    }
-    // The first step at which k tokens, or m of weight, are reached, into S (all threads; S.bin is kBins where there is none).
-    __device__ __forceinline__ void find(SampleShared &S, uint32_t k, u64 m) const {
-        __syncthreads();
-        if (threadIdx.x == 0) S.bin = kBins;
-        __syncthreads();
-        uint32_t n = before;
-        u64 w = mass_before;
-#pragma unroll
-        for (int i = 0; i < B; i++) {
-            if (n < k && w < m && (n + count[i] >= k || w + mass[i] >= m)) {
-                S.bin = threadIdx.x * B + i;
-                S.base_count = n;
-                S.base_mass = w;
-                S.n_list = count[i];
-            }
-            n += count[i];
-            w += mass[i];
-        }
-        __syncthreads();
-    }
+// A counter of the histogram: what it has, and what lies before it.
+struct Found {
+    int bin;                      // kBins: none
+    uint32_t base_count, count;
+    u64 base_mass, mass;
 };
 
-// The lowest token of [0, V) at which the running sum of value(token, logit) passes `target`; the sum over the row is more than that.
-template <typename T, int N, typename F>
-__device__ __forceinline__ int descend(const Row<T, N> &row, SampleShared &S, u64 target, F value) {
-    using R = Row<T, N>;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    int lo = 0, hi = row.V;
+// The waves' sums of the counters (wave w: its kBins / W ones); a barrier behind it.
+template <int N>
+__device__ __forceinline__ void sum_counters(SampleShared &S) {
+    constexpr int B = kBins / N;
+    uint32_t n = 0;
+    u64 m = 0;
+#pragma unroll
+    for (int i = 0; i < B; i++) {
+        n += S.count[threadIdx.x * B + i];
+        m += S.mass[threadIdx.x * B + i];
+    }
+    n = wave_total(n);
+    m = wave_total(m);
+    if ((threadIdx.x & 63) == 0) {
+        S.part32[threadIdx.x >> 6] = n;
+        S.part[threadIdx.x >> 6] = m;
+    }
+    __syncthreads();
+}
+// The first counter at which k tokens, or m of weight, are reached; every wave finds it by itself.
+template <int N>
+__device__ __forceinline__ Found find(const SampleShared &S, uint32_t k, u64 m) {
+    constexpr int B = kBins / N, W = N / 64;
+    const int lane = threadIdx.x & 63;
+    Found f{kBins, 0, 0, 0, 0};
+    int w = 0;
+    for (; w < W; w++) {
+        const uint32_t n = S.part32[w];
+        const u64 x = S.part[w];
+        if (f.base_count + n >= k || f.base_mass + x >= m) break;
+        f.base_count += n;
+        f.base_mass += x;
+    }
+    if (w == W) return f;
+    uint32_t count[B], n = 0;
+    u64 mass[B], x = 0;
+#pragma unroll
+    for (int i = 0; i < B; i++) {
+        count[i] = S.count[(w * 64 + lane) * B + i];
+        mass[i] = S.mass[(w * 64 + lane) * B + i];
+        n += count[i];
+        x += mass[i];
+    }
+    const uint32_t to = f.base_count + wave_scan(n);
+    const u64 mass_to = f.base_mass + wave_scan(x);
+    const int hit = __ffsll((long long)__ballot(to >= k || mass_to >= m)) - 1;
+    uint32_t before = to - n, at = 0, mine = 0;
+    u64 mass_before = mass_to - x, mass_mine = 0;
+    bool there = false;
+#pragma unroll
+    for (int i = 0; i < B; i++)
+        if (!there) {
+            there = before + count[i] >= k || mass_before + mass[i] >= m;
+            if (there) {
+                at = i;
+                mine = count[i];
+                mass_mine = mass[i];
+            } else {
+                before += count[i];
+                mass_before += mass[i];
+            }
+        }
+    return Found{(w * 64 + hit) * B + (int)from_lane(at, hit), from_lane(before, hit), from_lane(mine, hit), from_lane(mass_before, hit), from_lane(mass_mine, hit)};
+}
+
+// The lowest token of [lo, hi) at which the running sum of value(token, logit), from lo on, passes `target`; the sum over the range is more than that.
+template <typename T, int N, int NV, typename F>
+__device__ __forceinline__ int descend(const Row<T, N, NV> &row, SampleShared &S, u64 target, int lo, int hi, F value) {
+    using R = Row<T, N, NV>;
+    const int lane = threadIdx.x & 63, wave = R::wave();
     while (hi - lo > R::TILE) {
         const int c = R::range(hi - lo), a = min(lo + wave * c, hi), b = min(a + c, hi);
         u64 sum = 0;
         row.tokens(a, b, [&](int v, float l) { sum += value(v, l); });
-        sum = wave_sum64(sum);
+        sum = wave_total(sum);
         __syncthreads();
         if (lane == 0) S.part[wave] = sum;
         __syncthreads();
@@ -266,14 +352,16 @@ __device__ __forceinline__ int descend(const Row<T, N> &row, SampleShared &S, u6
         u64 mine[R::VE], sum = 0;
 #pragma unroll
         for (int e = 0; e < R::VE; e++) mine[e] = 0;
-        row.pieces(lo, hi, [&](int at, const u32x4 &r) {
+        const int at = lo + lane * R::VE;
+        if (at < hi) {
+            const u32x4 r = row.load(at);
 #pragma unroll
             for (int e = 0; e < R::VE; e++) {
                 mine[e] = at + e < hi ? value(at + e, R::get(r, e)) : 0;
                 sum += mine[e];
             }
-        });
-        const u64 incl = wave_scan64(sum), past = __ballot(incl > target);
+        }
+        const u64 incl = wave_scan(sum), past = __ballot(incl > target);
         if (past && lane == __ffsll((long long)past) - 1) {
             u64 run = incl - sum;
             int e = 0;
@@ -282,221 +370,381 @@ __device__ __forceinline__ int descend(const Row<T, N> &row, SampleShared &S, u6
                 run += mine[i];
                 e += run <= target ? 1 : 0;
             }
-            S.token = lo + lane * R::VE + e;
+            S.token = at + e;
         }
     }
     __syncthreads();
     return S.token;
 }
 
-// The step of `steps` that holds the border of the first k tokens, or of m of weight, has been found (S): the rank of the last token inside, and the weight inside.
-// in_step(v, l): whether a token is in the step.
-template <typename T, int N, typename F>
-__device__ __forceinline__ void border(const Row<T, N> &row, SampleShared &S, const Weights &weight, uint32_t k, u64 m, F in_step, u64 &least, u64 &inside) {
-    const int tid = threadIdx.x;
-    uint32_t base = S.base_count, n = S.n_list;
-    u64 base_mass = S.base_mass;
-    uint32_t key_lo = 0, key_hi = 0xFFFFFFFFu;
-    auto in = [&](int v, float l) {
-        const uint32_t key = key_of(l);
-        return v < row.V && key >= key_lo && key <= key_hi && in_step(l);
-    };
-    while (n > (uint32_t)kList) {
-        __syncthreads();
-        if (tid == 0) {
-            S.key_lo = 0xFFFFFFFFu;
-            S.key_hi = 0;
+// The tokens for which in(logit) holds to the list, by no order: how many; more than kList: too many.
+template <typename T, int N, int NV, typename F>
+__device__ __forceinline__ uint32_t collect(Row<T, N, NV> &row, SampleShared &S, F in) {
+    __syncthreads();
+    if (threadIdx.x == 0) S.n_list = 0;
+    __syncthreads();
+    row.all_kept([&](int v, float l) {
+        if (in(l)) {
+            const uint32_t i = atomicAdd(&S.n_list, 1u);
+            if (i < (uint32_t)kList) S.list[i].rank = rank_of(key_of(l), v);
         }
-        __syncthreads();
-        uint32_t lo = 0xFFFFFFFFu, hi = 0;
-        row.all([&](int v, float l) {
-            if (in(v, l)) {
-                lo = min(lo, key_of(l));
-                hi = max(hi, key_of(l));
-            }
-        });
+    });
+    __syncthreads();
+    return S.n_list;
+}
+
+// A token of the list, by N / kList neighbouring lanes: its weight (which goes to the list), and how many tokens and how much weight rank ahead of it.
+template <int N>
+struct Listed {
+    static constexpr int G = N / kList;
+    u64 rank, mass, run;
+    double real;
+    uint32_t ahead;
+    bool there, first;
+    __device__ __forceinline__ int token() const { return (int)~(uint32_t)rank; }
+    template <typename F>
+    static __device__ __forceinline__ void others(uint32_t n, F f) {
+#pragma unroll 4
+        for (uint32_t j = threadIdx.x % G; j < n; j += G) f(j);
+    }
+    template <typename U>
+    static __device__ __forceinline__ void join(U &v) {
 #pragma unroll
-        for (int o = 32; o > 0; o >>= 1) {
-            lo = min(lo, (uint32_t)__shfl_xor(lo, o, 64));
-            hi = max(hi, (uint32_t)__shfl_xor(hi, o, 64));
-        }
-        if ((tid & 63) == 0) {
-            atomicMin(&S.key_lo, lo);
-            atomicMax(&S.key_hi, hi);
-        }
-        for (int i = tid; i < kBins; i += N) {
-            S.count[i] = 0;
-            S.mass[i] = 0;
+        for (int o = 1; o < G; o <<= 1) v += __shfl_xor(v, o, 64);
+    }
+    __device__ __forceinline__ Listed(SampleShared &S, const Weights &weight, uint32_t n) {
+        const int i = threadIdx.x / G;
+        there = i < (int)n;
+        first = threadIdx.x % G == 0;
+        rank = there ? S.list[i].rank : 0;
+        real = there ? weight.real(weight.exponent(logit_of((uint32_t)(rank >> 32)))) : 0.0;
+        mass = Weights::whole(real);
+        if (there && first) S.list[i].mass = mass;
+        if (threadIdx.x == 0) {
+            S.sum = S.stay = 0;
+            S.least = ~0ull;
         }
         __syncthreads();
-        key_lo = S.key_lo;
-        key_hi = S.key_hi;
-        if (key_lo >= key_hi) break;
-        const int shift = max(0, 32 - __clz(key_hi - key_lo) - 11);      // 2^11 steps of keys
-        row.all([&](int v, float l) {
-            if (in(v, l)) {
-                const uint32_t i = (key_hi - key_of(l)) >> shift;
+        ahead = 0;
+        run = 0;
+        others(n, [&](uint32_t j) {
+            const Ranked o = S.list[j];
+            const bool higher = o.rank > rank;
+            ahead += higher ? 1 : 0;
+            run += higher ? o.mass : 0;
+        });
+        join(ahead);
+        join(run);
+    }
+};
+
+// Parameters of a row, as the ranking takes them.
+struct Limits {
+    uint32_t k;                   // tokens
+    float p;                      // by_mass: share of the weight of the first k
+    bool by_mass;
+    u64 w_min;
+};
+
+// The draw's place in the sum of weights.
+__device__ __forceinline__ u64 place_of(float u, u64 sum) { return min(share_of(fminf(u, 0.99999994f), sum, false), sum - 1); }
+
+// The list holds all tokens that stay: their probabilities (over zeros) and the draw.  `all`: the weight that top-p is a share of, 0: that of the first k.
+template <int N>
+__device__ __forceinline__ void finish(SampleShared &S, const Weights &weight, const Limits &lim, u64 all, uint32_t n, float *out, float u, int32_t *token) {
+    const Listed<N> t(S, weight, n);
+    bool stays = t.there && t.ahead < lim.k;
+    if (lim.by_mass) {
+        if (!all) {
+            if (stays && t.first) atomicAdd(&S.sum, t.mass);
+            __syncthreads();
+            all = S.sum;
+        }
+        stays = stays && (t.ahead == 0 || t.run < share_of(lim.p, all, true));
+    }
+    stays = stays && t.mass >= lim.w_min;
+    if (t.first) {
+        S.stay_mass[threadIdx.x / Listed<N>::G] = stays ? t.mass : 0;
+        if (stays) atomicAdd(&S.stay, t.mass);
+    }
+    __syncthreads();
+    const u64 sum = S.stay;
+    if (out && stays && t.first) out[t.token()] = (float)(t.real * (1.0 / ((double)sum * 0x1p-45)));
+    if (token) {
+        const u64 target = place_of(u, sum);
+        u64 before = 0;
+        Listed<N>::others(n, [&](uint32_t j) { before += (uint32_t)S.list[j].rank > (uint32_t)t.rank ? S.stay_mass[j] : 0; });
+        Listed<N>::join(before);
+        if (stays && t.first && before <= target && target < before + t.mass) *token = t.token();
+    }
+}
+
+// The border of the first k tokens, or of m of weight, lies in step f.bin: the rank of the last token inside, and the weight inside.
+// True: the counters have been used.
+template <typename T, int N, int NV>
+__device__ __forceinline__ bool border(Row<T, N, NV> &row, SampleShared &S, const Weights &weight, uint32_t k, u64 m, Found f, u64 &least, u64 &inside) {
+    // its tokens, and keys; those of bf16 logits are their upper halves
+    constexpr int LOW = sizeof(T) == 4 ? 0 : 16;
+    const int step = f.bin;
+    uint32_t lo = key_of(plain_logit(weight.reach(((float)step + 0.5f) / kPerOctave))) >> LOW, hi = key_of(plain_logit(weight.below(((float)step - 0.5f) / kPerOctave))) >> LOW;
+    auto in = [&](float l) {
+        const uint32_t key = key_of(l) >> LOW;
+        return key >= lo && key <= hi && Weights::step(weight.exponent(l)) == step;
+    };
+    uint32_t base = f.base_count, n = collect(row, S, in);
+    u64 base_mass = f.base_mass;
+    const bool used = n > (uint32_t)kList;
+    while (n > (uint32_t)kList) {
+        const int shift = max(0, 32 - __clz(hi - lo) - 11);  // 2^11 steps of keys at most
+        __syncthreads();
+        clear_counters<N>(S, true);
+        __syncthreads();
+        row.all([&](int, float l) {
+            if (in(l)) {
+                const uint32_t i = (hi - (key_of(l) >> LOW)) >> shift;
                 atomicAdd(&S.count[i], 1u);
                 atomicAdd(&S.mass[i], weight(l));
             }
         });
         __syncthreads();
-        Steps<N> steps;
-        steps.read(S);
-        steps.find(S, k - base, m - base_mass);
-        base += S.base_count;
-        base_mass += S.base_mass;
-        n = S.n_list;
-        const uint32_t top = key_hi - (S.bin << shift);
-        key_lo = max(key_lo, top - min(top, (1u << shift) - 1));
-        key_hi = top;
-    }
-    __syncthreads();
-    if (tid == 0) {
-        S.n_list = 0;
-        S.least = ~0ull;
-        S.sum = 0;
-    }
-    __syncthreads();
-    if (n > (uint32_t)kList) {
-        // all equal: the first of them by token
-        const uint32_t key = key_lo;
-        u64 w = 0;
-        if (tid == 0) {
-            const float l = __uint_as_float(key & 0x80000000u ? key ^ 0x80000000u : ~key);
-            S.sum = weight(l);
+        sum_counters<N>(S);
+        f = find<N>(S, k - base, m - base_mass);
+        if (f.bin == kBins) break;                           // (the logits changed while they were read)
+        base += f.base_count;
+        base_mass += f.base_mass;
+        hi -= (uint32_t)f.bin << shift;
+        lo = max(lo, hi - min(hi, (1u << shift) - 1));
+        n = f.count;
+        if (shift == 0 && n > (uint32_t)kList) {
+            // all equal: the first of them by token
+            const u64 w = f.mass / n;
+            u64 keep = k - base;
+            if (w) keep = min(keep, (m - base_mass - 1) / w + 1);      // (m is more than base_mass)
+            keep = min(max(keep, (u64)1), (u64)n);
+            const int last = descend(row, S, keep - 1, 0, row.V, [&](int, float l) { return (u64)(in(l) ? 1 : 0); });
+            least = rank_of(LOW && !(hi >> 15) ? hi << LOW | 0xFFFFu : hi << LOW, last);      // (keys of negative numbers are turned around)
+            inside = base_mass + keep * w;
+            return true;
         }
-        __syncthreads();
-        w = S.sum;
-        u64 keep = k - base;
-        if (w) keep = min(keep, (m - base_mass - 1) / w + 1);      // (m is more than base_mass)
-        keep = min(max(keep, (u64)1), (u64)n);
-        const int last = descend(row, S, keep - 1, [&](int v, float l) { return (u64)(v < row.V && key_of(l) == key ? 1 : 0); });
-        least = rank_of(key, last);
-        inside = base_mass + keep * w;
-        return;
+        if (n <= (uint32_t)kList) n = collect(row, S, in);
     }
-    row.all([&](int v, float l) {
-        if (in(v, l)) {
-            const uint32_t i = atomicAdd(&S.n_list, 1u);
-            if (i < (uint32_t)kList) {
-                S.list_rank[i] = rank_of(key_of(l), v);
-                S.list_mass[i] = weight(l);
-            }
-        }
-    });
-    __syncthreads();
-    n = min(S.n_list, (uint32_t)kList);
-    if (tid < (int)n) {
-        const u64 mine = S.list_rank[tid];
-        uint32_t ahead = base;
-        u64 run = base_mass;
-        for (uint32_t i = 0; i < n; i++)
-            if (S.list_rank[i] > mine) {
-                ahead++;
-                run += S.list_mass[i];
-            }
-        if (ahead < k && run < m) {
-            atomicMin(&S.least, mine);
-            atomicAdd(&S.sum, S.list_mass[tid]);
-        }
+    const Listed<N> t(S, weight, min(n, (uint32_t)kList));
+    if (t.there && t.first && base + t.ahead < k && base_mass + t.run < m) {
+        atomicMin(&S.least, t.rank);
+        atomicAdd(&S.sum, t.mass);
     }
     __syncthreads();
     least = S.least;
     inside = base_mass + S.sum;
+    return used;
 }
 
-template <typename T, int N>
+template <typename T, int N, int NV>
 __global__ __launch_bounds__(N) void k_sample(SampleRows a) {
-    __shared__ SampleShared S;
-    const int r = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, set = r / a.each;
-    const Row<T, N> row{reinterpret_cast<const T *>(a.logits) + (size_t)r * a.stride, a.V};
+    __shared__ __align__(16) SampleShared S;
+    using R = Row<T, N, NV>;
+    const int r = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = R::wave(), set = r / a.each;
+    R row;
+    row.x = reinterpret_cast<const T *>(a.logits) + (size_t)r * a.stride;
+    row.V = a.V;
+    row.keep();
     const float temperature = a.temperature ? a.temperature[set] : a.temperature_all, p = a.top_p ? a.top_p[set] : a.top_p_all,
-                p_min = a.min_p ? a.min_p[set] : a.min_p_all;
+                p_min = a.min_p ? a.min_p[set] : a.min_p_all, u = a.tokens ? a.u[r] : 0.f;
     const bool greedy = !(temperature > 0.f);
     int k = greedy ? 1 : a.top_k ? a.top_k[set] : a.top_k_all;
     if (k <= 0 || k > a.V) k = a.V;
+    clear_counters<N>(S, true);
+    if (tid < kPerOctave) S.roots[tid] = exp2((double)tid / kPerOctave);
 
-    float top = -INFINITY;
-    row.all([&](int, float l) { top = fmaxf(top, l); });
-    top = wave_max(top);
+    float mine = -INFINITY;
+    row.all_kept([&](int, float l) { mine = fmaxf(mine, l); });
+    float top = wave_largest(mine);
     if (lane == 0) S.top[wave] = top;
-    for (int i = tid; i < kBins; i += N) {
-        S.count[i] = 0;
-        S.mass[i] = 0;
-    }
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < N / 64; i++) top = fmaxf(top, S.top[i]);
     float *out = a.probs ? a.probs + (size_t)r * a.V : nullptr;
+    int32_t *token = a.tokens ? a.tokens + r : nullptr;
+    struct __attribute__((packed, aligned(4))) Quad {
+        f32x4 v;
+    };
+    auto clear = [&] {
+        for (int i = 4 * tid; i < a.V; i += 4 * N)
+            if (i + 4 <= a.V) reinterpret_cast<Quad *>(out + i)->v = f32x4{0.f, 0.f, 0.f, 0.f};
+            else
+                for (int e = i; e < a.V; e++) out[e] = 0.f;
+    };
     if (top == -INFINITY) {                                  // nothing to draw from
-        if (out)
-            for (int i = tid; i < a.V; i += N) out[i] = 0.f;
-        if (a.tokens && tid == 0) a.tokens[r] = -1;
+        if (out) clear();
+        if (token && tid == 0) *token = -1;
         return;
     }
-    const double c = 1.4426950408889634 / (greedy ? 1.0 : (double)temperature);
-    const Weights weight{top, c};
-    const bool by_mass = p < 1.f && k > 1;
-    u64 least = 0;
-    if (k < a.V || by_mass) {
-        const float per = (float)((double)(kBins / 46.0) * c);
-        auto step_of = [&](float l) {
-            const float t = l == top ? 0.f : (top - l) * per;
-            return t < (float)kBins ? (int)t : kBins;        // (kBins: no weight; also for NaN)
-        };
-        row.all([&](int v, float l) {
-            const int i = v < a.V ? step_of(l) : kBins;
-            if (i < kBins) {
+    const Weights weight{(double)top, 1.4426950408889634 / (greedy ? 1.0 : (double)temperature), S.roots};
+    Limits lim{(uint32_t)k, p, p < 1.f && k > 1, 1};
+    if (p_min > 0.f) lim.w_min = max((u64)ceil((double)fminf(p_min, 1.f) * (double)(1ull << 45)), (u64)1);
+
+    // ---- few tokens at most
+    const bool few = k <= kList * 3 / 4;
+    if (few || (k == a.V && !lim.by_mass && p_min > 0.f)) {
+        float cut = -kMost;
+        if (k == 1) {
+            cut = top;
+        } else if (few) {
+            const int i = Weights::step(weight.exponent(mine));
+            if (i < kSteps) {
                 atomicAdd(&S.count[i], 1u);
-                if (by_mass) atomicAdd(&S.mass[i], weight(l));
+                atomicAdd(&S.octave[i >> 5], 1u);
             }
-        });
-        __syncthreads();
-        Steps<N> steps;
-        steps.read(S);
-        u64 all = steps.mass_before;
-#pragma unroll
-        for (int i = 0; i < Steps<N>::B; i++) all += steps.mass[i];
-        __syncthreads();
-        if (tid == N - 1) S.sum = all;
-        __syncthreads();
-        all = S.sum;
-        if (k < a.V) {
-            steps.find(S, k, ~0ull);
-            const int at = S.bin;
-            if (at < kBins) border(row, S, weight, k, ~0ull, [&](float l) { return step_of(l) == at; }, least, all);
+            __syncthreads();
+            // (every wave finds the k-th by itself: the octave, then the step)
+            const uint32_t o = S.octave[lane], to = wave_scan(o);
+            const u64 past = __ballot(to >= (uint32_t)k);
+            if (past) {
+                const int at = __ffsll((long long)past) - 1;
+                const uint32_t before = from_lane(to - o, at), in = before + wave_scan(lane < 32 ? S.count[at * 32 + lane] : 0u);
+                const int step = at * 32 + __ffsll((long long)__ballot(in >= (uint32_t)k)) - 1;
+                cut = weight.reach(((float)step + 0.5f) / kPerOctave);
+            } else {
+                cut = weight.reach(46.5f);                   // (fewer lanes have a token with a weight)
+            }
         }
-        if (by_mass) {
+        if (!lim.by_mass && p_min > 0.f) cut = fmaxf(cut, weight.reach(-__builtin_amdgcn_logf(fminf(p_min, 1.f)) * 1.0001f + 0.001f));      // (log2)
+        if (out) clear();
+        const uint32_t n = collect(row, S, [&](float l) { return l >= cut; });
+        if (n <= (uint32_t)kList) return finish<N>(S, weight, lim, 0, n, out, u, token);
+        clear_counters<N>(S, true);
+        __syncthreads();
+    }
+
+    // ---- by a share of the weight, or by many tokens (what is kept of the largest rows would cost the registers of the passes below)
+    Row<T, N, (NV > 8 && N == 1024 ? 0 : NV)> again;
+    again.x = row.x;
+    again.V = row.V;
+    if constexpr (NV <= 8 || N < 1024)
+#pragma unroll
+        for (int j = 0; j < NV; j++) again.kept[j] = row.kept[j];
+    u64 least = 0, sum = 0;
+    const bool counted = k < a.V;
+    if (counted || lim.by_mass) {
+        auto histogram = [&] {
+            again.all([&](int, float l) {
+                const double x = weight.exponent(l);
+                const int i = Weights::step(x);
+                if (i < kSteps) {
+                    if (counted) atomicAdd(&S.count[i], 1u);
+                    if (lim.by_mass) atomicAdd(&S.mass[i], Weights::whole(weight.real(x)));
+                }
+            });
+            __syncthreads();
+            sum_counters<N>(S);
+        };
+        histogram();
+        u64 all = 0;
+#pragma unroll
+        for (int i = 0; i < N / 64; i++) all += S.part[i];
+        // what stays may fit the list: all tokens down to the end of a step
+        auto listed = [&](int step, u64 of) {
+            const float cut = weight.reach(((float)step + 0.5f) / kPerOctave);
+            const uint32_t n = collect(again, S, [&](float l) { return l >= cut; });
+            if (n > (uint32_t)kList) return false;
+            if (out) clear();
+            __syncthreads();
+            finish<N>(S, weight, lim, of, n, out, u, token);
+            return true;
+        };
+        if (counted) {
+            const Found f = find<N>(S, k, ~0ull);
+            if (f.bin < kSteps) {
+                if (f.base_count + f.count <= (uint32_t)kList && listed(f.bin, 0)) return;
+                const bool spoilt = border(again, S, weight, k, ~0ull, f, least, all);
+                if (lim.by_mass && spoilt) {
+                    __syncthreads();
+                    clear_counters<N>(S, true);
+                    __syncthreads();
+                    histogram();
+                }
+            }
+        }
+        if (lim.by_mass) {
             const u64 m = max(share_of(p, all, true), (u64)1);
-            steps.find(S, ~0u, m);
-            const int at = S.bin;
-            if (at < kBins) border(row, S, weight, ~0u, m, [&](float l) { return step_of(l) == at; }, least, all);
+            const Found f = find<N>(S, ~0u, m);
+            if (f.bin < kSteps) {
+                if (listed(f.bin, all)) return;
+                border(again, S, weight, ~0u, m, f, least, all);
+            }
+            sum = all;
         }
     }
-    const u64 w_min = p_min > 0.f ? max((u64)ceil((double)fminf(p_min, 1.f) * (double)(1ull << 45)), (u64)1) : 1;
+
+    // ---- all
+    const float l_least = least ? logit_of((uint32_t)(least >> 32)) : -INFINITY;
+    const int v_last = (int)~(uint32_t)least;                // of the tokens with the least logit
+    auto stays = [&](int v, float l) { return l > l_least || (l == l_least && v <= v_last); };
     auto value = [&](int v, float l) -> u64 {
-        if (v >= a.V || rank_of(key_of(l), v) < least) return 0;
+        if (!stays(v, l)) return 0;
         const u64 w = weight(l);
-        return w >= w_min ? w : 0;
+        return w >= lim.w_min ? w : 0;
     };
-    u64 sum = 0;
-    row.all([&](int v, float l) { sum += value(v, l); });
-    sum = group_sum64<N>(S, sum);
+    const int range = R::range(a.V);
+    if (token || !sum || lim.w_min > 1) {
+        u64 of_wave = 0;
+        again.all([&](int v, float l) { of_wave += value(v, l); });
+        of_wave = wave_total(of_wave);
+        __syncthreads();
+        if (lane == 0) S.part[wave] = of_wave;
+        __syncthreads();
+        sum = 0;
+#pragma unroll
+        for (int i = 0; i < N / 64; i++) sum += S.part[i];
+    }
     if (out) {
         const double inv = 1.0 / ((double)sum * 0x1p-45);
-        row.all([&](int v, float l) {
-            if (v < a.V) out[v] = value(v, l) ? (float)(weight.real(l) * inv) : 0.f;
+        again.pieces(min(wave * range, a.V), min(wave * range + range, a.V), [&](int at, const u32x4 &raw) {
+            float y[R::VE];
+#pragma unroll
+            for (int e = 0; e < R::VE; e++) {
+                const float l = R::get(raw, e);
+                y[e] = 0.f;
+                if (stays(at + e, l)) {
+                    const double w = weight.real(weight.exponent(l));
+                    if (Weights::whole(w) >= lim.w_min) y[e] = (float)(w * inv);
+                }
+            }
+#pragma unroll
+            for (int e = 0; e < R::VE; e += 4)
+                if (at + e + 4 <= a.V) reinterpret_cast<Quad *>(out + at + e)->v = f32x4{y[e], y[e + 1], y[e + 2], y[e + 3]};
+                else
+#pragma unroll
+                    for (int i = 0; i < 3; i++)
+                        if (at + e + i < a.V) out[at + e + i] = y[e + i];
         });
     }
-    if (a.tokens) {
-        const u64 target = min(share_of(fminf(a.u[r], 0.99999994f), sum, false), sum - 1);
-        const int token = descend(row, S, target, value);
-        if (tid == 0) a.tokens[r] = token;
+    if (token) {
+        u64 target = place_of(u, sum);
+        int w = 0;
+        for (; w < N / 64 - 1 && S.part[w] <= target; w++) target -= S.part[w];
+        const int found = descend(again, S, target, min(w * range, a.V - 1), min(w * range + range, a.V), value);
+        if (tid == 0) *token = found;
     }
 }
 
 // ---------------------------------------------------------------------------------------- entry points
+
+template <typename T, int N, int NV>
+static void sample_launch_as(const SampleRows &a, int rows, hipStream_t st) {
+    hipLaunchKernelGGL((k_sample<T, N, NV>), dim3(rows), dim3(N), 0, st, a);
+}
+
+// The row stays in registers where it fits them.
+template <typename T>
+static void sample_launch(const SampleRows &a, int rows, hipStream_t st) {
+    constexpr int VE = 16 / sizeof(T);
+    if (a.V <= 256 * 4 * VE) sample_launch_as<T, 256, 4>(a, rows, st);
+    else if (a.V <= 512 * 16 * VE && rows >= 512) sample_launch_as<T, 512, 16>(a, rows, st);
+    else if (a.V <= 1024 * 8 * VE) sample_launch_as<T, 1024, 8>(a, rows, st);
+    else if (a.V <= 1024 * 16 * VE) sample_launch_as<T, 1024, 16>(a, rows, st);
+    else sample_launch_as<T, 1024, 0>(a, rows, st);
+}
 
 static int32_t sample_enqueue(const csd_filter *f, const void *logits, int64_t stride, int32_t dtype, int32_t rows, int32_t V, const float *u,
                               int32_t *tokens, float *probs, void *stream) {
@@ -512,8 +760,8 @@ static int32_t sample_enqueue(const csd_filter *f, const void *logits, int64_t s
     if ((uintptr_t)logits % (dtype == CSD_DTYPE_FP32 ? 4 : 2) || (uintptr_t)probs % 4) return CSD_EINVAL;
     const SampleRows a{logits, (long long)stride, V, f->rows_each, u, tokens, probs, f->temperature, f->top_p, f->min_p, f->top_k,
                        f->temperature_all, f->top_p_all, f->min_p_all, f->top_k_all};
-    if (dtype == CSD_DTYPE_FP32) hipLaunchKernelGGL((k_sample<float, 1024>), dim3(rows), dim3(1024), 0, (hipStream_t)stream, a);
-    else hipLaunchKernelGGL((k_sample<bf16_t, 1024>), dim3(rows), dim3(1024), 0, (hipStream_t)stream, a);
+    if (dtype == CSD_DTYPE_FP32) sample_launch<float>(a, rows, (hipStream_t)stream);
+    else sample_launch<bf16_t>(a, rows, (hipStream_t)stream);
     CSD_LAUNCH_CHECK();
     return CSD_OK;
 }
