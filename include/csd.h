@@ -458,8 +458,8 @@ int32_t csd_pages_share(const csd_pages *pages, const int32_t *source, const int
  *   temperature  0 (or anything that is not positive): the first of the ranking alone
  * A token that stays has the probability w_v / (sum of w over those that stay), the others 0.  The token drawn by u in [0, 1) is the lowest one at which the
  * running sum of the weights that stay, by token, passes u times their sum.  Weights are summed as whole numbers of 2^-45 (rounded to nearest; a
- * token of less than 2^-46 has none), so the result does not depend on how a row is spread over the chip.  NaN counts as -inf; infinite logits share the
- * weight; a row without any logit above -inf gives token -1 and probabilities of 0.
+ * token of less than 2^-46 has none), so the result does not depend on how a row is spread over the chip.  NaN counts as -inf, inf as the
+ * largest number of its type; a row without any logit above -inf gives token -1 and probabilities of 0.
  * Each parameter is an array [rows / rows_each] on the device, for rows_each consecutive rows an entry, or NULL: then the number beside it goes for all rows
  * (CSD_EINVAL: temperature_all or top_p_all negative or NaN, min_p_all outside [0, 1]).
  */

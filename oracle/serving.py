@@ -5,11 +5,11 @@ from __future__ import annotations
 import numpy as np
 
 
-def weights(logits, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0):
+def weights(logits, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, largest=np.finfo(np.float32).max):
     """(weights of a row by token, slack of every decision): w in 64 bits, 0 for tokens that are left out; slack[v] is how far token v is from being decided
-    otherwise, in units of the largest weight (inf where no sum or comparison of weights decides)."""
+    otherwise, in units of the largest weight (inf where no sum or comparison of weights decides).  largest: the number that infinity counts as."""
     x = np.asarray(logits, dtype=np.float64)
-    x = np.where(np.isnan(x), -np.inf, x)
+    x = np.where(np.isnan(x), -np.inf, np.minimum(x, np.float64(largest)))
     n = len(x)
     slack = np.full(n, np.inf)
     m = x.max()

@@ -38,49 +38,65 @@ struct SampleRows {
 
 // ---------------------------------------------------------------------------------------- numbers
 
-// NaN counts as -inf, -0 as 0
-__device__ __forceinline__ float plain_logit(float v) { return fmaxf(v, -INFINITY) + 0.f; }
+// Logits are used as they are: NaN fails every comparison and has no weight, inf has that of the largest number of its type.
+template <typename T> static constexpr float kLargest = sizeof(T) == 4 ? kMost : 3.3895313892515355e38f;
+template <typename T>
 __device__ __forceinline__ uint32_t key_of(float v) {
-    const uint32_t b = __float_as_uint(v);
+    const uint32_t b = __float_as_uint(fminf(v, kLargest<T>) + 0.f);     // (-0 is 0)
     return b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);
 }
 __device__ __forceinline__ float logit_of(uint32_t key) { return __uint_as_float(key & 0x80000000u ? key ^ 0x80000000u : ~key); }
 __device__ __forceinline__ u64 rank_of(uint32_t key, int v) { return (u64)key << 32 | (uint32_t)~v; }
 
-// Weights of a row.  x = (l - M) c, c = log2(e) / T, is cut to [-48, 0]; n = round(32 x) is the token's step (negative), and with f = x - n / 32,
-// |f| <= 1 / 64, 2^x = 2^(n / 32) 2^f: a table of 2^(i / 32) and the powers of ln 2 over the factorials up to the fifth (off by 2^-48).
+__device__ __forceinline__ double fma_of(double a, double b, double c) {      // (the compiler makes two instructions of it, with c moved to the result first)
+    double r;
+    asm("v_fma_f64 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "s"(c));
+    return r;
+}
+
+// Weights of a row.  x = (l - M) c, c = log2(e) / T, is cut to [-48, 0] (NaN: -48); n = round(32 x) is minus the token's step, and with f = x - n / 32,
+// |f| <= 1 / 64, 2^x = 2^(n / 32) 2^f: a table of 2^(i / 32) and the powers of ln 2 over the factorials up to the fifth (off by 2^-48).  About twenty instructions,
+// five cycles each whatever they are, and they bound the passes that weigh every token.
 struct Weights {
-    double top, c;
+    double top, c;                // (c is at least 10^-300: -inf times it is -inf)
     const double *roots;          // 2^(i / 32), in LDS
-    __device__ __forceinline__ double exponent(float l) const {
-        const double d = fmin((double)l - top, 0.0);         // (inf - inf: 0)
-        return fmax(d * c, -48.0);                           // (-inf * 0: -48)
-    }
+    __device__ __forceinline__ double exponent(float l) const { return fmin(fmax(((double)l - top) * c, -48.0), 0.0); }
     static constexpr double kRound = 1.5 * (1ull << 47);     // a number of this size has steps of 1 / 32
+    // -32 x, rounded: the low half of x + kRound
     static __device__ __forceinline__ int step(double x) { return -(int)(uint32_t)__double_as_longlong(x + kRound); }
-    __device__ __forceinline__ double real(double x) const {
+    // 2^f, and 2^(n / 32)
+    __device__ __forceinline__ void factors(double x, double &p, double &root) const {
         const double t = x + kRound, f = x - (t - kRound);
         const int n = (int)(uint32_t)__double_as_longlong(t);
-        double p = 0.0013333558146428443;
-        p = fma(p, f, 0.009618129107628477);
-        p = fma(p, f, 0.05550410866482158);
-        p = fma(p, f, 0.2402265069591007);
-        p = fma(p, f, 0.6931471805599453);
+        root = ldexp(roots[n & (kPerOctave - 1)], n >> 5);
+        p = fma_of(f, 0.0013333558146428443, 0.009618129107628477);
+        p = fma_of(p, f, 0.05550410866482158);
+        p = fma_of(p, f, 0.2402265069591007);
+        p = fma_of(p, f, 0.6931471805599453);
         p = fma(p, f, 1.0);
-        const u64 w = (u64)__double_as_longlong(p * roots[n & (kPerOctave - 1)]);
-        return __longlong_as_double((long long)(w + ((u64)(uint32_t)((n >> 5) << 20) << 32)));       // times 2^(n / 32, rounded down)
+    }
+    __device__ __forceinline__ double real(double x) const {
+        double p, root;
+        factors(x, p, root);
+        return p * root;
     }
     // times 2^45, to the nearest whole number: 128 + w has steps of 2^-45
-    static __device__ __forceinline__ u64 whole(double w) { return (u64)__double_as_longlong(w + 128.0) & ((1ull << 52) - 1); }
-    __device__ __forceinline__ u64 operator()(float l) const { return whole(real(exponent(l))); }
+    static __device__ __forceinline__ u64 bits_of(double w) { return (u64)__double_as_longlong(w) & ((1ull << 52) - 1); }
+    static __device__ __forceinline__ u64 whole(double w) { return bits_of(w + 128.0); }
+    __device__ __forceinline__ u64 at(double x) const {
+        double p, root;
+        factors(x, p, root);
+        return bits_of(fma(p, root, 128.0));
+    }
+    __device__ __forceinline__ u64 operator()(float l) const { return at(exponent(l)); }
     // A logit that every token within x octaves of M reaches, and few others; one that no token further down than x octaves passes.
     __device__ __forceinline__ float reach(float x) const {
         const double l = top - (double)x / c;
-        return top == INFINITY ? INFINITY : fmaxf((float)(l - fmax(fabs(l), fabs(top)) * 0x1p-20), -kMost);
+        return fmaxf((float)(l - fmax(fabs(l), fabs(top)) * 0x1p-20), -kMost);
     }
     __device__ __forceinline__ float below(float x) const {
         const double l = x > 0.f ? top - (double)x / c : top;
-        return top == INFINITY ? INFINITY : fminf((float)(l + fmax(fabs(l), fabs(top)) * 0x1p-20), kMost);
+        return fminf((float)(l + fmax(fabs(l), fabs(top)) * 0x1p-20), kMost);
     }
 };
 
@@ -165,8 +181,8 @@ struct Row {
         return r;
     }
     static __device__ __forceinline__ float get(const u32x4 &r, int e) {
-        if constexpr (sizeof(T) == 4) return plain_logit(__uint_as_float(r[e]));
-        else return plain_logit(__uint_as_float(e & 1 ? r[e / 2] & 0xFFFF0000u : r[e / 2] << 16));
+        if constexpr (sizeof(T) == 4) return __uint_as_float(r[e]);
+        else return __uint_as_float(e & 1 ? r[e / 2] & 0xFFFF0000u : r[e / 2] << 16);
     }
     // f(first token, piece) for the pieces of VE tokens of [lo, hi) that are this lane's; lo and hi are the wave's
     template <typename F>
@@ -183,6 +199,7 @@ struct Row {
             for (int j = 0; j < AHEAD; j++) {
                 const int at = base + j * TILE + lane * VE;
                 if (at < hi) f(at, r[j]);
+                __builtin_amdgcn_sched_barrier(0);           // (a piece at a time: the registers of more than one's numbers are not there)
             }
         }
     }
@@ -203,7 +220,8 @@ struct Row {
 #pragma unroll
             for (int j = 0; j < NV; j++) {
                 const int at = wave() * c + j * TILE + (threadIdx.x & 63) * VE;
-                kept[j] = u32x4{0xFF80FF80u, 0xFF80FF80u, 0xFF80FF80u, 0xFF80FF80u};      // (-inf, or, in fp32, NaN, which counts as that)
+                constexpr uint32_t none = sizeof(T) == 4 ? 0xFF800000u : 0xFF80FF80u;      // -inf
+                kept[j] = u32x4{none, none, none, none};
                 if (j * TILE < c && at < V) kept[j] = load(at);
             }
         }
@@ -215,15 +233,17 @@ struct Row {
         tokens(min(wave() * c, V), min(wave() * c + c, V), f);
     }
     template <typename F>
-    __device__ __forceinline__ void all_kept(F f) {
+    __device__ __forceinline__ void all_kept(F f) const {
         if constexpr (NV > 0) {
             const int c = range(V), at = wave() * c + (threadIdx.x & 63) * VE;
 #pragma unroll
             for (int j = 0; j < NV; j++) {
-                asm volatile("" : "+v"(kept[j]));            // (nothing that one pass makes of them is kept for the next)
+                u32x4 r = kept[j];
+                asm volatile("" : "+v"(r));                  // (nothing that one pass makes of them is kept for the next)
                 if (j * TILE < c)
 #pragma unroll
-                    for (int e = 0; e < VE; e++) f(at + j * TILE + e, get(kept[j], e));
+                    for (int e = 0; e < VE; e++) f(at + j * TILE + e, get(r, e));
+                __builtin_amdgcn_sched_barrier(0);
             }
         } else {
             all(f);
@@ -377,16 +397,30 @@ __device__ __forceinline__ int descend(const Row<T, N, NV> &row, SampleShared &S
     return S.token;
 }
 
-// The tokens for which in(logit) holds to the list, by no order: how many; more than kList: too many.
+// The tokens for which in(logit) holds: how many.
 template <typename T, int N, int NV, typename F>
-__device__ __forceinline__ uint32_t collect(Row<T, N, NV> &row, SampleShared &S, F in) {
+__device__ __forceinline__ uint32_t count(const Row<T, N, NV> &row, SampleShared &S, F in) {
+    uint32_t n = 0;
+    row.all_kept([&](int, float l) { n += in(l) ? 1 : 0; });
+    n = wave_total(n);
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) S.part32[threadIdx.x >> 6] = n;
+    __syncthreads();
+    n = 0;
+#pragma unroll
+    for (int i = 0; i < N / 64; i++) n += S.part32[i];
+    return n;
+}
+// They go to the list, by no order: how many; more than kList: too many.
+template <typename T, int N, int NV, typename F>
+__device__ __forceinline__ uint32_t collect(const Row<T, N, NV> &row, SampleShared &S, F in) {
     __syncthreads();
     if (threadIdx.x == 0) S.n_list = 0;
     __syncthreads();
     row.all_kept([&](int v, float l) {
         if (in(l)) {
             const uint32_t i = atomicAdd(&S.n_list, 1u);
-            if (i < (uint32_t)kList) S.list[i].rank = rank_of(key_of(l), v);
+            if (i < (uint32_t)kList) S.list[i].rank = rank_of(key_of<T>(l), v);
         }
     });
     __syncthreads();
@@ -438,6 +472,12 @@ struct Listed {
     }
 };
 
+// sum += v of all lanes, by every wave
+__device__ __forceinline__ void add(u64 &sum, u64 v) {
+    v = wave_total(v);
+    if (v && (threadIdx.x & 63) == 0) atomicAdd(&sum, v);
+}
+
 // Parameters of a row, as the ranking takes them.
 struct Limits {
     uint32_t k;                   // tokens
@@ -456,17 +496,15 @@ __device__ __forceinline__ void finish(SampleShared &S, const Weights &weight, c
     bool stays = t.there && t.ahead < lim.k;
     if (lim.by_mass) {
         if (!all) {
-            if (stays && t.first) atomicAdd(&S.sum, t.mass);
+            add(S.sum, stays && t.first ? t.mass : 0);
             __syncthreads();
             all = S.sum;
         }
         stays = stays && (t.ahead == 0 || t.run < share_of(lim.p, all, true));
     }
     stays = stays && t.mass >= lim.w_min;
-    if (t.first) {
-        S.stay_mass[threadIdx.x / Listed<N>::G] = stays ? t.mass : 0;
-        if (stays) atomicAdd(&S.stay, t.mass);
-    }
+    if (t.first) S.stay_mass[threadIdx.x / Listed<N>::G] = stays ? t.mass : 0;
+    add(S.stay, stays && t.first ? t.mass : 0);
     __syncthreads();
     const u64 sum = S.stay;
     if (out && stays && t.first) out[t.token()] = (float)(t.real * (1.0 / ((double)sum * 0x1p-45)));
@@ -482,26 +520,47 @@ __device__ __forceinline__ void finish(SampleShared &S, const Weights &weight, c
 // The border of the first k tokens, or of m of weight, lies in step f.bin: the rank of the last token inside, and the weight inside.
 // True: the counters have been used.
 template <typename T, int N, int NV>
-__device__ __forceinline__ bool border(Row<T, N, NV> &row, SampleShared &S, const Weights &weight, uint32_t k, u64 m, Found f, u64 &least, u64 &inside) {
+__device__ __forceinline__ bool border(const Row<T, N, NV> &row, SampleShared &S, const Weights &weight, uint32_t k, u64 m, Found f, u64 &least, u64 &inside) {
     // its tokens, and keys; those of bf16 logits are their upper halves
     constexpr int LOW = sizeof(T) == 4 ? 0 : 16;
     const int step = f.bin;
-    uint32_t lo = key_of(plain_logit(weight.reach(((float)step + 0.5f) / kPerOctave))) >> LOW, hi = key_of(plain_logit(weight.below(((float)step - 0.5f) / kPerOctave))) >> LOW;
+    uint32_t lo = key_of<T>(weight.reach(((float)step + 0.5f) / kPerOctave)) >> LOW, hi = key_of<T>(weight.below(((float)step - 0.5f) / kPerOctave)) >> LOW;
     auto in = [&](float l) {
-        const uint32_t key = key_of(l) >> LOW;
+        const uint32_t key = key_of<T>(l) >> LOW;
         return key >= lo && key <= hi && Weights::step(weight.exponent(l)) == step;
     };
-    uint32_t base = f.base_count, n = collect(row, S, in);
+    // (bf16: a step has few numbers in it, if not one)
+    if (hi - lo < 64) {
+        const uint32_t key = lo + (threadIdx.x & 63);
+        const u64 some = __ballot(in(logit_of(LOW && !(key >> 15) ? key << LOW | 0xFFFFu : key << LOW)));
+        if (some) {
+            hi = lo + 63 - __clzll((long long)some);
+            lo += __ffsll((long long)some) - 1;
+        }
+    }
+    auto full_key = [&] { return LOW && !(hi >> 15) ? hi << LOW | 0xFFFFu : hi << LOW; };     // (keys of negative numbers are turned around)
+    uint32_t base = f.base_count, n = count(row, S, in);
     u64 base_mass = f.base_mass;
     const bool used = n > (uint32_t)kList;
     while (n > (uint32_t)kList) {
+        if (lo == hi) {
+            // all equal: the first of them by token
+            const u64 w = weight(logit_of(full_key()));
+            u64 keep = k - base;
+            if (w) keep = min(keep, (m - base_mass - 1) / w + 1);      // (m is more than base_mass)
+            keep = min(max(keep, (u64)1), (u64)n);
+            const int last = descend(row, S, keep - 1, 0, row.V, [&](int, float l) { return (u64)(in(l) ? 1 : 0); });
+            least = rank_of(full_key(), last);
+            inside = base_mass + keep * w;
+            return true;
+        }
         const int shift = max(0, 32 - __clz(hi - lo) - 11);  // 2^11 steps of keys at most
         __syncthreads();
         clear_counters<N>(S, true);
         __syncthreads();
         row.all([&](int, float l) {
             if (in(l)) {
-                const uint32_t i = (hi - (key_of(l) >> LOW)) >> shift;
+                const uint32_t i = (hi - (key_of<T>(l) >> LOW)) >> shift;
                 atomicAdd(&S.count[i], 1u);
                 atomicAdd(&S.mass[i], weight(l));
             }
@@ -515,19 +574,8 @@ __device__ __forceinline__ bool border(Row<T, N, NV> &row, SampleShared &S, cons
         hi -= (uint32_t)f.bin << shift;
         lo = max(lo, hi - min(hi, (1u << shift) - 1));
         n = f.count;
-        if (shift == 0 && n > (uint32_t)kList) {
-            // all equal: the first of them by token
-            const u64 w = f.mass / n;
-            u64 keep = k - base;
-            if (w) keep = min(keep, (m - base_mass - 1) / w + 1);      // (m is more than base_mass)
-            keep = min(max(keep, (u64)1), (u64)n);
-            const int last = descend(row, S, keep - 1, 0, row.V, [&](int, float l) { return (u64)(in(l) ? 1 : 0); });
-            least = rank_of(LOW && !(hi >> 15) ? hi << LOW | 0xFFFFu : hi << LOW, last);      // (keys of negative numbers are turned around)
-            inside = base_mass + keep * w;
-            return true;
-        }
-        if (n <= (uint32_t)kList) n = collect(row, S, in);
     }
+    n = collect(row, S, in);
     const Listed<N> t(S, weight, min(n, (uint32_t)kList));
     if (t.there && t.first && base + t.ahead < k && base_mass + t.run < m) {
         atomicMin(&S.least, t.rank);
@@ -540,7 +588,7 @@ __device__ __forceinline__ bool border(Row<T, N, NV> &row, SampleShared &S, cons
 }
 
 template <typename T, int N, int NV>
-__global__ __launch_bounds__(N) void k_sample(SampleRows a) {
+__global__ __launch_bounds__(N, 4) void k_sample(SampleRows a) {
     __shared__ __align__(16) SampleShared S;
     using R = Row<T, N, NV>;
     const int r = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = R::wave(), set = r / a.each;
@@ -557,7 +605,8 @@ __global__ __launch_bounds__(N) void k_sample(SampleRows a) {
     if (tid < kPerOctave) S.roots[tid] = exp2((double)tid / kPerOctave);
 
     float mine = -INFINITY;
-    row.all_kept([&](int, float l) { mine = fmaxf(mine, l); });
+    row.all_kept([&](int, float l) { mine = fmaxf(mine, __builtin_canonicalizef(l)); });      // (a signalling NaN would be what v_max_f32 gives)
+    mine = fminf(mine, kLargest<T>);
     float top = wave_largest(mine);
     if (lane == 0) S.top[wave] = top;
     __syncthreads();
@@ -579,7 +628,7 @@ __global__ __launch_bounds__(N) void k_sample(SampleRows a) {
         if (token && tid == 0) *token = -1;
         return;
     }
-    const Weights weight{(double)top, 1.4426950408889634 / (greedy ? 1.0 : (double)temperature), S.roots};
+    const Weights weight{(double)top, fmax(1.4426950408889634 / (greedy ? 1.0 : (double)temperature), 1e-300), S.roots};
     Limits lim{(uint32_t)k, p, p < 1.f && k > 1, 1};
     if (p_min > 0.f) lim.w_min = max((u64)ceil((double)fminf(p_min, 1.f) * (double)(1ull << 45)), (u64)1);
 
@@ -616,70 +665,57 @@ __global__ __launch_bounds__(N) void k_sample(SampleRows a) {
         __syncthreads();
     }
 
-    // ---- by a share of the weight, or by many tokens (what is kept of the largest rows would cost the registers of the passes below)
-    Row<T, N, (NV > 8 && N == 1024 ? 0 : NV)> again;
-    again.x = row.x;
-    again.V = row.V;
-    if constexpr (NV <= 8 || N < 1024)
-#pragma unroll
-        for (int j = 0; j < NV; j++) again.kept[j] = row.kept[j];
+    // ---- by many tokens, or by a share of the weight (from here on the row is read again; what is kept of it would cost the registers of these passes)
+    const Row<T, N, 0> again{row.x, row.V, {}};
     u64 least = 0, sum = 0;
     const bool counted = k < a.V;
-    if (counted || lim.by_mass) {
-        auto histogram = [&] {
+    bool stand = false;                                      // the counters hold the histogram
+#pragma unroll 1
+    for (int pass = 0; pass < 2; pass++) {
+        if (pass ? !lim.by_mass : !counted) continue;
+        if (!stand) {
             again.all([&](int, float l) {
                 const double x = weight.exponent(l);
                 const int i = Weights::step(x);
-                if (i < kSteps) {
-                    if (counted) atomicAdd(&S.count[i], 1u);
-                    if (lim.by_mass) atomicAdd(&S.mass[i], Weights::whole(weight.real(x)));
+                if (counted && i < kSteps) atomicAdd(&S.count[i], 1u);
+                if (lim.by_mass) {
+                    const u64 w = weight.at(x);
+                    if (i < kSteps) atomicAdd(&S.mass[i], w);
                 }
             });
             __syncthreads();
             sum_counters<N>(S);
-        };
-        histogram();
-        u64 all = 0;
+            stand = true;
+            if (!sum)
 #pragma unroll
-        for (int i = 0; i < N / 64; i++) all += S.part[i];
-        // what stays may fit the list: all tokens down to the end of a step
-        auto listed = [&](int step, u64 of) {
-            const float cut = weight.reach(((float)step + 0.5f) / kPerOctave);
-            const uint32_t n = collect(again, S, [&](float l) { return l >= cut; });
-            if (n > (uint32_t)kList) return false;
-            if (out) clear();
-            __syncthreads();
-            finish<N>(S, weight, lim, of, n, out, u, token);
-            return true;
-        };
-        if (counted) {
-            const Found f = find<N>(S, k, ~0ull);
-            if (f.bin < kSteps) {
-                if (f.base_count + f.count <= (uint32_t)kList && listed(f.bin, 0)) return;
-                const bool spoilt = border(again, S, weight, k, ~0ull, f, least, all);
-                if (lim.by_mass && spoilt) {
-                    __syncthreads();
-                    clear_counters<N>(S, true);
-                    __syncthreads();
-                    histogram();
-                }
-            }
+                for (int i = 0; i < N / 64; i++) sum += S.part[i];
         }
-        if (lim.by_mass) {
-            const u64 m = max(share_of(p, all, true), (u64)1);
-            const Found f = find<N>(S, ~0u, m);
-            if (f.bin < kSteps) {
-                if (listed(f.bin, all)) return;
-                border(again, S, weight, ~0u, m, f, least, all);
-            }
-            sum = all;
+        const uint32_t first = pass ? ~0u : (uint32_t)k;
+        const u64 m = pass ? max(share_of(p, sum, true), (u64)1) : ~0ull;
+        const Found f = find<N>(S, first, m);
+        if (f.bin >= kSteps) continue;                       // (all tokens with a weight)
+        // what stays may fit the list: all tokens down to the end of the step
+        const float cut = weight.reach(((float)f.bin + 0.5f) / kPerOctave);
+        auto in = [&](float l) { return l >= cut; };
+        if (count(again, S, in) <= (uint32_t)kList) {
+            if (out) clear();
+            const uint32_t n = collect(again, S, in);
+            return finish<N>(S, weight, lim, pass ? sum : 0, n, out, u, token);
+        }
+        stand = !border(again, S, weight, first, m, f, least, sum);
+        if (!stand) {
+            __syncthreads();
+            clear_counters<N>(S, true);
+            __syncthreads();
         }
     }
+    if (!lim.by_mass) sum = 0;                               // (not known yet)
 
     // ---- all
     const float l_least = least ? logit_of((uint32_t)(least >> 32)) : -INFINITY;
+    const float l_above = l_least == kLargest<T> ? INFINITY : l_least;   // (inf counts as that)
     const int v_last = (int)~(uint32_t)least;                // of the tokens with the least logit
-    auto stays = [&](int v, float l) { return l > l_least || (l == l_least && v <= v_last); };
+    auto stays = [&](int v, float l) { return l > l_above || (l >= l_least && v <= v_last); };
     auto value = [&](int v, float l) -> u64 {
         if (!stays(v, l)) return 0;
         const u64 w = weight(l);
@@ -688,7 +724,8 @@ __global__ __launch_bounds__(N) void k_sample(SampleRows a) {
     const int range = R::range(a.V);
     if (token || !sum || lim.w_min > 1) {
         u64 of_wave = 0;
-        again.all([&](int v, float l) { of_wave += value(v, l); });
+        if (least || lim.w_min > 1) again.all([&](int v, float l) { of_wave += value(v, l); });
+        else again.all([&](int, float l) { of_wave += weight(l); });
         of_wave = wave_total(of_wave);
         __syncthreads();
         if (lane == 0) S.part[wave] = of_wave;

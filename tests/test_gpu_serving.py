@@ -26,12 +26,12 @@ def _need_gpu():
 
 # ------------------------------------------------------------------------------------------------ draws
 
-def check_rows(x, tokens, probs, u, sets):
+def check_rows(x, tokens, probs, u, sets, dtype=torch.float32):
     """x [rows][V] float64 as the kernel read them; sets: (temperature, top_k, top_p, min_p) of every row."""
     V = x.shape[1]
     E = 2 * V * 2.0 ** -45
     for r in range(len(x)):
-        w, slack = O.weights(x[r], *sets[r])
+        w, slack = O.weights(x[r], *sets[r], largest=torch.finfo(dtype).max)
         if probs is not None:
             p = probs[r].astype(np.float64)
             assert (p >= 0).all(), r
@@ -72,7 +72,7 @@ def run_rows(x, u=None, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, expect_s
     both = torch.full((rows, V), -1.0, device="cuda")
     again = P.sample(x, u, probs=both, **kw)
     assert torch.equal(again, tokens) and torch.equal(both, probs)
-    check_rows(x.double().cpu().numpy(), tokens.cpu().numpy(), probs.cpu().numpy(), u.cpu().numpy(), as_sets(rows, temperature, top_k, top_p, min_p))
+    check_rows(x.double().cpu().numpy(), tokens.cpu().numpy(), probs.cpu().numpy(), u.cpu().numpy(), as_sets(rows, temperature, top_k, top_p, min_p), x.dtype)
     return tokens, probs
 
 
@@ -169,6 +169,7 @@ def test_logits_that_are_not_finite(V, dtype, kw):
     if dtype == torch.bfloat16:
         x[7, :], x[8, :-1] = torch.finfo(dtype).min, torch.finfo(dtype).min
         x[2, 17] = torch.finfo(dtype).min
+    x[11, 20:30] = torch.finfo(dtype).max                    # as good as infinity
     run_rows(x.to(dtype), **kw)
 
 
@@ -194,6 +195,18 @@ def test_uniform_numbers_at_the_ends():
     stay = probs[0].nonzero()[:, 0]
     assert tokens.tolist() == [stay[0], stay[0], stay[-1], stay[-1], stay[0], stay[-1]]
     assert 0 <= P.sample(x[:1], torch.tensor([math.nan]).cuda()).item() < 3000
+
+
+@pytest.mark.parametrize("dtype,bits", [(torch.float32, 0x7F800001), (torch.float32, -0x7FFFFF), (torch.float32, 0x7FC00000), (torch.bfloat16, 0x7F81), (torch.bfloat16, -0x7F)])
+def test_every_kind_of_nan(dtype, bits):
+    for V in (1, 300, 5000):
+        x = logits(4, V, dtype, 3)
+        raw = x.view(torch.int32 if dtype == torch.float32 else torch.int16)
+        raw[0, :] = bits
+        raw[1, ::2] = bits
+        raw[2, V // 2:] = bits
+        for kw in (dict(), dict(top_k=5), dict(top_p=0.7), dict(min_p=0.1), dict(temperature=0.0)):
+            run_rows(x, **kw)
 
 
 def test_values_far_apart():
