@@ -153,11 +153,13 @@ __device__ __forceinline__ float wave_largest(float v) {
 
 // ---------------------------------------------------------------------------------------- a row, by N threads
 
-// Wave w has the w-th range of the row, tile by tile (a tile: 16 bytes of each lane).  NV tiles of a wave stay in registers, for the passes that do little with a
-// token; the others read the row again (so the code stays small).  NV = 0: all do.
-template <typename T, int N, int NV>
+// Wave w has the w-th range of the row, tile by tile (a tile: 16 bytes of each lane).  NV tiles of a wave stay in registers, for the first passes, which do little with a
+// token; the others read the row again.  (What a pass does is in the code once for each token of a tile, where the row is read, or of all NV: instructions that are not in
+// their cache cost more than all of the row's bytes.)  NV = 0: all passes read.  V is at least VE, or the row is TINY.
+template <typename T, int N, int NV, bool TINY = false>
 struct Row {
-    static constexpr int VE = 16 / sizeof(T), W = N / 64, TILE = 64 * VE, AHEAD = 4;
+    static constexpr int VE = 16 / sizeof(T), W = N / 64, TILE = 64 * VE;
+    static constexpr uint32_t kNone = sizeof(T) == 4 ? 0xFF800000u : 0xFF80FF80u;      // -inf
     const T *x;
     int V;
     u32x4 kept[NV ? NV : 1];
@@ -166,17 +168,28 @@ struct Row {
     struct __attribute__((packed, aligned(sizeof(T)))) Raw {
         u32x4 v;
     };
+    // tokens at .. at + VE - 1, at < V; -inf for those from V on
     __device__ __forceinline__ u32x4 load(int at) const {
-        if (at + VE <= V) return reinterpret_cast<const Raw *>(x + at)->v;
         u32x4 r;
+        if constexpr (TINY) {
 #pragma unroll
-        for (int i = 0; i < 4; i++) {
-            if constexpr (sizeof(T) == 4) {
-                r[i] = at + i < V ? __float_as_uint(x[at + i]) : 0xFF800000u;
-            } else {
-                const uint32_t lo = at + 2 * i < V ? x[at + 2 * i] : 0xFF80u, hi = at + 2 * i + 1 < V ? x[at + 2 * i + 1] : 0xFF80u;
-                r[i] = lo | hi << 16;
+            for (int i = 0; i < 4; i++) {
+                if constexpr (sizeof(T) == 4) {
+                    r[i] = at + i < V ? __float_as_uint(x[at + i]) : 0xFF800000u;
+                } else {
+                    const uint32_t lo = at + 2 * i < V ? x[at + 2 * i] : 0xFF80u, hi = at + 2 * i + 1 < V ? x[at + 2 * i + 1] : 0xFF80u;
+                    r[i] = lo | hi << 16;
+                }
             }
+            return r;
+        }
+        const int from = min(at, V - VE), s = at - from;     // the last piece is read from further ahead, and moved down
+        r = reinterpret_cast<const Raw *>(x + from)->v;
+        if (s) {
+            constexpr int D = 4 / (int)sizeof(T);            // tokens of a dword
+            if (s & (2 * D)) r = u32x4{r[2], r[3], kNone, kNone};
+            if (s & D) r = u32x4{r[1], r[2], r[3], kNone};
+            if (D == 2 && (s & 1)) r = u32x4{r[0] >> 16 | r[1] << 16, r[1] >> 16 | r[2] << 16, r[2] >> 16 | r[3] << 16, r[3] >> 16 | kNone << 16};
         }
         return r;
     }
@@ -184,23 +197,17 @@ struct Row {
         if constexpr (sizeof(T) == 4) return __uint_as_float(r[e]);
         else return __uint_as_float(e & 1 ? r[e / 2] & 0xFFFF0000u : r[e / 2] << 16);
     }
-    // f(first token, piece) for the pieces of VE tokens of [lo, hi) that are this lane's; lo and hi are the wave's
+    // f(first token, piece) for the pieces of VE tokens of [lo, hi) that are this lane's, the next one on its way; lo and hi are the wave's
     template <typename F>
     __device__ __forceinline__ void pieces(int lo, int hi, F f) const {
-        const int lane = threadIdx.x & 63;
-        for (int base = lo; base < hi; base += AHEAD * TILE) {
-            u32x4 r[AHEAD];
-#pragma unroll
-            for (int j = 0; j < AHEAD; j++) {
-                const int at = base + j * TILE + lane * VE;
-                if (at < hi) r[j] = load(at);
-            }
-#pragma unroll
-            for (int j = 0; j < AHEAD; j++) {
-                const int at = base + j * TILE + lane * VE;
-                if (at < hi) f(at, r[j]);
-                __builtin_amdgcn_sched_barrier(0);           // (a piece at a time: the registers of more than one's numbers are not there)
-            }
+        int at = lo + (threadIdx.x & 63) * VE;
+        u32x4 next;
+        if (at < hi) next = load(at);
+#pragma unroll 1
+        for (; lo < hi; lo += TILE, at += TILE) {
+            const u32x4 r = next;
+            if (at + TILE < hi) next = load(at + TILE);
+            if (at < hi) f(at, r);
         }
     }
     // f(token, logit); tokens from V on have -inf
@@ -214,39 +221,46 @@ struct Row {
     // tokens of a wave's range of n
     static __device__ __forceinline__ int range(int n) { return (n + W * TILE - 1) / (W * TILE) * TILE; }
     static __device__ __forceinline__ int wave() { return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); }
+    template <typename F>
+    __device__ __forceinline__ void all(F f) const {
+        const int c = range(V);
+        tokens(min(wave() * c, V), min(wave() * c + c, V), f);
+    }
     __device__ __forceinline__ void keep() {
         if constexpr (NV > 0) {
             const int c = range(V);
 #pragma unroll
             for (int j = 0; j < NV; j++) {
                 const int at = wave() * c + j * TILE + (threadIdx.x & 63) * VE;
-                constexpr uint32_t none = sizeof(T) == 4 ? 0xFF800000u : 0xFF80FF80u;      // -inf
-                kept[j] = u32x4{none, none, none, none};
+                kept[j] = u32x4{kNone, kNone, kNone, kNone};
                 if (j * TILE < c && at < V) kept[j] = load(at);
             }
         }
     }
-    // passes that do much, and little, with a token
+    // passes that do little with a token: from registers, or with four tiles on their way
     template <typename F>
-    __device__ __forceinline__ void all(F f) const {
-        const int c = range(V);
-        tokens(min(wave() * c, V), min(wave() * c + c, V), f);
-    }
-    template <typename F>
-    __device__ __forceinline__ void all_kept(F f) const {
+    __device__ __forceinline__ void all_pieces(F f) const {
+        const int c = range(V), lo = wave() * c;
         if constexpr (NV > 0) {
-            const int c = range(V), at = wave() * c + (threadIdx.x & 63) * VE;
 #pragma unroll
             for (int j = 0; j < NV; j++) {
                 u32x4 r = kept[j];
                 asm volatile("" : "+v"(r));                  // (nothing that one pass makes of them is kept for the next)
-                if (j * TILE < c)
-#pragma unroll
-                    for (int e = 0; e < VE; e++) f(at + j * TILE + e, get(r, e));
+                if (j * TILE < c) f(lo + j * TILE + (int)(threadIdx.x & 63) * VE, r);
                 __builtin_amdgcn_sched_barrier(0);
             }
         } else {
-            all(f);
+            constexpr int AHEAD = 4;
+            const int hi = min(lo + c, V);
+#pragma unroll 1
+            for (int at = lo + (threadIdx.x & 63) * VE; at < hi; at += AHEAD * TILE) {
+                u32x4 r[AHEAD];
+#pragma unroll
+                for (int j = 0; j < AHEAD; j++) r[j] = load(min(at + j * TILE, V - 1));
+#pragma unroll
+                for (int j = 0; j < AHEAD; j++)
+                    if (at + j * TILE < hi) f(at + j * TILE, r[j]);
+            }
         }
     }
 };
@@ -262,7 +276,7 @@ struct SampleShared {
     u64 stay_mass[kList];
     double roots[kPerOctave];
     u64 part[16];
-    uint32_t part32[16];
+    uint32_t part32[16], about[16];
     float top[16];
     uint32_t n_list;
     u64 least, sum, stay;
@@ -282,7 +296,10 @@ struct Found {
     int bin;                      // kBins: none
     uint32_t base_count, count;
     u64 base_mass, mass;
+    uint32_t about;               // a histogram of weights: sixteen times the tokens that there are likely up to the end of its lane's counters
 };
+// About how many tokens a step of so much weight has (within a percent or so: their weights are).
+__device__ __forceinline__ float likely(u64 mass, int step) { return (float)mass * __builtin_amdgcn_exp2f((float)step / kPerOctave - 45.f); }
 
 // The waves' sums of the counters (wave w: its kBins / W ones); a barrier behind it.
 template <int N>
@@ -290,16 +307,21 @@ __device__ __forceinline__ void sum_counters(SampleShared &S) {
     constexpr int B = kBins / N;
     uint32_t n = 0;
     u64 m = 0;
+    float some = 0.f;
 #pragma unroll
     for (int i = 0; i < B; i++) {
+        const u64 mass = S.mass[threadIdx.x * B + i];
         n += S.count[threadIdx.x * B + i];
-        m += S.mass[threadIdx.x * B + i];
+        m += mass;
+        some += likely(mass, threadIdx.x * B + i);
     }
     n = wave_total(n);
     m = wave_total(m);
+    const uint32_t about = wave_total((uint32_t)(some * 16.f));      // (in sixteenths)
     if ((threadIdx.x & 63) == 0) {
         S.part32[threadIdx.x >> 6] = n;
         S.part[threadIdx.x >> 6] = m;
+        S.about[threadIdx.x >> 6] = about;
     }
     __syncthreads();
 }
@@ -308,7 +330,7 @@ template <int N>
 __device__ __forceinline__ Found find(const SampleShared &S, uint32_t k, u64 m) {
     constexpr int B = kBins / N, W = N / 64;
     const int lane = threadIdx.x & 63;
-    Found f{kBins, 0, 0, 0, 0};
+    Found f{kBins, 0, 0, 0, 0, 0};
     int w = 0;
     for (; w < W; w++) {
         const uint32_t n = S.part32[w];
@@ -316,17 +338,21 @@ __device__ __forceinline__ Found find(const SampleShared &S, uint32_t k, u64 m) 
         if (f.base_count + n >= k || f.base_mass + x >= m) break;
         f.base_count += n;
         f.base_mass += x;
+        f.about += S.about[w];
     }
     if (w == W) return f;
     uint32_t count[B], n = 0;
     u64 mass[B], x = 0;
+    float some = 0.f;
 #pragma unroll
     for (int i = 0; i < B; i++) {
         count[i] = S.count[(w * 64 + lane) * B + i];
         mass[i] = S.mass[(w * 64 + lane) * B + i];
         n += count[i];
         x += mass[i];
+        some += likely(mass[i], (w * 64 + lane) * B + i);
     }
+    const uint32_t part = (uint32_t)(some * 16.f);
     const uint32_t to = f.base_count + wave_scan(n);
     const u64 mass_to = f.base_mass + wave_scan(x);
     const int hit = __ffsll((long long)__ballot(to >= k || mass_to >= m)) - 1;
@@ -346,13 +372,13 @@ __device__ __forceinline__ Found find(const SampleShared &S, uint32_t k, u64 m) 
                 mass_before += mass[i];
             }
         }
-    return Found{(w * 64 + hit) * B + (int)from_lane(at, hit), from_lane(before, hit), from_lane(mine, hit), from_lane(mass_before, hit), from_lane(mass_mine, hit)};
+    return Found{(w * 64 + hit) * B + (int)from_lane(at, hit), from_lane(before, hit), from_lane(mine, hit), from_lane(mass_before, hit), from_lane(mass_mine, hit),
+                 f.about + from_lane(wave_scan(part), hit)};
 }
 
 // The lowest token of [lo, hi) at which the running sum of value(token, logit), from lo on, passes `target`; the sum over the range is more than that.
-template <typename T, int N, int NV, typename F>
-__device__ __forceinline__ int descend(const Row<T, N, NV> &row, SampleShared &S, u64 target, int lo, int hi, F value) {
-    using R = Row<T, N, NV>;
+template <typename R, typename F>
+__device__ __forceinline__ int descend(const R &row, SampleShared &S, u64 target, int lo, int hi, F value) {
     const int lane = threadIdx.x & 63, wave = R::wave();
     while (hi - lo > R::TILE) {
         const int c = R::range(hi - lo), a = min(lo + wave * c, hi), b = min(a + c, hi);
@@ -363,7 +389,7 @@ __device__ __forceinline__ int descend(const Row<T, N, NV> &row, SampleShared &S
         if (lane == 0) S.part[wave] = sum;
         __syncthreads();
         int w = 0;
-        for (; w < N / 64 - 1 && S.part[w] <= target; w++) target -= S.part[w];
+        for (; w < R::W - 1 && S.part[w] <= target; w++) target -= S.part[w];
         lo = min(lo + w * c, hi - 1);
         hi = min(lo + c, hi);
     }
@@ -397,30 +423,25 @@ __device__ __forceinline__ int descend(const Row<T, N, NV> &row, SampleShared &S
     return S.token;
 }
 
-// The tokens for which in(logit) holds: how many.
-template <typename T, int N, int NV, typename F>
-__device__ __forceinline__ uint32_t count(const Row<T, N, NV> &row, SampleShared &S, F in) {
-    uint32_t n = 0;
-    row.all_kept([&](int, float l) { n += in(l) ? 1 : 0; });
-    n = wave_total(n);
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) S.part32[threadIdx.x >> 6] = n;
-    __syncthreads();
-    n = 0;
-#pragma unroll
-    for (int i = 0; i < N / 64; i++) n += S.part32[i];
-    return n;
-}
-// They go to the list, by no order: how many; more than kList: too many.
-template <typename T, int N, int NV, typename F>
-__device__ __forceinline__ uint32_t collect(const Row<T, N, NV> &row, SampleShared &S, F in) {
+// The tokens for which in(logit) holds to the list, by no order: how many; more than kList: too many.
+template <typename T, typename R, typename F>
+__device__ __forceinline__ uint32_t collect(const R &row, SampleShared &S, F in) {
     __syncthreads();
     if (threadIdx.x == 0) S.n_list = 0;
     __syncthreads();
-    row.all_kept([&](int v, float l) {
-        if (in(l)) {
+    row.all_pieces([&](int at, const u32x4 &r) {
+        uint32_t hits = 0;
+#pragma unroll
+        for (int e = 0; e < R::VE; e++) hits |= in(R::get(r, e)) ? 1u << e : 0u;
+        while (hits) {
+            const int e = __ffs(hits) - 1;
+            hits &= hits - 1;
+            constexpr int D = 4 / (int)sizeof(T);
+            const int d = e / D;
+            const uint32_t w = d & 2 ? d & 1 ? r[3] : r[2] : d & 1 ? r[1] : r[0];
+            const float l = __uint_as_float(D == 1 ? w : e & 1 ? w & 0xFFFF0000u : w << 16);
             const uint32_t i = atomicAdd(&S.n_list, 1u);
-            if (i < (uint32_t)kList) S.list[i].rank = rank_of(key_of<T>(l), v);
+            if (i < (uint32_t)kList) S.list[i].rank = rank_of(key_of<T>(l), at + e);
         }
     });
     __syncthreads();
@@ -519,38 +540,47 @@ __device__ __forceinline__ void finish(SampleShared &S, const Weights &weight, c
 
 // The border of the first k tokens, or of m of weight, lies in step f.bin: the rank of the last token inside, and the weight inside.
 // True: the counters have been used.
-template <typename T, int N, int NV>
-__device__ __forceinline__ bool border(const Row<T, N, NV> &row, SampleShared &S, const Weights &weight, uint32_t k, u64 m, Found f, u64 &least, u64 &inside) {
-    // its tokens, and keys; those of bf16 logits are their upper halves
+template <typename T, int N, typename R>
+__device__ __forceinline__ bool border(const R &row, SampleShared &S, const Weights &weight, uint32_t k, u64 m, Found f, u64 &least, u64 &inside) {
+    // its logits lie between two keys; those of bf16 logits are their upper halves
     constexpr int LOW = sizeof(T) == 4 ? 0 : 16;
     const int step = f.bin;
     uint32_t lo = key_of<T>(weight.reach(((float)step + 0.5f) / kPerOctave)) >> LOW, hi = key_of<T>(weight.below(((float)step - 0.5f) / kPerOctave)) >> LOW;
-    auto in = [&](float l) {
-        const uint32_t key = key_of<T>(l) >> LOW;
-        return key >= lo && key <= hi && Weights::step(weight.exponent(l)) == step;
+    auto full_key = [&](uint32_t key) { return LOW && !(key >> 15) ? key << LOW | 0xFFFFu : key << LOW; };       // (keys of negative numbers are turned around)
+    float from, to;
+    auto between = [&] {
+        if (hi == 0x7FFFFFFFu >> LOW) hi--;                  // (-0, which no token's key is)
+        lo = min(lo, hi);
+        from = logit_of(full_key(lo));
+        to = logit_of(full_key(hi));
+        if (to == kLargest<T>) to = INFINITY;
     };
+    auto in = [&](float l) { return l >= from && l <= to && Weights::step(weight.exponent(l)) == step; };
     // (bf16: a step has few numbers in it, if not one)
     if (hi - lo < 64) {
         const uint32_t key = lo + (threadIdx.x & 63);
-        const u64 some = __ballot(in(logit_of(LOW && !(key >> 15) ? key << LOW | 0xFFFFu : key << LOW)));
+        const u64 some = __ballot(key <= hi && Weights::step(weight.exponent(logit_of(full_key(key)))) == step);
         if (some) {
             hi = lo + 63 - __clzll((long long)some);
             lo += __ffsll((long long)some) - 1;
         }
     }
-    auto full_key = [&] { return LOW && !(hi >> 15) ? hi << LOW | 0xFFFFu : hi << LOW; };     // (keys of negative numbers are turned around)
-    uint32_t base = f.base_count, n = count(row, S, in);
+    between();
+    uint32_t base = f.base_count;
     u64 base_mass = f.base_mass;
+    // (as many as are likely, if they were not counted)
+    uint32_t n = f.count ? f.count : (uint32_t)likely(f.mass, step);
+    if (n <= (uint32_t)kList) n = collect<T>(row, S, in);
     const bool used = n > (uint32_t)kList;
     while (n > (uint32_t)kList) {
         if (lo == hi) {
             // all equal: the first of them by token
-            const u64 w = weight(logit_of(full_key()));
+            const u64 w = weight(from);
             u64 keep = k - base;
             if (w) keep = min(keep, (m - base_mass - 1) / w + 1);      // (m is more than base_mass)
-            keep = min(max(keep, (u64)1), (u64)n);
-            const int last = descend(row, S, keep - 1, 0, row.V, [&](int, float l) { return (u64)(in(l) ? 1 : 0); });
-            least = rank_of(full_key(), last);
+            keep = max(keep, (u64)1);
+            const int last = descend(row, S, keep - 1, 0, row.V, [&](int, float l) { return (u64)(l >= from && l <= to ? 1 : 0); });
+            least = rank_of(full_key(lo), last);
             inside = base_mass + keep * w;
             return true;
         }
@@ -560,9 +590,10 @@ __device__ __forceinline__ bool border(const Row<T, N, NV> &row, SampleShared &S
         __syncthreads();
         row.all([&](int, float l) {
             if (in(l)) {
-                const uint32_t i = (hi - (key_of<T>(l) >> LOW)) >> shift;
-                atomicAdd(&S.count[i], 1u);
-                atomicAdd(&S.mass[i], weight(l));
+                const uint32_t key = key_of<T>(l) >> LOW;    // (between lo and hi, so less than 2^11 steps from it)
+                if (key < lo || key > hi) return;
+                atomicAdd(&S.count[(hi - key) >> shift], 1u);
+                atomicAdd(&S.mass[(hi - key) >> shift], weight(l));
             }
         });
         __syncthreads();
@@ -573,9 +604,10 @@ __device__ __forceinline__ bool border(const Row<T, N, NV> &row, SampleShared &S
         base_mass += f.base_mass;
         hi -= (uint32_t)f.bin << shift;
         lo = max(lo, hi - min(hi, (1u << shift) - 1));
+        between();
         n = f.count;
+        if (n <= (uint32_t)kList) n = collect<T>(row, S, in);
     }
-    n = collect(row, S, in);
     const Listed<N> t(S, weight, min(n, (uint32_t)kList));
     if (t.there && t.first && base + t.ahead < k && base_mass + t.run < m) {
         atomicMin(&S.least, t.rank);
@@ -587,10 +619,10 @@ __device__ __forceinline__ bool border(const Row<T, N, NV> &row, SampleShared &S
     return used;
 }
 
-template <typename T, int N, int NV>
+template <typename T, int N, int NV, bool TINY>
 __global__ __launch_bounds__(N, 4) void k_sample(SampleRows a) {
     __shared__ __align__(16) SampleShared S;
-    using R = Row<T, N, NV>;
+    using R = Row<T, N, NV, TINY>;
     const int r = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = R::wave(), set = r / a.each;
     R row;
     row.x = reinterpret_cast<const T *>(a.logits) + (size_t)r * a.stride;
@@ -605,7 +637,10 @@ __global__ __launch_bounds__(N, 4) void k_sample(SampleRows a) {
     if (tid < kPerOctave) S.roots[tid] = exp2((double)tid / kPerOctave);
 
     float mine = -INFINITY;
-    row.all_kept([&](int, float l) { mine = fmaxf(mine, __builtin_canonicalizef(l)); });      // (a signalling NaN would be what v_max_f32 gives)
+    row.all_pieces([&](int, const u32x4 &piece) {
+#pragma unroll
+        for (int e = 0; e < R::VE; e++) mine = fmaxf(mine, __builtin_canonicalizef(R::get(piece, e)));      // (a signalling NaN would be what v_max_f32 gives)
+    });
     mine = fminf(mine, kLargest<T>);
     float top = wave_largest(mine);
     if (lane == 0) S.top[wave] = top;
@@ -659,14 +694,14 @@ __global__ __launch_bounds__(N, 4) void k_sample(SampleRows a) {
         }
         if (!lim.by_mass && p_min > 0.f) cut = fmaxf(cut, weight.reach(-__builtin_amdgcn_logf(fminf(p_min, 1.f)) * 1.0001f + 0.001f));      // (log2)
         if (out) clear();
-        const uint32_t n = collect(row, S, [&](float l) { return l >= cut; });
+        const uint32_t n = collect<T>(row, S, [&](float l) { return l >= cut; });
         if (n <= (uint32_t)kList) return finish<N>(S, weight, lim, 0, n, out, u, token);
         clear_counters<N>(S, true);
         __syncthreads();
     }
 
     // ---- by many tokens, or by a share of the weight (from here on the row is read again; what is kept of it would cost the registers of these passes)
-    const Row<T, N, 0> again{row.x, row.V, {}};
+    const Row<T, N, 0, TINY> again{row.x, row.V, {}};
     u64 least = 0, sum = 0;
     const bool counted = k < a.V;
     bool stand = false;                                      // the counters hold the histogram
@@ -697,12 +732,16 @@ __global__ __launch_bounds__(N, 4) void k_sample(SampleRows a) {
         // what stays may fit the list: all tokens down to the end of the step
         const float cut = weight.reach(((float)f.bin + 0.5f) / kPerOctave);
         auto in = [&](float l) { return l >= cut; };
-        if (count(again, S, in) <= (uint32_t)kList) {
-            if (out) clear();
-            const uint32_t n = collect(again, S, in);
-            return finish<N>(S, weight, lim, pass ? sum : 0, n, out, u, token);
+        const uint32_t about = counted ? f.base_count + f.count : f.about / 16;
+        if (about <= (uint32_t)kList + kList / 8) {
+            const uint32_t n = collect<T>(again, S, in);
+            if (n <= (uint32_t)kList) {
+                if (out) clear();
+                __syncthreads();
+                return finish<N>(S, weight, lim, pass ? sum : 0, n, out, u, token);
+            }
         }
-        stand = !border(again, S, weight, first, m, f, least, sum);
+        stand = !border<T, N>(again, S, weight, first, m, f, least, sum);
         if (!stand) {
             __syncthreads();
             clear_counters<N>(S, true);
@@ -717,9 +756,8 @@ __global__ __launch_bounds__(N, 4) void k_sample(SampleRows a) {
     const int v_last = (int)~(uint32_t)least;                // of the tokens with the least logit
     auto stays = [&](int v, float l) { return l > l_above || (l >= l_least && v <= v_last); };
     auto value = [&](int v, float l) -> u64 {
-        if (!stays(v, l)) return 0;
         const u64 w = weight(l);
-        return w >= lim.w_min ? w : 0;
+        return stays(v, l) && w >= lim.w_min ? w : 0;
     };
     const int range = R::range(a.V);
     if (token || !sum || lim.w_min > 1) {
@@ -767,16 +805,17 @@ __global__ __launch_bounds__(N, 4) void k_sample(SampleRows a) {
 
 // ---------------------------------------------------------------------------------------- entry points
 
-template <typename T, int N, int NV>
+template <typename T, int N, int NV, bool TINY = false>
 static void sample_launch_as(const SampleRows &a, int rows, hipStream_t st) {
-    hipLaunchKernelGGL((k_sample<T, N, NV>), dim3(rows), dim3(N), 0, st, a);
+    hipLaunchKernelGGL((k_sample<T, N, NV, TINY>), dim3(rows), dim3(N), 0, st, a);
 }
 
 // The row stays in registers where it fits them.
 template <typename T>
 static void sample_launch(const SampleRows &a, int rows, hipStream_t st) {
     constexpr int VE = 16 / sizeof(T);
-    if (a.V <= 256 * 4 * VE) sample_launch_as<T, 256, 4>(a, rows, st);
+    if (a.V < VE) sample_launch_as<T, 256, 1, true>(a, rows, st);
+    else if (a.V <= 256 * 4 * VE) sample_launch_as<T, 256, 4>(a, rows, st);
     else if (a.V <= 512 * 16 * VE && rows >= 512) sample_launch_as<T, 512, 16>(a, rows, st);
     else if (a.V <= 1024 * 8 * VE) sample_launch_as<T, 1024, 8>(a, rows, st);
     else if (a.V <= 1024 * 16 * VE) sample_launch_as<T, 1024, 16>(a, rows, st);

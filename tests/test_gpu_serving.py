@@ -137,6 +137,18 @@ def test_equal_logits_go_by_the_lowest_token(V, levels, dtype, kw):
         assert probs.nonzero()[:, 1].view(4, 7).tolist() == [list(range(7))] * 4
 
 
+@pytest.mark.parametrize("kw", [dict(top_k=300), dict(top_k=1500, top_p=0.6), dict(top_p=0.3), dict(top_p=0.55), dict(top_p=0.9)], ids=str)
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_crowds_around_zero(dtype, kw):
+    """Hundreds of 0, -0 and of the numbers next to them on either side."""
+    near = torch.tensor([0.0, -0.0, 1e-30, -1e-30, 1e-38, -1e-38, 1e-3, -1e-3, 1e-45, -1e-45])
+    x = near[torch.randint(0, 10, (5, 6000), generator=torch.Generator().manual_seed(1))]
+    x[1] = x[1] * (x[1] != 0)                                # no -0
+    x[2] = -x[2].abs()                                       # no number above it
+    x[3, ::2] = torch.where(x[3, ::2] == 0, torch.tensor(-0.0), x[3, ::2])
+    run_rows(x.to(dtype).cuda(), **kw)
+
+
 @pytest.mark.parametrize("V", [37, 1000, 40000])
 def test_crowded_steps(V):
     """Logits that differ by less than a step of any histogram, all of them above one another: thousands to be told apart by their last bits."""
