@@ -136,6 +136,10 @@ __device__ __forceinline__ U wave_scan(U v) {
 }
 __device__ __forceinline__ uint32_t from_lane(uint32_t v, int lane) { return (uint32_t)__builtin_amdgcn_readlane((int)v, lane); }
 __device__ __forceinline__ u64 from_lane(u64 v, int lane) { return (u64)from_lane((uint32_t)(v >> 32), lane) << 32 | from_lane((uint32_t)v, lane); }
+// (what all lanes have alike, said so: branches on it are the scalar unit's)
+__device__ __forceinline__ uint32_t uniform(uint32_t v) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)v); }
+__device__ __forceinline__ float uniform(float v) { return __uint_as_float(uniform(__float_as_uint(v))); }
+__device__ __forceinline__ u64 uniform(u64 v) { return (u64)uniform((uint32_t)(v >> 32)) << 32 | uniform((uint32_t)v); }
 template <typename U>
 __device__ __forceinline__ U wave_total(U v) { return from_lane(wave_scan(v), 63); }
 __device__ __forceinline__ float wave_largest(float v) {
@@ -168,9 +172,12 @@ struct Row {
     struct __attribute__((packed, aligned(sizeof(T)))) Raw {
         u32x4 v;
     };
-    // tokens at .. at + VE - 1, at < V; -inf for those from V on
-    __device__ __forceinline__ u32x4 load(int at) const {
-        u32x4 r;
+    // This lane's piece of the tile that begins at `base`; -inf for tokens from V on.  (The wave's own branch: what the last tile takes would be four times the rest.)
+    __device__ __forceinline__ u32x4 load(int base) const {
+        const int at = base + (threadIdx.x & 63) * VE;
+        if (!TINY && base + TILE <= V) return raw(at);
+        u32x4 r{kNone, kNone, kNone, kNone};
+        if (at >= V) return r;
         if constexpr (TINY) {
 #pragma unroll
             for (int i = 0; i < 4; i++) {
@@ -184,30 +191,28 @@ struct Row {
             return r;
         }
         const int from = min(at, V - VE), s = at - from;     // the last piece is read from further ahead, and moved down
-        r = reinterpret_cast<const Raw *>(x + from)->v;
-        if (s) {
-            constexpr int D = 4 / (int)sizeof(T);            // tokens of a dword
-            if (s & (2 * D)) r = u32x4{r[2], r[3], kNone, kNone};
-            if (s & D) r = u32x4{r[1], r[2], r[3], kNone};
-            if (D == 2 && (s & 1)) r = u32x4{r[0] >> 16 | r[1] << 16, r[1] >> 16 | r[2] << 16, r[2] >> 16 | r[3] << 16, r[3] >> 16 | kNone << 16};
-        }
+        r = raw(from);
+        constexpr int D = 4 / (int)sizeof(T);                // tokens of a dword
+        if (s & (2 * D)) r = u32x4{r[2], r[3], kNone, kNone};
+        if (s & D) r = u32x4{r[1], r[2], r[3], kNone};
+        if (D == 2 && (s & 1)) r = u32x4{r[0] >> 16 | r[1] << 16, r[1] >> 16 | r[2] << 16, r[2] >> 16 | r[3] << 16, r[3] >> 16 | kNone << 16};
         return r;
     }
+    __device__ __forceinline__ u32x4 raw(int at) const { return reinterpret_cast<const Raw *>(reinterpret_cast<const char *>(x) + (uint32_t)at * (uint32_t)sizeof(T))->v; }
     static __device__ __forceinline__ float get(const u32x4 &r, int e) {
         if constexpr (sizeof(T) == 4) return __uint_as_float(r[e]);
         else return __uint_as_float(e & 1 ? r[e / 2] & 0xFFFF0000u : r[e / 2] << 16);
     }
-    // f(first token, piece) for the pieces of VE tokens of [lo, hi) that are this lane's, the next one on its way; lo and hi are the wave's
+    // f(first token, piece) for this lane's pieces of VE tokens of the tiles from lo to hi, the next one on its way; lo and hi are the wave's
     template <typename F>
     __device__ __forceinline__ void pieces(int lo, int hi, F f) const {
-        int at = lo + (threadIdx.x & 63) * VE;
-        u32x4 next;
-        if (at < hi) next = load(at);
+        if (lo >= hi) return;
+        u32x4 next = load(lo);
 #pragma unroll 1
-        for (; lo < hi; lo += TILE, at += TILE) {
+        for (; lo < hi; lo += TILE) {
             const u32x4 r = next;
-            if (at + TILE < hi) next = load(at + TILE);
-            if (at < hi) f(at, r);
+            if (lo + TILE < hi) next = load(lo + TILE);
+            f(lo + (int)(threadIdx.x & 63) * VE, r);
         }
     }
     // f(token, logit); tokens from V on have -inf
@@ -231,9 +236,8 @@ struct Row {
             const int c = range(V);
 #pragma unroll
             for (int j = 0; j < NV; j++) {
-                const int at = wave() * c + j * TILE + (threadIdx.x & 63) * VE;
                 kept[j] = u32x4{kNone, kNone, kNone, kNone};
-                if (j * TILE < c && at < V) kept[j] = load(at);
+                if (j * TILE < c && wave() * c + j * TILE < V) kept[j] = load(wave() * c + j * TILE);
             }
         }
     }
@@ -253,13 +257,14 @@ struct Row {
             constexpr int AHEAD = 4;
             const int hi = min(lo + c, V);
 #pragma unroll 1
-            for (int at = lo + (threadIdx.x & 63) * VE; at < hi; at += AHEAD * TILE) {
+            for (int base = lo; base < hi; base += AHEAD * TILE) {
                 u32x4 r[AHEAD];
 #pragma unroll
-                for (int j = 0; j < AHEAD; j++) r[j] = load(min(at + j * TILE, V - 1));
+                for (int j = 0; j < AHEAD; j++)
+                    if (base + j * TILE < hi) r[j] = load(base + j * TILE);
 #pragma unroll
                 for (int j = 0; j < AHEAD; j++)
-                    if (at + j * TILE < hi) f(at + j * TILE, r[j]);
+                    if (base + j * TILE < hi) f(base + j * TILE + (int)(threadIdx.x & 63) * VE, r[j]);
             }
         }
     }
@@ -333,12 +338,12 @@ __device__ __forceinline__ Found find(const SampleShared &S, uint32_t k, u64 m) 
     Found f{kBins, 0, 0, 0, 0, 0};
     int w = 0;
     for (; w < W; w++) {
-        const uint32_t n = S.part32[w];
-        const u64 x = S.part[w];
+        const uint32_t n = uniform(S.part32[w]);
+        const u64 x = uniform(S.part[w]);
         if (f.base_count + n >= k || f.base_mass + x >= m) break;
         f.base_count += n;
         f.base_mass += x;
-        f.about += S.about[w];
+        f.about += uniform(S.about[w]);
     }
     if (w == W) return f;
     uint32_t count[B], n = 0;
@@ -379,33 +384,30 @@ __device__ __forceinline__ Found find(const SampleShared &S, uint32_t k, u64 m) 
 // The lowest token of [lo, hi) at which the running sum of value(token, logit), from lo on, passes `target`; the sum over the range is more than that.
 template <typename R, typename F>
 __device__ __forceinline__ int descend(const R &row, SampleShared &S, u64 target, int lo, int hi, F value) {
+    using U = decltype(value(0, 0.f));
     const int lane = threadIdx.x & 63, wave = R::wave();
     while (hi - lo > R::TILE) {
         const int c = R::range(hi - lo), a = min(lo + wave * c, hi), b = min(a + c, hi);
-        u64 sum = 0;
+        U sum = 0;
         row.tokens(a, b, [&](int v, float l) { sum += value(v, l); });
         sum = wave_total(sum);
         __syncthreads();
         if (lane == 0) S.part[wave] = sum;
         __syncthreads();
         int w = 0;
-        for (; w < R::W - 1 && S.part[w] <= target; w++) target -= S.part[w];
+        for (; w < R::W - 1 && uniform(S.part[w]) <= target; w++) target -= uniform(S.part[w]);
         lo = min(lo + w * c, hi - 1);
         hi = min(lo + c, hi);
     }
     __syncthreads();
     if (wave == 0) {
         u64 mine[R::VE], sum = 0;
-#pragma unroll
-        for (int e = 0; e < R::VE; e++) mine[e] = 0;
         const int at = lo + lane * R::VE;
-        if (at < hi) {
-            const u32x4 r = row.load(at);
+        const u32x4 r = row.load(lo);
 #pragma unroll
-            for (int e = 0; e < R::VE; e++) {
-                mine[e] = at + e < hi ? value(at + e, R::get(r, e)) : 0;
-                sum += mine[e];
-            }
+        for (int e = 0; e < R::VE; e++) {
+            mine[e] = value(at + e, R::get(r, e));
+            sum += mine[e];
         }
         const u64 incl = wave_scan(sum), past = __ballot(incl > target);
         if (past && lane == __ffsll((long long)past) - 1) {
@@ -423,16 +425,19 @@ __device__ __forceinline__ int descend(const R &row, SampleShared &S, u64 target
     return S.token;
 }
 
-// The tokens for which in(logit) holds to the list, by no order: how many; more than kList: too many.
+// a && b without a branch between them
+__device__ __forceinline__ bool both(bool a, bool b) { return ((int)a & (int)b) != 0; }
+
+// The tokens with logits of [from, to] for which in(logit) holds to the list, by no order: how many; more than kList: too many.
 template <typename T, typename R, typename F>
-__device__ __forceinline__ uint32_t collect(const R &row, SampleShared &S, F in) {
+__device__ __forceinline__ uint32_t collect(const R &row, SampleShared &S, float from, float to, F in) {
     __syncthreads();
     if (threadIdx.x == 0) S.n_list = 0;
     __syncthreads();
     row.all_pieces([&](int at, const u32x4 &r) {
         uint32_t hits = 0;
 #pragma unroll
-        for (int e = 0; e < R::VE; e++) hits |= in(R::get(r, e)) ? 1u << e : 0u;
+        for (int e = 0; e < R::VE; e++) hits |= both(R::get(r, e) >= from, R::get(r, e) <= to) ? 1u << e : 0u;
         while (hits) {
             const int e = __ffs(hits) - 1;
             hits &= hits - 1;
@@ -440,12 +445,13 @@ __device__ __forceinline__ uint32_t collect(const R &row, SampleShared &S, F in)
             const int d = e / D;
             const uint32_t w = d & 2 ? d & 1 ? r[3] : r[2] : d & 1 ? r[1] : r[0];
             const float l = __uint_as_float(D == 1 ? w : e & 1 ? w & 0xFFFF0000u : w << 16);
+            if (!in(l)) continue;
             const uint32_t i = atomicAdd(&S.n_list, 1u);
             if (i < (uint32_t)kList) S.list[i].rank = rank_of(key_of<T>(l), at + e);
         }
     });
     __syncthreads();
-    return S.n_list;
+    return uniform(S.n_list);
 }
 
 // A token of the list, by N / kList neighbouring lanes: its weight (which goes to the list), and how many tokens and how much weight rank ahead of it.
@@ -545,7 +551,7 @@ __device__ __forceinline__ bool border(const R &row, SampleShared &S, const Weig
     // its logits lie between two keys; those of bf16 logits are their upper halves
     constexpr int LOW = sizeof(T) == 4 ? 0 : 16;
     const int step = f.bin;
-    uint32_t lo = key_of<T>(weight.reach(((float)step + 0.5f) / kPerOctave)) >> LOW, hi = key_of<T>(weight.below(((float)step - 0.5f) / kPerOctave)) >> LOW;
+    uint32_t lo = uniform(key_of<T>(weight.reach(((float)step + 0.5f) / kPerOctave)) >> LOW), hi = uniform(key_of<T>(weight.below(((float)step - 0.5f) / kPerOctave)) >> LOW);
     auto full_key = [&](uint32_t key) { return LOW && !(key >> 15) ? key << LOW | 0xFFFFu : key << LOW; };       // (keys of negative numbers are turned around)
     float from, to;
     auto between = [&] {
@@ -555,22 +561,22 @@ __device__ __forceinline__ bool border(const R &row, SampleShared &S, const Weig
         to = logit_of(full_key(hi));
         if (to == kLargest<T>) to = INFINITY;
     };
-    auto in = [&](float l) { return l >= from && l <= to && Weights::step(weight.exponent(l)) == step; };
+    auto in = [&](float l) { return Weights::step(weight.exponent(l)) == step; };
     // (bf16: a step has few numbers in it, if not one)
     if (hi - lo < 64) {
         const uint32_t key = lo + (threadIdx.x & 63);
         const u64 some = __ballot(key <= hi && Weights::step(weight.exponent(logit_of(full_key(key)))) == step);
         if (some) {
-            hi = lo + 63 - __clzll((long long)some);
-            lo += __ffsll((long long)some) - 1;
+            hi = uniform(lo + 63 - __clzll((long long)some));
+            lo = uniform(lo + __ffsll((long long)some) - 1);
         }
     }
     between();
     uint32_t base = f.base_count;
     u64 base_mass = f.base_mass;
     // (as many as are likely, if they were not counted)
-    uint32_t n = f.count ? f.count : (uint32_t)likely(f.mass, step);
-    if (n <= (uint32_t)kList) n = collect<T>(row, S, in);
+    uint32_t n = uniform(f.count ? f.count : (uint32_t)likely(f.mass, step));
+    if (n <= (uint32_t)kList) n = collect<T>(row, S, from, to, in);
     const bool used = n > (uint32_t)kList;
     while (n > (uint32_t)kList) {
         if (lo == hi) {
@@ -579,9 +585,9 @@ __device__ __forceinline__ bool border(const R &row, SampleShared &S, const Weig
             u64 keep = k - base;
             if (w) keep = min(keep, (m - base_mass - 1) / w + 1);      // (m is more than base_mass)
             keep = max(keep, (u64)1);
-            const int last = descend(row, S, keep - 1, 0, row.V, [&](int, float l) { return (u64)(l >= from && l <= to ? 1 : 0); });
-            least = rank_of(full_key(lo), last);
-            inside = base_mass + keep * w;
+            const int last = descend(row, S, keep - 1, 0, row.V, [&](int, float l) { return both(l >= from, l <= to) ? 1u : 0u; });
+            least = uniform(rank_of(full_key(lo), last));
+            inside = uniform(base_mass + keep * w);
             return true;
         }
         const int shift = max(0, 32 - __clz(hi - lo) - 11);  // 2^11 steps of keys at most
@@ -589,7 +595,7 @@ __device__ __forceinline__ bool border(const R &row, SampleShared &S, const Weig
         clear_counters<N>(S, true);
         __syncthreads();
         row.all([&](int, float l) {
-            if (in(l)) {
+            if (both(l >= from, l <= to) && in(l)) {
                 const uint32_t key = key_of<T>(l) >> LOW;    // (between lo and hi, so less than 2^11 steps from it)
                 if (key < lo || key > hi) return;
                 atomicAdd(&S.count[(hi - key) >> shift], 1u);
@@ -606,7 +612,7 @@ __device__ __forceinline__ bool border(const R &row, SampleShared &S, const Weig
         lo = max(lo, hi - min(hi, (1u << shift) - 1));
         between();
         n = f.count;
-        if (n <= (uint32_t)kList) n = collect<T>(row, S, in);
+        if (n <= (uint32_t)kList) n = collect<T>(row, S, from, to, in);
     }
     const Listed<N> t(S, weight, min(n, (uint32_t)kList));
     if (t.there && t.first && base + t.ahead < k && base_mass + t.run < m) {
@@ -614,8 +620,8 @@ __device__ __forceinline__ bool border(const R &row, SampleShared &S, const Weig
         atomicAdd(&S.sum, t.mass);
     }
     __syncthreads();
-    least = S.least;
-    inside = base_mass + S.sum;
+    least = uniform(S.least);
+    inside = uniform(base_mass + S.sum);
     return used;
 }
 
@@ -628,10 +634,10 @@ __global__ __launch_bounds__(N, 4) void k_sample(SampleRows a) {
     row.x = reinterpret_cast<const T *>(a.logits) + (size_t)r * a.stride;
     row.V = a.V;
     row.keep();
-    const float temperature = a.temperature ? a.temperature[set] : a.temperature_all, p = a.top_p ? a.top_p[set] : a.top_p_all,
-                p_min = a.min_p ? a.min_p[set] : a.min_p_all, u = a.tokens ? a.u[r] : 0.f;
+    const float temperature = uniform(a.temperature ? a.temperature[set] : a.temperature_all), p = uniform(a.top_p ? a.top_p[set] : a.top_p_all),
+                p_min = uniform(a.min_p ? a.min_p[set] : a.min_p_all), u = uniform(a.tokens ? a.u[r] : 0.f);
     const bool greedy = !(temperature > 0.f);
-    int k = greedy ? 1 : a.top_k ? a.top_k[set] : a.top_k_all;
+    int k = greedy ? 1 : __builtin_amdgcn_readfirstlane(a.top_k ? a.top_k[set] : a.top_k_all);
     if (k <= 0 || k > a.V) k = a.V;
     clear_counters<N>(S, true);
     if (tid < kPerOctave) S.roots[tid] = exp2((double)tid / kPerOctave);
@@ -647,6 +653,7 @@ __global__ __launch_bounds__(N, 4) void k_sample(SampleRows a) {
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < N / 64; i++) top = fmaxf(top, S.top[i]);
+    top = uniform(top);
     float *out = a.probs ? a.probs + (size_t)r * a.V : nullptr;
     int32_t *token = a.tokens ? a.tokens + r : nullptr;
     struct __attribute__((packed, aligned(4))) Quad {
@@ -665,7 +672,7 @@ __global__ __launch_bounds__(N, 4) void k_sample(SampleRows a) {
     }
     const Weights weight{(double)top, fmax(1.4426950408889634 / (greedy ? 1.0 : (double)temperature), 1e-300), S.roots};
     Limits lim{(uint32_t)k, p, p < 1.f && k > 1, 1};
-    if (p_min > 0.f) lim.w_min = max((u64)ceil((double)fminf(p_min, 1.f) * (double)(1ull << 45)), (u64)1);
+    if (p_min > 0.f) lim.w_min = uniform(max((u64)ceil((double)fminf(p_min, 1.f) * (double)(1ull << 45)), (u64)1));
 
     // ---- few tokens at most
     const bool few = k <= kList * 3 / 4;
@@ -694,7 +701,7 @@ __global__ __launch_bounds__(N, 4) void k_sample(SampleRows a) {
         }
         if (!lim.by_mass && p_min > 0.f) cut = fmaxf(cut, weight.reach(-__builtin_amdgcn_logf(fminf(p_min, 1.f)) * 1.0001f + 0.001f));      // (log2)
         if (out) clear();
-        const uint32_t n = collect<T>(row, S, [&](float l) { return l >= cut; });
+        const uint32_t n = collect<T>(row, S, cut, INFINITY, [](float) { return true; });
         if (n <= (uint32_t)kList) return finish<N>(S, weight, lim, 0, n, out, u, token);
         clear_counters<N>(S, true);
         __syncthreads();
@@ -712,10 +719,10 @@ __global__ __launch_bounds__(N, 4) void k_sample(SampleRows a) {
             again.all([&](int, float l) {
                 const double x = weight.exponent(l);
                 const int i = Weights::step(x);
-                if (counted && i < kSteps) atomicAdd(&S.count[i], 1u);
-                if (lim.by_mass) {
-                    const u64 w = weight.at(x);
-                    if (i < kSteps) atomicAdd(&S.mass[i], w);
+                const u64 w = weight.at(x);
+                if (i < kSteps) {
+                    if (counted) atomicAdd(&S.count[i], 1u);
+                    atomicAdd(&S.mass[i], w);
                 }
             });
             __syncthreads();
@@ -723,18 +730,17 @@ __global__ __launch_bounds__(N, 4) void k_sample(SampleRows a) {
             stand = true;
             if (!sum)
 #pragma unroll
-                for (int i = 0; i < N / 64; i++) sum += S.part[i];
+                for (int i = 0; i < N / 64; i++) sum += uniform(S.part[i]);
         }
         const uint32_t first = pass ? ~0u : (uint32_t)k;
-        const u64 m = pass ? max(share_of(p, sum, true), (u64)1) : ~0ull;
+        const u64 m = pass ? uniform(max(share_of(p, sum, true), (u64)1)) : ~0ull;
         const Found f = find<N>(S, first, m);
         if (f.bin >= kSteps) continue;                       // (all tokens with a weight)
         // what stays may fit the list: all tokens down to the end of the step
         const float cut = weight.reach(((float)f.bin + 0.5f) / kPerOctave);
-        auto in = [&](float l) { return l >= cut; };
         const uint32_t about = counted ? f.base_count + f.count : f.about / 16;
         if (about <= (uint32_t)kList + kList / 8) {
-            const uint32_t n = collect<T>(again, S, in);
+            const uint32_t n = collect<T>(again, S, cut, INFINITY, [](float) { return true; });
             if (n <= (uint32_t)kList) {
                 if (out) clear();
                 __syncthreads();
@@ -748,21 +754,22 @@ __global__ __launch_bounds__(N, 4) void k_sample(SampleRows a) {
             __syncthreads();
         }
     }
-    if (!lim.by_mass) sum = 0;                               // (not known yet)
 
     // ---- all
     const float l_least = least ? logit_of((uint32_t)(least >> 32)) : -INFINITY;
     const float l_above = l_least == kLargest<T> ? INFINITY : l_least;   // (inf counts as that)
     const int v_last = (int)~(uint32_t)least;                // of the tokens with the least logit
-    auto stays = [&](int v, float l) { return l > l_above || (l >= l_least && v <= v_last); };
+    auto stays = [&](int v, float l) { return !both(!(l > l_above), !both(l >= l_least, v <= v_last)); };
+    const bool bounded = lim.w_min > 1;
     auto value = [&](int v, float l) -> u64 {
         const u64 w = weight(l);
-        return stays(v, l) && w >= lim.w_min ? w : 0;
+        if (bounded) return both(stays(v, l), w >= lim.w_min) ? w : 0;
+        return stays(v, l) ? w : 0;
     };
     const int range = R::range(a.V);
-    if (token || !sum || lim.w_min > 1) {
+    if (token || !sum || bounded) {
         u64 of_wave = 0;
-        if (least || lim.w_min > 1) again.all([&](int v, float l) { of_wave += value(v, l); });
+        if (least || bounded) again.all([&](int v, float l) { of_wave += value(v, l); });
         else again.all([&](int, float l) { of_wave += weight(l); });
         of_wave = wave_total(of_wave);
         __syncthreads();
@@ -770,7 +777,7 @@ __global__ __launch_bounds__(N, 4) void k_sample(SampleRows a) {
         __syncthreads();
         sum = 0;
 #pragma unroll
-        for (int i = 0; i < N / 64; i++) sum += S.part[i];
+        for (int i = 0; i < N / 64; i++) sum += uniform(S.part[i]);
     }
     if (out) {
         const double inv = 1.0 / ((double)sum * 0x1p-45);
@@ -795,9 +802,9 @@ __global__ __launch_bounds__(N, 4) void k_sample(SampleRows a) {
         });
     }
     if (token) {
-        u64 target = place_of(u, sum);
+        u64 target = uniform(place_of(u, sum));
         int w = 0;
-        for (; w < N / 64 - 1 && S.part[w] <= target; w++) target -= S.part[w];
+        for (; w < N / 64 - 1 && uniform(S.part[w]) <= target; w++) target -= uniform(S.part[w]);
         const int found = descend(again, S, target, min(w * range, a.V - 1), min(w * range + range, a.V), value);
         if (tid == 0) *token = found;
     }
