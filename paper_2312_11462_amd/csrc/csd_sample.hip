@@ -14,9 +14,7 @@
 //   a share      the weights of all tokens are added up in steps of 1/32 octave; the step that holds the border is ranked, or divided again by the bits of
 //                its logits until few tokens are left or all are equal.  What stays is then a list as above or, if there are too many, goes
 //   all          by the sum over the row, and the draw descends it: the wave's range that holds the border, a range of each wave in it, a tile.
-#include "csd_internal.h"
-
-typedef unsigned long long u64;
+#include "csd_lanes.h"
 
 static constexpr int kList = 256;                            // tokens that are ranked against one another at most
 static constexpr int kBins = 2048;                           // counters of a histogram
@@ -114,34 +112,6 @@ __device__ __forceinline__ u64 share_of(float a, u64 z, bool up) {
 
 // ---------------------------------------------------------------------------------------- lanes
 
-// what another lane of the wave has, by data-parallel moves; `old` where there is none
-template <int CTRL, int ROWS>
-__device__ __forceinline__ uint32_t moved(uint32_t old, uint32_t v) {
-    return (uint32_t)__builtin_amdgcn_update_dpp((int)old, (int)v, CTRL, ROWS, 0xF, false);
-}
-template <int CTRL, int ROWS>
-__device__ __forceinline__ u64 moved(u64 old, u64 v) {
-    return (u64)moved<CTRL, ROWS>((uint32_t)(old >> 32), (uint32_t)(v >> 32)) << 32 | moved<CTRL, ROWS>((uint32_t)old, (uint32_t)v);
-}
-// inclusive running sum over the wave: within sixteen lanes, then from row to row
-template <typename U>
-__device__ __forceinline__ U wave_scan(U v) {
-    v += moved<0x111, 0xF>((U)0, v);
-    v += moved<0x112, 0xF>((U)0, v);
-    v += moved<0x114, 0xF>((U)0, v);
-    v += moved<0x118, 0xF>((U)0, v);
-    v += moved<0x142, 0xA>((U)0, v);
-    v += moved<0x143, 0xC>((U)0, v);
-    return v;
-}
-__device__ __forceinline__ uint32_t from_lane(uint32_t v, int lane) { return (uint32_t)__builtin_amdgcn_readlane((int)v, lane); }
-__device__ __forceinline__ u64 from_lane(u64 v, int lane) { return (u64)from_lane((uint32_t)(v >> 32), lane) << 32 | from_lane((uint32_t)v, lane); }
-// (what all lanes have alike, said so: branches on it are the scalar unit's)
-__device__ __forceinline__ uint32_t uniform(uint32_t v) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)v); }
-__device__ __forceinline__ float uniform(float v) { return __uint_as_float(uniform(__float_as_uint(v))); }
-__device__ __forceinline__ u64 uniform(u64 v) { return (u64)uniform((uint32_t)(v >> 32)) << 32 | uniform((uint32_t)v); }
-template <typename U>
-__device__ __forceinline__ U wave_total(U v) { return from_lane(wave_scan(v), 63); }
 __device__ __forceinline__ float wave_largest(float v) {
     auto step = [&](float o) { v = fmaxf(v, o); };
 #define CSD_MOVED(CTRL, ROWS) __uint_as_float(moved<CTRL, ROWS>(__float_as_uint(v), __float_as_uint(v)))
