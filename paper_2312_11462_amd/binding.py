@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 import threading
 
 import torch
@@ -519,6 +520,7 @@ class Pages:
             raise ValueError(f"{name}: {count} contiguous elements are required")
 
     def _given(self, **tensors):
+        """Raises for what is wrong with a call's tensors (the methods look at them in one expression, and come here if it does not hold)."""
         if _current_device() != self._dev:
             raise ValueError("the arrays are on another device than the current one")
         for name, t in tensors.items():
@@ -526,23 +528,26 @@ class Pages:
 
     def plan(self, cache_len, new_rows, rows):
         """csd_pages_plan: (row_start [sequences + 1], sequence [rows], position [rows], slot [rows] int64, served [sequences]); rows: the most rows of the step."""
-        self._given(cache_len=cache_len, new_rows=new_rows)
-        n = self.n_sequences
-        row_start = torch.empty(n + 1, dtype=torch.int32, device=self._device)
-        served = torch.empty(n, dtype=torch.int32, device=self._device)
-        sequence = torch.empty(rows, dtype=torch.int32, device=self._device)
-        position = torch.empty(rows, dtype=torch.int32, device=self._device)
+        n, dev = self.n_sequences, self._dev
+        if not (dev == cache_len.get_device() == new_rows.get_device() and torch.int32 is cache_len.dtype is new_rows.dtype and cache_len.is_contiguous()
+                and new_rows.is_contiguous() and n == cache_len.numel() == new_rows.numel() and _current_device() == dev):
+            self._given(cache_len=cache_len, new_rows=new_rows)
+        # (one tensor for all that is int32: a tensor made is a microsecond, as much as a step's kernel spends on its lengths)
+        row_start, sequence, position, served = torch.empty(2 * (n + rows) + 1, dtype=torch.int32, device=self._device).split((n + 1, rows, rows, n))
         slot = torch.empty(rows, dtype=torch.int64, device=self._device)
         rc = self._lib.csd_pages_plan(self._ref, cache_len.data_ptr(), new_rows.data_ptr(), rows, row_start.data_ptr(), sequence.data_ptr(),
-                                      position.data_ptr(), slot.data_ptr(), served.data_ptr(), _raw_stream(self._dev))
+                                      position.data_ptr(), slot.data_ptr(), served.data_ptr(), _raw_stream(dev))
         if rc:
             _chk(rc, "csd_pages_plan")
         return row_start, sequence, position, slot, served
 
     def release(self, keep_len):
         """csd_pages_release: sequence b keeps its first keep_len[b] rows (0: it has ended; negative: it is left alone)."""
-        self._given(keep_len=keep_len)
-        rc = self._lib.csd_pages_release(self._ref, keep_len.data_ptr(), _raw_stream(self._dev))
+        dev = self._dev
+        if not (dev == keep_len.get_device() and keep_len.dtype is torch.int32 and keep_len.is_contiguous() and keep_len.numel() == self.n_sequences
+                and _current_device() == dev):
+            self._given(keep_len=keep_len)
+        rc = self._lib.csd_pages_release(self._ref, keep_len.data_ptr(), _raw_stream(dev))
         if rc:
             _chk(rc, "csd_pages_release")
 
@@ -554,18 +559,51 @@ class Pages:
             _chk(rc, "csd_pages_share")
 
 
+# csd_filter as bytes: four addresses, the numbers beside them, the rows that share an entry
+_FILTER = struct.Struct("@4PfiffI")
+
+
 def _filter(logits, temperature, top_k, top_p, min_p):
-    """(csd_filter, rows, elements between rows) of a call; raises for what is wrong with its tensors."""
-    dev, shape, stride = logits.get_device(), logits.shape, logits.stride()
+    """(csd_filter as a buffer, rows, elements between rows) of a call; raises for what is wrong with its tensors."""
+    dev, shape = logits.get_device(), logits.shape
     if dev < 0:
         raise ValueError("logits: a device tensor is required")
     if _current_device() != dev:
         raise ValueError("logits: on another device than the current one")
     if logits.dtype not in _ROWS:
         raise TypeError(f"logits are float32 or bfloat16, got {logits.dtype}")
-    V = shape[-1]
-    rows = 1
-    step = V                                              # rows are the leading dimensions, which have to be one run of equal steps
+    if len(shape) == 2 and logits.stride(1) == 1:
+        rows, V = shape
+        step = logits.stride(0) if rows > 1 else V
+    else:
+        rows, step = _rows_of(shape, logits.stride())
+    addresses, numbers, sets = [None] * 4, [1.0, 0, 1.0, 0.0], 0
+    for i, value in enumerate((temperature, top_k, top_p, min_p)):
+        if value is None:
+            continue
+        if isinstance(value, torch.Tensor):
+            n = value.numel()
+            if value.get_device() != dev:
+                raise ValueError(f"{_PARAMETERS[i]}: a tensor on the logits' device is required")
+            if value.dtype is not (torch.int32 if i == 1 else torch.float32):
+                raise TypeError(f"{_PARAMETERS[i]}: expected {torch.int32 if i == 1 else torch.float32}, got {value.dtype}")
+            if not value.is_contiguous() or (rows and (n == 0 or rows % n)) or sets not in (0, n):
+                raise ValueError(f"{_PARAMETERS[i]}: contiguous, one entry for each row or for each of the same number of consecutive rows, all parameters alike")
+            sets = n
+            addresses[i] = value.data_ptr()
+        else:
+            numbers[i] = value
+    buffer = C.create_string_buffer(_FILTER.size)
+    _FILTER.pack_into(buffer, 0, *(a or 0 for a in addresses), *numbers, rows // sets or 1 if sets else 1)
+    return buffer, rows, step
+
+
+_PARAMETERS = "temperature", "top_k", "top_p", "min_p"
+
+
+def _rows_of(shape, stride):
+    """(rows, elements between rows) of logits [..., V] whose leading dimensions are one run of equal steps."""
+    rows, step = 1, shape[-1]
     for size, by in zip(reversed(shape[:-1]), reversed(stride[:-1])):
         if size > 1:
             if rows == 1:
@@ -573,27 +611,9 @@ def _filter(logits, temperature, top_k, top_p, min_p):
             elif by != step * rows:
                 raise ValueError("logits: rows at equal distances are required")
         rows *= size
-    if V > 1 and stride[-1] != 1:
+    if shape[-1] > 1 and stride[-1] != 1:
         raise ValueError("logits: contiguous rows are required")
-    f = Filter(None, None, None, None, 1.0, 0, 1.0, 0.0, 1)
-    sets = 0
-    for name, value, dtype in (("temperature", temperature, torch.float32), ("top_k", top_k, torch.int32), ("top_p", top_p, torch.float32),
-                               ("min_p", min_p, torch.float32)):
-        if isinstance(value, torch.Tensor):
-            if value.get_device() != dev:
-                raise ValueError(f"{name}: a tensor on the logits' device is required")
-            if value.dtype is not dtype:
-                raise TypeError(f"{name}: expected {dtype}, got {value.dtype}")
-            n = value.numel()
-            if not value.is_contiguous() or (rows and (n == 0 or rows % n)) or sets not in (0, n):
-                raise ValueError(f"{name}: contiguous, one entry for each row or for each of the same number of consecutive rows, all parameters alike")
-            sets = n
-            setattr(f, name, value.data_ptr())
-        elif value is not None:
-            setattr(f, name + "_all", value)
-    if sets:
-        f.rows_each = rows // sets or 1
-    return f, rows, step
+    return rows, step
 
 
 def sample(logits, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, probs=None, out=None):
@@ -601,14 +621,17 @@ def sample(logits, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, probs=None
     or tensors with an entry for every row or for every so many consecutive rows (a sequence's block); None: not set.  probs: a float32
     tensor [..., V] that takes the probabilities too."""
     f, rows, step = _filter(logits, temperature, top_k, top_p, min_p)
-    shape, V = logits.shape[:-1], logits.shape[-1]
+    shape, dev = logits.shape, logits.get_device()
+    if not (u.shape == shape[:-1] and u.dtype is torch.float32 and u.get_device() == dev and u.is_contiguous()):
+        _given("u", u, shape[:-1], torch.float32, logits)
     if out is None:
-        out = torch.empty(shape, dtype=torch.int32, device=logits.device)
-    for name, t, want, dtype in (("u", u, shape, torch.float32), ("out", out, shape, torch.int32), ("probs", probs, logits.shape, torch.float32)):
-        if t is not None:
-            _given(name, t, want, dtype, logits)
-    rc = lib().csd_sample(C.addressof(f), logits.data_ptr(), step, _ROWS[logits.dtype], rows, V, u.data_ptr(), out.data_ptr(),
-                          probs.data_ptr() if probs is not None else None, _raw_stream(logits.get_device()))
+        out = torch.empty(shape[:-1], dtype=torch.int32, device=logits.device)
+    else:
+        _given("out", out, shape[:-1], torch.int32, logits)
+    if probs is not None:
+        _given("probs", probs, shape, torch.float32, logits)
+    rc = lib().csd_sample(f, logits.data_ptr(), step, _ROWS[logits.dtype], rows, shape[-1], u.data_ptr(), out.data_ptr(),
+                          None if probs is None else probs.data_ptr(), _raw_stream(dev))
     if rc:
         _chk(rc, "csd_sample")
     return out
@@ -621,8 +644,7 @@ def filter_probs(logits, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, out=Non
         out = torch.empty(logits.shape, dtype=torch.float32, device=logits.device)
     else:
         _given("out", out, logits.shape, torch.float32, logits)
-    rc = lib().csd_filter_probs(C.addressof(f), logits.data_ptr(), step, _ROWS[logits.dtype], rows, logits.shape[-1], out.data_ptr(),
-                                _raw_stream(logits.get_device()))
+    rc = lib().csd_filter_probs(f, logits.data_ptr(), step, _ROWS[logits.dtype], rows, logits.shape[-1], out.data_ptr(), _raw_stream(logits.get_device()))
     if rc:
         _chk(rc, "csd_filter_probs")
     return out

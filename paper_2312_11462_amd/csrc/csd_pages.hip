@@ -8,7 +8,7 @@
 
 static constexpr int kRowsHere = 4096;                       // rows that the planning workgroup writes itself
 static constexpr int kFresh = 2048;                          // pages of a plan that are kept in LDS for the rows
-static constexpr int kAtOnce = 4;                            // pages of a release that a thread has on their way
+static constexpr int kAtOnce = 8;                            // pages that a thread has on their way (4112 pages taken and given back: by four 25 us)
 
 template <int N>
 struct PagesShared {
@@ -59,6 +59,15 @@ __device__ __forceinline__ int first_above(const P *run, int n, int x) {
         else lo = mid + 1;
     }
     return lo;
+}
+
+// The same for N numbers, a power of two, in as many steps whatever they are, so that several searches go side by side.
+template <int N>
+__device__ __forceinline__ int first_above(const int32_t (&run)[N], int x) {
+    int at = 0;
+#pragma unroll
+    for (int s = N / 2; s > 0; s >>= 1) at += run[at + s - 1] <= x ? s : 0;
+    return at;
 }
 
 struct PlanRows {
@@ -124,12 +133,22 @@ __global__ __launch_bounds__(N) void k_pages_plan(csd_pages p, PlanRows r, int s
         }
         const int count = (int)count64;
         __syncthreads();
-        for (int i = tid; i < count; i += N) {
-            const int page = p.free_pages[n_free - 1 - taken - i];           // (on its way while the sequence is looked for)
-            const int j = first_above(S.run, N, i), at = S.from[j] + i - (j ? S.run[j - 1] : 0);
-            p.table[(size_t)(b0 + j) * p.table_stride + at] = page;
-            if ((unsigned)page < (unsigned)p.n_pages) p.users[page] = 1;
-            if (i < kFresh) S.fresh[i] = page;
+        for (int i0 = tid; i0 < count; i0 += kAtOnce * N) {
+            int page[kAtOnce], j[kAtOnce];
+#pragma unroll
+            for (int u = 0; u < kAtOnce; u++)
+                if (i0 + u * N < count) page[u] = p.free_pages[n_free - 1 - taken - i0 - u * N];
+#pragma unroll
+            for (int u = 0; u < kAtOnce; u++)
+                if (i0 + u * N < count) j[u] = first_above(S.run, i0 + u * N);
+#pragma unroll
+            for (int u = 0; u < kAtOnce; u++) {
+                const int i = i0 + u * N;
+                if (i >= count) break;
+                p.table[(size_t)(b0 + j[u]) * p.table_stride + S.from[j[u]] + i - (j[u] ? S.run[j[u] - 1] : 0)] = page[u];
+                if ((unsigned)page[u] < (unsigned)p.n_pages) p.users[page[u]] = 1;
+                if (i < kFresh) S.fresh[i] = page[u];
+            }
         }
         taken += count;
         rows += (int)rows64;
@@ -199,7 +218,7 @@ struct Release {
     }
     // where item i is named
     __device__ __forceinline__ int32_t *entry(int b0, int i) const {
-        const int j = first_above(S.run, N, i), at = S.from[j] + i - (j ? S.run[j - 1] : 0);
+        const int j = first_above(S.run, i), at = S.from[j] + i - (j ? S.run[j - 1] : 0);
         return p.table + (size_t)(b0 + j) * p.table_stride + at;
     }
     __device__ __forceinline__ int page_of(const int32_t *entry) const {
