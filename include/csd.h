@@ -474,7 +474,7 @@ typedef struct csd_filter {
 } csd_filter;
 
 /* logits: [rows][V] of dtype CSD_DTYPE_FP32 or CSD_DTYPE_BF16, `stride` elements (>= V) from one row to the next, any alignment that the type has.  u[rows], tokens[rows];
- * probs: [rows][V] fp32, or NULL.  CSD_ESHAPE: V above 2^18, more than 2^22 rows. */
+ * probs: [rows][V] fp32, not overlapping the logits, or NULL.  CSD_ESHAPE: V above 2^18, more than 2^21 rows. */
 int32_t csd_sample(const csd_filter *filter, const void *logits, int64_t stride, int32_t dtype, int32_t rows, int32_t V, const float *u,
                    int32_t *tokens, float *probs, void *stream);
 /* The probabilities alone. */

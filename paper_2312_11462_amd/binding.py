@@ -625,7 +625,7 @@ def sample(logits, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, probs=None
     if not (u.shape == shape[:-1] and u.dtype is torch.float32 and u.get_device() == dev and u.is_contiguous()):
         _given("u", u, shape[:-1], torch.float32, logits)
     if out is None:
-        out = torch.empty(shape[:-1], dtype=torch.int32, device=logits.device)
+        out = torch.empty_like(u, dtype=torch.int32)
     else:
         _given("out", out, shape[:-1], torch.int32, logits)
     if probs is not None:
@@ -641,7 +641,7 @@ def filter_probs(logits, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, out=Non
     """csd_filter_probs: the probabilities [..., V] float32 of the draws that `sample` makes with these parameters, as `accept` and `tree_accept` take them."""
     f, rows, step = _filter(logits, temperature, top_k, top_p, min_p)
     if out is None:
-        out = torch.empty(logits.shape, dtype=torch.float32, device=logits.device)
+        out = torch.empty_like(logits, dtype=torch.float32, memory_format=torch.contiguous_format)
     else:
         _given("out", out, logits.shape, torch.float32, logits)
     rc = lib().csd_filter_probs(f, logits.data_ptr(), step, _ROWS[logits.dtype], rows, logits.shape[-1], out.data_ptr(), _raw_stream(logits.get_device()))

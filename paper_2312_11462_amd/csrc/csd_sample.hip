@@ -787,13 +787,17 @@ static void sample_launch_as(const SampleRows &a, int rows, hipStream_t st) {
     hipLaunchKernelGGL((k_sample<T, N, NV, TINY>), dim3(rows), dim3(N), 0, st, a);
 }
 
-// The row stays in registers where it fits them.
+// The row stays in registers where it fits them.  A workgroup of 1024 threads has a compute unit to itself, of 512 and 256 two and four share one: the more threads the sooner a
+// row is done, the more rows at once the less of the chip waits at a row's barriers.  us by 1024 threads and by 512, rows of 32000: 200 with top-k 14.2 and 16.3, 300 22.2 and 20.5,
+// 200 with top-p 35.5 and 40.6, 400 61.3 and 57.3, 500 67.4 and 59.1.  By 256 and by 512, short rows: one of 512 10.4 and 7.9, 64 of 4000 22.2 and 14.9, 300 of 2000 26.3 and
+// 17.4, 1000 of 512 23.4 and 25.9, 3000 of 2000 56 and 68 (1000 of 4000 35.9 and 30.9).
 template <typename T>
 static void sample_launch(const SampleRows &a, int rows, hipStream_t st) {
     constexpr int VE = 16 / sizeof(T);
     if (a.V < VE) sample_launch_as<T, 256, 1, true>(a, rows, st);
-    else if (a.V <= 256 * 4 * VE) sample_launch_as<T, 256, 4>(a, rows, st);
-    else if (a.V <= 512 * 16 * VE && rows >= 512) sample_launch_as<T, 512, 16>(a, rows, st);
+    else if (a.V <= 256 * 4 * VE && rows > 512) sample_launch_as<T, 256, 4>(a, rows, st);
+    else if (a.V <= 256 * 4 * VE) sample_launch_as<T, 512, 8>(a, rows, st);
+    else if (a.V <= 512 * 16 * VE && rows > 256) sample_launch_as<T, 512, 16>(a, rows, st);
     else if (a.V <= 1024 * 8 * VE) sample_launch_as<T, 1024, 8>(a, rows, st);
     else if (a.V <= 1024 * 16 * VE) sample_launch_as<T, 1024, 16>(a, rows, st);
     else sample_launch_as<T, 1024, 0>(a, rows, st);
@@ -807,10 +811,14 @@ static int32_t sample_enqueue(const csd_filter *f, const void *logits, int64_t s
     if (!f->temperature && !(f->temperature_all >= 0.f)) return CSD_EINVAL;
     if (!f->top_p && !(f->top_p_all >= 0.f)) return CSD_EINVAL;
     if (!f->min_p && !(f->min_p_all >= 0.f && f->min_p_all <= 1.f)) return CSD_EINVAL;
-    if (V > (1 << 18) || rows > (1 << 22)) return CSD_ESHAPE;
+    if (V > (1 << 18) || rows > (1 << 21)) return CSD_ESHAPE;       // (work items of a launch are counted in 32 bits)
     if (rows == 0) return CSD_OK;
     if (!logits) return CSD_ENULL;
-    if ((uintptr_t)logits % (dtype == CSD_DTYPE_FP32 ? 4 : 2) || (uintptr_t)probs % 4) return CSD_EINVAL;
+    const size_t size = dtype == CSD_DTYPE_FP32 ? 4 : 2;
+    if ((uintptr_t)logits % size || ((uintptr_t)probs | (uintptr_t)u | (uintptr_t)tokens) % 4) return CSD_EINVAL;
+    // rows are read again behind the first probabilities
+    const char *from = (const char *)logits, *to = from + ((size_t)(rows - 1) * stride + V) * size;
+    if (probs && (const char *)probs < to && from < (const char *)(probs + (size_t)rows * V)) return CSD_EINVAL;
     const SampleRows a{logits, (long long)stride, V, f->rows_each, u, tokens, probs, f->temperature, f->top_p, f->min_p, f->top_k,
                        f->temperature_all, f->top_p_all, f->min_p_all, f->top_k_all};
     if (dtype == CSD_DTYPE_FP32) sample_launch<float>(a, rows, (hipStream_t)stream);

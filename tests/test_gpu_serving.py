@@ -103,7 +103,7 @@ def test_large_vocabularies(V, dtype, kw):
 
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
-@pytest.mark.parametrize("rows,V", [(300, 700), (600, 2003), (40, 32000)])
+@pytest.mark.parametrize("rows,V", [(300, 700), (600, 2003), (300, 9001), (40, 32000)])
 def test_every_row_has_its_own_settings(rows, V, dtype):
     g = torch.Generator().manual_seed(rows)
     t = torch.rand(rows, generator=g) * 1.5

@@ -123,13 +123,16 @@ def test_draws_refuse_what_they_cannot_do(L):
         assert L.csd_filter_probs(C.addressof(f), 256, 100, 0, 2, 100, 256, None) == code, change
     f = Filter(None, None, None, None, 1.0, 0, 1.0, 0.0, 1)
     ref = C.addressof(f)
-    good = dict(f=ref, x=256, stride=100, dtype=1, rows=2, V=100, probs=256)
+    good = dict(f=ref, x=256, stride=100, dtype=1, rows=2, V=100, probs=1024)
     for change, code in [(dict(f=None), ENULL), (dict(x=None), ENULL), (dict(x=257), EINVAL), (dict(x=258, dtype=0), EINVAL), (dict(stride=99), EINVAL),
                          (dict(dtype=2), EINVAL), (dict(dtype=-1), EINVAL), (dict(rows=-1), EINVAL), (dict(V=0), EINVAL), (dict(V=(1 << 18) + 1, stride=1 << 19), ESHAPE),
-                         (dict(rows=(1 << 22) + 1), ESHAPE), (dict(probs=258), EINVAL)]:
+                         (dict(rows=(1 << 21) + 1), ESHAPE), (dict(probs=1026), EINVAL),
+                         (dict(probs=256), EINVAL), (dict(probs=652), EINVAL), (dict(x=1824 - 4), EINVAL)]:
         a = dict(good, **change)
         assert L.csd_filter_probs(a["f"], a["x"], a["stride"], a["dtype"], a["rows"], a["V"], a["probs"], None) == code, change
         assert L.csd_sample(a["f"], a["x"], a["stride"], a["dtype"], a["rows"], a["V"], 256, 256, a["probs"], None) == code, change
+    assert L.csd_sample(ref, 256, 100, 1, 2, 100, 1026, 256, None, None) == EINVAL
+    assert L.csd_sample(ref, 256, 100, 1, 2, 100, 1024, 258, None, None) == EINVAL
     assert L.csd_sample(ref, 256, 100, 1, 2, 100, None, 256, None, None) == ENULL
     assert L.csd_sample(ref, 256, 100, 1, 2, 100, 256, None, None, None) == ENULL
     assert L.csd_filter_probs(ref, 256, 100, 1, 2, 100, None, None) == ENULL
