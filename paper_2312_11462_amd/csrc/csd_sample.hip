@@ -32,6 +32,9 @@ struct SampleRows {
     const int32_t *top_k;
     float temperature_all, top_p_all, min_p_all;
     int32_t top_k_all;
+    // Probabilities of 16 MiB and more are stored past the caches (656 rows of 50001 48 us, through them 54; 136 of 32128 34.6 and 38); what a review reads
+    // next are fewer.
+    bool past;
 };
 
 // ---------------------------------------------------------------------------------------- numbers
@@ -595,6 +598,13 @@ __device__ __forceinline__ bool border(const R &row, SampleShared &S, const Weig
     return used;
 }
 
+// Four probabilities at any place; `past`: past the caches.
+__device__ __forceinline__ void store_quad(float *to, f32x4 v, bool past) {
+    typedef f32x4 __attribute__((aligned(4))) quad;
+    if (past) __builtin_nontemporal_store(v, reinterpret_cast<quad *>(to));
+    else *reinterpret_cast<quad *>(to) = v;
+}
+
 template <typename T, int N, int NV, bool TINY>
 __global__ __launch_bounds__(N, 4) void k_sample(SampleRows a) {
     __shared__ __align__(16) SampleShared S;
@@ -626,12 +636,9 @@ __global__ __launch_bounds__(N, 4) void k_sample(SampleRows a) {
     top = uniform(top);
     float *out = a.probs ? a.probs + (size_t)r * a.V : nullptr;
     int32_t *token = a.tokens ? a.tokens + r : nullptr;
-    struct __attribute__((packed, aligned(4))) Quad {
-        f32x4 v;
-    };
     auto clear = [&] {
         for (int i = 4 * tid; i < a.V; i += 4 * N)
-            if (i + 4 <= a.V) reinterpret_cast<Quad *>(out + i)->v = f32x4{0.f, 0.f, 0.f, 0.f};
+            if (i + 4 <= a.V) store_quad(out + i, f32x4{0.f, 0.f, 0.f, 0.f}, a.past);
             else
                 for (int e = i; e < a.V; e++) out[e] = 0.f;
     };
@@ -764,7 +771,7 @@ __global__ __launch_bounds__(N, 4) void k_sample(SampleRows a) {
             }
 #pragma unroll
             for (int e = 0; e < R::VE; e += 4)
-                if (at + e + 4 <= a.V) reinterpret_cast<Quad *>(out + at + e)->v = f32x4{y[e], y[e + 1], y[e + 2], y[e + 3]};
+                if (at + e + 4 <= a.V) store_quad(out + at + e, f32x4{y[e], y[e + 1], y[e + 2], y[e + 3]}, a.past);
                 else
 #pragma unroll
                     for (int i = 0; i < 3; i++)
@@ -820,7 +827,7 @@ static int32_t sample_enqueue(const csd_filter *f, const void *logits, int64_t s
     const char *from = (const char *)logits, *to = from + ((size_t)(rows - 1) * stride + V) * size;
     if (probs && (const char *)probs < to && from < (const char *)(probs + (size_t)rows * V)) return CSD_EINVAL;
     const SampleRows a{logits, (long long)stride, V, f->rows_each, u, tokens, probs, f->temperature, f->top_p, f->min_p, f->top_k,
-                       f->temperature_all, f->top_p_all, f->min_p_all, f->top_k_all};
+                       f->temperature_all, f->top_p_all, f->min_p_all, f->top_k_all, (long long)rows * V >= 1 << 22};
     if (dtype == CSD_DTYPE_FP32) sample_launch<float>(a, rows, (hipStream_t)stream);
     else sample_launch<bf16_t>(a, rows, (hipStream_t)stream);
     CSD_LAUNCH_CHECK();
