@@ -14,6 +14,7 @@
 //   a share      the weights of all tokens are added up in steps of 1/32 octave; the step that holds the border is ranked, or divided again by the bits of
 //                its logits until few tokens are left or all are equal.  What stays is then a list as above or, if there are too many, goes
 //   all          by the sum over the row, and the draw descends it: the wave's range that holds the border, a range of each wave in it, a tile.
+#include "csd_epilogue.h"
 #include "csd_lanes.h"
 
 static constexpr int kList = 256;                            // tokens that are ranked against one another at most
@@ -598,11 +599,10 @@ __device__ __forceinline__ bool border(const R &row, SampleShared &S, const Weig
     return used;
 }
 
-// Four probabilities at any place; `past`: past the caches.
-__device__ __forceinline__ void store_quad(float *to, f32x4 v, bool past) {
-    typedef f32x4 __attribute__((aligned(4))) quad;
-    if (past) __builtin_nontemporal_store(v, reinterpret_cast<quad *>(to));
-    else *reinterpret_cast<quad *>(to) = v;
+// Four probabilities of a row from token v on; `past`: past the caches.
+__device__ __forceinline__ void store_quad(__amdgpu_buffer_rsrc_t row, int v, f32x4 p, bool past) {
+    if (past) __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, p), row, 4 * v, 0, 2);      // (2: not to be kept)
+    else __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, p), row, 4 * v, 0, 0);
 }
 
 template <typename T, int N, int NV, bool TINY>
@@ -635,10 +635,11 @@ __global__ __launch_bounds__(N, 4) void k_sample(SampleRows a) {
     for (int i = 0; i < N / 64; i++) top = fmaxf(top, S.top[i]);
     top = uniform(top);
     float *out = a.probs ? a.probs + (size_t)r * a.V : nullptr;
+    const __amdgpu_buffer_rsrc_t out_row = ch_rsrc(out, (size_t)a.V * 4);
     int32_t *token = a.tokens ? a.tokens + r : nullptr;
     auto clear = [&] {
         for (int i = 4 * tid; i < a.V; i += 4 * N)
-            if (i + 4 <= a.V) store_quad(out + i, f32x4{0.f, 0.f, 0.f, 0.f}, a.past);
+            if (i + 4 <= a.V) store_quad(out_row, i, f32x4{0.f, 0.f, 0.f, 0.f}, a.past);
             else
                 for (int e = i; e < a.V; e++) out[e] = 0.f;
     };
@@ -771,7 +772,7 @@ __global__ __launch_bounds__(N, 4) void k_sample(SampleRows a) {
             }
 #pragma unroll
             for (int e = 0; e < R::VE; e += 4)
-                if (at + e + 4 <= a.V) store_quad(out + at + e, f32x4{y[e], y[e + 1], y[e + 2], y[e + 3]}, a.past);
+                if (at + e + 4 <= a.V) store_quad(out_row, at + e, f32x4{y[e], y[e + 1], y[e + 2], y[e + 3]}, a.past);
                 else
 #pragma unroll
                     for (int i = 0; i < 3; i++)

@@ -95,6 +95,14 @@ def test_small_vocabularies(V, dtype, kw):
     run_rows(logits(5, V, dtype, V), **kw)
 
 
+@pytest.mark.parametrize("rows", [3, 600])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_vocabularies_of_a_few_pieces(rows, dtype):
+    for V in (4, 5, 6, 7, 8, 9, 10, 13, 15, 16, 17, 31, 255, 256, 257, 511, 513, 1023, 1025, 4096, 4097, 8191, 8193):
+        for kw in (dict(), dict(top_k=5, top_p=0.9)):
+            run_rows(logits(rows, V, dtype, V, likely=4)[:3 if V > 600 else rows], **kw)
+
+
 @pytest.mark.parametrize("kw", [SETTINGS[i] for i in (0, 1, 4, 5, 8)], ids=str)
 @pytest.mark.parametrize("V,dtype", [(32000, torch.float32), (32128, torch.bfloat16), (50001, torch.float32), (65537, torch.bfloat16), (131072, torch.float32),
                                      (131072, torch.bfloat16), (1 << 18, torch.float32), (1 << 18, torch.bfloat16)])
@@ -463,15 +471,18 @@ def test_cross_attention_of_blocks_and_chunks(rows, cache, d, length, new):
 
 
 @pytest.mark.parametrize("cache,d", [("bf16", 64), ("fp8", 128)])
-def test_cross_attention_of_prompts_that_fill_the_chip(cache, d):
-    """More items than are shared out: a workgroup for each; one encoder has no row, another one row."""
-    length, new = [90, 0, 1, 200, 65, 130], [300, 257, 400, 260, 300, 290]
-    c = States(cache, "bf16", length, new, kv_heads=96, group=2, d=d, page=16, seed=d)
-    q = c.random_rows(c.total, heads=192)
+@pytest.mark.parametrize("many", [False, True])
+def test_cross_attention_of_prompts_that_fill_the_chip(cache, d, many):
+    """More items than are shared out: a workgroup for each; some encoders have no row, one row, or as many as another.  many: more sequences than a wave has lanes."""
+    if many:
+        length, new, kv_heads = [(37 * b) % 150 for b in range(70)], [400 - b % 7 for b in range(70)], 4
+    else:
+        length, new, kv_heads = [90, 0, 1, 200, 65, 200], [300, 257, 400, 260, 300, 290], 96
+    c = States(cache, "bf16", length, new, kv_heads=kv_heads, group=2, d=d, page=16, seed=d)
+    q = c.random_rows(c.total, heads=2 * kv_heads)
     out = c.cross(q, d ** -0.5, max(new))
-    some = np.array([0, 299, 300, 556, 557, 956, 957, 1216, 1500, c.total - 1])
     k, v = c.values(c.k, c.ks)[0][:, :2], c.values(c.v, c.vs)[0][:, :2]
-    for r in some:                                           # (the first two key-value heads and the rows at the sequences' ends)
+    for r in np.unique(np.concatenate([c.start[:-1], c.start[1:] - 1, c.start[:-1] + 256])):         # (the first two key-value heads, rows at the ends of sequences and row tiles)
         b = int(np.searchsorted(c.start, r, side="right")) - 1
         one = q[r:r + 1, :4].double().cpu().numpy()
         want = O.cross_attention(k, v, c.table[b:b + 1], [0, 1], [length[b]], one, d ** -0.5)
