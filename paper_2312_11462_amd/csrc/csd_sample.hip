@@ -428,6 +428,36 @@ __device__ __forceinline__ uint32_t collect(const R &row, SampleShared &S, float
     return uniform(S.n_list);
 }
 
+// f(token, logit) for the tokens of the waves' ranges for which stays(first token of the piece, place in it, logit) holds, 64 at a time: a weight takes two to three times what the look and a queue in LDS
+// take, and of a vocabulary with a border few tokens stay (256 rows of 131072 in bf16, top-p: the sum 28.0 us without).  The queues lie where the counters were.
+template <typename R, typename S_, typename F>
+__device__ __forceinline__ void gather(const R &row, SampleShared &S, S_ stays, F f) {
+    static_assert(sizeof(S.mass) >= R::W * 128 * sizeof(u64), "");
+    const int lane = threadIdx.x & 63, wave = R::wave(), c = R::range(row.V);
+    u64 *queue = S.mass + wave * 128;                        // a ring: from `head` on, `n` tokens
+    int head = 0, n = 0;
+    auto one = [&](u64 t) { f((int)(uint32_t)(t >> 32), __uint_as_float((uint32_t)t)); };
+    row.pieces(min(wave * c, row.V), min(wave * c + c, row.V), [&](int at, const u32x4 &r) {
+#pragma unroll
+        for (int e = 0; e < R::VE; e++) {
+            const float l = R::get(r, e);
+            const bool in = stays(at, e, l);
+            const u64 mask = __builtin_amdgcn_ballot_w64(in);
+            if (in) queue[(head + n + __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0))) & 127] = (u64)(uint32_t)(at + e) << 32 | __float_as_uint(l);
+            n += __popcll(mask);
+            if (n >= 64) {
+                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+                one(queue[(head + lane) & 127]);
+                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+                head = (head + 64) & 127;
+                n -= 64;
+            }
+        }
+    });
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    if (lane < n) one(queue[(head + lane) & 127]);
+}
+
 // A token of the list, by N / kList neighbouring lanes: its weight (which goes to the list), and how many tokens and how much weight rank ahead of it.
 template <int N>
 struct Listed {
@@ -535,7 +565,8 @@ __device__ __forceinline__ bool border(const R &row, SampleShared &S, const Weig
         to = logit_of(full_key(hi));
         if (to == kLargest<T>) to = INFINITY;
     };
-    auto in = [&](float l) { return Weights::step(weight.exponent(l)) == step; };
+    bool all_in = false;                                     // all numbers between them are the step's
+    auto in = [&](float l) { return all_in || Weights::step(weight.exponent(l)) == step; };
     // (bf16: a step has few numbers in it, if not one)
     if (hi - lo < 64) {
         const uint32_t key = lo + (threadIdx.x & 63);
@@ -543,6 +574,7 @@ __device__ __forceinline__ bool border(const R &row, SampleShared &S, const Weig
         if (some) {
             hi = uniform(lo + 63 - __clzll((long long)some));
             lo = uniform(lo + __ffsll((long long)some) - 1);
+            all_in = true;
         }
     }
     between();
@@ -552,6 +584,48 @@ __device__ __forceinline__ bool border(const R &row, SampleShared &S, const Weig
     uint32_t n = uniform(f.count ? f.count : (uint32_t)likely(f.mass, step));
     if (n <= (uint32_t)kList) n = collect<T>(row, S, from, to, in);
     const bool used = n > (uint32_t)kList;
+    if (used && hi - lo < 3 && to < INFINITY) {
+        // Many tokens of three numbers at most (bf16, mostly): how many each wave has of each is known after one pass, and so where the border lies among equal ones
+        // (256 rows of 131072 in bf16, top-p: 25 us by the keys as below).
+        float number[3];
+        uint32_t have[3] = {0, 0, 0};
+#pragma unroll
+        for (int i = 0; i < 3; i++) number[i] = uniform(hi - lo >= (uint32_t)i ? logit_of(full_key(hi - i)) : NAN);
+        row.all_pieces([&](int, const u32x4 &r) {
+#pragma unroll
+            for (int e = 0; e < R::VE; e++)
+#pragma unroll
+                for (int i = 0; i < 3; i++) have[i] += __popcll(__builtin_amdgcn_ballot_w64(R::get(r, e) == number[i]));
+        });
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < 3; i++)
+            if ((threadIdx.x & 63) == 0) S.count[i * R::W + R::wave()] = have[i];
+        __syncthreads();
+#pragma unroll 1
+        for (int i = 0; i < 3 && hi - lo >= (uint32_t)i; i++) {
+            const float l = logit_of(full_key(hi - i));
+            const u64 w = weight(l);
+            uint32_t all = 0;
+            for (int x = 0; x < R::W; x++) all += uniform(S.count[i * R::W + x]);
+            if (base + all < k && base_mass + all * w < m) {
+                base += all;
+                base_mass += all * w;
+                continue;
+            }
+            u64 keep = k - base;
+            if (w) keep = min(keep, (m - base_mass - 1) / w + 1);      // (m is more than base_mass)
+            keep = uniform(max(keep, (u64)1));
+            uint32_t before = 0;
+            int x = 0;
+            for (; x < R::W - 1 && before + uniform(S.count[i * R::W + x]) < keep; x++) before += uniform(S.count[i * R::W + x]);
+            const int c = R::range(row.V);
+            const int last = descend(row, S, keep - 1 - before, min(x * c, row.V - 1), min(x * c + c, row.V), [&](int, float v) { return v == l ? 1u : 0u; });
+            least = uniform(rank_of(full_key(hi - i), last));
+            inside = uniform(base_mass + keep * w);
+            return true;
+        }
+    }
     while (n > (uint32_t)kList) {
         if (lo == hi) {
             // all equal: the first of them by token
@@ -573,10 +647,14 @@ __device__ __forceinline__ bool border(const R &row, SampleShared &S, const Weig
                 const uint32_t key = key_of<T>(l) >> LOW;    // (between lo and hi, so less than 2^11 steps from it)
                 if (key < lo || key > hi) return;
                 atomicAdd(&S.count[(hi - key) >> shift], 1u);
-                atomicAdd(&S.mass[(hi - key) >> shift], weight(l));
+                if (shift) atomicAdd(&S.mass[(hi - key) >> shift], weight(l));
             }
         });
         __syncthreads();
+        if (shift == 0) {                                    // (a number each: its tokens weigh alike)
+            for (uint32_t i = threadIdx.x; i <= hi - lo; i += N) S.mass[i] = S.count[i] ? S.count[i] * weight(logit_of(full_key(hi - i))) : 0;
+            __syncthreads();
+        }
         sum_counters<N>(S);
         f = find<N>(S, k - base, m - base_mass);
         if (f.bin == kBins) break;                           // (the logits changed while they were read)
@@ -690,6 +768,7 @@ __global__ __launch_bounds__(N, 4) void k_sample(SampleRows a) {
     u64 least = 0, sum = 0;
     const bool counted = k < a.V;
     bool stand = false;                                      // the counters hold the histogram
+    uint32_t likely_stay = (uint32_t)a.V;
 #pragma unroll 1
     for (int pass = 0; pass < 2; pass++) {
         if (pass ? !lim.by_mass : !counted) continue;
@@ -717,6 +796,7 @@ __global__ __launch_bounds__(N, 4) void k_sample(SampleRows a) {
         // what stays may fit the list: all tokens down to the end of the step
         const float cut = weight.reach(((float)f.bin + 0.5f) / kPerOctave);
         const uint32_t about = counted ? f.base_count + f.count : f.about / 16;
+        likely_stay = about;
         if (about <= (uint32_t)kList + kList / 8) {
             const uint32_t n = collect<T>(again, S, cut, INFINITY, [](float) { return true; });
             if (n <= (uint32_t)kList) {
@@ -737,18 +817,29 @@ __global__ __launch_bounds__(N, 4) void k_sample(SampleRows a) {
     const float l_least = least ? logit_of((uint32_t)(least >> 32)) : -INFINITY;
     const float l_above = l_least == kLargest<T> ? INFINITY : l_least;   // (inf counts as that)
     const int v_last = (int)~(uint32_t)least;                // of the tokens with the least logit
-    auto stays = [&](int v, float l) { return !both(!(l > l_above), !both(l >= l_least, v <= v_last)); };
+    auto stays = [&](int at, int e, float l) { return !both(!(l > l_above), !both(l >= l_least, e <= v_last - at)); };
     const bool bounded = lim.w_min > 1;
     auto value = [&](int v, float l) -> u64 {
         const u64 w = weight(l);
-        if (bounded) return both(stays(v, l), w >= lim.w_min) ? w : 0;
-        return stays(v, l) ? w : 0;
+        if (bounded) return both(stays(v, 0, l), w >= lim.w_min) ? w : 0;
+        return stays(v, 0, l) ? w : 0;
     };
+    const bool seldom = least && likely_stay * 3 < (uint32_t)a.V;      // (one in three: as fast either way)
     const int range = R::range(a.V);
     if (token || !sum || bounded) {
         u64 of_wave = 0;
-        if (least || bounded) again.all([&](int v, float l) { of_wave += value(v, l); });
-        else again.all([&](int, float l) { of_wave += weight(l); });
+        auto weigh = [&](int, float l) {
+            const u64 w = weight(l);
+            of_wave += w >= lim.w_min ? w : 0;
+        };
+        if (seldom) {
+            __syncthreads();                                 // (the counters have been read)
+            gather(again, S, stays, weigh);
+        } else if (least || bounded) {
+            again.all([&](int v, float l) { of_wave += value(v, l); });
+        } else {
+            again.all([&](int, float l) { of_wave += weight(l); });
+        }
         of_wave = wave_total(of_wave);
         __syncthreads();
         if (lane == 0) S.part[wave] = of_wave;
@@ -757,18 +848,22 @@ __global__ __launch_bounds__(N, 4) void k_sample(SampleRows a) {
 #pragma unroll
         for (int i = 0; i < N / 64; i++) sum += uniform(S.part[i]);
     }
-    if (out) {
-        const double inv = 1.0 / ((double)sum * 0x1p-45);
+    const double inv = 1.0 / ((double)sum * 0x1p-45);
+    if (out && seldom) {
+        clear();
+        __syncthreads();                                     // (zeros before probabilities; and the counters have been read)
+        gather(again, S, stays, [&](int v, float l) {
+            const double w = weight.real(weight.exponent(l));
+            if (Weights::whole(w) >= lim.w_min) out[v] = (float)(w * inv);
+        });
+    } else if (out) {
         again.pieces(min(wave * range, a.V), min(wave * range + range, a.V), [&](int at, const u32x4 &raw) {
             float y[R::VE];
 #pragma unroll
             for (int e = 0; e < R::VE; e++) {
                 const float l = R::get(raw, e);
-                y[e] = 0.f;
-                if (stays(at + e, l)) {
-                    const double w = weight.real(weight.exponent(l));
-                    if (Weights::whole(w) >= lim.w_min) y[e] = (float)(w * inv);
-                }
+                const double w = weight.real(weight.exponent(l));
+                y[e] = both(stays(at, e, l), Weights::whole(w) >= lim.w_min) ? (float)(w * inv) : 0.f;
             }
 #pragma unroll
             for (int e = 0; e < R::VE; e += 4)
