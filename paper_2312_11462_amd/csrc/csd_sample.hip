@@ -14,6 +14,10 @@
 //   a share      the weights of all tokens are added up in steps of 1/32 octave; the step that holds the border is ranked, or divided again by the bits of
 //                its logits until few tokens are left or all are equal.  What stays is then a list as above or, if there are too many, goes
 //   all          by the sum over the row, and the draw descends it: the wave's range that holds the border, a range of each wave in it, a tile.
+// Memory bounds the first (656 rows of 50001 in bf16 into probabilities 46 us, 4.3 TB/s) or, for a row alone, its barriers and trips (one of 32000: 9.4 us, 6 of them in the
+// kernel: 1 to read it, 0.8 for the cut, 1.5 for the list, 2.7 to rank and draw).  The others are bound by the instructions of the weights, 24 a token in the
+// histogram: of 256 rows of 32000 with top-p (36.5 us) 7.8 us are the histogram, 7 the border, 6 the sum, 2.6 the draw; of 131072 in bf16 (103 us, for the rows in which most tokens stay)
+// 26, 26, 28 and 5.
 #include "csd_epilogue.h"
 #include "csd_lanes.h"
 
@@ -263,10 +267,9 @@ struct SampleShared {
 };
 
 template <int N>
-__device__ __forceinline__ void clear_counters(SampleShared &S, bool masses) {
+__device__ __forceinline__ void clear_counters(SampleShared &S) {
     for (int i = threadIdx.x; i < kBins / 4; i += N) reinterpret_cast<u32x4 *>(S.count)[i] = u32x4{0u, 0u, 0u, 0u};
-    if (masses)
-        for (int i = threadIdx.x; i < kBins / 2; i += N) reinterpret_cast<u32x4 *>(S.mass)[i] = u32x4{0u, 0u, 0u, 0u};
+    for (int i = threadIdx.x; i < kBins / 2; i += N) reinterpret_cast<u32x4 *>(S.mass)[i] = u32x4{0u, 0u, 0u, 0u};
     if (threadIdx.x < 64) S.octave[threadIdx.x] = 0;
 }
 
@@ -428,10 +431,11 @@ __device__ __forceinline__ uint32_t collect(const R &row, SampleShared &S, float
     return uniform(S.n_list);
 }
 
-// f(token, logit) for the tokens of the waves' ranges for which stays(first token of the piece, place in it, logit) holds, 64 at a time: a weight takes two to three times what the look and a queue in LDS
-// take, and of a vocabulary with a border few tokens stay (256 rows of 131072 in bf16, top-p: the sum 28.0 us without).  The queues lie where the counters were.
-template <typename R, typename S_, typename F>
-__device__ __forceinline__ void gather(const R &row, SampleShared &S, S_ stays, F f) {
+// f(token, logit) for the tokens of the waves' ranges for which stays(first token of the piece, place in it, logit) holds, 64 at a time: a weight takes two to three
+// times what the look and a queue in LDS take, and of a vocabulary with a border few tokens stay (256 rows of 131072 in bf16, top-p: the sum 19 us, 28 over all
+// tokens).  The queues lie where the counters were.
+template <typename R, typename STAYS, typename F>
+__device__ __forceinline__ void gather(const R &row, SampleShared &S, STAYS stays, F f) {
     static_assert(sizeof(S.mass) >= R::W * 128 * sizeof(u64), "");
     const int lane = threadIdx.x & 63, wave = R::wave(), c = R::range(row.V);
     u64 *queue = S.mass + wave * 128;                        // a ring: from `head` on, `n` tokens
@@ -443,7 +447,8 @@ __device__ __forceinline__ void gather(const R &row, SampleShared &S, S_ stays, 
             const float l = R::get(r, e);
             const bool in = stays(at, e, l);
             const u64 mask = __builtin_amdgcn_ballot_w64(in);
-            if (in) queue[(head + n + __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0))) & 127] = (u64)(uint32_t)(at + e) << 32 | __float_as_uint(l);
+            const int place = head + n + __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0));
+            if (in) queue[place & 127] = (u64)(uint32_t)(at + e) << 32 | __float_as_uint(l);
             n += __popcll(mask);
             if (n >= 64) {
                 __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
@@ -590,7 +595,7 @@ __device__ __forceinline__ bool border(const R &row, SampleShared &S, const Weig
         float number[3];
         uint32_t have[3] = {0, 0, 0};
 #pragma unroll
-        for (int i = 0; i < 3; i++) number[i] = uniform(hi - lo >= (uint32_t)i ? logit_of(full_key(hi - i)) : NAN);
+        for (int i = 0; i < 3; i++) number[i] = uniform(hi - lo >= (uint32_t)i && hi - i != 0x7FFFFFFFu >> LOW ? logit_of(full_key(hi - i)) : NAN);      // (-0 is 0)
         row.all_pieces([&](int, const u32x4 &r) {
 #pragma unroll
             for (int e = 0; e < R::VE; e++)
@@ -640,7 +645,7 @@ __device__ __forceinline__ bool border(const R &row, SampleShared &S, const Weig
         }
         const int shift = max(0, 32 - __clz(hi - lo) - 11);  // 2^11 steps of keys at most
         __syncthreads();
-        clear_counters<N>(S, true);
+        clear_counters<N>(S);
         __syncthreads();
         row.all([&](int, float l) {
             if (both(l >= from, l <= to) && in(l)) {
@@ -697,7 +702,7 @@ __global__ __launch_bounds__(N, 4) void k_sample(SampleRows a) {
     const bool greedy = !(temperature > 0.f);
     int k = greedy ? 1 : __builtin_amdgcn_readfirstlane(a.top_k ? a.top_k[set] : a.top_k_all);
     if (k <= 0 || k > a.V) k = a.V;
-    clear_counters<N>(S, true);
+    clear_counters<N>(S);
     if (tid < kPerOctave) S.roots[tid] = exp2((double)tid / kPerOctave);
 
     float mine = -INFINITY;
@@ -759,7 +764,7 @@ __global__ __launch_bounds__(N, 4) void k_sample(SampleRows a) {
         if (out) clear();
         const uint32_t n = collect<T>(row, S, cut, INFINITY, [](float) { return true; });
         if (n <= (uint32_t)kList) return finish<N>(S, weight, lim, 0, n, out, u, token);
-        clear_counters<N>(S, true);
+        clear_counters<N>(S);
         __syncthreads();
     }
 
@@ -808,7 +813,7 @@ __global__ __launch_bounds__(N, 4) void k_sample(SampleRows a) {
         stand = !border<T, N>(again, S, weight, first, m, f, least, sum);
         if (!stand) {
             __syncthreads();
-            clear_counters<N>(S, true);
+            clear_counters<N>(S);
             __syncthreads();
         }
     }

@@ -157,6 +157,19 @@ def test_crowds_around_zero(dtype, kw):
     run_rows(x.to(dtype).cuda(), **kw)
 
 
+@pytest.mark.parametrize("dtype,least", [(torch.bfloat16, 2.0 ** -133), (torch.float32, 2.0 ** -149)])
+def test_zero_beside_the_smallest_numbers_in_one_step(dtype, least):
+    """0 and -0 are one number, though there are three between the least negative number and it; the temperature leaves just these in a step."""
+    x = torch.zeros(3, 900)
+    x[0, 300:600], x[0, 600:] = -least, -1.0
+    x[1, ::3], x[1, 1::3] = -least, -0.0
+    x[2, ::2], x[2, 1::4] = -0.0, -least
+    for k in (250, 400, 700):
+        run_rows(x.to(dtype).cuda(), temperature=1.3 * 64 * least, top_k=k)
+    for p in (0.3, 0.55, 0.8):
+        run_rows(x.to(dtype).cuda(), temperature=1.3 * 64 * least, top_p=p)
+
+
 @pytest.mark.parametrize("V", [37, 1000, 40000])
 def test_crowded_steps(V):
     """Logits that differ by less than a step of any histogram, all of them above one another: thousands to be told apart by their last bits."""
