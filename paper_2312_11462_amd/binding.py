@@ -603,6 +603,10 @@ _PARAMETERS = "temperature", "top_k", "top_p", "min_p"
 
 def _rows_of(shape, stride):
     """(rows, elements between rows) of logits [..., V] whose leading dimensions are one run of equal steps."""
+    if not shape or shape[-1] == 0:
+        raise ValueError("logits: [..., V] with V >= 1 is required")
+    if 0 in shape:
+        return 0, shape[-1]
     rows, step = 1, shape[-1]
     for size, by in zip(reversed(shape[:-1]), reversed(stride[:-1])):
         if size > 1:

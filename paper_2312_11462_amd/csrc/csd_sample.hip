@@ -14,10 +14,10 @@
 //   a share      the weights of all tokens are added up in steps of 1/32 octave; the step that holds the border is ranked, or divided again by the bits of
 //                its logits until few tokens are left or all are equal.  What stays is then a list as above or, if there are too many, goes
 //   all          by the sum over the row, and the draw descends it: the wave's range that holds the border, a range of each wave in it, a tile.
-// Memory bounds the first (656 rows of 50001 in bf16 into probabilities 46 us, 4.3 TB/s) or, for a row alone, its barriers and trips (one of 32000: 9.4 us, 6 of them in the
-// kernel: 1 to read it, 0.8 for the cut, 1.5 for the list, 2.7 to rank and draw).  The others are bound by the instructions of the weights, 24 a token in the
-// histogram: of 256 rows of 32000 with top-p (36.5 us) 7.8 us are the histogram, 7 the border, 6 the sum, 2.6 the draw; of 131072 in bf16 (103 us, for the rows in which most tokens stay)
-// 26, 26, 28 and 5.
+// Memory bounds the first (656 rows of 50001 in bf16 into probabilities 46 us, 4.3 TB/s) or, for a row alone, its barriers and trips (one of 32000: 9 us, 6 of
+// them in the workgroup: 1 to read it, 0.8 for the cut, 1.5 for the list, 2.7 to rank and draw).  The others are bound by the instructions of the weights, 24 a
+// token in the histogram: of 256 rows of 32000 with top-p (36 us) 7.8 us are the histogram, 7 the border, 6 the sum, 2.6 the draw; of 131072 in bf16 (103 us, for the
+// rows in which most tokens stay) 26, 26, 28 and 5.
 #include "csd_epilogue.h"
 #include "csd_lanes.h"
 
@@ -736,6 +736,8 @@ __global__ __launch_bounds__(N, 4) void k_sample(SampleRows a) {
     if (p_min > 0.f) lim.w_min = uniform(max((u64)ceil((double)fminf(p_min, 1.f) * (double)(1ull << 45)), (u64)1));
 
     // ---- few tokens at most
+    // (What the list takes in is k tokens and some more: the others of k's step, and of the lanes whose largest ones were counted.  For larger k it would overflow
+    // too often, and the row starts over: us for top-k 180, 192 and 193 of a row of 32000 13.8, 14.0 and 23.5, of 656 of 50001 in bf16 46, 75 and 84.)
     const bool few = k <= kList * 3 / 4;
     if (few || (k == a.V && !lim.by_mass && p_min > 0.f)) {
         float cut = -kMost;

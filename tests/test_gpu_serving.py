@@ -783,3 +783,12 @@ def test_refusals_of_the_binding():
         c.kv.cross_attention(0, c.dev[0], c.dev[1], c.dev[2], q[:, :, :32], 0.1)
     with pytest.raises(P.CsdError):
         c.kv.cross_attention(0, c.dev[0], c.dev[1], c.dev[2], q, math.nan)
+
+
+def test_no_rows_of_logits_are_no_tokens():
+    import paper_2312_11462_amd as P
+    for shape in ((0, 64), (2, 0, 64), (0, 3, 64)):
+        x = torch.empty(shape, device="cuda")
+        t = P.sample(x, torch.empty(shape[:-1], device="cuda"), top_k=3)
+        assert t.shape == shape[:-1] and t.dtype is torch.int32
+        assert P.filter_probs(x, top_p=0.5).shape == shape

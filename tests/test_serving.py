@@ -163,3 +163,18 @@ def test_the_binding_refuses_tensors_of_the_host():
         P.filter_probs(torch.zeros(2, 8))
     with pytest.raises(ValueError):
         P.Pages.new(4, 16, 2, 2, device="cpu")
+
+
+def test_rows_of_any_leading_dimensions():
+    from paper_2312_11462_amd.binding import _rows_of
+    for shape in ((7,), (3, 7), (2, 3, 7), (2, 1, 3, 7), (1, 1, 7)):
+        x = torch.zeros(shape)
+        rows = x.numel() // 7
+        assert _rows_of(x.shape, x.stride()) == (rows, 7)
+    for shape in ((0, 7), (2, 0, 7), (0, 2, 7), (2, 0, 3, 7)):
+        assert _rows_of(shape, torch.zeros(shape).stride())[0] == 0
+    wide = torch.zeros(2, 3, 11)[..., :7]
+    assert _rows_of(wide.shape, wide.stride()) == (6, 11)
+    for x in (torch.zeros(2, 4, 7)[:, :3], torch.zeros(3, 7, 2)[..., 0], torch.zeros(()), torch.zeros(3, 0)):
+        with pytest.raises(ValueError):
+            _rows_of(x.shape, x.stride())
