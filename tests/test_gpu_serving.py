@@ -792,3 +792,28 @@ def test_no_rows_of_logits_are_no_tokens():
         t = P.sample(x, torch.empty(shape[:-1], device="cuda"), top_k=3)
         assert t.shape == shape[:-1] and t.dtype is torch.int32
         assert P.filter_probs(x, top_p=0.5).shape == shape
+
+
+def test_offsets_beyond_32_bits():
+    """Rows, distances between rows, probabilities and slots behind the 2^31st element."""
+    import paper_2312_11462_amd as P
+    V = 131072
+    rows = (1 << 31) // V + 3
+    few = logits(3, V, torch.bfloat16, 21)
+    u = torch.full((rows,), 0.37, device="cuda")
+    at = [0, rows - 2, rows - 1]
+    want = P.sample(few, u[:3], top_p=0.9), P.filter_probs(few, top_p=0.9)
+    x = torch.full((rows, V), -math.inf, dtype=torch.bfloat16, device="cuda")
+    x[at] = few
+    probs = torch.full((rows, V), -1.0, device="cuda")
+    tokens = P.sample(x, u, top_p=0.9, probs=probs)
+    assert torch.equal(tokens[at], want[0]) and torch.equal(probs[at], want[1])
+    assert int((tokens == -1).sum()) == rows - 3 and not probs[1:rows - 2].any()
+    far = x.flatten()[:V * (rows - 1)].as_strided((2, V), (V * (rows - 2), 1))
+    assert torch.equal(P.sample(far, u[:2], top_p=0.9), want[0][:2])
+    del x, probs, far
+    n, i32 = 3 << 20, dict(dtype=torch.int32, device="cuda")
+    pages = P.Pages(torch.full((2, 4), -1, **i32), torch.zeros(2, **i32), torch.arange(n, **i32), torch.full((1,), n, **i32), torch.zeros(n, **i32), 1024)
+    _, sequence, position, slot, served = pages.plan(torch.tensor([5, 1024], **i32), torch.tensor([2, 1], **i32), 4)
+    assert sequence.tolist() == [0, 0, 1, -1] and position.tolist() == [5, 6, 1024, -1] and served.tolist() == [1, 1]
+    assert slot.tolist() == [(n - 1) * 1024 + 5, (n - 1) * 1024 + 6, (n - 3) * 1024, -1]
