@@ -177,11 +177,12 @@ __global__ __launch_bounds__(512, 2) void k_paged_attn_chunk(PagedAttn a, int mi
         }
     };
     // Where rows of the block, or places without a row, are among a tile's keys: values that no row attends are taken out of LDS again, and those
-    // that are not finite (see odd_halves).  A thread looks at what it stored.
+    // that are not finite (see odd_halves).  A thread looks at what it stored.  (Places behind the table's end, which a sequence may be said to reach, have a page
+    // in `here`, that of the last row: `len` leaves them out.)
     auto mend = [&](int kt, int buf) {
         const int tile = min(kt, n_kt - 1);
         const unsigned here = here_mask(tile);
-        if (tile * kKeys + kKeys <= seq.t && here == 0xFu) return;
+        if (tile * kKeys + kKeys <= min(seq.t, len) && here == 0xFu) return;
         bool odd = false;
 #pragma unroll
         for (int x = 0; x < NP; x++) {
