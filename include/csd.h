@@ -425,7 +425,7 @@ typedef struct csd_pages {
 /*
  * Before a step: sequence b has cache_len[b] rows and gets new_rows[b] more.  Its table is continued to hold them all, by pages from the stack's end on, in
  * order of (sequence, place), each with one user.  served[b] is 1, or 0 where the rows cannot be had: they do not fit the
- * table (such a sequence counts for nothing below); pages are missing and the pages wanted up to and with sequence b are more than there are; or there are rows and
+ * table, or some would lie in a page that the sequence holds and that has other users too (such a sequence counts for nothing below); pages are missing and the pages wanted up to and with sequence b are more than there are; or there are rows and
  * the rows up to and with it are more than `rows`.  A sequence that is not served keeps what it holds and has no rows in this step.
  *   row_start[n_sequences + 1]  sums of the served sequences' rows, as the paged calls take them
  *   sequence, position[rows], slot[rows] (int64)   of every row: its sequence, its position and where its place lies, page * page_rows + position % page_rows
@@ -445,6 +445,9 @@ int32_t csd_pages_release(const csd_pages *pages, const int32_t *keep_len, void 
  * A common prompt: sequence b, which holds nothing yet, takes over the pages of the first length[b] / page_rows * page_rows rows of sequence source[b] (whole
  * pages only, and as many as that one holds), which get one user more.  source[b] outside [0, n_sequences), or b itself, or a sequence that has a
  * source of its own in this call: left alone.
+ * What lies in a page with several users is not written: csd_pages_plan does not serve a sequence whose new rows begin in one (it was cut inside a
+ * shared page, or gave the page away before its rows were there).  Release it to the page's first row and plan the rows from there on anew, or wait until
+ * the others have given the page up.
  */
 int32_t csd_pages_share(const csd_pages *pages, const int32_t *source, const int32_t *length, void *stream);
 

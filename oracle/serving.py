@@ -67,6 +67,10 @@ class Pages:
             t, n = max(int(cache_len[b]), 0), max(int(new_rows[b]), 0)
             need = max(-(-(t + n) // R) - self.held[b], 0)
             ok = -(-(t + n) // R) <= width
+            if ok and n:
+                # rows of a page that others use too are not this sequence's to write
+                mine = self.table[b][t // R:min(self.held[b], -(-(t + n) // R))]
+                ok = not any(0 <= page < self.n_pages and self.users[page] > 1 for page in mine)
             if ok:
                 wanted += need
                 total += n

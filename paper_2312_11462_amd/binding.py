@@ -527,7 +527,8 @@ class Pages:
             self._check(name, t, self.n_sequences)
 
     def plan(self, cache_len, new_rows, rows):
-        """csd_pages_plan: (row_start [sequences + 1], sequence [rows], position [rows], slot [rows] int64, served [sequences]); rows: the most rows of the step."""
+        """csd_pages_plan: (row_start [sequences + 1], sequence [rows], position [rows], slot [rows] int64, served [sequences]); rows: the most rows of the step.
+        A sequence whose new rows would lie in a page that others use too is not served."""
         n, dev = self.n_sequences, self._dev
         if not (dev == cache_len.get_device() == new_rows.get_device() and torch.int32 is cache_len.dtype is new_rows.dtype and cache_len.is_contiguous()
                 and new_rows.is_contiguous() and n == cache_len.numel() == new_rows.numel() and _current_device() == dev):
@@ -552,7 +553,8 @@ class Pages:
             _chk(rc, "csd_pages_release")
 
     def share(self, source, length):
-        """csd_pages_share: sequences that hold nothing take over the whole pages of the first length[b] rows of source[b] (negative: none)."""
+        """csd_pages_share: sequences that hold nothing take over the whole pages of the first length[b] rows of source[b] (negative: none).  Shared pages are
+        not written: one that is cut inside them, the source too, has to release back to the page's first row before it gets new rows."""
         self._given(source=source, length=length)
         rc = self._lib.csd_pages_share(self._ref, source.data_ptr(), length.data_ptr(), _raw_stream(self._dev))
         if rc:

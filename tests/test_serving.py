@@ -178,3 +178,24 @@ def test_rows_of_any_leading_dimensions():
     for x in (torch.zeros(2, 4, 7)[:, :3], torch.zeros(3, 7, 2)[..., 0], torch.zeros(()), torch.zeros(3, 0)):
         with pytest.raises(ValueError):
             _rows_of(x.shape, x.stride())
+
+
+def test_oracle_rows_of_shared_pages_are_nobodys_to_write():
+    p = O.Pages([[-1] * 5 for _ in range(3)], [0, 0, 0], list(range(11, -1, -1)), [0] * 12, 16)
+    p.plan([0, 0, 0], [48, 0, 0], 48)
+    p.share([-1, 0, -1], [0, 48, 0])
+    p.release([-1, 40, -1])                                  # the one that took the pages is cut inside the last of them
+    assert p.users[:3] == [2, 2, 2]
+    before = [list(r) for r in p.table], list(p.held), list(p.free), list(p.users)
+    row_start, seq, pos, slot, served = p.plan([48, 40, 0], [1, 8, 2], 16)
+    assert served == [1, 0, 1] and row_start == [0, 1, 1, 3] and slot[:4] == [48, 64, 65, -1]      # it counts for nothing, and keeps what it holds
+    assert p.table[1] == before[0][1] and p.held[1] == 3 and p.users[:5] == [2, 2, 2, 1, 1]
+    assert p.plan([48, 40, 0], [0, 0, 0], 4)[4] == [1, 1, 1]                                       # without rows there is nothing to write
+    p.release([40, -1, 0])                                   # and the one that gave them
+    assert p.plan([40, 40, 0], [3, 3, 3], 16)[4] == [0, 0, 1]
+    p.release([-1, 32, 0])                                   # back to the page's first row: the rows from there on go to a page of its own
+    row_start, seq, pos, slot, served = p.plan([40, 32, 0], [3, 16, 0], 19)
+    assert served == [1, 1, 1] and slot[:3] == [40, 41, 42] and p.users[:3] == [2, 2, 1] and p.table[1][2] == slot[3] // 16 not in p.table[0][:3]
+    assert p.plan([10, 8, 0], [30, 100, 0], 130)[4] == [0, 0, 1]                                   # (100 rows do not fit its table; the 30 begin in a shared page)
+    p.release([-1, 0, -1])
+    assert p.plan([10, 0, 0], [30, 0, 0], 30)[4] == [1, 1, 1]
