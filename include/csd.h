@@ -464,7 +464,7 @@ int32_t csd_pages_share(const csd_pages *pages, const int32_t *source, const int
  * token of less than 2^-46 has none), so the result does not depend on how a row is spread over the chip.  NaN counts as -inf, inf as the
  * largest number of its type; a row without any logit above -inf gives token -1 and probabilities of 0.
  * Each parameter is an array [rows / rows_each] on the device, for rows_each consecutive rows an entry, or NULL: then the number beside it goes for all rows
- * (CSD_EINVAL: temperature_all or top_p_all negative or NaN, min_p_all outside [0, 1]).
+ * (CSD_EINVAL: temperature_all or top_p_all negative or NaN, min_p_all outside [0, 1]; an array, and rows no multiple of rows_each).
  */
 typedef struct csd_filter {
     const float *temperature;

@@ -918,6 +918,8 @@ static int32_t sample_enqueue(const csd_filter *f, const void *logits, int64_t s
     if (!f || (f->rows_each < 1)) return f ? CSD_EINVAL : CSD_ENULL;
     if (dtype != CSD_DTYPE_FP32 && dtype != CSD_DTYPE_BF16) return CSD_EINVAL;
     if (rows < 0 || V < 1 || stride < V) return CSD_EINVAL;
+    // (the arrays end with the last whole set)
+    if ((f->temperature || f->top_k || f->top_p || f->min_p) && rows % f->rows_each) return CSD_EINVAL;
     if (!f->temperature && !(f->temperature_all >= 0.f)) return CSD_EINVAL;
     if (!f->top_p && !(f->top_p_all >= 0.f)) return CSD_EINVAL;
     if (!f->min_p && !(f->min_p_all >= 0.f && f->min_p_all <= 1.f)) return CSD_EINVAL;

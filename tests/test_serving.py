@@ -199,3 +199,15 @@ def test_oracle_rows_of_shared_pages_are_nobodys_to_write():
     assert p.plan([10, 8, 0], [30, 100, 0], 130)[4] == [0, 0, 1]                                   # (100 rows do not fit its table; the 30 begin in a shared page)
     p.release([-1, 0, -1])
     assert p.plan([10, 0, 0], [30, 0, 0], 30)[4] == [1, 1, 1]
+
+
+def test_draws_refuse_rows_that_their_parameters_do_not_cover(L):
+    """Five rows by two: the arrays have two entries, and the last row would read a third."""
+    from paper_2312_11462_amd.binding import Filter
+    for name in ("temperature", "top_k", "top_p", "min_p"):
+        for rows, each in ((5, 2), (1, 2), (7, 3), (2, 1 << 30)):
+            f = Filter(None, None, None, None, 1.0, 0, 1.0, 0.0, each)
+            setattr(f, name, 256)
+            assert L.csd_sample(C.addressof(f), 256, 100, 1, rows, 100, 256, 256, None, None) == EINVAL, (name, rows, each)
+            assert L.csd_filter_probs(C.addressof(f), 256, 100, 1, rows, 100, 4096, None) == EINVAL, (name, rows, each)
+            assert L.csd_sample(C.addressof(f), None, 100, 1, 0, 100, None, None, None, None) == 0
