@@ -415,7 +415,8 @@ int32_t csd_paged_cross_attention(const csd_paged_kv *kv, int32_t layer, const i
  *   free_pages[n_pages], n_free[1]     a stack: pages are taken from its end
  *   users[n_pages]                     tables that name a page; 0 for those in the stack
  * page_rows as in csd_paged_kv.  Lengths that are negative count as 0, n_free and held are cut to their ranges, entries that name no page are passed over.
- * Calls on the same arrays must not overlap.  CSD_ESHAPE: more than 2^20 sequences, 2^30 table entries or pages, table_stride * page_rows above 2^30.
+ * Calls on the same arrays must not overlap.  CSD_ESHAPE: more than 2^20 sequences, 2^30 table entries or pages, 2^22 rows of a step, table_stride * page_rows above
+ * 2^30.
  */
 typedef struct csd_pages {
     int32_t n_pages, page_rows, n_sequences, table_stride;

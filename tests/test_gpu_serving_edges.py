@@ -119,3 +119,18 @@ def test_shared_prompts_that_are_cut_anywhere(sequences, page):
         assert all(c.ref.users[x] == n for x, n in used.items())
     c.release(np.zeros(sequences, dtype=int))
     assert int(c.gpu.n_free) == c.ref.n_pages and not c.gpu.users.any()
+
+
+def test_thousands_of_sequences_most_of_them_without_rows():
+    """More sequences than the row kernel keeps the starts of in LDS; runs of sequences without rows, at both ends too, and rows behind the last."""
+    for sequences, share in ((4096, 0.5), (4097, 0.5), (5000, 0.02), (9001, 0.6)):
+        c = Both(3 * sequences, 16, sequences, 4, seed=sequences)
+        new = np.where(c.rng.random(sequences) < share, c.rng.integers(1, 40, sequences), 0)
+        new[:17] = new[-70:] = 0
+        length = c.rng.integers(0, 25, sequences)
+        rows = int(new.sum())
+        assert sum(c.plan(length, new, rows + 300)[4]) == sequences
+        c.plan(length + new, np.ones(sequences, dtype=int), sequences)
+        c.release(np.where(c.rng.random(sequences) < 0.3, -1, length))
+        c.release(np.zeros(sequences, dtype=int))
+        assert int(c.gpu.n_free) == c.ref.n_pages
