@@ -1,7 +1,7 @@
 // Draws from logits by temperature, top-k, top-p and min-p, and the probabilities of such draws.
 //
 // With M the largest logit of a row and w_v = 2^((l_v - M) log2(e) / T), every weight is the whole number round(w_v 2^45): sums do not depend on their
-// order, so neither do the sets that they bound nor the tokens (2^18 of them fit 63 bits; what weights of 64 bits would add to the sums decides
+// order, so neither do the sets that they bound nor the tokens (2^18 of them make 2^63, so sums have no sign; what weights of 64 bits would add to the sums decides
 // for uniform numbers within 2^-38 or so of a border).  Tokens are ranked by (logit, lowest token first), which is the order of one 64-bit number, key << 32 | ~token.
 // Each parameter keeps a start of the ranking, so together they keep the tokens from a least such number on:
 //   top-k   the first k

@@ -1,13 +1,15 @@
 """The calls of a serving step where they could go wrong: chunks over tables that their lengths pass, sequences cut inside pages that others use, thousands of
 sequences, rows of equal logits, borders among tokens of equal weight.  The plain forms are oracle/serving.py's; the bounds are test_gpu_serving's."""
 import math
+from fractions import Fraction
 
 import numpy as np
 import pytest
 import torch
 
+from oracle import serving as O
 from test_gpu_paged import Paged
-from test_gpu_serving import Both, States
+from test_gpu_serving import Both, States, as_sets, logits
 
 pytestmark = pytest.mark.gpu
 
@@ -134,3 +136,81 @@ def test_thousands_of_sequences_most_of_them_without_rows():
         c.release(np.where(c.rng.random(sequences) < 0.3, -1, length))
         c.release(np.zeros(sequences, dtype=int))
         assert int(c.gpu.n_free) == c.ref.n_pages
+
+
+# ------------------------------------------------------------------------------------------------ sets and draws at their borders
+
+def strictly(x, u=None, **kw):
+    """Draws and filters rows x and looks at every token: one that stays where the plain form leaves it out, or the other way round, has to lie at a border within
+    the sums' error E (or weigh nothing); the probabilities and the draw go by the set that the kernel kept."""
+    import paper_2312_11462_amd as P
+    rows, V = x.shape
+    if u is None:
+        u = torch.tensor(np.random.default_rng(V).integers(0, 1 << 24, rows) * 2.0 ** -24, dtype=torch.float32).cuda()
+    probs = torch.full((rows, V), -1.0, device="cuda")
+    tokens = P.sample(x, u, probs=probs, **kw).tolist()
+    assert torch.equal(probs, P.filter_probs(x, **kw)) and P.sample(x, u, **kw).tolist() == tokens
+    p, xx, uu = probs.cpu().numpy().astype(np.float64), x.double().cpu().numpy(), u.cpu().numpy()
+    sets = as_sets(rows, *(kw.get(n, d) for n, d in (("temperature", 1.0), ("top_k", 0), ("top_p", 1.0), ("min_p", 0.0))))
+    E, largest = 2 * V * 2.0 ** -45, torch.finfo(x.dtype).max
+    for r in range(rows):
+        (w, slack), (full, _) = O.weights(xx[r], *sets[r], largest=largest), O.weights(xx[r], sets[r][0], largest=largest)
+        kept, name = p[r] > 0, f"row {r} {sets[r]}"
+        if not full.sum() > 0:
+            assert tokens[r] == -1 and not p[r].any(), name
+            continue
+        other = np.flatnonzero((kept != (w > 0)) & ~(slack <= E) & ~(~kept & (w <= 2.0 ** -45)))
+        assert not len(other), f"{name}: tokens {other[:8]} stay or go"
+        full = np.where(kept, full, 0.0)
+        z = full.sum()
+        tol = full / z * (2.0 ** -24 + 2 * E / z) + 2.0 ** -45
+        assert (np.abs(p[r] - full / z) <= tol).all(), f"{name}: off by {(np.abs(p[r] - full / z) / tol).max():.2f} times the bound"
+        at, run, t = min(max(float(uu[r]), 0.0), 1 - 2.0 ** -24) * z, np.cumsum(full), tokens[r]
+        assert 0 <= t < V and kept[t] and run[t] - full[t] <= at + E and at - E < run[t], f"{name}: token {t} for u {uu[r]}"
+
+
+LIMITS = [dict(), dict(temperature=0.0), dict(top_k=40), dict(top_k=193), dict(top_p=0.9), dict(top_p=0.5), dict(min_p=0.05), dict(top_k=50, top_p=0.8),
+          dict(temperature=1.7, top_k=300, top_p=0.95, min_p=0.01), dict(top_k=900, top_p=0.37), dict(top_p=0.5, min_p=0.5)]
+
+
+@pytest.mark.parametrize("kw", LIMITS, ids=str)
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_every_token_that_stays_or_goes(dtype, kw):
+    for V in (1, 5, 255, 1000, 4099, 32000):
+        strictly(logits(4, V, dtype, V + 3, likely=min(V, 20)), **kw)
+    strictly(logits(2, 131072, dtype, 8), **kw)
+
+
+@pytest.mark.parametrize("kw", LIMITS, ids=str)
+@pytest.mark.parametrize("V,levels", [(1000, 1), (1000, 2), (32000, 1), (32000, 3), (32000, 40), (5000, 700)])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_every_token_that_stays_or_goes_among_equal_ones(V, levels, dtype, kw):
+    x = torch.randint(0, levels, (3, V), generator=torch.Generator().manual_seed(V + levels)).float() * 0.125 - 2.0
+    x[2, ::5] = -math.inf
+    strictly(x.to(dtype).cuda(), **kw)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_every_token_that_stays_or_goes_by_settings_of_its_own(dtype):
+    g = torch.Generator().manual_seed(5)
+    for rows, V in ((300, 700), (24, 32000)):
+        k = torch.randint(-3, 400, (rows,), generator=g, dtype=torch.int32)
+        t, p, m = torch.rand(rows, generator=g) * 1.5, torch.rand(rows, generator=g) * 1.2, torch.rand(rows, generator=g) * 0.3 - 0.1
+        t[::7] = 0
+        strictly(logits(rows, V, dtype, 17), temperature=t.cuda(), top_k=k.cuda(), top_p=p.cuda(), min_p=m.cuda())
+
+
+@pytest.mark.parametrize("V", [1, 7, 1000, 1024, 32000, 131072, 1 << 18])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_sets_and_draws_of_equal_logits_are_exact(V, dtype):
+    """All weights are 1, so every sum is a whole number: the first k tokens, the first ceil(p k) of those, and token floor(u n) of n.  (2^18 weights make 2^63.)"""
+    import paper_2312_11462_amd as P
+    half = [i / 512 for i in range(0, 512, 37)]
+    u = [0.0, 2.0 ** -24, 0.25, 0.5, 0.5 - 2.0 ** -24, 1 - 2.0 ** -24] + half
+    x = torch.full((len(u), V), 0.75, dtype=dtype, device="cuda")
+    for k, p in ((0, 1.0), (0, 0.5), (0, 0.37), (0, 1 - 2.0 ** -24), (7, 1.0), (300, 1.0), (900, 0.37), (193, 0.5), (0, 0.0), (1024, 0.5)):
+        first = min(k, V) if k > 0 else V
+        n = max(math.ceil(Fraction(float(np.float32(p))) * first), 1)
+        tokens, probs = (f(x, *a, top_k=k, top_p=p) for f, a in ((P.sample, (torch.tensor(u, dtype=torch.float32, device="cuda"),)), (P.filter_probs, ())))
+        assert tokens.tolist() == [math.floor(Fraction(a) * n) for a in u], (k, p)
+        assert (probs[:, :n] == np.float32(1 / n)).all() and not probs[:, n:].any(), (k, p)
