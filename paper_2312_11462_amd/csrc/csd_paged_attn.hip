@@ -49,8 +49,8 @@ __device__ __forceinline__ float lanes_sum(float a, int log_w) {
 // feature per lane behind them 63 and 38.  Five rows of 4 heads of 16 over 32 keys 7.4.)
 static constexpr int kAnyWaves = 8;
 
-template <typename TQ, typename TP>
-__global__ __launch_bounds__(64 * kAnyWaves) void k_paged_attn_any(PagedAttn a, int log_w) {
+template <typename TQ, typename TP, bool CROSS>
+__global__ __launch_bounds__(64 * kAnyWaves) void k_paged_attn_any(PagedAttnOf<CROSS> a, int log_w) {
     __shared__ float s_o[kAnyWaves][256], s_m[kAnyWaves], s_l[kAnyWaves], s_w[kAnyWaves][64];
     __shared__ size_t s_at[kAnyWaves][64];
     __shared__ bool s_any[kAnyWaves];                        // the wave has met a key that the row attends
@@ -188,7 +188,10 @@ static void any_launch(const PagedAttn &a, hipStream_t st) {
     int log_w = 0;
     while (4 << log_w < a.p.D) log_w++;
     const int keys = a.p.table_stride << a.p.page_shift, waves = keys > 4 * 64 ? 8 : 4;
-    hipLaunchKernelGGL((k_paged_attn_any<TQ, TP>), dim3(a.r.rows, a.p.Hkv * a.group), dim3(64 * waves), 0, st, a, log_w);
+    csd_paged_by_cross(a, [&](auto x) {
+        constexpr bool CROSS = std::is_same<decltype(x), PagedAttnOf<true>>::value;
+        hipLaunchKernelGGL((k_paged_attn_any<TQ, TP, CROSS>), dim3(a.r.rows, a.p.Hkv * a.group), dim3(64 * waves), 0, st, x, log_w);
+    });
 }
 
 int32_t csd_paged_attention_enqueue(const PagedAttn &a, int32_t pool_dtype, int32_t q_dtype, hipStream_t st) {

@@ -13,8 +13,8 @@
 #include "csd_paged_tiles.h"
 
 static constexpr int kChunkRows = 256;
-template <int DH, bool F8>
-__global__ __launch_bounds__(512, 2) void k_paged_attn_chunk(PagedAttn a, int min_rows) {
+template <int DH, bool F8, bool CROSS>
+__global__ __launch_bounds__(512, 2) void k_paged_attn_chunk(PagedAttnOf<CROSS> a, int min_rows) {
     constexpr int ES = F8 ? 1 : 2, LB = F8 && DH == 64 ? 8 : 16;         // bytes that a lane loads
     constexpr int LPR = DH * ES / LB;                        // lanes that load a row
     constexpr int RPP = 512 / LPR, NP = kKeys / RPP;         // rows per pass of the workgroup, passes per tile
@@ -33,7 +33,7 @@ __global__ __launch_bounds__(512, 2) void k_paged_attn_chunk(PagedAttn a, int mi
     const int kvh = blockIdx.x % p.Hkv;
     int b = -1, rt = 0, total = 0;
     PagedSeq seq{0, 0, 0};
-    const bool by_length = a.cross && a.r.B <= 64;
+    const bool by_length = CROSS && a.r.B <= 64;
     if (by_length) {
         // Every row tile of a sequence has all of its encoder's keys: the sequences with the most keys first, so that the last workgroups are short ones (4 x 1024 rows
         // over 1000 to 4096 encoder rows, 32 heads of 128: 192 us, in the order of the sequences 226).
@@ -93,7 +93,8 @@ __global__ __launch_bounds__(512, 2) void k_paged_attn_chunk(PagedAttn a, int mi
     if (b < 0) return;
     const int rows = min(seq.m * a.group - rt * BM, BM);     // of this item
     const int len = a.keys(seq.t, (rt * BM + rows - 1) / a.group);      // keys that some row attends
-    const int n_kt = tiles_of(len);
+    int n_kt = tiles_of<CROSS>(len);
+    if (CROSS) asm("" : "+s"(n_kt));                         // (a loop that is known to run once at least: 203.9 us where this takes 202)
 
     // The page table, 16 tiles at a time: lane x holds where the x-th group of 16 keys from tile `base` on lies in the pools (bytes; one without a
     // page: in page 0, which the masks leave out), and bit x of `here` says that it has a page.  The window moves by eight tiles.
@@ -102,7 +103,7 @@ __global__ __launch_bounds__(512, 2) void k_paged_attn_chunk(PagedAttn a, int mi
         unsigned long long here;
     };
     auto pages_from = [&](int tile) {
-        const int key = min((tile * 4 + lane) * 16, cap - 1) & ~15;
+        const int key = (tile * 4 + lane) * 16;              // (behind the table's end, which a sequence may be said to reach, there is no page)
         const int page = paged_page(p, b, key);
         return Pages{paged_row(p, max(page, 0), kvh, key) * (DH * ES), __ballot(page >= 0)};
     };
@@ -177,12 +178,11 @@ __global__ __launch_bounds__(512, 2) void k_paged_attn_chunk(PagedAttn a, int mi
         }
     };
     // Where rows of the block, or places without a row, are among a tile's keys: values that no row attends are taken out of LDS again, and those
-    // that are not finite (see odd_halves).  A thread looks at what it stored.  (Places behind the table's end, which a sequence may be said to reach, have a page
-    // in `here`, that of the last row: `len` leaves them out.)
+    // that are not finite (see odd_halves).  A thread looks at what it stored.
     auto mend = [&](int kt, int buf) {
         const int tile = min(kt, n_kt - 1);
         const unsigned here = here_mask(tile);
-        if (tile * kKeys + kKeys <= min(seq.t, len) && here == 0xFu) return;
+        if (tile * kKeys + kKeys <= seq.t && here == 0xFu) return;
         bool odd = false;
 #pragma unroll
         for (int x = 0; x < NP; x++) {
@@ -420,8 +420,11 @@ __global__ __launch_bounds__(512, 2) void k_paged_attn_chunk(PagedAttn a, int mi
 void csd_paged_chunk_enqueue(const PagedAttn &a, int min_rows, int32_t pool_dtype, hipStream_t st) {
     // row tiles at most: full ones, and a last one per sequence that takes part
     const long long items = ((long long)a.r.rows * a.group / kChunkRows + csd_paged_batch(a, min_rows)) * a.p.Hkv;
-    auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)items), dim3(512), 0, st, a, min_rows); };
     const bool f8 = pool_dtype == CSD_DTYPE_FP8;
-    if (a.p.D == 128) f8 ? launch(k_paged_attn_chunk<128, true>) : launch(k_paged_attn_chunk<128, false>);
-    else f8 ? launch(k_paged_attn_chunk<64, true>) : launch(k_paged_attn_chunk<64, false>);
+    csd_paged_by_cross(a, [&](auto x) {
+        constexpr bool CROSS = std::is_same<decltype(x), PagedAttnOf<true>>::value;
+        auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)items), dim3(512), 0, st, x, min_rows); };
+        if (a.p.D == 128) f8 ? launch(k_paged_attn_chunk<128, true, CROSS>) : launch(k_paged_attn_chunk<128, false, CROSS>);
+        else f8 ? launch(k_paged_attn_chunk<64, true, CROSS>) : launch(k_paged_attn_chunk<64, false, CROSS>);
+    });
 }

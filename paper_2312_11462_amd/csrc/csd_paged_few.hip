@@ -87,8 +87,8 @@ __device__ __forceinline__ f32x4 mfma16(u32x4 a, u32x4 b, f32x4 c) {
 }
 
 // RT: 16-row tiles of queries.
-template <int DH, bool F8, int RT>
-__global__ __launch_bounds__(256, 2) void k_paged_attn_few(PagedAttn a) {
+template <int DH, bool F8, int RT, bool CROSS>
+__global__ __launch_bounds__(256, 2) void k_paged_attn_few(PagedAttnOf<CROSS> a) {
     using Tile = FewTile<DH, F8>;
     constexpr int F = DH / 16, R = 16 * RT;
     constexpr int NB = (F8 && (RT == 1 || DH == 64) ? 2 : 1) + (DH == 64 ? 1 : 0);     // tiles in flight per wave, as registers allow
@@ -490,7 +490,10 @@ __global__ __launch_bounds__(256, 2) void k_paged_attn_few(PagedAttn a) {
 
 template <int DH, bool F8, int RT>
 static void few_launch(const PagedAttn &a, hipStream_t st) {
-    hipLaunchKernelGGL((k_paged_attn_few<DH, F8, RT>), dim3(CSD_PAGED_FEW_GRID), dim3(256), 0, st, a);
+    csd_paged_by_cross(a, [&](auto x) {
+        constexpr bool CROSS = std::is_same<decltype(x), PagedAttnOf<true>>::value;
+        hipLaunchKernelGGL((k_paged_attn_few<DH, F8, RT, CROSS>), dim3(CSD_PAGED_FEW_GRID), dim3(256), 0, st, x);
+    });
 }
 
 template <int DH, bool F8>

@@ -18,8 +18,8 @@
 
 // The grid is a fixed number of workgroups, which take equal, contiguous shares of all items' key tiles (as k_paged_attn_few does; the parts of an item
 // are joined by the workgroup that finishes last).
-template <int DH, bool F8>
-__global__ __launch_bounds__(256, 2) void k_paged_attn_many(PagedAttn a, int min_rows) {
+template <int DH, bool F8, bool CROSS>
+__global__ __launch_bounds__(256, 2) void k_paged_attn_many(PagedAttnOf<CROSS> a, int min_rows) {
     constexpr int ES = F8 ? 1 : 2, LPR = DH * ES / 16;       // lanes that load a row
     constexpr int RPP = 256 / LPR, NP = kKeys / RPP;         // rows per pass of the workgroup, passes per tile
     constexpr int PIECES = kKeys * DH / 8;                   // 16-byte pieces of a staged tile
@@ -88,7 +88,7 @@ __global__ __launch_bounds__(256, 2) void k_paged_attn_many(PagedAttn a, int min
     int sum = 0, longest = 0;
     for (int b = lane; b < batch; b += 64) {
         sum += s_units[b];
-        longest = max(longest, COST + tiles_of(a.keys(s_t[b], s_m[b] - 1)));
+        longest = max(longest, COST + tiles_of<CROSS>(a.keys(s_t[b], s_m[b] - 1)));
     }
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) {
@@ -508,8 +508,11 @@ void csd_paged_many_enqueue(const PagedAttn &a, int min_rows, int32_t pool_dtype
     const long long likely = (full * most * a.group / CSD_PAGED_MANY_ROWS + full) * a.p.Hkv;
     if (!fits || (likely > CSD_PAGED_MANY_ITEMS && most > CSD_PAGED_FINE_ROWS && most * a.group >= CSD_PAGED_CHUNK_ROWS))
         return csd_paged_chunk_enqueue(a, min_rows, pool_dtype, st);
-    auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(CSD_PAGED_MANY_GRID), dim3(256), 0, st, a, min_rows); };
     const bool f8 = pool_dtype == CSD_DTYPE_FP8;
-    if (a.p.D == 128) f8 ? launch(k_paged_attn_many<128, true>) : launch(k_paged_attn_many<128, false>);
-    else f8 ? launch(k_paged_attn_many<64, true>) : launch(k_paged_attn_many<64, false>);
+    csd_paged_by_cross(a, [&](auto x) {
+        constexpr bool CROSS = std::is_same<decltype(x), PagedAttnOf<true>>::value;
+        auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(CSD_PAGED_MANY_GRID), dim3(256), 0, st, x, min_rows); };
+        if (a.p.D == 128) f8 ? launch(k_paged_attn_many<128, true, CROSS>) : launch(k_paged_attn_many<128, false, CROSS>);
+        else f8 ? launch(k_paged_attn_many<64, true, CROSS>) : launch(k_paged_attn_many<64, false, CROSS>);
+    });
 }

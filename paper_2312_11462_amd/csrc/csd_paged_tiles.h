@@ -27,9 +27,14 @@ template <int DH> __device__ __forceinline__ int v_piece(int row, int c) {
     return row * (DH / 8) + (c ^ (DH == 128 ? (row & 3) << 2 : ((row >> 1) & 1) << 2));
 }
 
-// The key tiles of so many keys; rows that have nothing to attend go through one.
-__device__ __forceinline__ int tiles_of(int keys) { return max((keys + kKeys - 1) / kKeys, 1); }
+// The key tiles of so many keys; rows of an encoder without any go through one.
+template <bool CROSS>
+__device__ __forceinline__ int tiles_of(int keys) {
+    const int n = (keys + kKeys - 1) / kKeys;
+    return CROSS ? max(n, 1) : n;
+}
 // The key tiles that row tile rt of a sequence goes through: those up to the last position that one of its rows attends.
-__device__ __forceinline__ int row_tile_keys(const PagedAttn &a, int rt, int m, int t) {
-    return tiles_of(a.keys(t, min(((rt + 1) * CSD_PAGED_MANY_ROWS - 1) / a.group, m - 1)));
+template <bool CROSS>
+__device__ __forceinline__ int row_tile_keys(const PagedAttnOf<CROSS> &a, int rt, int m, int t) {
+    return tiles_of<CROSS>(a.keys(t, min(((rt + 1) * CSD_PAGED_MANY_ROWS - 1) / a.group, m - 1)));
 }
