@@ -399,8 +399,8 @@ int32_t csd_paged_commit(const csd_paged_kv *kv, const int32_t *cache_len, const
 /*
  * Cross-attention over pages (the encoder-decoder reviewers of Section 5.1, in batches of different lengths): position j of a sequence is row j of its encoder's
  * projected states, written once per prompt with csd_paged_write, and every row of the block or chunk attends positions 0 .. enc_len[b], those
- * excluded that have no page.  The rows of the call themselves are in no page.  A sequence with enc_len[b] <= 0 gives zeros.  Everything else is as for
- * csd_paged_attention: types, head sizes, strides, ragged rows, rounding, workspace, errors.
+ * excluded that have no page.  The rows of the call themselves are in no page.  A sequence with enc_len[b] <= 0 gives zeros.  Weights are rounded to 16 bits at
+ * most, however many rows there are.  Everything else is as for csd_paged_attention: types, head sizes, strides, ragged rows, workspace, errors.
  */
 int32_t csd_paged_cross_attention(const csd_paged_kv *kv, int32_t layer, const int32_t *row_start, const int32_t *enc_len, int32_t B,
                                   int32_t rows, int32_t max_rows, const void *q, int64_t q_stride, int32_t n_heads, int32_t dtype,

@@ -137,8 +137,8 @@ __device__ __forceinline__ u32x2 two_planes(float w0, float w1) {
     return u32x2{hi, lo};
 }
 
-// Blocks of tokens to review, trees among them, and single tokens are weighed in two planes, whatever else is in the call; the chunks of more rows than this
-// in one: bf16, off by half a step (2^-8 of a weight, random in sign; the sum of the weights is kept in fp32).
+// Blocks of tokens to review, trees among them, and single tokens are weighed in two planes, whatever else is in the call, and so is all cross-attention; the chunks
+// of more rows than this in one: bf16, off by half a step (2^-8 of a weight, random in sign; the sum of the weights is kept in fp32).
 #define CSD_PAGED_FINE_ROWS 64
 
 // The shares: T tiles over n workgroups, the first T % n of them one tile longer.

@@ -10,6 +10,8 @@
 // (2 chunks of 2048 rows, 8 x 4 heads of 128, 10239 and 4096 keys, bf16: 415 us, 993 TFLOP/s; two independent workgroups of four waves and 128 rows
 // per compute unit took 455; e4m3 406 against 433; heads of 64 256 against 284; a barrier behind each half of a tile instead: 411, but one fresh prompt of
 // 4099 rows, 32 heads, 215 instead of 193.)  Weights in two planes, as those of blocks of up to 64 rows are, would take 542 us, e4m3 531, heads of 64 348.
+// Cross-attention has them: as near to 64 bits as its output's rounding lets it be, however many rows there are (4 x 1024 rows over 1000 to 4096 encoder rows, 32 heads
+// of 128: 255 to 269 us, off by 1.66e-3 of the outputs' size; in one plane 196 to 202, off by 2.32e-3).
 #include "csd_paged_tiles.h"
 
 static constexpr int kChunkRows = 256;
@@ -36,7 +38,7 @@ __global__ __launch_bounds__(512, 2) void k_paged_attn_chunk(PagedAttnOf<CROSS> 
     const bool by_length = CROSS && a.r.B <= 64;
     if (by_length) {
         // Every row tile of a sequence has all of its encoder's keys: the sequences with the most keys first, so that the last workgroups are short ones (4 x 1024 rows
-        // over 1000 to 4096 encoder rows, 32 heads of 128: 192 us, in the order of the sequences 226).
+        // over 1000 to 4096 encoder rows, 32 heads of 128: 267 us, in the order of the sequences 303).
         PagedSeq s{0, 0, 0};
         int n = 0;
         if (lane < a.r.B) {
@@ -93,8 +95,7 @@ __global__ __launch_bounds__(512, 2) void k_paged_attn_chunk(PagedAttnOf<CROSS> 
     if (b < 0) return;
     const int rows = min(seq.m * a.group - rt * BM, BM);     // of this item
     const int len = a.keys(seq.t, (rt * BM + rows - 1) / a.group);      // keys that some row attends
-    int n_kt = tiles_of<CROSS>(len);
-    if (CROSS) asm("" : "+s"(n_kt));                         // (a loop that is known to run once at least: 203.9 us where this takes 202)
+    const int n_kt = tiles_of<CROSS>(len);
 
     // The page table, 16 tiles at a time: lane x holds where the x-th group of 16 keys from tile `base` on lies in the pools (bytes; one without a
     // page: in page 0, which the masks leave out), and bit x of `here` says that it has a page.  The window moves by eight tiles.
@@ -369,7 +370,8 @@ __global__ __launch_bounds__(512, 2) void k_paged_attn_chunk(PagedAttnOf<CROSS> 
             products(v_this, planes);
         }
     };
-    if (seq.m <= CSD_PAGED_FINE_ROWS) tiles(std::true_type{});
+    if constexpr (CROSS) tiles(std::true_type{});
+    else if (seq.m <= CSD_PAGED_FINE_ROWS) tiles(std::true_type{});
     else tiles(std::false_type{});
     __syncthreads();
     l_run = halves_sum(l_run + l_more);

@@ -9,8 +9,8 @@
 //   S^T = K q^T    A = K (32 keys x 16 features, one 16-byte read), B = q^T, in registers throughout
 //   O^T = V^T P^T  A = V^T (32 features x 16 keys, by LDS's transposing reads), B = P^T: a lane's scores of 16 keys are, in
 //                  order, keys 4 h .. 4 h + 3 and 8 + 4 h .. 8 + 4 h + 3 (h = lane / 32), and A's columns are read in that order
-// so that the weights never move between lanes.  The weights of sequences of up to 64 rows enter as two bf16 planes, those of longer chunks as one: a second plane
-// is half as many matrix instructions more, which bound this kernel (with it and without: a tree of 41 rows 22.4 and 21.4 us; 50 trees 112 and 105; 5 rows of 12 ragged
+// so that the weights never move between lanes.  The weights of sequences of up to 64 rows, and of cross-attention, enter as two bf16 planes, those of longer chunks as one:
+// a second plane is half as many matrix instructions more, which bound this kernel (with it and without: a tree of 41 rows 22.4 and 21.4 us; 50 trees 112 and 105; 5 rows of 12 ragged
 // sequences over up to 30000 keys, 8 x 8 heads of 128, e4m3 150 and 125; 4 chunks of 250 rows, 8 x 4 heads of 64, and 20 tokens 100 and 88).
 // Rows of 16-byte pieces are stored with the piece index xored by the row, K and V in different ways, so that each kind of read
 // spreads over all banks.
@@ -423,7 +423,8 @@ __global__ __launch_bounds__(256, 2) void k_paged_attn_many(PagedAttnOf<CROSS> a
             if (++kt == kt1) break;
         }
     };
-    if (seq.m <= CSD_PAGED_FINE_ROWS) turns(std::true_type{});
+    if constexpr (CROSS) turns(std::true_type{});
+    else if (seq.m <= CSD_PAGED_FINE_ROWS) turns(std::true_type{});
     else turns(std::false_type{});
     l_run = halves_sum(l_run + l_more);
 

@@ -59,6 +59,29 @@ def test_chunks_of_sequences_longer_than_their_tables(cls, entries, length, d, w
         assert ((got - want).abs()[fine] <= (2.0 ** -8 * want.abs() + 2 * (2.0 ** -8 + e) * size)[fine]).all()
 
 
+# ------------------------------------------------------------------------------------------------ weights of chunks
+
+@pytest.mark.parametrize("cache", ["bf16", "fp8"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("m,kv_heads,group", [(1, 2, 1), (64, 2, 2), (65, 2, 1), (100, 2, 8), (300, 2, 2), (260, 64, 8), (700, 80, 1)])
+def test_weights_over_an_encoder_are_not_rounded_to_bf16(m, kv_heads, group, d, cache):
+    """Tokens, blocks and chunks in every kernel: outputs small beside the values that they are sums of, in which a rounded weight shows."""
+    c = States(cache, "bf16", [700, 230], [m, m], kv_heads=kv_heads, group=group, d=d, seed=m + d)
+    q = c.random_rows(c.total, heads=kv_heads * group, loud=False) * 0.25
+    out = c.cross(q, d ** -0.5, m)
+    kk, vv = (torch.tensor(c.values(pool, scale)[0]) for pool, scale in ((c.k, c.ks), (c.v, c.vs)))
+    for b, n in enumerate(c.cached):
+        page, slot = torch.tensor(c.table[b])[torch.arange(n) // c.page].long(), torch.arange(n) % c.page
+        for h in range(2 * group):
+            qq, got = (x[c.start[b]:c.start[b + 1], h].double().cpu() for x in (q, out))
+            k, v = kk[page, h // group, slot], vv[page, h // group, slot]
+            p = torch.softmax(qq @ k.t().contiguous() * d ** -0.5, -1)
+            e = (d + 4) * 2.0 ** -24 * float(qq.norm(dim=-1).max() * k.norm(dim=-1).max()) * d ** -0.5 + 2.0 ** -21 + n * 2.0 ** -24
+            tol = 2.0 ** -8 * (p @ v).abs() + 2 * (2.0 ** -15 + e) * (p @ v.abs())
+            off = ((got - p @ v).abs() / tol).max().item()
+            assert off <= 1, f"off by {off:.2f} times the bound"
+
+
 # ------------------------------------------------------------------------------------------------ pages that others use
 
 def test_rows_of_shared_pages_are_nobodys_to_write():
