@@ -37,8 +37,10 @@ struct SampleRows {
     const int32_t *top_k;
     float temperature_all, top_p_all, min_p_all;
     int32_t top_k_all;
-    // Probabilities of 16 MiB and more are stored past the caches (656 rows of 50001 48 us, through them 54; 136 of 32128 34.6 and 38); what a review reads
-    // next are fewer.
+    // Probabilities are stored past the caches where these would not hold what a review uses: p and q with the logits of both, so from 144 MiB of logits and
+    // probabilities on.  us past and through them of p, q and accept, MiB of p, fp32, top-k and top-p: 16.6 33.0 and 33.4, 33 47 and 44, 54 56 and 51, 66 67.2 and 65.3,
+    // 73 73 and 77, 87 78 and 99, 129 117 and 133; top-p alone: 33 94 and 92, 66 149 and 150, 73 163 and 171, 129 240 and 258; bf16 logits, top-k and top-p: 45 130 and 107,
+    // 104 169 and 168, 114 177 and 180, 201 232 and 253.
     bool past;
 };
 
@@ -932,7 +934,7 @@ static int32_t sample_enqueue(const csd_filter *f, const void *logits, int64_t s
     const char *from = (const char *)logits, *to = from + ((size_t)(rows - 1) * stride + V) * size;
     if (probs && (const char *)probs < to && from < (const char *)(probs + (size_t)rows * V)) return CSD_EINVAL;
     const SampleRows a{logits, (long long)stride, V, f->rows_each, u, tokens, probs, f->temperature, f->top_p, f->min_p, f->top_k,
-                       f->temperature_all, f->top_p_all, f->min_p_all, f->top_k_all, (long long)rows * V >= 1 << 22};
+                       f->temperature_all, f->top_p_all, f->min_p_all, f->top_k_all, (long long)rows * V * (long long)(size + 4) >= 144ll << 20};
     if (dtype == CSD_DTYPE_FP32) sample_launch<float>(a, rows, (hipStream_t)stream);
     else sample_launch<bf16_t>(a, rows, (hipStream_t)stream);
     CSD_LAUNCH_CHECK();

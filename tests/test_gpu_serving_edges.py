@@ -237,3 +237,18 @@ def test_sets_and_draws_of_equal_logits_are_exact(V, dtype):
         tokens, probs = (f(x, *a, top_k=k, top_p=p) for f, a in ((P.sample, (torch.tensor(u, dtype=torch.float32, device="cuda"),)), (P.filter_probs, ())))
         assert tokens.tolist() == [math.floor(Fraction(a) * n) for a in u], (k, p)
         assert (probs[:, :n] == np.float32(1 / n)).all() and not probs[:, n:].any(), (k, p)
+
+
+@pytest.mark.parametrize("V", [131072, 131069])
+@pytest.mark.parametrize("rows,dtype", [(160, torch.float32), (210, torch.bfloat16)])
+def test_rows_of_large_batches_are_those_of_small_ones(rows, dtype, V):
+    """So many probabilities that they are stored past the caches: the same bits, and nothing beside them."""
+    import paper_2312_11462_amd as P
+    x = logits(rows, V, dtype, 31)
+    x[rows // 2] = -math.inf
+    for kw in (dict(), dict(temperature=0.0), dict(top_k=50, top_p=0.9), dict(top_p=0.9), dict(top_p=0.2), dict(min_p=0.05), dict(top_k=5000)):
+        out = torch.full((rows * V + 64,), 7.0, device="cuda")
+        probs = P.filter_probs(x, out=out[32:-32].view(rows, V), **kw)
+        assert (out[:32] == 7).all() and (out[-32:] == 7).all()
+        for at in range(0, rows, 70):
+            assert torch.equal(probs[at:at + 70], P.filter_probs(x[at:at + 70], **kw)), (kw, at)
