@@ -7,6 +7,8 @@ runtime PyTorch already brought into the process (one runtime, shared streams an
 from __future__ import annotations
 
 import ctypes as C
+import math
+import operator
 import os
 import struct
 import threading
@@ -596,11 +598,31 @@ def _filter(logits, temperature, top_k, top_p, min_p):
         else:
             numbers[i] = value
     buffer = C.create_string_buffer(_FILTER.size)
-    _FILTER.pack_into(buffer, 0, *(a or 0 for a in addresses), *numbers, rows // sets or 1 if sets else 1)
+    each = rows // sets or 1 if sets else 1
+    try:
+        _FILTER.pack_into(buffer, 0, *(a or 0 for a in addresses), *numbers, each)
+    except (struct.error, OverflowError):
+        _FILTER.pack_into(buffer, 0, *(a or 0 for a in addresses), *_in_range(numbers), each)
     return buffer, rows, step
 
 
+def _in_range(numbers):
+    """Parameters that csd_filter's types do not hold, as ones that mean the same: a top_k beyond int32, the others beyond fp32; raises for what is no such number."""
+    out = []
+    for name, value in zip(_PARAMETERS, numbers):
+        try:
+            if name == "top_k":
+                out.append(min(max(operator.index(value), 0), 2 ** 31 - 1))
+            else:
+                value = float(value)
+                out.append(value if math.isinf(value) else max(min(value, _FP32_MAX), -_FP32_MAX))
+        except (TypeError, ValueError, OverflowError):
+            raise TypeError(f"{name}: expected {'a whole number' if name == 'top_k' else 'a number'}, got {value!r}") from None
+    return out
+
+
 _PARAMETERS = "temperature", "top_k", "top_p", "min_p"
+_FP32_MAX = 3.4028234663852886e38
 
 
 def _rows_of(shape, stride):

@@ -252,3 +252,18 @@ def test_rows_of_large_batches_are_those_of_small_ones(rows, dtype, V):
         assert (out[:32] == 7).all() and (out[-32:] == 7).all()
         for at in range(0, rows, 70):
             assert torch.equal(probs[at:at + 70], P.filter_probs(x[at:at + 70], **kw)), (kw, at)
+
+
+def test_numbers_that_the_parameters_types_do_not_hold():
+    import paper_2312_11462_amd as P
+    x, u = logits(3, 700, torch.float32, 2), torch.tensor([0.1, 0.5, 0.9], device="cuda")
+    for k in (2 ** 31, 2 ** 40, 2 ** 63 - 1, -2 ** 40):
+        assert torch.equal(P.filter_probs(x, top_k=k, top_p=0.9), P.filter_probs(x, top_p=0.9)) and torch.equal(P.sample(x, u, top_k=k), P.sample(x, u))
+    assert torch.equal(P.filter_probs(x, temperature=1e39), P.filter_probs(x, temperature=math.inf))       # (logits of a few units: all alike)
+    assert torch.equal(P.filter_probs(x, top_p=1e300), P.filter_probs(x))
+    for bad in (dict(top_k=5.5), dict(temperature="warm"), dict(top_p=[0.9])):
+        with pytest.raises(TypeError):
+            P.sample(x, u, **bad)
+    for bad in (dict(temperature=-1e39), dict(top_p=-1e39), dict(min_p=1e39), dict(temperature=math.nan, top_k=2 ** 40)):
+        with pytest.raises(P.CsdError):
+            P.sample(x, u, **bad)

@@ -211,3 +211,18 @@ def test_draws_refuse_rows_that_their_parameters_do_not_cover(L):
             assert L.csd_sample(C.addressof(f), 256, 100, 1, rows, 100, 256, 256, None, None) == EINVAL, (name, rows, each)
             assert L.csd_filter_probs(C.addressof(f), 256, 100, 1, rows, 100, 4096, None) == EINVAL, (name, rows, each)
             assert L.csd_sample(C.addressof(f), None, 100, 1, 0, 100, None, None, None, None) == 0
+
+
+def test_numbers_that_the_parameters_types_do_not_hold():
+    """A top_k beyond int32 is more than there are; numbers beyond fp32 are its largest; what is no number is said to be none."""
+    import math
+    from paper_2312_11462_amd.binding import _in_range
+    big = float(np.finfo(np.float32).max)
+    assert _in_range([1e39, 2 ** 40, 1e300, 0.0]) == [big, 2 ** 31 - 1, big, 0.0]
+    assert _in_range([math.inf, -2 ** 70, 1, -1e39]) == [math.inf, 0, 1.0, -big]
+    assert math.isnan(_in_range([math.nan, 2 ** 40, 1.0, 0.0])[0])
+    for at, bad in ((0, "warm"), (1, 5.5), (1, None), (2, [0.5]), (3, 10 ** 400)):
+        numbers = [1.0, 0, 1.0, 0.0]
+        numbers[at] = bad
+        with pytest.raises(TypeError):
+            _in_range(numbers)
