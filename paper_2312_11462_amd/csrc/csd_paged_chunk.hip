@@ -11,7 +11,7 @@
 // per compute unit took 455; e4m3 406 against 433; heads of 64 256 against 284; a barrier behind each half of a tile instead: 411, but one fresh prompt of
 // 4099 rows, 32 heads, 215 instead of 193.)  Weights in two planes, as those of blocks of up to 64 rows are, would take 542 us, e4m3 531, heads of 64 348.
 // Cross-attention has them: as near to 64 bits as its output's rounding lets it be, however many rows there are (4 x 1024 rows over 1000 to 4096 encoder rows, 32 heads
-// of 128: 255 to 269 us, off by 1.66e-3 of the outputs' size; in one plane 196 to 202, off by 2.32e-3).
+// of 128: 255 to 274 us by the card, off by 1.66e-3 of the outputs' size; in one plane 196 to 202, off by 2.32e-3).
 #include "csd_paged_tiles.h"
 
 static constexpr int kChunkRows = 256;
